@@ -378,6 +378,51 @@ lgn_status lgn_prefix_decode(const uint32_t *stream_dev, const uint64_t *off_dev
 lgn_status lgn_dequantize(const void *codes, uint64_t n, const lgn_fp_format_t *fmt, lgn_dtype out_dt,
                           void *out, void *stream);
 
+/* ==== Operators of a training step around the compressed gradients ================
+ * The neural gradients of this library are the operands of two matrix products per layer (input gradient and
+ * weight gradient), reach the embedding table at the bottom of a language model, and end in
+ * weight gradients that are clipped by their global norm.  The entry points below are those steps.  They
+ * share the conventions above with these differences: matrices are given by pointer,
+ * extents and a leading dimension in elements (rows contiguous); any element-aligned pointer is taken unless
+ * stated; non-finite values are allowed and what becomes of them is stated. */
+
+/* ---- Matrix product in 8-bit floating point, one power-of-two scale per block of 128 ----
+ * E4M3 (largest value 448) and E5M2 (57344).  A block is 128 consecutive values of a row
+ * (LGN_BLOCK_ROW) or a 128 x 128 square (LGN_BLOCK_SQUARE: weights, whose codes serve both a product and its
+ * transpose); blocks at the end of a matrix are shorter.  Its scale is 2^e, e the smallest integer >= -127
+ * with max|x| 2^-e <= the format's largest value, over the finite entries of the block (-127 if all are
+ * zero); codes are x 2^-e rounded to nearest even; every non-finite entry becomes the NaN code. */
+typedef enum { LGN_E4M3 = 0, LGN_E5M2 = 1 } lgn_fp8;
+typedef enum { LGN_BLOCK_ROW = 0, LGN_BLOCK_SQUARE = 1 } lgn_fp8_block;
+
+/* Bytes of the codes and of the scales of a rows x cols operand.  Codes: row major, rows padded with zero
+ * codes to a multiple of 16 bytes.  Scales: E8M0 bytes (2^(byte-127)), 512 per 128 rows and 512
+ * columns, byte 16 (row mod 32) + 4 ((row mod 128) / 32) + (block mod 4) of tile (row / 128, block / 4), tiles of the
+ * same 128 rows one after another.  0 for an extent above 2^30. */
+size_t lgn_fp8_codes_bytes(uint64_t rows, uint64_t cols);
+size_t lgn_fp8_scales_bytes(uint64_t rows, uint64_t cols);
+
+/* Quantises x (rows x cols of dt, leading dimension ld >= cols) in one read, one launch, to
+ *   codes, scales      the operand itself: blocks along the columns;    both NULL: not written
+ *   codes_t, scales_t  the operand's transpose (cols x rows): LGN_BLOCK_ROW quantises it afresh with blocks along
+ *                      the rows of x, LGN_BLOCK_SQUARE transposes the same codes;  both NULL: not written
+ * (16-byte aligned).  The transpose is what a product that contracts over the rows of x takes. */
+lgn_status lgn_fp8_quantize(const void *x, uint64_t rows, uint64_t cols, uint64_t ld, lgn_dtype dt,
+                            lgn_fp8 fmt, lgn_fp8_block block, void *codes, void *scales,
+                            void *codes_t, void *scales_t, void *stream);
+
+/* out[i, j] = sum over c of A[i, c] B[j, c] (+ out[i, j] if accumulate), i < m, j < n, c < k, of the values that
+ * codes and scales stand for; a is m x k, b is n x k, either format each.  Sums in fp32, rounded
+ * once to out_dt.  out: leading dimension ldo >= n.  A layer Y = X W^T: its forward pass takes X and W, its
+ * input gradient dY and the transpose of W, its weight gradient the transposes of dY and X.
+ * k = 0 writes zeros (or leaves out as it is).  status_dev: device uint32, may be NULL; set to
+ * LGN_ERR_TIMEOUT if a bounded device-side wait ran out (the output is then invalid), else left alone.
+ * One launch, no workspace; the same inputs give the same bits on the same type of device. */
+lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt,
+                          const void *b, const void *b_scales, lgn_fp8 b_fmt,
+                          uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt,
+                          int accumulate, uint32_t *status_dev, void *stream);
+
 /* Self-test of the bounded device-side wait (no counterpart in the paper).
  * Same arguments and the same work as lgn_compress_layers, except that one
  * statistics tile of layer 0 is withheld from the queue, so layer 0's closed form

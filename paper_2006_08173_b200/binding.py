@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -27,6 +27,8 @@ F32, BF16 = 0, 1
 ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
 MODE_PRUNE, MODE_QUANTIZE = 0, 1
 SCALE_CENTRED, SCALE_FROM_MAX = 0, 1
+E4M3, E5M2 = 0, 1
+BLOCK_ROW, BLOCK_SQUARE = 0, 1
 
 
 class StatsT(C.Structure):
@@ -122,6 +124,14 @@ _lib.lgn_launches_per_call.restype = _i32
 _lib.lgn_stats_static_scratch.argtypes = [_vp, _u64, _i32, _vp, _vp]
 _lib.lgn_stats_static_scratch.restype = _i32
 STATS_STATIC_MAX_ELEMS = 1 << 28
+_lib.lgn_fp8_codes_bytes.argtypes = [_u64, _u64]
+_lib.lgn_fp8_codes_bytes.restype = _sz
+_lib.lgn_fp8_scales_bytes.argtypes = [_u64, _u64]
+_lib.lgn_fp8_scales_bytes.restype = _sz
+_lib.lgn_fp8_quantize.argtypes = [_vp, _u64, _u64, _u64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
+_lib.lgn_fp8_quantize.restype = _i32
+_lib.lgn_fp8_matmul.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
+_lib.lgn_fp8_matmul.restype = _i32
 
 
 class LgnError(RuntimeError):
@@ -449,4 +459,74 @@ def lgn_prefix_decode(stream_dev: torch.Tensor, off_dev: torch.Tensor, out: torc
     _check(_lib.lgn_prefix_decode(_dev(stream_dev, "stream_dev") if stream_dev.numel() else None,
                                   _dev(off_dev, "off_dev"), out.numel(), dtype_code(out), float(tau), tau_from_dev,
                                   _dev(out, "out") if out.numel() else None, _stream(stream)), "lgn_prefix_decode")
+    return out
+
+
+# --------------------------------------------------------------------------- 8-bit matrix product
+class Fp8Operand(NamedTuple):
+    """A matrix of ``rows`` x ``k`` in 8-bit codes with one scale per block of 128 along k."""
+    codes: torch.Tensor      # uint8, lgn_fp8_codes_bytes(rows, k)
+    scales: torch.Tensor     # uint8, lgn_fp8_scales_bytes(rows, k)
+    rows: int
+    k: int
+    fmt: int
+
+
+def _matrix(t: torch.Tensor, what: str) -> int:
+    """Leading dimension of a CUDA matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    if t.dim() != 2 or (t.size(1) > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    ld = t.stride(0) if t.size(0) > 1 else max(1, t.size(1))
+    if ld < t.size(1):
+        raise ValueError(f"{what} must have rows that do not overlap")
+    return ld
+
+
+def new_fp8_operand(rows: int, k: int, fmt: int, device) -> Fp8Operand:
+    return Fp8Operand(torch.empty(max(16, _lib.lgn_fp8_codes_bytes(rows, k)), dtype=torch.uint8, device=device),
+                      torch.empty(max(16, _lib.lgn_fp8_scales_bytes(rows, k)), dtype=torch.uint8, device=device), rows, k, fmt)
+
+
+def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, rowwise: bool = True,
+                     transposed: bool = False, out: Optional[Fp8Operand] = None, out_t: Optional[Fp8Operand] = None,
+                     stream=None) -> Tuple[Optional[Fp8Operand], Optional[Fp8Operand]]:
+    """(operand, operand of the transpose) of a matrix, each only if asked for (else None).  ``out`` and
+    ``out_t`` are operands of the same extents to write to (new_fp8_operand)."""
+    ld = _matrix(x, "x")
+    rows, cols = x.shape
+    if not (rowwise or transposed):
+        raise ValueError("neither the operand nor its transpose is asked for")
+    q = (out if out is not None else new_fp8_operand(rows, cols, fmt, x.device)) if rowwise else None
+    t = (out_t if out_t is not None else new_fp8_operand(cols, rows, fmt, x.device)) if transposed else None
+    for o, shape in ((q, (rows, cols, fmt)), (t, (cols, rows, fmt))):
+        if o is not None and tuple(o[2:]) != shape:
+            raise ValueError("out: extents or format differ from the matrix")
+    _check(_lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), int(fmt), int(block),
+                                 _dev(q.codes, "codes") if q else None, _dev(q.scales, "scales") if q else None,
+                                 _dev(t.codes, "codes_t") if t else None, _dev(t.scales, "scales_t") if t else None,
+                                 _stream(stream)), "lgn_fp8_quantize")
+    return q, t
+
+
+def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = None,
+                   out_dtype: torch.dtype = torch.bfloat16, accumulate: bool = False,
+                   status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[i, j] = sum over c of a[i, c] b[j, c] (+ out[i, j] with ``accumulate``)."""
+    if a.k != b.k:
+        raise ValueError("operands contract over different extents")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty(a.rows, b.rows, dtype=out_dtype, device=a.codes.device)
+    elif tuple(out.shape) != (a.rows, b.rows):
+        raise ValueError("out must be a.rows x b.rows")
+    for o in (a, b):
+        if o.codes.numel() < _lib.lgn_fp8_codes_bytes(o.rows, o.k) or o.scales.numel() < _lib.lgn_fp8_scales_bytes(o.rows, o.k):
+            raise ValueError("operand shorter than its extents")
+    _check(_lib.lgn_fp8_matmul(_dev(a.codes, "a.codes"), _dev(a.scales, "a.scales"), a.fmt,
+                               _dev(b.codes, "b.codes"), _dev(b.scales, "b.scales"), b.fmt, a.rows, b.rows, a.k,
+                               out.data_ptr() or None, _matrix(out, "out"), dtype_code(out), 1 if accumulate else 0,
+                               _dev(status, "status") if status is not None else None, _stream(stream)), "lgn_fp8_matmul")
     return out

@@ -1,0 +1,554 @@
+// out[i, j] (+)= sum over k of A[i, k] B[j, k], A and B in 8-bit floating point with one power-of-two scale
+// per row and block of 128 k (lgn_fp8_quantize).
+//
+// The tensor cores apply the scales: tcgen05.mma kind::mxf8f6f4 multiplies each group of 32 k by an E8M0
+// factor per row of either operand, read from tensor memory; a block of 128 is four groups with the same
+// byte.  Products and sums stay in fp32 in tensor memory over the whole of k and are rounded once, to the
+// output's type.
+//
+// One CTA works on tiles of 128 rows of one operand ("rows") by BN rows of the other ("cols"):
+//   warp 4  brings 128 x 128 and BN x 128 bytes of codes per step of k into a ring of shared-memory stages
+//           (TMA, 128-byte swizzle) and, every fourth step, the 512-byte scale tiles of four blocks;
+//   warp 5  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step;
+//   warps 0..3  read the finished tile from tensor memory, round and store.
+// Forms: persistent over tiles, or (SPLIT) one tile per cluster with the CTAs of a cluster taking
+// consecutive shares of k and adding their fp32 tiles through distributed shared memory in rank order.
+// SWAP: `rows` runs along the contiguous dimension of the output, so that the 32 lanes of a warp, which hold
+// 32 rows, write contiguous memory whatever the alignment.
+//
+// Every wait is bounded: one that runs out raises a flag on which all roles stop; the copies and MMAs in
+// flight are waited for (bounded too), tensor memory is freed and the kernel ends with *status set.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <mutex>
+
+#include "lgn.h"
+#include "lgn_fp8.cuh"
+#include "lgn_launch.h"
+#include "lgn_log.h"
+
+namespace lgn {
+
+constexpr int kMmThreads = 192;
+constexpr int kMmGroupRows = 16;                 // row tiles walked before the next column tile (L2 reuse)
+constexpr long long kMmWaitClocks = 4000000000ll;   // about two seconds
+
+struct MmArgs {
+    const uint8_t *sc_rows, *sc_cols;            // scale tiles
+    void *out;
+    uint64_t ldo;
+    uint32_t *status;
+    uint32_t rows, cols;                         // extents of the two operands
+    uint32_t kblocks, groups;                    // ceil(k / 128), ceil(k / 512)
+    uint32_t tiles_r, tiles_c;
+    uint32_t fmt_rows, fmt_cols;
+    uint32_t split_groups;                       // groups of four blocks per CTA of a cluster
+    uint32_t accumulate, vec;
+};
+
+template <int BN> struct MmShape {
+    static constexpr int kColBlocks = BN <= 128 ? 1 : 2;            // 128-row scale tiles a column tile touches
+    static constexpr int kStageBytes = 128 * 128 + BN * 128;
+    static constexpr int kScaleBytes = 512 * (1 + kColBlocks);
+    static constexpr int kStages = (int)((220 * 1024) / (kStageBytes + kScaleBytes)) > 8 ? 8 : (int)((220 * 1024) / (kStageBytes + kScaleBytes));
+    static constexpr int kAccs = BN <= 192 ? 2 : 1;                 // accumulator tiles in tensor memory
+    static constexpr int kScaleCol = kAccs * BN;                    // first tensor-memory column of the scales
+    static constexpr int kScaleCols = 4 * (1 + kColBlocks);
+    static constexpr int kScaleBufs = 4;
+    static constexpr int kSmem = 1024 + kStages * (kStageBytes + kScaleBytes) + 256;
+    static_assert(kScaleCol + kScaleBufs * kScaleCols <= 512, "tensor memory");
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait; gives up as soon as another role has.
+__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
+    const long long t0 = clock64();
+    for (;;) {
+        if (mbar_try(bar, parity)) return true;
+        if (*stop) return false;
+        if (clock64() - t0 > kMmWaitClocks) { *stop = 1u; return false; }
+    }
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
+    if (mbar_try(bar, parity)) return true;
+    return mbar_wait_slow(bar, parity, stop);
+}
+// Bounded wait for what is in flight after a stop.
+__device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!mbar_try(bar, parity))
+        if (clock64() - t0 > kMmWaitClocks) return;
+}
+
+__device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// Shared-memory descriptors.  Code tiles: rows of 128 bytes, 128-byte swizzle, 8 rows = 1024 bytes apart
+// from the next 8.  Scale tiles: no swizzle, groups of 8 rows of 16 bytes 128 bytes apart.
+__device__ __forceinline__ uint64_t desc_codes(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+}
+
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add) : "memory");
+}
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after()  { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, float *v) {
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+template <int ODT>
+__device__ __forceinline__ float load_out(const void *out, uint64_t i) {
+    if constexpr (ODT == LGN_F32) return static_cast<const float *>(out)[i];
+    else return __bfloat162float(static_cast<const __nv_bfloat16 *>(out)[i]);
+}
+template <int ODT>
+__device__ __forceinline__ void store_out(void *out, uint64_t i, float v) {
+    if constexpr (ODT == LGN_F32) static_cast<float *>(out)[i] = v;
+    else static_cast<__nv_bfloat16 *>(out)[i] = __float2bfloat16_rn(v);
+}
+__device__ __forceinline__ void st256(void *p, const uint32_t *w) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void ld256(const void *p, uint32_t *w) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+
+// 32 columns of one row, contiguous in memory from element i on and 32-byte aligned.
+template <int ODT>
+__device__ __forceinline__ void store_run(void *out, uint64_t i, float *v, bool accumulate) {
+    uint32_t w[8];
+    if constexpr (ODT == LGN_F32) {
+        float *p = static_cast<float *>(out) + i;
+        #pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+            if (accumulate) {
+                ld256(p + k, w);
+                #pragma unroll
+                for (int j = 0; j < 8; ++j) v[k + j] += __uint_as_float(w[j]);
+            }
+            #pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[k + j]);
+            st256(p + k, w);
+        }
+    } else {
+        __nv_bfloat16 *p = static_cast<__nv_bfloat16 *>(out) + i;
+        #pragma unroll
+        for (int k = 0; k < 32; k += 16) {
+            if (accumulate) {
+                ld256(p + k, w);
+                #pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[k + 2 * j] += __uint_as_float(w[j] << 16);
+                    v[k + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
+                }
+            }
+            #pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pack_bf16(v[k + 2 * j], v[k + 2 * j + 1]);
+            st256(p + k, w);
+        }
+    }
+}
+
+enum MmForm { kFormRows = 0, kFormSwap = 1, kFormSplit = 2 };
+
+template <int BN, int FORM, int ODT>
+__global__ void __launch_bounds__(kMmThreads, 1)
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const MmArgs p) {
+    using S = MmShape<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ volatile uint32_t stop;
+
+    const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t scales0 = smem0 + S::kStages * S::kStageBytes;
+    const uint32_t bar0 = smem_u32(bars);
+    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+    auto empty = [&](uint32_t s) { return bar0 + 8 * (S::kStages + s); };
+    auto acc_full = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + a); };
+    auto acc_empty = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + S::kAccs + a); };
+    const uint32_t drained = bar0 + 8 * (2 * S::kStages + 2 * S::kAccs);
+
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 128); }
+        mbar_init(drained, 1);
+        stop = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 4 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_rows) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_cols) : "memory");
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_base_s;
+
+    // this CTA's tiles and steps of k
+    uint32_t rank = 0, nrank = 1, tile0 = blockIdx.x, tile_step = gridDim.x, kb0 = 0, kb1 = p.kblocks;
+    if constexpr (FORM == kFormSplit) {
+        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(nrank));
+        tile0 = blockIdx.x / nrank;
+        tile_step = 0x7fffffffu;
+        kb0 = rank * p.split_groups * 4;
+        kb1 = min(p.kblocks, kb0 + p.split_groups * 4);
+    }
+    const uint32_t tiles = p.tiles_r * p.tiles_c;
+    auto tile_at = [&](uint32_t t, uint32_t &tr, uint32_t &tc) {
+        const uint32_t span = kMmGroupRows * p.tiles_c, g = t / span, in = t % span;
+        const uint32_t h = min((uint32_t)kMmGroupRows, p.tiles_r - g * kMmGroupRows);
+        tr = g * kMmGroupRows + in % h;
+        tc = in / h;
+    };
+
+    if (warp == 4) {
+        if (lane == 0) {
+            dep_wait();
+            uint32_t it = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
+                uint32_t tr, tc;
+                tile_at(t, tr, tc);
+                const uint32_t sb0 = (tc * BN) >> 7, sb_n = (p.cols + 127) >> 7;
+                for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
+                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
+                    if (!(ok = mbar_wait(empty(s), ph ^ 1, &stop))) break;
+                    const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
+                    uint32_t bytes = S::kStageBytes;
+                    const bool with_scales = (kb & 3) == 0, second = S::kColBlocks > 1 && sb0 + 1 < sb_n;
+                    if (with_scales) bytes += 1024 + (second ? 512 : 0);
+                    mbar_expect(full(s), bytes);
+                    tma_tile(a, &map_rows, full(s), (int)(kb * 128), (int)(tr * 128));
+                    tma_tile(a + 128 * 128, &map_cols, full(s), (int)(kb * 128), (int)(tc * BN));
+                    if (with_scales) {
+                        const uint64_t g = kb >> 2;
+                        bulk_copy(sc, p.sc_rows + ((uint64_t)tr * p.groups + g) * 512, 512, full(s));
+                        bulk_copy(sc + 512, p.sc_cols + ((uint64_t)sb0 * p.groups + g) * 512, 512, full(s));
+                        if (second) bulk_copy(sc + 1024, p.sc_cols + ((uint64_t)(sb0 + 1) * p.groups + g) * 512, 512, full(s));
+                    }
+                }
+            }
+            if (!ok)                                                            // wait for the copies in flight
+                for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
+                    mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
+        }
+    } else if (warp == 5) {
+        if (lane == 0) {
+            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | (1u << 27);
+            uint32_t it = 0, n = 0, grp = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tiles; t += tile_step, ++n) {
+                uint32_t tr, tc;
+                tile_at(t, tr, tc);
+                const uint32_t acc = n % S::kAccs, col_off = ((tc * BN) & 127) >> 5;
+                if (!(ok = mbar_wait(acc_empty(acc), ((n / S::kAccs) & 1) ^ 1, &stop))) break;
+                fence_after();
+                const uint32_t d = tmem + acc * BN;
+                uint32_t sa = 0, sb = 0;
+                for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
+                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
+                    if (!(ok = mbar_wait(full(s), ph, &stop))) break;
+                    fence_after();
+                    const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
+                    if ((kb & 3) == 0) {
+                        sa = tmem + S::kScaleCol + (grp++ % S::kScaleBufs) * S::kScaleCols;
+                        sb = sa + 4;
+                        #pragma unroll
+                        for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales(sa + 4 * b, desc_scales(sc + 512 * b));
+                    }
+                    const uint32_t idesc = idesc0 | ((kb & 3) << 4) | ((kb & 3) << 29);
+                    const uint64_t da = desc_codes(a), db = desc_codes(a + 128 * 128);
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_scaled(d, da + 2 * k, db + 2 * k, idesc, sa, sb + col_off, kb > kb0 || k > 0);
+                    mma_commit(empty(s));
+                }
+                if (ok) mma_commit(acc_full(acc));
+            }
+            if (!ok) { mma_commit(drained); mbar_drain(drained, 0); }
+        }
+    } else {
+        dep_wait();                                                             // the output may belong to work before this call
+        uint32_t n = 0;
+        const uint32_t lane_base = (warp * 32u) << 16;
+        for (uint32_t t = tile0; t < tiles; t += tile_step, ++n) {
+            uint32_t tr, tc;
+            tile_at(t, tr, tc);
+            const uint32_t acc = n % S::kAccs;
+            const uint32_t r = tr * 128 + warp * 32 + lane, c0 = tc * BN;
+            if (!mbar_wait(acc_full(acc), (n / S::kAccs) & 1, &stop)) break;
+            __syncwarp();
+            fence_after();
+            #pragma unroll 1
+            for (int c = 0; c < BN; c += 32) {
+                float v[32];
+                tmem_load32(tmem + lane_base + acc * BN + c, v);
+                tmem_load_wait();
+                if (c + 32 >= BN) { fence_before(); mbar_arrive(acc_empty(acc)); }
+                if constexpr (FORM == kFormSplit) {
+                    float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
+                    #pragma unroll
+                    for (int j = 0; j < 32; ++j) part[(c + j) * 128 + warp * 32 + lane] = v[j];
+                } else if constexpr (FORM == kFormSwap) {
+                    if (r < p.rows) {
+                        #pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (c0 + c + j < p.cols) {
+                                const uint64_t i = (uint64_t)(c0 + c + j) * p.ldo + r;
+                                store_out<ODT>(p.out, i, p.accumulate ? v[j] + load_out<ODT>(p.out, i) : v[j]);
+                            }
+                    }
+                } else {
+                    if (r < p.rows && c0 + c < p.cols) {
+                        const uint64_t i = (uint64_t)r * p.ldo + c0 + c;
+                        if (p.vec && c0 + c + 32 <= p.cols) store_run<ODT>(p.out, i, v, p.accumulate != 0);
+                        else {
+                            #pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (c0 + c + j < p.cols) store_out<ODT>(p.out, i + j, p.accumulate ? v[j] + load_out<ODT>(p.out, i + j) : v[j]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if constexpr (FORM == kFormSplit) {
+        // every CTA's partial tile is in its own shared memory: column c is added over the ranks, in rank
+        // order, by the CTA c mod nrank
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (threadIdx.x < 128 && tile0 < tiles) {
+            uint32_t tr, tc;
+            tile_at(tile0, tr, tc);
+            const uint32_t r = tr * 128 + threadIdx.x;
+            if (r < p.rows) {
+                #pragma unroll 2
+                for (uint32_t c = rank; c < (uint32_t)BN && tc * BN + c < p.cols; c += nrank) {
+                    float v = 0.0f;
+                    for (uint32_t q = 0; q < nrank; ++q) {
+                        uint32_t at;
+                        float x;
+                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem0 + (c * 128 + threadIdx.x) * 4), "r"(q));
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+                        v += x;
+                    }
+                    const uint64_t i = (uint64_t)(tc * BN + c) * p.ldo + r;
+                    store_out<ODT>(p.out, i, p.accumulate ? v + load_out<ODT>(p.out, i) : v);
+                }
+            }
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
+    if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
+}
+
+// k = 0: nothing is added.
+template <int ODT>
+__global__ void __launch_bounds__(256) zero_rows_kernel(void *out, uint64_t ldo, uint32_t rows, uint32_t cols) {
+    dep_wait();
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < (uint64_t)rows * cols; i += (uint64_t)gridDim.x * 256)
+        store_out<ODT>(out, (i / cols) * ldo + i % cols, 0.0f);
+}
+
+#define LGN_MM(BN, F, O) reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, F, O>)
+#define LGN_MM3(BN) {{LGN_MM(BN, kFormRows, LGN_F32), LGN_MM(BN, kFormSwap, LGN_F32), LGN_MM(BN, kFormSplit, LGN_F32)}, \
+                     {LGN_MM(BN, kFormRows, LGN_BF16), LGN_MM(BN, kFormSwap, LGN_BF16), LGN_MM(BN, kFormSplit, LGN_BF16)}}
+static const void *const kMmTable[4][2][3] = {LGN_MM3(64), LGN_MM3(128), LGN_MM3(192), LGN_MM3(256)};
+#undef LGN_MM3
+#undef LGN_MM
+static const int kMmBn[4] = {64, 128, 192, 256};
+static const int kMmSmem[4] = {MmShape<64>::kSmem, MmShape<128>::kSmem, MmShape<192>::kSmem, MmShape<256>::kSmem};
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiled encode_tiled() {
+    static EncodeTiled fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
+// rows x k codes, boxes of box_rows x 128 bytes; what lies outside reads as zero codes.
+static bool make_map(CUtensorMap *m, const void *codes, uint64_t rows, uint64_t k, uint32_t box_rows) {
+    const cuuint64_t dim[2] = {k, rows}, stride[1] = {fp8_pitch(k)};
+    const cuuint32_t box[2] = {128, box_rows}, es[2] = {1, 1};
+    return encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dim, stride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The kernels need more dynamic shared memory than the default limit; raised once per device and kernel.
+static bool allow_smem(int bn_index, int odt, int form) {
+    static std::mutex guard;
+    static bool done[64][4][2][3];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+    std::lock_guard<std::mutex> lock(guard);
+    if (dev < 64 && done[dev][bn_index][odt][form]) return true;
+    if (cudaFuncSetAttribute(kMmTable[bn_index][odt][form], cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem[bn_index]) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    if (dev < 64) done[dev][bn_index][odt][form] = true;
+    return true;
+}
+
+struct MmPlan { int bn_index; int form; bool swap; uint32_t split; uint32_t split_groups; };
+
+static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t ldo, bool vec, int sms) {
+    MmPlan best = {0, kFormSwap, true, 1, 0};
+    const uint64_t groups = (kblocks + 3) / 4;
+    double best_cost = 1e300;
+    for (int b = 0; b < 4; ++b) {
+        const uint64_t bn = (uint64_t)kMmBn[b];
+        for (int form = 0; form < 3; ++form) {
+            const bool swap = form != kFormRows;
+            if (form == kFormRows && !vec) continue;
+            const uint64_t r = swap ? n : m, c = swap ? m : n;
+            const uint64_t tiles = ((r + 127) / 128) * ((c + bn - 1) / bn);
+            for (uint64_t want = form == kFormSplit ? 2 : 1; want <= (form == kFormSplit ? 8u : 1u); want *= 2) {
+                const uint64_t per = (groups + want - 1) / want, s = form == kFormSplit ? (groups + per - 1) / per : 1;
+                if (form == kFormSplit && (s < 2 || tiles * s > (uint64_t)sms)) continue;
+                const uint64_t steps = form == kFormSplit ? (per * 4 < kblocks ? per * 4 : kblocks) : kblocks;
+                const double rounds = (double)((tiles * s + sms - 1) / sms);
+                // clocks: a step of k takes 2 BN of MMA (at least the time its bytes need), a tile an epilogue
+                const double step = 2.0 * bn > 300 ? 2.0 * bn : 300, epi = (bn == 256 ? 900 : 300) + (swap ? 2.0 * bn : 0) + (s > 1 ? 3000 : 0);
+                const double cost = rounds * (steps * step + epi);
+                if (cost < best_cost) { best_cost = cost; best = {b, form, swap, (uint32_t)s, (uint32_t)per}; }
+            }
+        }
+    }
+    (void)ldo;
+    return best;
+}
+
+}  // namespace lgn
+
+using namespace lgn;
+
+extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt, const void *b, const void *b_scales, lgn_fp8 b_fmt,
+                                     uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt, int accumulate,
+                                     uint32_t *status_dev, void *stream) {
+    if ((a_fmt != LGN_E4M3 && a_fmt != LGN_E5M2) || (b_fmt != LGN_E4M3 && b_fmt != LGN_E5M2)) return LGN_ERR_INVALID_ARG;
+    if (out_dt != LGN_F32 && out_dt != LGN_BF16) return LGN_ERR_INVALID_ARG;
+    if (m > kFp8MaxDim || n > kFp8MaxDim || k > kFp8MaxDim) return LGN_ERR_UNSUPPORTED;
+    if (m == 0 || n == 0) return LGN_OK;
+    if (ldo < n || ldo > (1ull << 40)) return LGN_ERR_INVALID_ARG;
+    const uint64_t es = out_dt == LGN_F32 ? 4 : 2, ob = ((m - 1) * ldo + n) * es;
+    if (out == nullptr || !aligned_to(out, es) || !aligned_to(status_dev, 4)) return LGN_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (k == 0) {
+        if (accumulate) return LGN_OK;
+        uint32_t rows = (uint32_t)m, cols = (uint32_t)n;
+        void *args[] = {&out, &ldo, &rows, &cols};
+        const void *fn = out_dt == LGN_F32 ? reinterpret_cast<const void *>(&zero_rows_kernel<LGN_F32>) : reinterpret_cast<const void *>(&zero_rows_kernel<LGN_BF16>);
+        const uint64_t want = (m * n + 255) / 256;
+        return launch_dependent(fn, dim3((unsigned)(want < 4096 ? want : 4096)), dim3(256), args, 0, stream);
+    }
+    if (a == nullptr || b == nullptr || a_scales == nullptr || b_scales == nullptr) return LGN_ERR_INVALID_ARG;
+    if (!aligned_to(a, 16) || !aligned_to(b, 16) || !aligned_to(a_scales, 16) || !aligned_to(b_scales, 16)) return LGN_ERR_INVALID_ARG;
+    if (ranges_overlap(out, ob, a, lgn_fp8_codes_bytes(m, k)) || ranges_overlap(out, ob, b, lgn_fp8_codes_bytes(n, k)) ||
+        ranges_overlap(out, ob, a_scales, lgn_fp8_scales_bytes(m, k)) || ranges_overlap(out, ob, b_scales, lgn_fp8_scales_bytes(n, k)))
+        return LGN_ERR_INVALID_ARG;
+    if (sms < 1 || encode_tiled() == nullptr) return LGN_ERR_CUDA;
+    const bool vec = aligned_to(out, 32) && (ldo * es) % 32 == 0;
+    const uint64_t kblocks = (k + 127) / 128;
+    const MmPlan plan = plan_matmul(m, n, kblocks, ldo, vec, sms);
+    const uint32_t bn = (uint32_t)kMmBn[plan.bn_index];
+    MmArgs p = {};
+    const void *cr = plan.swap ? b : a, *cc = plan.swap ? a : b;
+    p.sc_rows = static_cast<const uint8_t *>(plan.swap ? b_scales : a_scales);
+    p.sc_cols = static_cast<const uint8_t *>(plan.swap ? a_scales : b_scales);
+    p.rows = (uint32_t)(plan.swap ? n : m);
+    p.cols = (uint32_t)(plan.swap ? m : n);
+    p.fmt_rows = (uint32_t)(plan.swap ? b_fmt : a_fmt);
+    p.fmt_cols = (uint32_t)(plan.swap ? a_fmt : b_fmt);
+    p.out = out; p.ldo = ldo; p.status = status_dev;
+    p.kblocks = (uint32_t)kblocks;
+    p.groups = (uint32_t)((kblocks + 3) / 4);
+    p.tiles_r = (p.rows + 127) / 128;
+    p.tiles_c = (p.cols + bn - 1) / bn;
+    p.split_groups = plan.split_groups;
+    p.accumulate = accumulate != 0;
+    p.vec = vec;
+    const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c;
+    if (tiles > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
+    CUtensorMap mr, mc;
+    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, bn)) return LGN_ERR_CUDA;
+    if (!allow_smem(plan.bn_index, out_dt, plan.form)) return LGN_ERR_CUDA;
+    const uint64_t grid = plan.form == kFormSplit ? tiles * plan.split : (tiles < (uint64_t)sms ? tiles : (uint64_t)sms);
+    log_line("fp8_matmul: m %llu n %llu k %llu, tile 128 x %u, form %d, split %u, %llu CTAs", (unsigned long long)m, (unsigned long long)n,
+             (unsigned long long)k, bn, plan.form, plan.split, (unsigned long long)grid);
+    void *args[] = {&mr, &mc, &p};
+    return launch_dependent(kMmTable[plan.bn_index][out_dt][plan.form], dim3((unsigned)grid), dim3(kMmThreads), args,
+                            (size_t)kMmSmem[plan.bn_index], stream, plan.form == kFormSplit ? plan.split : 1);
+}

@@ -1,0 +1,58 @@
+// Launch helper of the operators around the compression path: a kernel that may become resident
+// while the kernel before it on the stream is still running (programmatic stream serialisation).
+// A kernel launched this way executes griddepcontrol.wait before its first access to global
+// memory, which returns when everything before it on the stream has finished and is visible.
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "lgn.h"
+
+namespace lgn {
+
+inline lgn_status launch_dependent(const void *fn, dim3 grid, dim3 block, void **args, size_t smem, void *stream,
+                                   unsigned cluster = 1) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    if (cudaLaunchKernelExC(&cfg, fn, args) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
+    return LGN_OK;
+}
+
+// SM count of the current device (0: the runtime refused).
+inline int sm_count() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms;
+}
+
+inline bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline bool ranges_overlap(const void *a, uint64_t an, const void *b, uint64_t bn) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return an > 0 && bn > 0 && x < y + bn && y < x + an;
+}
+
+}  // namespace lgn
+
+#ifdef __CUDACC__
+namespace lgn {
+__device__ __forceinline__ void dep_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void dep_wait()   { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+}  // namespace lgn
+#endif
