@@ -423,6 +423,68 @@ lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt,
                           uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt,
                           int accumulate, uint32_t *status_dev, void *stream);
 
+/* ---- Embedding lookup with scaling, and the gradient of the table ----
+ * out[t, :] = scale * table[id_t, :], formed in fp32 and rounded once; a row of zeros for an id outside
+ * [0, vocab) (the other ranks' ids, for a table split by vocabulary).
+ *   ids            device, `tokens` integers of ids_bits (32 or 64) bits
+ *   n_outside_dev  device, may be NULL: the number of ids outside the table is added to it
+ * Rows of table and out are ld_table and ld_out elements apart.  tokens and vocab up to 2^30 and 2^31 - 2. */
+lgn_status lgn_embedding(const void *table, uint64_t vocab, uint64_t dim, uint64_t ld_table, lgn_dtype table_dt,
+                         const void *ids, int ids_bits, uint64_t tokens, double scale,
+                         void *out, uint64_t ld_out, lgn_dtype out_dt, uint64_t *n_outside_dev, void *stream);
+
+/* dtable[v, :] = scale * sum of dout[t, :] over the tokens with id_t = v (+ dtable[v, :] if accumulate); tokens
+ * whose id is padding_idx or lies outside [0, vocab) are left out (padding_idx = -1: none is padding).
+ * Without accumulate every row of the table is written, rows without a token with zeros; with it
+ * those rows are not touched.  Sums in fp32, rounded once to table_dt, in an order that depends on
+ * the ids alone: the same inputs give the same bits.
+ *   ws  device scratch of lgn_embedding_grad_workspace_bytes(tokens, vocab, dim), 16-byte aligned
+ * Two launches, three for more than 32 tokens, no allocation. */
+size_t lgn_embedding_grad_workspace_bytes(uint64_t tokens, uint64_t vocab, uint64_t dim);
+lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn_dtype dout_dt,
+                              const void *ids, int ids_bits, uint64_t tokens,
+                              uint64_t vocab, uint64_t dim, double scale, int64_t padding_idx,
+                              void *dtable, uint64_t ld_table, lgn_dtype table_dt, int accumulate,
+                              void *ws, size_t ws_bytes, void *stream);
+
+/* ---- Global gradient norm over many tensors, and clipping ----
+ * norm = sqrt(sum of x^2 over all tensors); coef = max_norm / norm where the norm is finite and
+ * above max_norm, else 1; out = x coef in fp32, rounded once to the tensor's type.  Tensors of different types may
+ * be mixed, any element-aligned pointer is taken, n may be 0; out may be g itself (in place; nothing is written
+ * when coef is 1) or must not overlap it.  A norm that is not finite leaves the values as they are; the record
+ * says so.  Sums in a fixed order: the same bits on every run on the same type of device. */
+typedef struct {
+    const void *g;         /* device, n elements of dt                                  */
+    void       *out;       /* device, the same type; not used by lgn_grad_norm            */
+    uint64_t    n;         /* up to 2^40                                                */
+    int32_t     dt;        /* lgn_dtype                                                 */
+    int32_t     reserved;  /* 0                                                         */
+} lgn_grad_t;
+
+typedef struct {
+    float    norm;         /* sqrt(sum_sq) rounded to fp32                                      */
+    float    coef;         /* what the tensors were multiplied by (lgn_grad_norm: 1)             */
+    uint64_t n_nonfinite;  /* infinities and NaN among all values                               */
+    double   sum_sq;       /* sum of squares, fp64: what ranks with a shard each add up          */
+} lgn_norm_t;
+
+/* Scratch, in bytes, for `count` tensors.  0 for count < 0. */
+size_t lgn_clip_workspace_bytes(int count);
+
+/* The record only.   grads: host array.  record_dev: device, one lgn_norm_t, 8-byte aligned.  ws: device,
+ * 16-byte aligned.  Two launches for up to 512 tensors, one more for each further 512. */
+lgn_status lgn_grad_norm(const lgn_grad_t *grads, int count, lgn_norm_t *record_dev,
+                         void *ws, size_t ws_bytes, void *stream);
+
+/* The record, and every tensor scaled, without a host round trip.  max_norm >= 0.  Two launches per 512 tensors. */
+lgn_status lgn_clip_grad_norm(const lgn_grad_t *grads, int count, double max_norm, lgn_norm_t *record_dev,
+                              void *ws, size_t ws_bytes, void *stream);
+
+/* Every tensor scaled by the record's sum_sq (after lgn_grad_norm, and, for sharded gradients, a sum of that field over
+ * the ranks); norm and coef of the record are written anew.  One launch per 512 tensors. */
+lgn_status lgn_clip_apply(const lgn_grad_t *grads, int count, double max_norm, lgn_norm_t *record_dev,
+                          void *stream);
+
 /* Self-test of the bounded device-side wait (no counterpart in the paper).
  * Same arguments and the same work as lgn_compress_layers, except that one
  * statistics tile of layer 0 is withheld from the queue, so layer 0's closed form

@@ -66,6 +66,15 @@ class LayerResultT(C.Structure):
                 ("n_underflow", C.c_uint64)]
 
 
+class GradT(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("dt", C.c_int32), ("reserved", C.c_int32)]
+
+
+class NormT(C.Structure):
+    _fields_ = [("norm", C.c_float), ("coef", C.c_float), ("n_nonfinite", C.c_uint64), ("sum_sq", C.c_double)]
+
+
+assert C.sizeof(GradT) == 32 and C.sizeof(NormT) == 24
 assert C.sizeof(StatsT) == 48 and C.sizeof(LayerT) == 96 and C.sizeof(LayerResultT) == 120
 
 _vp, _u64, _sz, _dbl, _i32 = C.c_void_p, C.c_uint64, C.c_size_t, C.c_double, C.c_int
@@ -132,6 +141,20 @@ _lib.lgn_fp8_quantize.argtypes = [_vp, _u64, _u64, _u64, _i32, _i32, _i32, _vp, 
 _lib.lgn_fp8_quantize.restype = _i32
 _lib.lgn_fp8_matmul.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
 _lib.lgn_fp8_matmul.restype = _i32
+_lib.lgn_embedding.argtypes = [_vp, _u64, _u64, _u64, _i32, _vp, _i32, _u64, _dbl, _vp, _u64, _i32, _vp, _vp]
+_lib.lgn_embedding.restype = _i32
+_lib.lgn_embedding_grad_workspace_bytes.argtypes = [_u64, _u64, _u64]
+_lib.lgn_embedding_grad_workspace_bytes.restype = _sz
+_lib.lgn_embedding_grad.argtypes = [_vp, _u64, _i32, _vp, _i32, _u64, _u64, _u64, _dbl, C.c_int64, _vp, _u64, _i32, _i32, _vp, _sz, _vp]
+_lib.lgn_embedding_grad.restype = _i32
+_lib.lgn_clip_workspace_bytes.argtypes = [_i32]
+_lib.lgn_clip_workspace_bytes.restype = _sz
+_lib.lgn_grad_norm.argtypes = [C.POINTER(GradT), _i32, _vp, _vp, _sz, _vp]
+_lib.lgn_grad_norm.restype = _i32
+_lib.lgn_clip_grad_norm.argtypes = [C.POINTER(GradT), _i32, _dbl, _vp, _vp, _sz, _vp]
+_lib.lgn_clip_grad_norm.restype = _i32
+_lib.lgn_clip_apply.argtypes = [C.POINTER(GradT), _i32, _dbl, _vp, _vp]
+_lib.lgn_clip_apply.restype = _i32
 
 
 class LgnError(RuntimeError):
@@ -530,3 +553,126 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
                                out.data_ptr() or None, _matrix(out, "out"), dtype_code(out), 1 if accumulate else 0,
                                _dev(status, "status") if status is not None else None, _stream(stream)), "lgn_fp8_matmul")
     return out
+
+
+# --------------------------------------------------------------------------- embedding
+def _ids(ids: torch.Tensor) -> int:
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"ids are int32 or int64, got {ids.dtype}")
+    return 32 if ids.dtype == torch.int32 else 64
+
+
+def lgn_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                  out_dtype: Optional[torch.dtype] = None, n_outside: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """scale * table[ids], zeros for ids outside the table: ids.numel() x dim.  ``n_outside``: int64 CUDA tensor of
+    one element to which the number of ids outside the table is added."""
+    ld = _matrix(table, "table")
+    n, dim = ids.numel(), table.size(1)
+    if out is None:
+        out = torch.empty(n, dim, dtype=out_dtype or table.dtype, device=table.device)
+    elif tuple(out.shape) != (n, dim):
+        raise ValueError("out must be ids.numel() x dim")
+    if n_outside is not None and n_outside.dtype != torch.int64:
+        raise TypeError("n_outside is int64")
+    _check(_lib.lgn_embedding(table.data_ptr() or None, table.size(0), dim, ld, dtype_code(table),
+                              _dev(ids, "ids") or None, _ids(ids), n, float(scale), out.data_ptr() or None, _matrix(out, "out"),
+                              dtype_code(out), _dev(n_outside, "n_outside") if n_outside is not None else None, _stream(stream)),
+           "lgn_embedding")
+    return out
+
+
+def new_embedding_grad_workspace(tokens: int, vocab: int, dim: int, device) -> torch.Tensor:
+    return torch.empty(max(16, int(_lib.lgn_embedding_grad_workspace_bytes(tokens, vocab, dim))), dtype=torch.uint8, device=device)
+
+
+def lgn_embedding_grad(dout: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, padding_idx: int = -1,
+                       out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                       accumulate: bool = False, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of the table (vocab x dim) from ``dout`` (ids.numel() x dim); with ``accumulate`` added to ``out``."""
+    ld = _matrix(dout, "dout")
+    n, dim = dout.shape
+    if ids.numel() != n:
+        raise ValueError("dout must have one row per id")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty(vocab, dim, dtype=out_dtype, device=dout.device)
+    elif tuple(out.shape) != (vocab, dim):
+        raise ValueError("out must be vocab x dim")
+    if ws is None:
+        ws = new_embedding_grad_workspace(n, vocab, dim, dout.device)
+    _check(_lib.lgn_embedding_grad(dout.data_ptr() or None, ld, dtype_code(dout), _dev(ids, "ids") or None, _ids(ids), n, vocab, dim,
+                                   float(scale), int(padding_idx), out.data_ptr() or None, _matrix(out, "out"), dtype_code(out),
+                                   1 if accumulate else 0, _dev(ws, "ws"), ws.numel() * ws.element_size(), _stream(stream)),
+           "lgn_embedding_grad")
+    return out
+
+
+# --------------------------------------------------------------------------- gradient norm and clipping
+class Grads(NamedTuple):
+    """Descriptors of a list of tensors, kept from step to step as long as the tensors stay where they are."""
+    array: C.Array
+    count: int
+    tensors: tuple           # keeps them alive
+
+
+def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> Grads:
+    """``outs``: where the clipped gradients go, tensor by tensor; None: in place."""
+    outs = grads if outs is None else outs
+    if len(outs) != len(grads):
+        raise ValueError("one out per gradient")
+    arr = (GradT * max(1, len(grads)))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        if o.numel() != g.numel() or o.dtype != g.dtype:
+            raise ValueError("out must have its gradient's size and type")
+        arr[i] = GradT(_dev(g, "gradient") or None, _dev(o, "out") or None, g.numel(), dtype_code(g), 0)
+    return Grads(arr, len(grads), (tuple(grads), tuple(outs)))
+
+
+def new_norm_record(device) -> torch.Tensor:
+    return torch.zeros(C.sizeof(NormT), dtype=torch.uint8, device=device)
+
+
+def norm_of(record: torch.Tensor) -> torch.Tensor:
+    """The record's norm as a float32 scalar on the device (a view)."""
+    return record.view(torch.float32)[0]
+
+
+def sum_sq_of(record: torch.Tensor) -> torch.Tensor:
+    """The record's sum of squares as a float64 scalar on the device (a view): what sharded ranks all-reduce before
+    lgn_clip_apply."""
+    return record.view(torch.float64)[2]
+
+
+def read_norm_record(record: torch.Tensor) -> Dict[str, float]:
+    """Host copy of a record (synchronises)."""
+    r = NormT.from_buffer_copy(record.cpu().numpy().tobytes())
+    return {"norm": r.norm, "coef": r.coef, "n_nonfinite": r.n_nonfinite, "sum_sq": r.sum_sq}
+
+
+def new_clip_workspace(device, count: int = 512) -> torch.Tensor:
+    return torch.empty(int(_lib.lgn_clip_workspace_bytes(count)), dtype=torch.uint8, device=device)
+
+
+def _record(record: torch.Tensor) -> int:
+    if record.numel() * record.element_size() < C.sizeof(NormT):
+        raise ValueError("record too small")
+    return _dev(record, "record")
+
+
+def lgn_grad_norm(grads: Grads, record: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """The record of the tensors' global norm; nothing is scaled."""
+    _check(_lib.lgn_grad_norm(grads.array, grads.count, _record(record), _dev(ws, "ws"), ws.numel() * ws.element_size(),
+                              _stream(stream)), "lgn_grad_norm")
+
+
+def lgn_clip_grad_norm(grads: Grads, max_norm: float, record: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """The record, and every tensor scaled by min(1, max_norm / norm); no host round trip."""
+    _check(_lib.lgn_clip_grad_norm(grads.array, grads.count, float(max_norm), _record(record), _dev(ws, "ws"),
+                                   ws.numel() * ws.element_size(), _stream(stream)), "lgn_clip_grad_norm")
+
+
+def lgn_clip_apply(grads: Grads, max_norm: float, record: torch.Tensor, stream=None) -> None:
+    """Every tensor scaled by the norm that the record's sum of squares gives."""
+    _check(_lib.lgn_clip_apply(grads.array, grads.count, float(max_norm), _record(record), _stream(stream)), "lgn_clip_apply")

@@ -1,0 +1,410 @@
+// Global gradient norm over many tensors, and clipping.
+//
+//   S = sum over all tensors of x^2,  norm = sqrt(S),  coef = min(1, max_norm / norm),  out = round(x coef).
+//
+// Bound by memory: every gradient is read for the sum and read again (from L2 for what still lies there) to
+// be scaled.  Two launches for up to kClipPerLaunch tensors: the first leaves one partial sum per CTA in the
+// workspace; every CTA of the second adds all of them in the same order, forms the coefficient itself and
+// scales its share, so that no grid-wide wait is needed.  The descriptors travel in the
+// kernels' parameters.
+//
+// Squares are formed and added in fp32 over one 32-byte chunk (8 or 16 values) and carried in fp64 from there
+// on.  A chunk whose fp32 sum is not within [2^-80, inf), where squares may have overflowed or lost their
+// low end, is added again in fp64, value by value; there the non-finite values are counted too.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "lgn.h"
+#include "lgn_launch.h"
+#include "lgn_log.h"
+
+namespace lgn {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipTileBytes = 32768;              // 4 chunks of 32 bytes per thread
+constexpr int kClipPerLaunch = 512;                // tensors described in one launch's parameters
+constexpr int kClipSmallList = 64;                 // ... in the parameters of the small form
+constexpr uint32_t kClipSlots = 1024;              // partial sums per launch
+
+struct ClipPartial { double sum; unsigned long long bad; };
+
+template <int N> struct ClipList {
+    const char *g[N];
+    char *out[N];
+    uint64_t n[N];                                 // elements; bit 63: bf16
+    uint32_t first[N];                             // first tile
+    uint32_t count, tiles;
+};
+
+// A tensor's tiles are cut at multiples of the tile size from the 32-byte boundary at or below its first
+// element, so that every chunk but the first and last is whole and aligned.
+struct ClipTensor {
+    const char *g;
+    char *out;
+    uint64_t n;
+    uint32_t es, lead;                             // element size; bytes between the boundary and the first element
+};
+
+template <int N>
+__device__ __forceinline__ ClipTensor clip_tensor(const ClipList<N> &l, uint32_t i) {
+    ClipTensor t;
+    t.g = l.g[i];
+    t.out = l.out[i];
+    t.es = l.n[i] >> 63 ? 2u : 4u;
+    t.n = l.n[i] & ~(1ull << 63);
+    t.lead = (uint32_t)(reinterpret_cast<uintptr_t>(t.g) & 31u);
+    return t;
+}
+
+template <int N>
+__device__ __forceinline__ uint32_t clip_find(const ClipList<N> &l, uint32_t tile) {     // the tensor a tile lies in
+    uint32_t lo = 0, hi = l.count;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (l.first[mid] <= tile) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+struct Words { uint32_t w[8]; };
+
+__device__ __forceinline__ Words load_words(const char *p) {
+    Words c;
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(c.w[0]), "=r"(c.w[1]), "=r"(c.w[2]), "=r"(c.w[3]), "=r"(c.w[4]), "=r"(c.w[5]), "=r"(c.w[6]), "=r"(c.w[7]) : "l"(p) : "memory");
+    return c;
+}
+__device__ __forceinline__ void store_words(char *p, const Words &c) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "r"(c.w[0]), "r"(c.w[1]), "r"(c.w[2]), "r"(c.w[3]), "r"(c.w[4]), "r"(c.w[5]), "r"(c.w[6]), "r"(c.w[7]) : "memory");
+}
+
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+__device__ __noinline__ void add_exactly(const Words &c, uint32_t es, double &sum, unsigned long long &bad) {
+    for (int k = 0; k < 8; ++k) {
+        const float a = es == 4 ? __uint_as_float(c.w[k]) : bf_lo(c.w[k]), b = es == 4 ? 0.0f : bf_hi(c.w[k]);
+        sum += (double)a * (double)a + (double)b * (double)b;
+        bad += (isfinite(a) ? 0 : 1) + (isfinite(b) ? 0 : 1);
+    }
+}
+
+__device__ __forceinline__ void add_chunk(const Words &c, uint32_t es, double &sum, unsigned long long &bad) {
+    float s = 0.0f;
+    if (es == 4) {
+        float t = 0.0f;
+        #pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            s = fmaf(__uint_as_float(c.w[k]), __uint_as_float(c.w[k]), s);
+            t = fmaf(__uint_as_float(c.w[k + 1]), __uint_as_float(c.w[k + 1]), t);
+        }
+        s += t;
+    } else {
+        float t = 0.0f;
+        #pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            s = fmaf(bf_lo(c.w[k]), bf_lo(c.w[k]), s);
+            t = fmaf(bf_hi(c.w[k]), bf_hi(c.w[k]), t);
+        }
+        s += t;
+    }
+    if (s >= 0x1p-80f && s < __int_as_float(0x7f800000)) sum += (double)s;
+    else add_exactly(c, es, sum, bad);
+}
+
+__device__ __forceinline__ float load_elem(const char *p, uint32_t es) {
+    return es == 4 ? *reinterpret_cast<const float *>(p) : __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short *>(p) << 16);
+}
+
+// Chunk number c of a tensor with the values outside it as zeros.
+__device__ __noinline__ Words load_edge(const ClipTensor &t, uint64_t c) {
+    Words w;
+    for (int k = 0; k < 8; ++k) w.w[k] = 0u;
+    const int64_t b0 = (int64_t)(c * 32) - t.lead, end = (int64_t)(t.n * t.es);          // byte offset from the first element
+    for (int b = 0; b < 32; b += (int)t.es) {
+        const int64_t at = b0 + b;
+        if (at < 0 || at >= end) continue;
+        if (t.es == 4) w.w[b >> 2] = *reinterpret_cast<const uint32_t *>(t.g + at);
+        else w.w[b >> 2] |= (uint32_t)*reinterpret_cast<const unsigned short *>(t.g + at) << (8 * (b & 2));
+    }
+    return w;
+}
+
+__device__ __forceinline__ double block_sum(double v, unsigned long long &bad, double *sh, unsigned long long *shb) {
+    #pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        v += __shfl_down_sync(0xffffffffu, v, d);
+        bad += __shfl_down_sync(0xffffffffu, bad, d);
+    }
+    if ((threadIdx.x & 31) == 0) { sh[threadIdx.x >> 5] = v; shb[threadIdx.x >> 5] = bad; }
+    __syncthreads();
+    double s = 0.0;
+    unsigned long long b = 0;
+    #pragma unroll
+    for (int w = 0; w < kClipThreads / 32; ++w) { s += sh[w]; b += shb[w]; }
+    bad = b;
+    return s;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads)
+norm_kernel(const __grid_constant__ ClipList<N> l, ClipPartial *part) {
+    __shared__ double sh[kClipThreads / 32];
+    __shared__ unsigned long long shb[kClipThreads / 32];
+    dep_launch();
+    dep_wait();
+    const uint32_t t0 = (uint32_t)((uint64_t)l.tiles * blockIdx.x / gridDim.x), t1 = (uint32_t)((uint64_t)l.tiles * (blockIdx.x + 1) / gridDim.x);
+    double sum = 0.0;
+    unsigned long long bad = 0;
+    if (t0 < t1) {
+        uint32_t i = clip_find(l, t0);
+        for (uint32_t t = t0; t < t1;) {
+            const ClipTensor x = clip_tensor(l, i);
+            const uint32_t next = i + 1 < l.count ? l.first[i + 1] : l.tiles, stop = min(t1, next);
+            const uint64_t bytes = x.lead + x.n * x.es, whole = bytes / 32;          // chunks [1 if lead, whole) lie inside
+            const char *base = x.g - x.lead;
+            for (; t < stop; ++t) {
+                const uint64_t c0 = (uint64_t)(t - l.first[i]) * (kClipTileBytes / 32) + threadIdx.x;
+                Words c[4];
+                bool in[4];
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint64_t at = c0 + k * kClipThreads;
+                    in[k] = at < whole && !(at == 0 && x.lead != 0);
+                    if (in[k]) c[k] = load_words(base + at * 32);
+                }
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint64_t at = c0 + k * kClipThreads;
+                    if (in[k]) add_chunk(c[k], x.es, sum, bad);
+                    else if (at * 32 < bytes) add_exactly(load_edge(x, at), x.es, sum, bad);
+                }
+            }
+            ++i;
+        }
+    }
+    sum = block_sum(sum, bad, sh, shb);
+    if (threadIdx.x == 0) { part[blockIdx.x].sum = sum; part[blockIdx.x].bad = bad; }
+}
+
+__device__ __forceinline__ float clip_coef(double sum, double max_norm, bool clip) {
+    const double norm = sqrt(sum);
+    return clip && norm > max_norm && norm < __longlong_as_double(0x7ff0000000000000ll) ? (float)(max_norm / norm) : 1.0f;
+}
+
+__device__ __forceinline__ Words scaled_words(const Words &c, uint32_t es, float coef) {
+    Words r;
+    #pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if (es == 4) r.w[k] = __float_as_uint(__uint_as_float(c.w[k]) * coef);
+        else {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(bf_lo(c.w[k]) * coef, bf_hi(c.w[k]) * coef);
+            r.w[k] = *reinterpret_cast<const uint32_t *>(&p);
+        }
+    }
+    return r;
+}
+
+// SCALE: scale (or, for a coefficient of 1, copy) every tensor; otherwise only the record is written.
+// from_record: the sum is the record's (which a caller may have reduced over ranks), not the partial sums'.
+template <int N, bool SCALE>
+__global__ void __launch_bounds__(kClipThreads)
+clip_kernel(const __grid_constant__ ClipList<N> l, const ClipPartial *part, uint32_t nparts, double max_norm,
+            uint32_t clip, uint32_t from_record, uint32_t write_record, lgn_norm_t *record) {
+    __shared__ double sh[kClipThreads / 32];
+    __shared__ unsigned long long shb[kClipThreads / 32];
+    dep_wait();
+    double sum = 0.0;
+    unsigned long long bad = 0;
+    if (from_record) {
+        sum = record->sum_sq;
+        bad = record->n_nonfinite;
+    } else {
+        for (uint32_t i = threadIdx.x; i < nparts; i += kClipThreads) { sum += part[i].sum; bad += part[i].bad; }
+        sum = block_sum(sum, bad, sh, shb);
+    }
+    const float coef = clip_coef(sum, max_norm, clip != 0);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && write_record) {
+        record->norm = (float)sqrt(sum);
+        record->coef = coef;
+        if (!from_record) { record->n_nonfinite = bad; record->sum_sq = sum; }
+    }
+    if constexpr (SCALE) {
+        // from the last tile to the first: the order in which L2 still holds them
+        const uint32_t t0 = (uint32_t)((uint64_t)l.tiles * blockIdx.x / gridDim.x), t1 = (uint32_t)((uint64_t)l.tiles * (blockIdx.x + 1) / gridDim.x);
+        if (t0 >= t1) return;
+        uint32_t i = clip_find(l, t1 - 1);
+        for (uint32_t t = t1; t > t0;) {
+            const ClipTensor x = clip_tensor(l, i);
+            const uint32_t stop = max(t0, l.first[i]);
+            const uint64_t bytes = x.lead + x.n * x.es, whole = bytes / 32;
+            const char *base = x.g - x.lead;
+            char *obase = x.out - x.lead;
+            const bool skip = coef == 1.0f && x.out == x.g, same = ((reinterpret_cast<uintptr_t>(x.out) ^ reinterpret_cast<uintptr_t>(x.g)) & 31u) == 0;
+            if (skip) { t = stop; --i; continue; }
+            for (; t > stop; --t) {
+                const uint64_t c0 = (uint64_t)(t - 1 - l.first[i]) * (kClipTileBytes / 32) + threadIdx.x;
+                Words c[4];
+                bool in[4];
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint64_t at = c0 + k * kClipThreads;
+                    in[k] = same && at < whole && !(at == 0 && x.lead != 0);
+                    if (in[k]) c[k] = load_words(base + at * 32);
+                }
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint64_t at = c0 + k * kClipThreads;
+                    if (in[k]) store_words(obase + at * 32, scaled_words(c[k], x.es, coef));
+                    else if (same && at * 32 < bytes) {                       // first or last chunk: value by value
+                        const int64_t b0 = (int64_t)(at * 32) - x.lead, end = (int64_t)(x.n * x.es);
+                        for (int b = 0; b < 32; b += (int)x.es) {
+                            const int64_t p = b0 + b;
+                            if (p < 0 || p >= end) continue;
+                            const float v = load_elem(x.g + p, x.es) * coef;
+                            if (x.es == 4) *reinterpret_cast<float *>(x.out + p) = v;
+                            else *reinterpret_cast<__nv_bfloat16 *>(x.out + p) = __float2bfloat16_rn(v);
+                        }
+                    }
+                }
+                if (!same) {                                                  // input and output aligned differently: value by value, coalesced
+                    const int64_t lo = (int64_t)(t - 1 - l.first[i]) * kClipTileBytes - x.lead, hi = lo + kClipTileBytes;
+                    const int64_t from = lo < 0 ? 0 : lo, to = hi < (int64_t)(x.n * x.es) ? hi : (int64_t)(x.n * x.es);
+                    for (int64_t p = from + (int64_t)threadIdx.x * x.es; p < to; p += (int64_t)kClipThreads * x.es) {
+                        const float v = load_elem(x.g + p, x.es) * coef;
+                        if (x.es == 4) *reinterpret_cast<float *>(x.out + p) = v;
+                        else *reinterpret_cast<__nv_bfloat16 *>(x.out + p) = __float2bfloat16_rn(v);
+                    }
+                }
+            }
+            --i;
+        }
+    }
+}
+
+template <int N>
+static void fill_list(ClipList<N> &l, const lgn_grad_t *grads, int count) {
+    uint32_t tiles = 0, c = 0;
+    for (int i = 0; i < count; ++i) {
+        if (grads[i].n == 0) continue;
+        const uint64_t es = grads[i].dt == LGN_BF16 ? 2 : 4;
+        l.g[c] = static_cast<const char *>(grads[i].g);
+        l.out[c] = static_cast<char *>(grads[i].out);
+        l.n[c] = grads[i].n | (grads[i].dt == LGN_BF16 ? 1ull << 63 : 0ull);
+        l.first[c] = tiles;
+        tiles += (uint32_t)(((reinterpret_cast<uintptr_t>(grads[i].g) & 31u) + grads[i].n * es + kClipTileBytes - 1) / kClipTileBytes);
+        ++c;
+    }
+    l.count = c;
+    l.tiles = tiles;
+}
+
+struct ClipCall {
+    double max_norm;
+    uint32_t clip, from_record;
+    bool norm, scale;
+    lgn_norm_t *record;
+    ClipPartial *part;
+    void *stream;
+    int sms;
+};
+
+template <int N>
+static lgn_status run_pass(const lgn_grad_t *grads, int count, const ClipCall &k, bool second, uint32_t slot, uint32_t &slots, bool write_record, uint32_t nparts) {
+    ClipList<N> l;
+    fill_list(l, grads, count);
+    uint32_t grid = (uint32_t)(k.sms * 4 < (int)kClipSlots ? k.sms * 4 : (int)kClipSlots);
+    if (l.tiles < grid) grid = l.tiles;
+    if (grid < 1) grid = 1;
+    if (!second) {
+        ClipPartial *part = k.part + slot;
+        void *args[] = {&l, &part};
+        slots = grid;
+        return launch_dependent(reinterpret_cast<const void *>(&norm_kernel<N>), dim3(grid), dim3(kClipThreads), args, 0, k.stream);
+    }
+    const ClipPartial *part = k.part;
+    double max_norm = k.max_norm;
+    uint32_t clip = k.clip, from = k.from_record, write = write_record;
+    lgn_norm_t *record = k.record;
+    void *args[] = {&l, &part, &nparts, &max_norm, &clip, &from, &write, &record};
+    if (k.scale) return launch_dependent(reinterpret_cast<const void *>(&clip_kernel<N, true>), dim3(grid), dim3(kClipThreads), args, 0, k.stream);
+    return launch_dependent(reinterpret_cast<const void *>(&clip_kernel<N, false>), dim3(1), dim3(kClipThreads), args, 0, k.stream);
+}
+
+static lgn_status run_clip(const lgn_grad_t *grads, int count, const ClipCall &k) {
+    uint32_t slot = 0, slots = 0;
+    for (int pass = k.norm ? 0 : 1; pass < 2; ++pass) {
+        for (int i = 0; i == 0 || i < count; i += kClipPerLaunch) {
+            const int c = count - i < kClipPerLaunch ? count - i : kClipPerLaunch;
+            const lgn_status s = c <= kClipSmallList ? run_pass<kClipSmallList>(grads + i, c, k, pass == 1, slot, slots, i == 0, slot)
+                                                     : run_pass<kClipPerLaunch>(grads + i, c, k, pass == 1, slot, slots, i == 0, slot);
+            if (s != LGN_OK) return s;
+            if (pass == 0) slot += slots;
+            else if (!k.scale) break;
+        }
+    }
+    return LGN_OK;
+}
+
+static lgn_status check_grads(const lgn_grad_t *grads, int count, bool with_out) {
+    if (count < 0 || (count > 0 && grads == nullptr)) return LGN_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        const lgn_grad_t &x = grads[i];
+        if ((x.dt != LGN_F32 && x.dt != LGN_BF16) || x.reserved != 0) return LGN_ERR_INVALID_ARG;
+        if (x.n > (1ull << 40)) return LGN_ERR_UNSUPPORTED;
+        if (x.n == 0) continue;
+        const uint64_t es = x.dt == LGN_BF16 ? 2 : 4;
+        if (x.g == nullptr || !aligned_to(x.g, es)) return LGN_ERR_INVALID_ARG;
+        if (!with_out) continue;
+        if (x.out == nullptr || !aligned_to(x.out, es)) return LGN_ERR_INVALID_ARG;
+        if (x.out != x.g && ranges_overlap(x.g, x.n * es, x.out, x.n * es)) return LGN_ERR_INVALID_ARG;
+    }
+    // the tile numbers of one launch are 32 bits wide
+    for (int i = 0; i < count; i += kClipPerLaunch) {
+        uint64_t tiles = 0;
+        for (int j = i; j < count && j < i + kClipPerLaunch; ++j) tiles += (grads[j].n * (grads[j].dt == LGN_BF16 ? 2 : 4)) / kClipTileBytes + 2;
+        if (tiles > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
+    }
+    return LGN_OK;
+}
+
+}  // namespace lgn
+
+using namespace lgn;
+
+extern "C" size_t lgn_clip_workspace_bytes(int count) {
+    if (count < 0) return 0;
+    const size_t launches = count == 0 ? 1 : ((size_t)count + kClipPerLaunch - 1) / kClipPerLaunch;
+    return launches * kClipSlots * sizeof(ClipPartial);
+}
+
+static lgn_status norm_and_clip(const lgn_grad_t *grads, int count, double max_norm, bool clip, lgn_norm_t *record, void *ws, size_t ws_bytes, void *stream) {
+    const lgn_status s = check_grads(grads, count, clip);
+    if (s != LGN_OK) return s;
+    if (clip && !(max_norm >= 0.0)) return LGN_ERR_INVALID_ARG;
+    if (record == nullptr || !aligned_to(record, 8) || ws == nullptr || !aligned_to(ws, 16)) return LGN_ERR_INVALID_ARG;
+    if (ws_bytes < lgn_clip_workspace_bytes(count)) return LGN_ERR_WORKSPACE;
+    const int sms = sm_count();
+    if (sms < 1) return LGN_ERR_CUDA;
+    const ClipCall k = {max_norm, clip, 0, true, clip, record, static_cast<ClipPartial *>(ws), stream, sms};
+    return run_clip(grads, count, k);
+}
+
+extern "C" lgn_status lgn_grad_norm(const lgn_grad_t *grads, int count, lgn_norm_t *record_dev, void *ws, size_t ws_bytes, void *stream) {
+    return norm_and_clip(grads, count, 0.0, false, record_dev, ws, ws_bytes, stream);
+}
+
+extern "C" lgn_status lgn_clip_grad_norm(const lgn_grad_t *grads, int count, double max_norm, lgn_norm_t *record_dev, void *ws, size_t ws_bytes, void *stream) {
+    return norm_and_clip(grads, count, max_norm, true, record_dev, ws, ws_bytes, stream);
+}
+
+extern "C" lgn_status lgn_clip_apply(const lgn_grad_t *grads, int count, double max_norm, lgn_norm_t *record_dev, void *stream) {
+    const lgn_status s = check_grads(grads, count, true);
+    if (s != LGN_OK) return s;
+    if (!(max_norm >= 0.0) || record_dev == nullptr || !aligned_to(record_dev, 8)) return LGN_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms < 1) return LGN_ERR_CUDA;
+    const ClipCall k = {max_norm, 1, 1, false, true, record_dev, nullptr, stream, sms};
+    return run_clip(grads, count, k);
+}

@@ -86,8 +86,8 @@ __device__ __forceinline__ void load_values(const char *p, int valid, float *x) 
     for (int k = 0; k < N; ++k) {
         x[k] = 0.0f;
         if (k < valid) {
-            if constexpr (DT == LGN_F32) x[k] = __ldg(reinterpret_cast<const float *>(p) + k);
-            else x[k] = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const unsigned short *>(p) + k) << 16);
+            if constexpr (DT == LGN_F32) x[k] = __uint_as_float(ldro_u32(p + 4 * k));
+            else x[k] = __uint_as_float(ldro_u16(p + 2 * k) << 16);
         }
     }
 }

@@ -54,5 +54,23 @@ inline bool ranges_overlap(const void *a, uint64_t an, const void *b, uint64_t b
 namespace lgn {
 __device__ __forceinline__ void dep_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void dep_wait()   { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Read-only loads that stay behind dep_wait(): the compiler may move a plain load of memory it takes to be
+// constant for the kernel's whole run (__ldg, const __restrict__) across it.
+__device__ __forceinline__ uint32_t ldro_u32(const void *p) {
+    uint32_t v;
+    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint64_t ldro_u64(const void *p) {
+    uint64_t v;
+    asm volatile("ld.global.nc.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ldro_u16(const void *p) {
+    uint16_t v;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(v) : "l"(p) : "memory");
+    return v;
+}
 }  // namespace lgn
 #endif
