@@ -157,6 +157,11 @@ _lib.lgn_clip_apply.argtypes = [C.POINTER(GradT), _i32, _dbl, _vp, _vp]
 _lib.lgn_clip_apply.restype = _i32
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+_uint8 = torch.uint8
+_DT_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 class LgnError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -174,11 +179,10 @@ def raw():
 
 
 def dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"gradient tensors are float32 or bfloat16, got {t.dtype}")
+    code = _DT_CODE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"gradient tensors are float32 or bfloat16, got {t.dtype}")
+    return code
 
 
 def _dev(t: torch.Tensor, what: str) -> int:
@@ -190,8 +194,8 @@ def _dev(t: torch.Tensor, what: str) -> int:
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:          # the current stream of the current device, without a Stream object (3.5 us -> 0.2 us a call)
+        return _raw_stream(_current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -499,17 +503,37 @@ def _matrix(t: torch.Tensor, what: str) -> int:
     """Leading dimension of a CUDA matrix whose rows are contiguous."""
     if not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor")
-    if t.dim() != 2 or (t.size(1) > 1 and t.stride(1) != 1):
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{what} must be a matrix with contiguous rows")
-    ld = t.stride(0) if t.size(0) > 1 else max(1, t.size(1))
-    if ld < t.size(1):
+    rows, cols = shape
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    if rows <= 1:
+        return cols or 1
+    if ld < cols:
         raise ValueError(f"{what} must have rows that do not overlap")
     return ld
 
 
+def _fp8_bytes(rows: int, k: int) -> Tuple[int, int]:
+    """lgn_fp8_codes_bytes and lgn_fp8_scales_bytes, without two calls into the library."""
+    return rows * ((k + 15) & -16), ((rows + 127) >> 7) * ((k + 511) >> 9) * 512
+
+
 def new_fp8_operand(rows: int, k: int, fmt: int, device) -> Fp8Operand:
-    return Fp8Operand(torch.empty(max(16, _lib.lgn_fp8_codes_bytes(rows, k)), dtype=torch.uint8, device=device),
-                      torch.empty(max(16, _lib.lgn_fp8_scales_bytes(rows, k)), dtype=torch.uint8, device=device), rows, k, fmt)
+    codes, scales = _fp8_bytes(rows, k)
+    return Fp8Operand(torch.empty(codes or 16, dtype=_uint8, device=device),
+                      torch.empty(scales or 16, dtype=_uint8, device=device), rows, k, fmt)
+
+
+def _check_operand(o: Fp8Operand, what: str) -> None:
+    codes, scales = _fp8_bytes(o.rows, o.k)
+    if not (o.codes.is_cuda and o.scales.is_cuda and o.codes.is_contiguous() and o.scales.is_contiguous()):
+        raise ValueError(f"{what} must hold contiguous CUDA tensors")
+    if o.codes.nbytes < codes or o.scales.nbytes < scales:
+        raise ValueError(f"{what} is shorter than its extents")
 
 
 def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, rowwise: bool = True,
@@ -521,15 +545,27 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
     rows, cols = x.shape
     if not (rowwise or transposed):
         raise ValueError("neither the operand nor its transpose is asked for")
-    q = (out if out is not None else new_fp8_operand(rows, cols, fmt, x.device)) if rowwise else None
-    t = (out_t if out_t is not None else new_fp8_operand(cols, rows, fmt, x.device)) if transposed else None
-    for o, shape in ((q, (rows, cols, fmt)), (t, (cols, rows, fmt))):
-        if o is not None and tuple(o[2:]) != shape:
-            raise ValueError("out: extents or format differ from the matrix")
-    _check(_lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), int(fmt), int(block),
-                                 _dev(q.codes, "codes") if q else None, _dev(q.scales, "scales") if q else None,
-                                 _dev(t.codes, "codes_t") if t else None, _dev(t.scales, "scales_t") if t else None,
-                                 _stream(stream)), "lgn_fp8_quantize")
+    q = t = pq = sq = pt = st = None
+    if rowwise:
+        if out is None:
+            q = new_fp8_operand(rows, cols, fmt, x.device)
+        else:
+            q = out
+            if (q.rows, q.k, q.fmt) != (rows, cols, fmt):
+                raise ValueError("out: extents or format differ from the matrix")
+            _check_operand(q, "out")
+        pq, sq = q.codes.data_ptr(), q.scales.data_ptr()
+    if transposed:
+        if out_t is None:
+            t = new_fp8_operand(cols, rows, fmt, x.device)
+        else:
+            t = out_t
+            if (t.rows, t.k, t.fmt) != (cols, rows, fmt):
+                raise ValueError("out_t: extents or format differ from the transpose")
+            _check_operand(t, "out_t")
+        pt, st = t.codes.data_ptr(), t.scales.data_ptr()
+    _check(_lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), fmt, block, pq, sq, pt, st, _stream(stream)),
+           "lgn_fp8_quantize")
     return q, t
 
 
@@ -537,20 +573,22 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
                    out_dtype: torch.dtype = torch.bfloat16, accumulate: bool = False,
                    status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[i, j] = sum over c of a[i, c] b[j, c] (+ out[i, j] with ``accumulate``)."""
-    if a.k != b.k:
+    m, k, n = a.rows, a.k, b.rows
+    if k != b.k:
         raise ValueError("operands contract over different extents")
+    _check_operand(a, "a")
+    _check_operand(b, "b")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty(a.rows, b.rows, dtype=out_dtype, device=a.codes.device)
-    elif tuple(out.shape) != (a.rows, b.rows):
-        raise ValueError("out must be a.rows x b.rows")
-    for o in (a, b):
-        if o.codes.numel() < _lib.lgn_fp8_codes_bytes(o.rows, o.k) or o.scales.numel() < _lib.lgn_fp8_scales_bytes(o.rows, o.k):
-            raise ValueError("operand shorter than its extents")
-    _check(_lib.lgn_fp8_matmul(_dev(a.codes, "a.codes"), _dev(a.scales, "a.scales"), a.fmt,
-                               _dev(b.codes, "b.codes"), _dev(b.scales, "b.scales"), b.fmt, a.rows, b.rows, a.k,
-                               out.data_ptr() or None, _matrix(out, "out"), dtype_code(out), 1 if accumulate else 0,
+        out = torch.empty((m, n), dtype=out_dtype, device=a.codes.device)
+        ldo = n or 1
+    else:
+        if tuple(out.shape) != (m, n):
+            raise ValueError("out must be a.rows x b.rows")
+        ldo = _matrix(out, "out")
+    _check(_lib.lgn_fp8_matmul(a.codes.data_ptr(), a.scales.data_ptr(), a.fmt, b.codes.data_ptr(), b.scales.data_ptr(), b.fmt,
+                               m, n, k, out.data_ptr() or None, ldo, dtype_code(out), 1 if accumulate else 0,
                                _dev(status, "status") if status is not None else None, _stream(stream)), "lgn_fp8_matmul")
     return out
 

@@ -6,15 +6,25 @@
 // byte.  Products and sums stay in fp32 in tensor memory over the whole of k and are rounded once, to the
 // output's type.
 //
-// One CTA works on tiles of 128 rows of one operand ("rows") by BN rows of the other ("cols"):
-//   warp 4  brings 128 x 128 and BN x 128 bytes of codes per step of k into a ring of shared-memory stages
-//           (TMA, 128-byte swizzle) and, every fourth step, the 512-byte scale tiles of four blocks;
-//   warp 5  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step;
-//   warps 0..3  read the finished tile from tensor memory, round and store.
-// Forms: persistent over tiles, or (SPLIT) one tile per cluster with the CTAs of a cluster taking
+// Two kernels share one shape.  fp8_pair_kernel, for large products: two CTAs (one SM each) work on a tile of
+// 256 rows of one operand ("rows") by BN rows of the other ("cols"), each CTA bringing its own 128 rows and one half
+// of the BN, so that a step of k (128) costs an SM 32 KiB of shared-memory writes and as many operand reads for 512
+// clocks of MMA.  A single CTA's 128 x 192 tile needs 1.7 times that traffic per flop and stops at 54 % of the tensor
+// pipe (8192 x 8192 x 4096: 258 us, bound by shared memory).  fp8_matmul_kernel, for small ones: one CTA per tile of
+// 128 x BN, persistent over tiles, or (SPLIT) one tile per cluster with the CTAs of a cluster taking
 // consecutive shares of k and adding their fp32 tiles through distributed shared memory in rank order.
+//   warp 8  brings codes into a ring of shared-memory stages (TMA, 128-byte swizzle) and, every fourth step, the
+//           512-byte scale tiles of four blocks;
+//   warp 9  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step;
+//   warps 0..7  read the finished tile from tensor memory (warp w: lanes 32 (w mod 4) on, column half w / 4), round
+//           and store.
 // SWAP: `rows` runs along the contiguous dimension of the output, so that the 32 lanes of a warp, which hold
 // 32 rows, write contiguous memory whatever the alignment.
+//
+// fp32 outputs: the tensor cores' additions truncate, which biases a sum towards zero by about 2e-10 of its
+// size per k (measured: 2.0e-7 at k = 1024, 1e-6 and more from 8192).  Every 1024 k the tile is therefore added to sums in
+// registers (round to nearest) and a fresh one begun in the other half of tensor memory; the error then stays at
+// 3e-7 whatever k.  For bf16 outputs, rounded at 2e-3, the sum stays in tensor memory.
 //
 // Every wait is bounded: one that runs out raises a flag on which all roles stop; the copies and MMAs in
 // flight are waited for (bounded too), tensor memory is freed and the kernel ends with *status set.
@@ -31,7 +41,8 @@
 
 namespace lgn {
 
-constexpr int kMmThreads = 192;
+constexpr int kMmThreads = 320;                // warps 0..7: epilogue, 8: copies, 9: MMA
+constexpr int kMmEpiThreads = 256;
 constexpr int kMmGroupRows = 16;                 // row tiles walked before the next column tile (L2 reuse)
 constexpr long long kMmWaitClocks = 4000000000ll;   // about two seconds
 
@@ -45,14 +56,18 @@ struct MmArgs {
     uint32_t tiles_r, tiles_c;
     uint32_t fmt_rows, fmt_cols;
     uint32_t split_groups;                       // groups of four blocks per CTA of a cluster
-    uint32_t accumulate, vec;
+    uint32_t accumulate;
 };
 
-template <int BN> struct MmShape {
+constexpr uint32_t kMmChunk = 8;                 // steps of k (128 each) that stay in tensor memory, fp32 outputs
+
+// CTAS: 1 (fp8_matmul_kernel) or 2 (fp8_pair_kernel); bytes and stages per CTA.
+template <int BN, int CTAS> struct MmShape {
     static constexpr int kColBlocks = BN <= 128 ? 1 : 2;            // 128-row scale tiles a column tile touches
-    static constexpr int kStageBytes = 128 * 128 + BN * 128;
+    static constexpr int kStageBytes = 128 * 128 + BN / CTAS * 128;
     static constexpr int kScaleBytes = 512 * (1 + kColBlocks);
-    static constexpr int kStages = (int)((220 * 1024) / (kStageBytes + kScaleBytes)) > 8 ? 8 : (int)((220 * 1024) / (kStageBytes + kScaleBytes));
+    static constexpr int kFit = (int)((220 * 1024) / (kStageBytes + kScaleBytes));
+    static constexpr int kStages = kFit > 8 ? 8 : kFit;
     static constexpr int kAccs = BN <= 192 ? 2 : 1;                 // accumulator tiles in tensor memory
     static constexpr int kScaleCol = kAccs * BN;                    // first tensor-memory column of the scales
     static constexpr int kScaleCols = 4 * (1 + kColBlocks);
@@ -204,10 +219,92 @@ __device__ __forceinline__ void store_run(void *out, uint64_t i, float *v, bool 
 
 enum MmForm { kFormRows = 0, kFormSwap = 1, kFormSplit = 2 };
 
+// 32 values `step` elements apart from element i on, of which the first `count` exist; eight at a time, so that few
+// addresses and old values are live at once.
+template <int ODT>
+__device__ __forceinline__ void store_strided(void *out, uint64_t i, uint64_t step, uint32_t count, float *v, bool accumulate) {
+    #pragma unroll
+    for (int k = 0; k < 32; k += 8) {
+        if (accumulate) {
+            #pragma unroll
+            for (int j = 0; j < 8; ++j) if (k + j < (int)count) v[k + j] += load_out<ODT>(out, i + j * step);
+        }
+        #pragma unroll
+        for (int j = 0; j < 8; ++j) if (k + j < (int)count) store_out<ODT>(out, i + j * step, v[k + j]);
+        i += 8 * step;
+        asm volatile("" ::: "memory");
+    }
+}
+
+// 32 columns c .. c + 31 of row r of the output tile, held by one lane.
+template <int FORM, int ODT>
+__device__ __forceinline__ void store_columns(const MmArgs &p, uint32_t r, uint32_t c, float *v) {
+    if (r >= p.rows || c >= p.cols) return;
+    const uint32_t count = min(32u, p.cols - c);
+    if constexpr (FORM == kFormSwap) {
+        store_strided<ODT>(p.out, (uint64_t)c * p.ldo + r, p.ldo, count, v, p.accumulate != 0);
+    } else {
+        const uint64_t i = (uint64_t)r * p.ldo + c;
+        if (count == 32) store_run<ODT>(p.out, i, v, p.accumulate != 0);
+        else store_strided<ODT>(p.out, i, 1, count, v, p.accumulate != 0);
+    }
+}
+
+__device__ __forceinline__ void tile_at(const MmArgs &p, uint32_t t, uint32_t &tr, uint32_t &tc) {
+    const uint32_t span = kMmGroupRows * p.tiles_c, g = t / span, in = t % span;
+    const uint32_t h = min((uint32_t)kMmGroupRows, p.tiles_r - g * kMmGroupRows);
+    tr = g * kMmGroupRows + in % h;
+    tc = in / h;
+}
+
+// An epilogue warp's part of one tile, the BN / 2 columns from tmem_at on: waits for the accumulator(s), adds chunks up
+// (fp32 outputs), hands 32 columns at a time to `put`.  `n` counts accumulators; false: a wait ran out.
+template <int BN, int ACCS, bool CHUNKS, class Full, class Release, class Put>
+__device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, uint32_t &n, volatile uint32_t *stop, Full acc_full, Release release, Put put) {
+    constexpr int kCols = BN / 2;
+    if constexpr (CHUNKS) {
+        float sum[kCols];
+        for (uint32_t ch = 0; ch < chunks; ++ch, ++n) {
+            const uint32_t acc = n % ACCS;
+            if (!mbar_wait(acc_full(acc), (n / ACCS) & 1, stop)) return false;
+            __syncwarp();
+            fence_after();
+            #pragma unroll
+            for (int c = 0; c < kCols; c += 32) {
+                float v[32];
+                tmem_load32(tmem_at + acc * BN + c, v);
+                tmem_load_wait();
+                #pragma unroll
+                for (int j = 0; j < 32; ++j) sum[c + j] = ch == 0 ? v[j] : sum[c + j] + v[j];
+            }
+            fence_before();
+            release(acc);
+        }
+        #pragma unroll
+        for (int c = 0; c < kCols; c += 32) put(c, sum + c);
+    } else {
+        const uint32_t acc = n % ACCS;
+        if (!mbar_wait(acc_full(acc), (n / ACCS) & 1, stop)) return false;
+        __syncwarp();
+        fence_after();
+        #pragma unroll 1
+        for (int c = 0; c < kCols; c += 32) {
+            float v[32];
+            tmem_load32(tmem_at + acc * BN + c, v);
+            tmem_load_wait();
+            if (c + 32 >= kCols) { fence_before(); release(acc); }
+            put(c, v);
+        }
+        ++n;
+    }
+    return true;
+}
+
 template <int BN, int FORM, int ODT>
 __global__ void __launch_bounds__(kMmThreads, 1)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const MmArgs p) {
-    using S = MmShape<BN>;
+    using S = MmShape<BN, 1>;
+    constexpr bool kChunked = ODT == LGN_F32;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
     __shared__ uint32_t tmem_base_s;
@@ -225,16 +322,16 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 128); }
+        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), kMmEpiThreads); }
         mbar_init(drained, 1);
         stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 4 && lane == 0) {
+    if (warp == 8 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_rows) : "memory");
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_cols) : "memory");
     }
-    if (warp == 5) {
+    if (warp == 9) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -254,21 +351,15 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         kb1 = min(p.kblocks, kb0 + p.split_groups * 4);
     }
     const uint32_t tiles = p.tiles_r * p.tiles_c;
-    auto tile_at = [&](uint32_t t, uint32_t &tr, uint32_t &tc) {
-        const uint32_t span = kMmGroupRows * p.tiles_c, g = t / span, in = t % span;
-        const uint32_t h = min((uint32_t)kMmGroupRows, p.tiles_r - g * kMmGroupRows);
-        tr = g * kMmGroupRows + in % h;
-        tc = in / h;
-    };
 
-    if (warp == 4) {
+    if (warp == 8) {
         if (lane == 0) {
             dep_wait();
             uint32_t it = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
                 uint32_t tr, tc;
-                tile_at(t, tr, tc);
+                tile_at(p, t, tr, tc);
                 const uint32_t sb0 = (tc * BN) >> 7, sb_n = (p.cols + 127) >> 7;
                 for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
@@ -292,83 +383,60 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                 for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
                     mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
         }
-    } else if (warp == 5) {
+    } else if (warp == 9) {
         if (lane == 0) {
             const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | (1u << 27);
             uint32_t it = 0, n = 0, grp = 0;
             bool ok = true;
-            for (uint32_t t = tile0; ok && t < tiles; t += tile_step, ++n) {
-                uint32_t tr, tc;
-                tile_at(t, tr, tc);
-                const uint32_t acc = n % S::kAccs, col_off = ((tc * BN) & 127) >> 5;
-                if (!(ok = mbar_wait(acc_empty(acc), ((n / S::kAccs) & 1) ^ 1, &stop))) break;
-                fence_after();
-                const uint32_t d = tmem + acc * BN;
-                uint32_t sa = 0, sb = 0;
-                for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
-                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (!(ok = mbar_wait(full(s), ph, &stop))) break;
+            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
+                uint32_t tr, tc, sa = 0, sb = 0;
+                tile_at(p, t, tr, tc);
+                const uint32_t col_off = ((tc * BN) & 127) >> 5;
+                for (uint32_t c0 = kb0; ok && c0 < kb1; ++n) {                   // one accumulator per chunk of k
+                    const uint32_t c1 = kChunked ? min(kb1, c0 + kMmChunk) : kb1, acc = n % S::kAccs, d = tmem + acc * BN;
+                    if (!(ok = mbar_wait(acc_empty(acc), ((n / S::kAccs) & 1) ^ 1, &stop))) break;
                     fence_after();
-                    const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
-                    if ((kb & 3) == 0) {
-                        sa = tmem + S::kScaleCol + (grp++ % S::kScaleBufs) * S::kScaleCols;
-                        sb = sa + 4;
+                    for (uint32_t kb = c0; kb < c1; ++kb, ++it) {
+                        const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
+                        if (!(ok = mbar_wait(full(s), ph, &stop))) break;
+                        fence_after();
+                        const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
+                        if ((kb & 3) == 0) {
+                            sa = tmem + S::kScaleCol + (grp++ % S::kScaleBufs) * S::kScaleCols;
+                            sb = sa + 4;
+                            #pragma unroll
+                            for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales(sa + 4 * b, desc_scales(sc + 512 * b));
+                        }
+                        const uint32_t idesc = idesc0 | ((kb & 3) << 4) | ((kb & 3) << 29);
+                        const uint64_t da = desc_codes(a), db = desc_codes(a + 128 * 128);
                         #pragma unroll
-                        for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales(sa + 4 * b, desc_scales(sc + 512 * b));
+                        for (int k = 0; k < 4; ++k) mma_scaled(d, da + 2 * k, db + 2 * k, idesc, sa, sb + col_off, kb > c0 || k > 0);
+                        mma_commit(empty(s));
                     }
-                    const uint32_t idesc = idesc0 | ((kb & 3) << 4) | ((kb & 3) << 29);
-                    const uint64_t da = desc_codes(a), db = desc_codes(a + 128 * 128);
-                    #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_scaled(d, da + 2 * k, db + 2 * k, idesc, sa, sb + col_off, kb > kb0 || k > 0);
-                    mma_commit(empty(s));
+                    if (ok) mma_commit(acc_full(acc));
+                    c0 = c1;
                 }
-                if (ok) mma_commit(acc_full(acc));
             }
             if (!ok) { mma_commit(drained); mbar_drain(drained, 0); }
         }
     } else {
         dep_wait();                                                             // the output may belong to work before this call
         uint32_t n = 0;
-        const uint32_t lane_base = (warp * 32u) << 16;
-        for (uint32_t t = tile0; t < tiles; t += tile_step, ++n) {
+        const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, chunks = (kb1 - kb0 + kMmChunk - 1) / kMmChunk;
+        for (uint32_t t = tile0; t < tiles; t += tile_step) {
             uint32_t tr, tc;
-            tile_at(t, tr, tc);
-            const uint32_t acc = n % S::kAccs;
-            const uint32_t r = tr * 128 + warp * 32 + lane, c0 = tc * BN;
-            if (!mbar_wait(acc_full(acc), (n / S::kAccs) & 1, &stop)) break;
-            __syncwarp();
-            fence_after();
-            #pragma unroll 1
-            for (int c = 0; c < BN; c += 32) {
-                float v[32];
-                tmem_load32(tmem + lane_base + acc * BN + c, v);
-                tmem_load_wait();
-                if (c + 32 >= BN) { fence_before(); mbar_arrive(acc_empty(acc)); }
-                if constexpr (FORM == kFormSplit) {
-                    float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
-                    #pragma unroll
-                    for (int j = 0; j < 32; ++j) part[(c + j) * 128 + warp * 32 + lane] = v[j];
-                } else if constexpr (FORM == kFormSwap) {
-                    if (r < p.rows) {
+            tile_at(p, t, tr, tc);
+            const uint32_t r = tr * 128 + quad * 32 + lane, c0 = tc * BN + col0;
+            const bool ok = drain_tile<BN, S::kAccs, kChunked>(tmem_at, chunks, n, &stop, acc_full,
+                [&](uint32_t acc) { mbar_arrive(acc_empty(acc)); },
+                [&](uint32_t c, float *v) {
+                    if constexpr (FORM == kFormSplit) {
+                        float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
                         #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c0 + c + j < p.cols) {
-                                const uint64_t i = (uint64_t)(c0 + c + j) * p.ldo + r;
-                                store_out<ODT>(p.out, i, p.accumulate ? v[j] + load_out<ODT>(p.out, i) : v[j]);
-                            }
-                    }
-                } else {
-                    if (r < p.rows && c0 + c < p.cols) {
-                        const uint64_t i = (uint64_t)r * p.ldo + c0 + c;
-                        if (p.vec && c0 + c + 32 <= p.cols) store_run<ODT>(p.out, i, v, p.accumulate != 0);
-                        else {
-                            #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (c0 + c + j < p.cols) store_out<ODT>(p.out, i + j, p.accumulate ? v[j] + load_out<ODT>(p.out, i + j) : v[j]);
-                        }
-                    }
-                }
-            }
+                        for (int j = 0; j < 32; ++j) part[(col0 + c + j) * 128 + quad * 32 + lane] = v[j];
+                    } else store_columns<FORM, ODT>(p, r, c0 + c, v);
+                });
+            if (!ok) break;
         }
     }
     __syncwarp();
@@ -376,18 +444,18 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         // every CTA's partial tile is in its own shared memory: column c is added over the ranks, in rank
         // order, by the CTA c mod nrank
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (threadIdx.x < 128 && tile0 < tiles) {
+        if (threadIdx.x < kMmEpiThreads && tile0 < tiles) {
             uint32_t tr, tc;
-            tile_at(tile0, tr, tc);
-            const uint32_t r = tr * 128 + threadIdx.x;
+            tile_at(p, tile0, tr, tc);
+            const uint32_t at_row = threadIdx.x & 127, r = tr * 128 + at_row;
             if (r < p.rows) {
                 #pragma unroll 2
-                for (uint32_t c = rank; c < (uint32_t)BN && tc * BN + c < p.cols; c += nrank) {
+                for (uint32_t c = rank + (threadIdx.x >> 7) * nrank; c < (uint32_t)BN && tc * BN + c < p.cols; c += 2 * nrank) {
                     float v = 0.0f;
                     for (uint32_t q = 0; q < nrank; ++q) {
                         uint32_t at;
                         float x;
-                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem0 + (c * 128 + threadIdx.x) * 4), "r"(q));
+                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem0 + (c * 128 + at_row) * 4), "r"(q));
                         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
                         v += x;
                     }
@@ -403,7 +471,175 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     __syncthreads();
     fence_after();
     if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
-    if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
+}
+
+// ------------------------------------------------------------------ pairs of CTAs
+// The CTA of rank 0 issues the MMAs of both (cta_group::2); full barriers live there and count the bytes of both CTAs'
+// copies, empty and accumulator barriers are signalled in both.
+__device__ __forceinline__ uint32_t in_leader(uint32_t addr) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void tma_tile_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void mma_scaled_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add) : "memory");
+}
+__device__ __forceinline__ void copy_scales_pair(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {                        // the barrier at this offset in both CTAs
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 :: "r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_sync() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int BN, int FORM, int ODT>
+__global__ void __launch_bounds__(kMmThreads, 1) __cluster_dims__(2, 1, 1)
+fp8_pair_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols,
+                const __grid_constant__ CUtensorMap map_sc_rows, const __grid_constant__ CUtensorMap map_sc_cols, const MmArgs p) {
+    using S = MmShape<BN, 2>;
+    constexpr bool kChunked = ODT == LGN_F32;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ volatile uint32_t stop;
+
+    const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t scales0 = smem0 + S::kStages * S::kStageBytes;
+    const uint32_t bar0 = smem_u32(bars);
+    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+    auto empty = [&](uint32_t s) { return bar0 + 8 * (S::kStages + s); };
+    auto acc_full = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + a); };
+    auto acc_empty = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + S::kAccs + a); };
+    const uint32_t drained = bar0 + 8 * (2 * S::kStages + 2 * S::kAccs);
+
+    uint32_t rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 2 * kMmEpiThreads); }
+        mbar_init(drained, 1);
+        stop = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_rows) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_cols) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_sc_rows) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_sc_cols) : "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    pair_sync();                                            // barriers of both CTAs are set up, tensor memory of both allocated
+    fence_after();
+    const uint32_t tmem = tmem_base_s;
+    const uint32_t tile0 = blockIdx.x >> 1, tile_step = gridDim.x >> 1, tiles = p.tiles_r * p.tiles_c;
+
+    if (warp == 8) {
+        if (lane == 0) {
+            dep_wait();
+            uint32_t it = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
+                uint32_t tr, tc;
+                tile_at(p, t, tr, tc);
+                const uint32_t row0 = tr * 256 + rank * 128, sr0 = row0 >> 7, sc0 = (tc * BN) >> 7;
+                for (uint32_t kb = 0; kb < p.kblocks; ++kb, ++it) {
+                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
+                    if (!(ok = mbar_wait(empty(s), ph ^ 1, &stop))) break;
+                    const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
+                    const bool with_scales = (kb & 3) == 0;
+                    if (rank == 0) mbar_expect(full(s), 2 * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));
+                    const uint32_t bar = in_leader(full(s));
+                    tma_tile_pair(a, &map_rows, bar, (int)(kb * 128), (int)row0);
+                    tma_tile_pair(a + 128 * 128, &map_cols, bar, (int)(kb * 128), (int)(tc * BN + rank * (BN / 2)));
+                    if (with_scales) {                                          // tiles past the end read as zeros
+                        const uint32_t g = kb >> 2;
+                        tma_tile_pair(sc, &map_sc_rows, bar, 0, (int)(sr0 * p.groups + g));
+                        #pragma unroll
+                        for (int b = 0; b < S::kColBlocks; ++b)
+                            tma_tile_pair(sc + 512 * (1 + b), &map_sc_cols, bar, 0, (int)((sc0 + b) * p.groups + g));
+                    }
+                }
+            }
+            if (!ok && rank == 0)                                               // wait for the copies in flight, the other CTA's too
+                for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
+                    mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | (2u << 27);
+            uint32_t it = 0, n = 0, grp = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
+                uint32_t tr, tc, sa = 0, sb = 0;
+                tile_at(p, t, tr, tc);
+                const uint32_t col_off = ((tc * BN) & 127) >> 5;
+                for (uint32_t c0 = 0; ok && c0 < p.kblocks; ++n) {
+                    const uint32_t c1 = kChunked ? min(p.kblocks, c0 + kMmChunk) : p.kblocks, acc = n % S::kAccs, d = tmem + acc * BN;
+                    if (!(ok = mbar_wait(acc_empty(acc), ((n / S::kAccs) & 1) ^ 1, &stop))) break;
+                    fence_after();
+                    for (uint32_t kb = c0; kb < c1; ++kb, ++it) {
+                        const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
+                        if (!(ok = mbar_wait(full(s), ph, &stop))) break;
+                        fence_after();
+                        const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
+                        if ((kb & 3) == 0) {
+                            sa = tmem + S::kScaleCol + (grp++ % S::kScaleBufs) * S::kScaleCols;
+                            sb = sa + 4;
+                            #pragma unroll
+                            for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales_pair(sa + 4 * b, desc_scales(sc + 512 * b));
+                        }
+                        const uint32_t idesc = idesc0 | ((kb & 3) << 4) | ((kb & 3) << 29);
+                        const uint64_t da = desc_codes(a), db = desc_codes(a + 128 * 128);
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) mma_scaled_pair(d, da + 2 * k, db + 2 * k, idesc, sa, sb + col_off, kb > c0 || k > 0);
+                        mma_commit_pair(empty(s));
+                    }
+                    if (ok) mma_commit_pair(acc_full(acc));
+                    c0 = c1;
+                }
+            }
+            if (!ok) { mma_commit_pair(drained); mbar_drain(drained, 0); }
+        }
+    } else {
+        dep_wait();                                                             // the output may belong to work before this call
+        uint32_t n = 0;
+        const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, chunks = (p.kblocks + kMmChunk - 1) / kMmChunk;
+        for (uint32_t t = tile0; t < tiles; t += tile_step) {
+            uint32_t tr, tc;
+            tile_at(p, t, tr, tc);
+            const uint32_t r = tr * 256 + rank * 128 + quad * 32 + lane, c0 = tc * BN + col0;
+            const bool ok = drain_tile<BN, S::kAccs, kChunked>(tmem_at, chunks, n, &stop, acc_full,
+                [&](uint32_t acc) { mbar_arrive_remote(in_leader(acc_empty(acc))); },
+                [&](uint32_t c, float *v) { store_columns<FORM, ODT>(p, r, c0 + c, v); });
+            if (!ok) break;
+        }
+    }
+    fence_before();
+    __syncthreads();
+    pair_sync();                                            // nothing of either CTA is in flight any more
+    fence_after();
+    if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem));
 }
 
 // k = 0: nothing is added.
@@ -414,14 +650,19 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(void *out, uint64_t ldo,
         store_out<ODT>(out, (i / cols) * ldo + i % cols, 0.0f);
 }
 
-#define LGN_MM(BN, F, O) reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, F, O>)
-#define LGN_MM3(BN) {{LGN_MM(BN, kFormRows, LGN_F32), LGN_MM(BN, kFormSwap, LGN_F32), LGN_MM(BN, kFormSplit, LGN_F32)}, \
-                     {LGN_MM(BN, kFormRows, LGN_BF16), LGN_MM(BN, kFormSwap, LGN_BF16), LGN_MM(BN, kFormSplit, LGN_BF16)}}
-static const void *const kMmTable[4][2][3] = {LGN_MM3(64), LGN_MM3(128), LGN_MM3(192), LGN_MM3(256)};
+// The kernels a call may take.  `pair`: fp8_pair_kernel.
+struct MmKernel { const void *fn; int bn, pair, form, odt, smem; };
+#define LGN_MM1(BN, F, O) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, F, O>), BN, 0, F, O, MmShape<BN, 1>::kSmem}
+#define LGN_MM2(BN, F, O) {reinterpret_cast<const void *>(&fp8_pair_kernel<BN, F, O>), BN, 1, F, O, MmShape<BN, 2>::kSmem}
+#define LGN_MM3(BN, O) LGN_MM1(BN, kFormRows, O), LGN_MM1(BN, kFormSwap, O), LGN_MM1(BN, kFormSplit, O)
+static const MmKernel kMmKernels[] = {
+    LGN_MM3(64, LGN_F32), LGN_MM3(64, LGN_BF16), LGN_MM3(128, LGN_F32), LGN_MM3(128, LGN_BF16),
+    LGN_MM2(192, kFormRows, LGN_F32), LGN_MM2(192, kFormSwap, LGN_F32), LGN_MM2(192, kFormRows, LGN_BF16), LGN_MM2(192, kFormSwap, LGN_BF16),
+    LGN_MM2(256, kFormRows, LGN_BF16), LGN_MM2(256, kFormSwap, LGN_BF16)};
+#undef LGN_MM1
+#undef LGN_MM2
 #undef LGN_MM3
-#undef LGN_MM
-static const int kMmBn[4] = {64, 128, 192, 256};
-static const int kMmSmem[4] = {MmShape<64>::kSmem, MmShape<128>::kSmem, MmShape<192>::kSmem, MmShape<256>::kSmem};
+constexpr int kMmCount = (int)(sizeof kMmKernels / sizeof kMmKernels[0]);
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -446,48 +687,54 @@ static bool make_map(CUtensorMap *m, const void *codes, uint64_t rows, uint64_t 
                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Scale tiles as rows of 128 words.
+static bool make_scale_map(CUtensorMap *m, const void *scales, uint64_t tiles) {
+    const cuuint64_t dim[2] = {128, tiles}, stride[1] = {512};
+    const cuuint32_t box[2] = {128, 1}, es[2] = {1, 1};
+    return encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void *>(scales), dim, stride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The kernels need more dynamic shared memory than the default limit; raised once per device and kernel.
-static bool allow_smem(int bn_index, int odt, int form) {
+static bool allow_smem(int kernel) {
     static std::mutex guard;
-    static bool done[64][4][2][3];
+    static bool done[64][kMmCount];
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
     std::lock_guard<std::mutex> lock(guard);
-    if (dev < 64 && done[dev][bn_index][odt][form]) return true;
-    if (cudaFuncSetAttribute(kMmTable[bn_index][odt][form], cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem[bn_index]) != cudaSuccess) {
+    if (dev < 64 && done[dev][kernel]) return true;
+    if (cudaFuncSetAttribute(kMmKernels[kernel].fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmKernels[kernel].smem) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
     }
-    if (dev < 64) done[dev][bn_index][odt][form] = true;
+    if (dev < 64) done[dev][kernel] = true;
     return true;
 }
 
-struct MmPlan { int bn_index; int form; bool swap; uint32_t split; uint32_t split_groups; };
+struct MmPlan { int kernel; uint32_t split, split_groups; };
 
-static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t ldo, bool vec, int sms) {
-    MmPlan best = {0, kFormSwap, true, 1, 0};
+// The kernel of least estimated time, in clocks of an SM: rounds of the grid times the steps of k of a tile, plus
+// what a tile costs beyond them.
+static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, bool vec, int odt, int sms) {
+    MmPlan best = {-1, 1, 0};
     const uint64_t groups = (kblocks + 3) / 4;
     double best_cost = 1e300;
-    for (int b = 0; b < 4; ++b) {
-        const uint64_t bn = (uint64_t)kMmBn[b];
-        for (int form = 0; form < 3; ++form) {
-            const bool swap = form != kFormRows;
-            if (form == kFormRows && !vec) continue;
-            const uint64_t r = swap ? n : m, c = swap ? m : n;
-            const uint64_t tiles = ((r + 127) / 128) * ((c + bn - 1) / bn);
-            for (uint64_t want = form == kFormSplit ? 2 : 1; want <= (form == kFormSplit ? 8u : 1u); want *= 2) {
-                const uint64_t per = (groups + want - 1) / want, s = form == kFormSplit ? (groups + per - 1) / per : 1;
-                if (form == kFormSplit && (s < 2 || tiles * s > (uint64_t)sms)) continue;
-                const uint64_t steps = form == kFormSplit ? (per * 4 < kblocks ? per * 4 : kblocks) : kblocks;
-                const double rounds = (double)((tiles * s + sms - 1) / sms);
-                // clocks: a step of k takes 2 BN of MMA (at least the time its bytes need), a tile an epilogue
-                const double step = 2.0 * bn > 300 ? 2.0 * bn : 300, epi = (bn == 256 ? 900 : 300) + (swap ? 2.0 * bn : 0) + (s > 1 ? 3000 : 0);
-                const double cost = rounds * (steps * step + epi);
-                if (cost < best_cost) { best_cost = cost; best = {b, form, swap, (uint32_t)s, (uint32_t)per}; }
-            }
+    for (int i = 0; i < kMmCount; ++i) {
+        const MmKernel &q = kMmKernels[i];
+        if (q.odt != odt || (q.form == kFormRows && !vec)) continue;
+        const uint64_t rows = q.pair ? 256 : 128, bn = (uint64_t)q.bn, r = q.form == kFormRows ? m : n, c = q.form == kFormRows ? n : m;
+        const uint64_t tiles = ((r + rows - 1) / rows) * ((c + bn - 1) / bn), slots = (uint64_t)(q.pair ? sms / 2 : sms);
+        for (uint64_t want = q.form == kFormSplit ? 2 : 1; want <= (q.form == kFormSplit ? 8u : 1u); want *= 2) {
+            const uint64_t per = (groups + want - 1) / want, s = q.form == kFormSplit ? (groups + per - 1) / per : 1;
+            if (q.form == kFormSplit && (s < 2 || tiles * s > slots)) continue;
+            const uint64_t steps = q.form == kFormSplit && per * 4 < kblocks ? per * 4 : kblocks;
+            const double rounds = (double)((tiles * s + slots - 1) / slots);
+            const double step = q.pair ? (bn == 256 ? 600 : 500) : (bn == 128 ? 500 : 400);
+            const double tile = (bn == 256 ? 1500 : 400) + (q.form == kFormSwap ? 4.0 * bn : 0) + (s > 1 ? 3000 : 0);
+            const double cost = rounds * (steps * step + tile);
+            if (cost < best_cost) { best_cost = cost; best = {i, (uint32_t)s, (uint32_t)per}; }
         }
     }
-    (void)ldo;
     return best;
 }
 
@@ -522,33 +769,40 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     if (sms < 1 || encode_tiled() == nullptr) return LGN_ERR_CUDA;
     const bool vec = aligned_to(out, 32) && (ldo * es) % 32 == 0;
     const uint64_t kblocks = (k + 127) / 128;
-    const MmPlan plan = plan_matmul(m, n, kblocks, ldo, vec, sms);
-    const uint32_t bn = (uint32_t)kMmBn[plan.bn_index];
+    const MmPlan plan = plan_matmul(m, n, kblocks, vec, out_dt, sms);
+    if (plan.kernel < 0) return LGN_ERR_UNSUPPORTED;
+    const MmKernel &q = kMmKernels[plan.kernel];
+    const bool swap = q.form != kFormRows;
+    const uint32_t bn = (uint32_t)q.bn, tile_rows = q.pair ? 256 : 128;
     MmArgs p = {};
-    const void *cr = plan.swap ? b : a, *cc = plan.swap ? a : b;
-    p.sc_rows = static_cast<const uint8_t *>(plan.swap ? b_scales : a_scales);
-    p.sc_cols = static_cast<const uint8_t *>(plan.swap ? a_scales : b_scales);
-    p.rows = (uint32_t)(plan.swap ? n : m);
-    p.cols = (uint32_t)(plan.swap ? m : n);
-    p.fmt_rows = (uint32_t)(plan.swap ? b_fmt : a_fmt);
-    p.fmt_cols = (uint32_t)(plan.swap ? a_fmt : b_fmt);
+    const void *cr = swap ? b : a, *cc = swap ? a : b;
+    p.sc_rows = static_cast<const uint8_t *>(swap ? b_scales : a_scales);
+    p.sc_cols = static_cast<const uint8_t *>(swap ? a_scales : b_scales);
+    p.rows = (uint32_t)(swap ? n : m);
+    p.cols = (uint32_t)(swap ? m : n);
+    p.fmt_rows = (uint32_t)(swap ? b_fmt : a_fmt);
+    p.fmt_cols = (uint32_t)(swap ? a_fmt : b_fmt);
     p.out = out; p.ldo = ldo; p.status = status_dev;
     p.kblocks = (uint32_t)kblocks;
     p.groups = (uint32_t)((kblocks + 3) / 4);
-    p.tiles_r = (p.rows + 127) / 128;
+    p.tiles_r = (p.rows + tile_rows - 1) / tile_rows;
     p.tiles_c = (p.cols + bn - 1) / bn;
     p.split_groups = plan.split_groups;
     p.accumulate = accumulate != 0;
-    p.vec = vec;
-    const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c;
-    if (tiles > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
-    CUtensorMap mr, mc;
-    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, bn)) return LGN_ERR_CUDA;
-    if (!allow_smem(plan.bn_index, out_dt, plan.form)) return LGN_ERR_CUDA;
-    const uint64_t grid = plan.form == kFormSplit ? tiles * plan.split : (tiles < (uint64_t)sms ? tiles : (uint64_t)sms);
-    log_line("fp8_matmul: m %llu n %llu k %llu, tile 128 x %u, form %d, split %u, %llu CTAs", (unsigned long long)m, (unsigned long long)n,
-             (unsigned long long)k, bn, plan.form, plan.split, (unsigned long long)grid);
+    const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c, slots = (uint64_t)(q.pair ? sms / 2 : sms);
+    if (tiles > 0x3fffffffull) return LGN_ERR_UNSUPPORTED;
+    CUtensorMap mr, mc, sr, sc;
+    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, q.pair ? bn / 2 : bn)) return LGN_ERR_CUDA;
+    if (!allow_smem(plan.kernel)) return LGN_ERR_CUDA;
+    uint64_t grid = q.form == kFormSplit ? tiles * plan.split : (tiles < slots ? tiles : slots);
+    log_line("fp8_matmul: m %llu n %llu k %llu, %s, tile %u x %u, form %d, split %u, %llu tiles", (unsigned long long)m, (unsigned long long)n,
+             (unsigned long long)k, q.pair ? "pairs" : "single", tile_rows, bn, q.form, plan.split, (unsigned long long)tiles);
+    if (q.pair) {
+        if (!make_scale_map(&sr, p.sc_rows, (uint64_t)((p.rows + 127) / 128) * p.groups) ||
+            !make_scale_map(&sc, p.sc_cols, (uint64_t)((p.cols + 127) / 128) * p.groups)) return LGN_ERR_CUDA;
+        void *args[] = {&mr, &mc, &sr, &sc, &p};
+        return launch_dependent(q.fn, dim3((unsigned)(2 * grid)), dim3(kMmThreads), args, (size_t)q.smem, stream);
+    }
     void *args[] = {&mr, &mc, &p};
-    return launch_dependent(kMmTable[plan.bn_index][out_dt][plan.form], dim3((unsigned)grid), dim3(kMmThreads), args,
-                            (size_t)kMmSmem[plan.bn_index], stream, plan.form == kFormSplit ? plan.split : 1);
+    return launch_dependent(q.fn, dim3((unsigned)grid), dim3(kMmThreads), args, (size_t)q.smem, stream, q.form == kFormSplit ? plan.split : 1);
 }

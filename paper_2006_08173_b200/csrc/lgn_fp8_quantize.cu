@@ -24,14 +24,14 @@ __device__ __forceinline__ uint32_t finite_abs(float x) {
 }
 
 // Biased exponent e + 127 (the E8M0 byte) of a block whose largest finite magnitude has pattern a.
-// `top` is 8 (E4M3) or 15 (E5M2).
-__device__ __forceinline__ uint32_t scale_byte(uint32_t a, int top) {
-    const int e = (int)(a >> 23) - top + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);      // + 127 - 127
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t a) {
+    const int e = (int)(a >> 23) - (FMT == LGN_E4M3 ? 8 : 15) + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);      // + 127 - 127
     return (uint32_t)max(e, 0);
 }
 
-// 2^-e for a biased exponent 0..247.
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+// Pattern of 2^-e for a biased exponent 0..247.
+__device__ __forceinline__ uint32_t inverse_scale(uint32_t byte) { return (254u - byte) << 23; }
 
 template <int FMT>
 __device__ __forceinline__ uint32_t code_pair(float lo, float hi) {                   // two codes, lo in bits 0..7
@@ -40,57 +40,99 @@ __device__ __forceinline__ uint32_t code_pair(float lo, float hi) {             
     else                           asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-
-// x 2^-e with every non-finite x turned into NaN (the saturating conversion would store an infinity
-// as the largest code; the NaN code keeps it visible in every sum it takes part in).
-__device__ __forceinline__ float scaled(float x, float inv) {
-    const float y = x * inv;
-    return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __int_as_float(0x7fffffff) : y;
-}
-
 template <int FMT>
-__device__ __forceinline__ uint32_t code_quad(const float *x, float inv) {
-    return code_pair<FMT>(scaled(x[0], inv), scaled(x[1], inv)) | code_pair<FMT>(scaled(x[2], inv), scaled(x[3], inv)) << 16;
+__device__ __forceinline__ uint32_t code_quad(float a, float b, float c, float d) {
+    return __byte_perm(code_pair<FMT>(a, b), code_pair<FMT>(c, d), 0x5410);
 }
 
-// N consecutive values starting at p, of which the first `valid` exist (others read as 0).
-template <int DT, int N, bool VEC>
-__device__ __forceinline__ void load_values(const char *p, int valid, float *x) {
-    if constexpr (VEC) {
-        if (valid >= N) {
-            if constexpr (DT == LGN_F32) {
-                #pragma unroll
-                for (int k = 0; k < N; k += 4) {
-                    float4 v;
-                    asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0,%1,%2,%3}, [%4];"
-                                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p + 4 * k));
-                    x[k] = v.x; x[k + 1] = v.y; x[k + 2] = v.z; x[k + 3] = v.w;
-                }
-            } else {
-                #pragma unroll
-                for (int k = 0; k < N; k += 8) {
-                    uint32_t w[4];
-                    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
-                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p + 2 * k));
-                    #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[k + 2 * j] = __uint_as_float(w[j] << 16);
-                        x[k + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-                    }
-                }
-            }
+// Every non-finite x becomes NaN (the saturating conversion would store an infinity as the largest
+// code; the NaN code keeps it visible in every sum it takes part in).
+__device__ __forceinline__ float nan_if_not_finite(float x) {
+    return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __int_as_float(0x7fffffff) : x;
+}
+
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// Two bf16 values times two powers of two: exact above the subnormals.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {                          // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// N consecutive values of a row as they lie in memory: N words of fp32, N/2 of two bf16 each.  A value costs
+// about six instructions per copy written, so bf16 stays packed for maxima and scaling.
+template <int DT, int N> struct Values {
+    static constexpr int kWords = DT == LGN_F32 ? N : N / 2;
+    uint32_t w[kWords];
+
+    // of which the first `valid` exist (others read as 0)
+    template <bool VEC>
+    __device__ __forceinline__ void load(const char *p, int valid) {
+        if (VEC && valid >= N) {
+            #pragma unroll
+            for (int k = 0; k < kWords; k += 4)
+                asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "l"(p + 4 * k) : "memory");
             return;
         }
-    }
-    #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        x[k] = 0.0f;
-        if (k < valid) {
-            if constexpr (DT == LGN_F32) x[k] = __uint_as_float(ldro_u32(p + 4 * k));
-            else x[k] = __uint_as_float(ldro_u16(p + 2 * k) << 16);
+        #pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+            w[k] = 0u;
+            if constexpr (DT == LGN_F32) {
+                if (k < valid) w[k] = ldro_u32(p + 4 * k);
+            } else {
+                if (2 * k < valid) w[k] = ldro_u16(p + 4 * k);
+                if (2 * k + 1 < valid) w[k] |= ldro_u16(p + 4 * k + 2) << 16;
+            }
         }
     }
-}
+    __device__ __forceinline__ float at(int k) const {
+        if constexpr (DT == LGN_F32) return __uint_as_float(w[k]);
+        else return k & 1 ? bf_hi(w[k >> 1]) : bf_lo(w[k >> 1]);
+    }
+    // fp32 pattern of the largest magnitude: at least 0x7f800000 if any value is not finite
+    __device__ __forceinline__ uint32_t max_abs() const {
+        if constexpr (DT == LGN_F32) {
+            float m = fabsf(__uint_as_float(w[0]));
+            #pragma unroll
+            for (int k = 1; k < kWords; ++k) m = max_nan(m, fabsf(__uint_as_float(w[k])));
+            return __float_as_uint(m) & 0x7fffffffu;
+        } else {
+            uint32_t m = w[0] & 0x7fff7fffu;
+            #pragma unroll
+            for (int k = 1; k < kWords; ++k) m = __vmaxu2(m, w[k] & 0x7fff7fffu);
+            return max(m << 16, m & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ uint32_t max_abs_finite() const {
+        uint32_t a = 0;
+        #pragma unroll
+        for (int k = 0; k < N; ++k) a = max(a, finite_abs(at(k)));
+        return a;
+    }
+    // codes of values 4q .. 4q + 3, all with the scale whose inverse has pattern inv
+    template <int FMT>
+    __device__ __forceinline__ uint32_t quad(int q, uint32_t inv, bool special) const {
+        if (special) {
+            const float f = __uint_as_float(inv);
+            return code_quad<FMT>(nan_if_not_finite(at(4 * q)) * f, nan_if_not_finite(at(4 * q + 1)) * f,
+                                  nan_if_not_finite(at(4 * q + 2)) * f, nan_if_not_finite(at(4 * q + 3)) * f);
+        }
+        if constexpr (DT == LGN_F32) {
+            const float f = __uint_as_float(inv);
+            return code_quad<FMT>(at(4 * q) * f, at(4 * q + 1) * f, at(4 * q + 2) * f, at(4 * q + 3) * f);
+        } else {
+            const uint32_t f = __byte_perm(inv, inv, 0x3232), a = mul_bf16x2(w[2 * q], f), b = mul_bf16x2(w[2 * q + 1], f);
+            return code_quad<FMT>(bf_lo(a), bf_hi(a), bf_lo(b), bf_hi(b));
+        }
+    }
+};
 
 // ------------------------------------------------------------------ row blocks only
 // One warp takes 512 consecutive columns of one row, 16 per lane: a block of 128 lies in 8 lanes
@@ -98,8 +140,8 @@ __device__ __forceinline__ void load_values(const char *p, int valid, float *x) 
 // are one word of the scale tile.
 template <int DT, int FMT, bool VEC>
 __global__ void __launch_bounds__(256)
-fp8_rows_kernel(const char *__restrict__ x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t groups,
-                uint8_t *__restrict__ codes, uint32_t ldq, uint32_t *__restrict__ scales) {
+fp8_rows_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t groups,
+                uint8_t *codes, uint32_t ldq, uint32_t *scales) {
     dep_launch();
     dep_wait();
     constexpr int ES = DT == LGN_F32 ? 4 : 2;
@@ -108,19 +150,18 @@ fp8_rows_kernel(const char *__restrict__ x, uint64_t ld, uint32_t rows, uint32_t
     const uint32_t row = (uint32_t)(unit / groups), grp = (uint32_t)(unit % groups);
     if (row >= rows) return;
     const uint32_t c0 = grp * 512 + lane * 16;
-    float v[16];
-    load_values<DT, 16, VEC>(x + ((uint64_t)row * ld + c0) * ES, (int)min((int64_t)16, (int64_t)cols - (int64_t)c0), v);
-    uint32_t a = 0;
-    #pragma unroll
-    for (int k = 0; k < 16; ++k) a = max(a, finite_abs(v[k]));
+    Values<DT, 16> v;
+    v.template load<VEC>(x + ((uint64_t)row * ld + c0) * ES, (int)min((int64_t)16, (int64_t)cols - (int64_t)c0));
+    uint32_t a = v.max_abs();
+    const bool special = __any_sync(0xffffffffu, a >= 0x7f800000u);
+    if (special) a = v.max_abs_finite();
     #pragma unroll
     for (int d = 1; d < 8; d <<= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, d));
-    const uint32_t byte = scale_byte(a, FMT == LGN_E4M3 ? 8 : 15);
-    const float inv = inverse_scale(byte);
+    const uint32_t byte = scale_byte<FMT>(a), inv = inverse_scale(byte);
     if (c0 < ldq) {
         uint4 q;
-        q.x = code_quad<FMT>(v, inv); q.y = code_quad<FMT>(v + 4, inv);
-        q.z = code_quad<FMT>(v + 8, inv); q.w = code_quad<FMT>(v + 12, inv);
+        q.x = v.template quad<FMT>(0, inv, special); q.y = v.template quad<FMT>(1, inv, special);
+        q.z = v.template quad<FMT>(2, inv, special); q.w = v.template quad<FMT>(3, inv, special);
         *reinterpret_cast<uint4 *>(codes + (uint64_t)row * ldq + c0) = q;
     }
     uint32_t word = byte << (8 * (lane >> 3));
@@ -131,92 +172,139 @@ fp8_rows_kernel(const char *__restrict__ x, uint64_t ld, uint32_t rows, uint32_t
 
 // ------------------------------------------------------------------ 128 x 128 tiles
 // Transposed copies and square blocks.  A CTA keeps its tile in registers (thread: 8 consecutive
-// rows x 8 consecutive columns), so the tile is read once for both copies.  Transposed codes go
-// through shared memory as units of 8 bytes (8 rows of one column); unit u of column c sits at
-// place u ^ (c / 8), which spreads the 16 lanes that write units of columns 8 apart over all banks.
+// rows x 8 consecutive columns), so the tile is read once for both copies.  Maxima go through shared memory:
+// every thread leaves its 8 row and 8 column maxima, then one thread per row and one per column adds up 16 of
+// them and forms the scale.  Transposed codes leave through shared memory as units of 8 bytes (8 rows of one column);
+// unit u of column c sits at place u ^ (c / 8), which spreads the 16 lanes that write units of columns 8
+// apart over all banks.
 template <int DT, int FMT, bool SQUARE, bool VEC>
-__global__ void __launch_bounds__(256)
-fp8_tile_kernel(const char *__restrict__ x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t col_tiles,
-                uint8_t *__restrict__ codes, uint32_t ldq, uint8_t *__restrict__ scales, uint32_t groups,
-                uint8_t *__restrict__ codes_t, uint32_t ldq_t, uint8_t *__restrict__ scales_t, uint32_t groups_t) {
-    __shared__ uint32_t col_max[128];
-    __shared__ uint32_t all_max;
+__global__ void __launch_bounds__(256, DT == LGN_F32 ? 2 : 3)
+fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t col_tiles,
+                uint8_t *codes, uint32_t ldq, uint8_t *scales, uint32_t groups,
+                uint8_t *codes_t, uint32_t ldq_t, uint8_t *scales_t, uint32_t groups_t) {
     __shared__ __align__(16) uint2 tr[128 * 16];
+    __shared__ uint32_t rmax[128 * 17];
+    __shared__ __align__(16) uint32_t cmax[16 * 128];
+    __shared__ uint32_t rinv[128];
+    __shared__ __align__(16) uint32_t cinv[128];
+    __shared__ uint32_t wmax[8];
     dep_launch();
-    if (threadIdx.x < 128) col_max[threadIdx.x] = 0u;
-    if (threadIdx.x == 0) all_max = 0u;
     dep_wait();
     constexpr int ES = DT == LGN_F32 ? 4 : 2;
-    constexpr int kTop = FMT == LGN_E4M3 ? 8 : 15;
     const uint32_t rt = blockIdx.x / col_tiles, ct = blockIdx.x % col_tiles;
-    const uint32_t cl = (threadIdx.x & 15) * 8, rl = (threadIdx.x >> 4) * 8;          // within the tile
+    const uint32_t cg = threadIdx.x & 15, rg = threadIdx.x >> 4, cl = cg * 8, rl = rg * 8;          // within the tile
     const uint32_t c0 = ct * 128 + cl, r0 = rt * 128 + rl;
-    float v[8][8];
+    Values<DT, 8> v[8];
     const int valid = (int)min((int64_t)8, (int64_t)cols - (int64_t)c0);
     #pragma unroll
     for (int i = 0; i < 8; ++i)
-        load_values<DT, 8, VEC>(x + ((uint64_t)(r0 + i) * ld + c0) * ES, r0 + i < rows ? valid : 0, v[i]);
+        v[i].template load<VEC>(x + ((uint64_t)(r0 + i) * ld + c0) * ES, r0 + i < rows ? valid : 0);
 
-    uint32_t rmax[8], cmax[8];
-    #pragma unroll
-    for (int j = 0; j < 8; ++j) cmax[j] = 0u;
-    #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        uint32_t a = 0;
+    bool special = false;
+    for (int round = 0; round < 2; ++round) {             // a second round, over finite values, only where some are not
+        uint32_t mine = 0;
         #pragma unroll
-        for (int j = 0; j < 8; ++j) { const uint32_t f = finite_abs(v[i][j]); a = max(a, f); cmax[j] = max(cmax[j], f); }
-        rmax[i] = a;
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t a = special ? v[i].max_abs_finite() : v[i].max_abs();
+            if constexpr (SQUARE) mine = max(mine, a);
+            else rmax[(rl + i) * 17 + cg] = a;
+        }
+        if constexpr (SQUARE) {
+            mine = __reduce_max_sync(0xffffffffu, mine);
+            if ((threadIdx.x & 31) == 0) wmax[threadIdx.x >> 5] = mine;
+        } else if (codes_t != nullptr) {
+            uint32_t m[8];
+            if (special) {
+                #pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    m[j] = 0u;
+                    #pragma unroll
+                    for (int i = 0; i < 8; ++i) m[j] = max(m[j], finite_abs(v[i].at(j)));
+                }
+            } else if constexpr (DT == LGN_F32) {
+                #pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float f = fabsf(v[0].at(j));
+                    #pragma unroll
+                    for (int i = 1; i < 8; ++i) f = max_nan(f, fabsf(v[i].at(j)));
+                    m[j] = __float_as_uint(f) & 0x7fffffffu;
+                }
+            } else {
+                #pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t t = v[0].w[q] & 0x7fff7fffu;
+                    #pragma unroll
+                    for (int i = 1; i < 8; ++i) t = __vmaxu2(t, v[i].w[q] & 0x7fff7fffu);
+                    m[2 * q] = t << 16;
+                    m[2 * q + 1] = t & 0xffff0000u;
+                }
+            }
+            *reinterpret_cast<uint4 *>(&cmax[rg * 128 + cl]) = make_uint4(m[0], m[1], m[2], m[3]);
+            *reinterpret_cast<uint4 *>(&cmax[rg * 128 + cl + 4]) = make_uint4(m[4], m[5], m[6], m[7]);
+        }
+        __syncthreads();
+        const uint32_t t = threadIdx.x & 127;
+        const bool is_col = threadIdx.x >= 128;
+        uint32_t a = 0;
+        if constexpr (SQUARE) {
+            #pragma unroll
+            for (int k = 0; k < 8; ++k) a = max(a, wmax[k]);
+        } else if (is_col) {
+            if (codes_t != nullptr) {
+                #pragma unroll
+                for (int k = 0; k < 16; ++k) a = max(a, cmax[k * 128 + t]);
+            }
+        } else {
+            #pragma unroll
+            for (int k = 0; k < 16; ++k) a = max(a, rmax[t * 17 + k]);
+        }
+        if (round == 0) {
+            special = __syncthreads_or(a >= 0x7f800000u);
+            if (special) continue;
+        }
+        const uint32_t byte = scale_byte<FMT>(a);
+        if (is_col) {
+            cinv[t] = inverse_scale(byte);
+            if (codes_t != nullptr) scales_t[4 * fp8_scale_word(ct * 128 + t, rt >> 2, groups_t) + (rt & 3)] = (uint8_t)byte;
+        } else {
+            rinv[t] = inverse_scale(byte);
+            if (codes != nullptr) scales[4 * fp8_scale_word(rt * 128 + t, ct >> 2, groups) + (ct & 3)] = (uint8_t)byte;
+        }
+        break;
     }
     __syncthreads();
-    uint32_t row_byte[8], col_byte[8];
-    if constexpr (SQUARE) {
-        uint32_t a = 0;
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) a = max(a, rmax[i]);
-        a = __reduce_max_sync(0xffffffffu, a);
-        if ((threadIdx.x & 31) == 0) atomicMax(&all_max, a);
-        __syncthreads();
-        const uint32_t b = scale_byte(all_max, kTop);
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) row_byte[i] = col_byte[i] = b;
-    } else {
+    if (codes != nullptr && c0 < ldq) {                                               // ldq is a multiple of 16
         #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            #pragma unroll
-            for (int d = 1; d < 16; d <<= 1) rmax[i] = max(rmax[i], __shfl_xor_sync(0xffffffffu, rmax[i], d));
-            row_byte[i] = scale_byte(rmax[i], kTop);
-        }
-        if (codes_t != nullptr) {
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t a = max(cmax[j], __shfl_xor_sync(0xffffffffu, cmax[j], 16));
-                if ((threadIdx.x & 16) == 0) atomicMax(&col_max[cl + j], a);
-            }
-            __syncthreads();
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) col_byte[j] = scale_byte(col_max[cl + j], kTop);
-        }
-    }
-    if (codes != nullptr) {
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float inv = inverse_scale(row_byte[i]);
-            if (r0 + i < rows && c0 < ldq)                                            // ldq is a multiple of 16
+            const uint32_t inv = rinv[rl + i];
+            if (r0 + i < rows)
                 *reinterpret_cast<uint2 *>(codes + (uint64_t)(r0 + i) * ldq + c0) =
-                    make_uint2(code_quad<FMT>(v[i], inv), code_quad<FMT>(v[i] + 4, inv));
-            if ((threadIdx.x & 15) == 0)
-                scales[4 * (uint64_t)fp8_scale_word(r0 + i, ct >> 2, groups) + (ct & 3)] = (uint8_t)row_byte[i];
+                    make_uint2(v[i].template quad<FMT>(0, inv, special), v[i].template quad<FMT>(1, inv, special));
         }
     }
     if (codes_t != nullptr) {
         #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float inv = inverse_scale(col_byte[j]);
-            float t[8];
-            #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = v[i][j];
-            tr[(cl + j) * 16 + ((threadIdx.x >> 4) ^ (threadIdx.x & 15))] = make_uint2(code_quad<FMT>(t, inv), code_quad<FMT>(t + 4, inv));
-            if (rl == 0) scales_t[4 * (uint64_t)fp8_scale_word(c0 + j, rt >> 2, groups_t) + (rt & 3)] = (uint8_t)col_byte[j];
+        for (int j = 0; j < 8; j += 2) {
+            const uint2 inv = *reinterpret_cast<const uint2 *>(&cinv[cl + j]);
+            float lo[8], hi[8];
+            if (DT == LGN_F32 || special) {
+                #pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float a = v[i].at(j), b = v[i].at(j + 1);
+                    lo[i] = (special ? nan_if_not_finite(a) : a) * __uint_as_float(inv.x);
+                    hi[i] = (special ? nan_if_not_finite(b) : b) * __uint_as_float(inv.y);
+                }
+            } else {
+                const uint32_t f = __byte_perm(inv.x, inv.y, 0x7632);
+                #pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t y = mul_bf16x2(v[i].w[j / 2], f);
+                    lo[i] = bf_lo(y);
+                    hi[i] = bf_hi(y);
+                }
+            }
+            tr[(cl + j) * 16 + (rg ^ cg)] = make_uint2(code_quad<FMT>(lo[0], lo[1], lo[2], lo[3]), code_quad<FMT>(lo[4], lo[5], lo[6], lo[7]));
+            tr[(cl + j + 1) * 16 + (rg ^ cg)] = make_uint2(code_quad<FMT>(hi[0], hi[1], hi[2], hi[3]), code_quad<FMT>(hi[4], hi[5], hi[6], hi[7]));
         }
         __syncthreads();
         #pragma unroll
