@@ -42,7 +42,7 @@
 namespace lgn {
 
 constexpr int kMmThreads = 320;                // warps 0..7: epilogue, 8: copies, 9: MMA
-constexpr int kMmEpiThreads = 256;
+constexpr int kMmEpiThreads = 256, kMmEpiWarps = 8;
 constexpr int kMmGroupRows = 16;                 // row tiles walked before the next column tile (L2 reuse)
 constexpr long long kMmWaitClocks = 4000000000ll;   // about two seconds
 
@@ -61,18 +61,22 @@ struct MmArgs {
 
 constexpr uint32_t kMmChunk = 8;                 // steps of k (128 each) that stay in tensor memory, fp32 outputs
 
+constexpr int kMmBuffer = 4096;                   // 32 rows x 128 bytes of output
+
 // CTAS: 1 (fp8_matmul_kernel) or 2 (fp8_pair_kernel); bytes and stages per CTA.
-template <int BN, int CTAS> struct MmShape {
+template <int BN, int CTAS, int ODT> struct MmShape {
+    static constexpr int kBuffers = ODT == LGN_F32 ? 2 : 1;         // output buffers of an epilogue warp
+    static constexpr int kStaging = kMmEpiWarps * kBuffers * kMmBuffer;
     static constexpr int kColBlocks = BN <= 128 ? 1 : 2;            // 128-row scale tiles a column tile touches
     static constexpr int kStageBytes = 128 * 128 + BN / CTAS * 128;
     static constexpr int kScaleBytes = 512 * (1 + kColBlocks);
-    static constexpr int kFit = (int)((220 * 1024) / (kStageBytes + kScaleBytes));
+    static constexpr int kFit = (int)((225 * 1024 - kStaging) / (kStageBytes + kScaleBytes));
     static constexpr int kStages = kFit > 8 ? 8 : kFit;
     static constexpr int kAccs = BN <= 192 ? 2 : 1;                 // accumulator tiles in tensor memory
     static constexpr int kScaleCol = kAccs * BN;                    // first tensor-memory column of the scales
     static constexpr int kScaleCols = 4 * (1 + kColBlocks);
     static constexpr int kScaleBufs = 4;
-    static constexpr int kSmem = 1024 + kStages * (kStageBytes + kScaleBytes) + 256;
+    static constexpr int kSmem = 1024 + kStaging + kStages * (kStageBytes + kScaleBytes);
     static_assert(kScaleCol + kScaleBufs * kScaleCols <= 512, "tensor memory");
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
@@ -168,63 +172,75 @@ __device__ __forceinline__ void store_out(void *out, uint64_t i, float v) {
     if constexpr (ODT == LGN_F32) static_cast<float *>(out)[i] = v;
     else static_cast<__nv_bfloat16 *>(out)[i] = __float2bfloat16_rn(v);
 }
-__device__ __forceinline__ void st256(void *p, const uint32_t *w) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-}
-__device__ __forceinline__ void ld256(const void *p, uint32_t *w) {
-    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
 
-// 32 columns of one row, contiguous in memory from element i on and 32-byte aligned.
-template <int ODT>
-__device__ __forceinline__ void store_run(void *out, uint64_t i, float *v, bool accumulate) {
-    uint32_t w[8];
-    if constexpr (ODT == LGN_F32) {
-        float *p = static_cast<float *>(out) + i;
+// Output columns that make 128 bytes.
+template <int ODT> struct OutRun { static constexpr int kCols = ODT == LGN_F32 ? 32 : 64; };
+
+__device__ __forceinline__ void ld128(const void *p, uint32_t *w) {
+    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
+}
+
+// A warp's 32 rows x 128 bytes of the output from row y, column x on; lane l holds row l in v.  They go through
+// the warp's staging buffer (128-byte swizzle, so that the lanes' writes spread over all banks) and one TMA store,
+// which leaves out what lies outside the matrix: stores of 32 bytes per lane to 32 different rows took 13 us per tile of
+// 256 x 192 fp32, four times as long as the tile's MMAs at k = 1024.
+// The warp's BUFS buffers from bufs on are used in turn.
+template <int ODT, int BUFS>
+__device__ __forceinline__ void store_staged(const MmArgs &p, const CUtensorMap *map, uint32_t bufs, uint32_t &turn, uint32_t y, uint32_t x, uint32_t lane, float *v) {
+    constexpr int kCols = OutRun<ODT>::kCols, kPer = kCols / 8;                         // elements per 16 bytes
+    if (p.accumulate && y + lane < p.rows) {
+        const uint64_t i = (uint64_t)(y + lane) * p.ldo + x;
         #pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-            if (accumulate) {
-                ld256(p + k, w);
+        for (int q = 0; q < 8; ++q) {
+            if (x + (q + 1) * kPer <= p.cols) {
+                uint32_t w[4];
+                ld128(static_cast<const char *>(p.out) + (i + q * kPer) * (16 / kPer), w);
                 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[k + j] += __uint_as_float(w[j]);
-            }
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[k + j]);
-            st256(p + k, w);
-        }
-    } else {
-        __nv_bfloat16 *p = static_cast<__nv_bfloat16 *>(out) + i;
-        #pragma unroll
-        for (int k = 0; k < 32; k += 16) {
-            if (accumulate) {
-                ld256(p + k, w);
-                #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[k + 2 * j] += __uint_as_float(w[j] << 16);
-                    v[k + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (ODT == LGN_F32) v[4 * q + j] += __uint_as_float(w[j]);
+                    else { v[8 * q + 2 * j] += __uint_as_float(w[j] << 16); v[8 * q + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
                 }
+            } else {
+                #pragma unroll
+                for (int j = 0; j < kPer; ++j) if (x + q * kPer + j < p.cols) v[q * kPer + j] += load_out<ODT>(p.out, i + q * kPer + j);
             }
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = pack_bf16(v[k + 2 * j], v[k + 2 * j + 1]);
-            st256(p + k, w);
         }
     }
+    const uint32_t buf = bufs + (turn++ % BUFS) * kMmBuffer;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(BUFS - 1) : "memory");   // the buffer's last contents have been read
+    __syncwarp();
+    #pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint32_t w[4];
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (ODT == LGN_F32) w[j] = __float_as_uint(v[4 * q + j]);
+            else w[j] = pack_bf16(v[8 * q + 2 * j], v[8 * q + 2 * j + 1]);
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
+                     :: "r"(buf + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0 && x < p.cols && y < p.rows) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                     :: "l"(map), "r"(buf), "r"(x), "r"(y) : "memory");
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");             // an empty group where nothing was stored
 }
 
 enum MmForm { kFormRows = 0, kFormSwap = 1, kFormSplit = 2 };
 
-// 32 values `step` elements apart from element i on, of which the first `count` exist; eight at a time, so that few
+// N values `step` elements apart from element i on, of which the first `count` exist; eight at a time, so that few
 // addresses and old values are live at once.
-template <int ODT>
+template <int ODT, int N>
 __device__ __forceinline__ void store_strided(void *out, uint64_t i, uint64_t step, uint32_t count, float *v, bool accumulate) {
     #pragma unroll
-    for (int k = 0; k < 32; k += 8) {
+    for (int k = 0; k < N; k += 8) {
         if (accumulate) {
             #pragma unroll
             for (int j = 0; j < 8; ++j) if (k + j < (int)count) v[k + j] += load_out<ODT>(out, i + j * step);
@@ -233,20 +249,6 @@ __device__ __forceinline__ void store_strided(void *out, uint64_t i, uint64_t st
         for (int j = 0; j < 8; ++j) if (k + j < (int)count) store_out<ODT>(out, i + j * step, v[k + j]);
         i += 8 * step;
         asm volatile("" ::: "memory");
-    }
-}
-
-// 32 columns c .. c + 31 of row r of the output tile, held by one lane.
-template <int FORM, int ODT>
-__device__ __forceinline__ void store_columns(const MmArgs &p, uint32_t r, uint32_t c, float *v) {
-    if (r >= p.rows || c >= p.cols) return;
-    const uint32_t count = min(32u, p.cols - c);
-    if constexpr (FORM == kFormSwap) {
-        store_strided<ODT>(p.out, (uint64_t)c * p.ldo + r, p.ldo, count, v, p.accumulate != 0);
-    } else {
-        const uint64_t i = (uint64_t)r * p.ldo + c;
-        if (count == 32) store_run<ODT>(p.out, i, v, p.accumulate != 0);
-        else store_strided<ODT>(p.out, i, 1, count, v, p.accumulate != 0);
     }
 }
 
@@ -259,9 +261,10 @@ __device__ __forceinline__ void tile_at(const MmArgs &p, uint32_t t, uint32_t &t
 
 // An epilogue warp's part of one tile, the BN / 2 columns from tmem_at on: waits for the accumulator(s), adds chunks up
 // (fp32 outputs), hands 32 columns at a time to `put`.  `n` counts accumulators; false: a wait ran out.
-template <int BN, int ACCS, bool CHUNKS, class Full, class Release, class Put>
+template <int BN, int ACCS, int RUN, bool CHUNKS, class Full, class Release, class Put>
 __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, uint32_t &n, volatile uint32_t *stop, Full acc_full, Release release, Put put) {
     constexpr int kCols = BN / 2;
+    static_assert(kCols % RUN == 0, "columns");
     if constexpr (CHUNKS) {
         float sum[kCols];
         for (uint32_t ch = 0; ch < chunks; ++ch, ++n) {
@@ -281,18 +284,19 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
             release(acc);
         }
         #pragma unroll
-        for (int c = 0; c < kCols; c += 32) put(c, sum + c);
+        for (int c = 0; c < kCols; c += RUN) put(c, sum + c);
     } else {
         const uint32_t acc = n % ACCS;
         if (!mbar_wait(acc_full(acc), (n / ACCS) & 1, stop)) return false;
         __syncwarp();
         fence_after();
         #pragma unroll 1
-        for (int c = 0; c < kCols; c += 32) {
-            float v[32];
-            tmem_load32(tmem_at + acc * BN + c, v);
+        for (int c = 0; c < kCols; c += RUN) {
+            float v[RUN];
+            #pragma unroll
+            for (int j = 0; j < RUN; j += 32) tmem_load32(tmem_at + acc * BN + c + j, v + j);
             tmem_load_wait();
-            if (c + 32 >= kCols) { fence_before(); release(acc); }
+            if (c + RUN >= kCols) { fence_before(); release(acc); }
             put(c, v);
         }
         ++n;
@@ -302,16 +306,17 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
 
 template <int BN, int FORM, int ODT>
 __global__ void __launch_bounds__(kMmThreads, 1)
-fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const MmArgs p) {
-    using S = MmShape<BN, 1>;
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const __grid_constant__ CUtensorMap map_out, const MmArgs p) {
+    using S = MmShape<BN, 1, ODT>;
     constexpr bool kChunked = ODT == LGN_F32;
+    constexpr int kRun = FORM == kFormRows ? OutRun<ODT>::kCols : 32;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t stop;
 
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t scales0 = smem0 + S::kStages * S::kStageBytes;
+    const uint32_t staging0 = smem0 + S::kStages * S::kStageBytes, scales0 = staging0 + S::kStaging;
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](uint32_t s) { return bar0 + 8 * s; };
     auto empty = [&](uint32_t s) { return bar0 + 8 * (S::kStages + s); };
@@ -322,7 +327,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), kMmEpiThreads); }
+        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), kMmEpiWarps); }
         mbar_init(drained, 1);
         stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -421,23 +426,27 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         }
     } else {
         dep_wait();                                                             // the output may belong to work before this call
-        uint32_t n = 0;
+        uint32_t n = 0, turn = 0;
         const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, chunks = (kb1 - kb0 + kMmChunk - 1) / kMmChunk;
         for (uint32_t t = tile0; t < tiles; t += tile_step) {
             uint32_t tr, tc;
             tile_at(p, t, tr, tc);
             const uint32_t r = tr * 128 + quad * 32 + lane, c0 = tc * BN + col0;
-            const bool ok = drain_tile<BN, S::kAccs, kChunked>(tmem_at, chunks, n, &stop, acc_full,
-                [&](uint32_t acc) { mbar_arrive(acc_empty(acc)); },
+            const bool ok = drain_tile<BN, S::kAccs, kRun, kChunked>(tmem_at, chunks, n, &stop, acc_full,
+                [&](uint32_t acc) { __syncwarp(); if (lane == 0) mbar_arrive(acc_empty(acc)); },
                 [&](uint32_t c, float *v) {
                     if constexpr (FORM == kFormSplit) {
                         float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
                         #pragma unroll
                         for (int j = 0; j < 32; ++j) part[(col0 + c + j) * 128 + quad * 32 + lane] = v[j];
-                    } else store_columns<FORM, ODT>(p, r, c0 + c, v);
+                    } else if constexpr (FORM == kFormSwap) {
+                        if (r < p.rows && c0 + c < p.cols)
+                            store_strided<ODT, kRun>(p.out, (uint64_t)(c0 + c) * p.ldo + r, p.ldo, p.cols - c0 - c, v, p.accumulate != 0);
+                    } else store_staged<ODT, S::kBuffers>(p, &map_out, staging0 + warp * (S::kBuffers * kMmBuffer), turn, r - lane, c0 + c, lane, v);
                 });
             if (!ok) break;
         }
+        if (FORM == kFormRows && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     if constexpr (FORM == kFormSplit) {
@@ -498,8 +507,10 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {                 
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
+// Relaxed: what it announces are tensor-memory reads that have completed, ordered by the tcgen05 fence; releasing the
+// thread's stores to the cluster as well held it up for 2000 to 4000 clocks.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
 __device__ __forceinline__ void pair_sync() {
     __syncwarp();
@@ -509,16 +520,18 @@ __device__ __forceinline__ void pair_sync() {
 template <int BN, int FORM, int ODT>
 __global__ void __launch_bounds__(kMmThreads, 1) __cluster_dims__(2, 1, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols,
-                const __grid_constant__ CUtensorMap map_sc_rows, const __grid_constant__ CUtensorMap map_sc_cols, const MmArgs p) {
-    using S = MmShape<BN, 2>;
+                const __grid_constant__ CUtensorMap map_sc_rows, const __grid_constant__ CUtensorMap map_sc_cols,
+                const __grid_constant__ CUtensorMap map_out, const MmArgs p) {
+    using S = MmShape<BN, 2, ODT>;
     constexpr bool kChunked = ODT == LGN_F32;
+    constexpr int kRun = FORM == kFormRows ? OutRun<ODT>::kCols : 32;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t stop;
 
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t scales0 = smem0 + S::kStages * S::kStageBytes;
+    const uint32_t staging0 = smem0 + S::kStages * S::kStageBytes, scales0 = staging0 + S::kStaging;
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](uint32_t s) { return bar0 + 8 * s; };
     auto empty = [&](uint32_t s) { return bar0 + 8 * (S::kStages + s); };
@@ -531,7 +544,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_const
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 2 * kMmEpiThreads); }
+        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 2 * kMmEpiWarps); }
         mbar_init(drained, 1);
         stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -622,17 +635,23 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_const
         }
     } else {
         dep_wait();                                                             // the output may belong to work before this call
-        uint32_t n = 0;
+        uint32_t n = 0, turn = 0;
         const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, chunks = (p.kblocks + kMmChunk - 1) / kMmChunk;
         for (uint32_t t = tile0; t < tiles; t += tile_step) {
             uint32_t tr, tc;
             tile_at(p, t, tr, tc);
             const uint32_t r = tr * 256 + rank * 128 + quad * 32 + lane, c0 = tc * BN + col0;
-            const bool ok = drain_tile<BN, S::kAccs, kChunked>(tmem_at, chunks, n, &stop, acc_full,
-                [&](uint32_t acc) { mbar_arrive_remote(in_leader(acc_empty(acc))); },
-                [&](uint32_t c, float *v) { store_columns<FORM, ODT>(p, r, c0 + c, v); });
+            const bool ok = drain_tile<BN, S::kAccs, kRun, kChunked>(tmem_at, chunks, n, &stop, acc_full,
+                [&](uint32_t acc) { __syncwarp(); if (lane == 0) mbar_arrive_remote(in_leader(acc_empty(acc))); },
+                [&](uint32_t c, float *v) {
+                    if constexpr (FORM == kFormSwap) {
+                        if (r < p.rows && c0 + c < p.cols)
+                            store_strided<ODT, kRun>(p.out, (uint64_t)(c0 + c) * p.ldo + r, p.ldo, p.cols - c0 - c, v, p.accumulate != 0);
+                    } else store_staged<ODT, S::kBuffers>(p, &map_out, staging0 + warp * (S::kBuffers * kMmBuffer), turn, r - lane, c0 + c, lane, v);
+                });
             if (!ok) break;
         }
+        if (FORM == kFormRows && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     fence_before();
     __syncthreads();
@@ -652,12 +671,13 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(void *out, uint64_t ldo,
 
 // The kernels a call may take.  `pair`: fp8_pair_kernel.
 struct MmKernel { const void *fn; int bn, pair, form, odt, smem; };
-#define LGN_MM1(BN, F, O) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, F, O>), BN, 0, F, O, MmShape<BN, 1>::kSmem}
-#define LGN_MM2(BN, F, O) {reinterpret_cast<const void *>(&fp8_pair_kernel<BN, F, O>), BN, 1, F, O, MmShape<BN, 2>::kSmem}
+#define LGN_MM1(BN, F, O) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, F, O>), BN, 0, F, O, MmShape<BN, 1, O>::kSmem}
+#define LGN_MM2(BN, F, O) {reinterpret_cast<const void *>(&fp8_pair_kernel<BN, F, O>), BN, 1, F, O, MmShape<BN, 2, O>::kSmem}
 #define LGN_MM3(BN, O) LGN_MM1(BN, kFormRows, O), LGN_MM1(BN, kFormSwap, O), LGN_MM1(BN, kFormSplit, O)
 static const MmKernel kMmKernels[] = {
-    LGN_MM3(64, LGN_F32), LGN_MM3(64, LGN_BF16), LGN_MM3(128, LGN_F32), LGN_MM3(128, LGN_BF16),
-    LGN_MM2(192, kFormRows, LGN_F32), LGN_MM2(192, kFormSwap, LGN_F32), LGN_MM2(192, kFormRows, LGN_BF16), LGN_MM2(192, kFormSwap, LGN_BF16),
+    LGN_MM1(64, kFormSwap, LGN_F32), LGN_MM1(64, kFormSplit, LGN_F32), LGN_MM1(64, kFormSwap, LGN_BF16), LGN_MM1(64, kFormSplit, LGN_BF16),
+    LGN_MM3(128, LGN_F32), LGN_MM3(128, LGN_BF16),
+    LGN_MM2(192, kFormRows, LGN_F32), LGN_MM2(192, kFormSwap, LGN_F32),
     LGN_MM2(256, kFormRows, LGN_BF16), LGN_MM2(256, kFormSwap, LGN_BF16)};
 #undef LGN_MM1
 #undef LGN_MM2
@@ -693,6 +713,16 @@ static bool make_scale_map(CUtensorMap *m, const void *scales, uint64_t tiles) {
     const cuuint32_t box[2] = {128, 1}, es[2] = {1, 1};
     return encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void *>(scales), dim, stride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The output: boxes of 32 rows x 128 bytes.  Needs 16-byte aligned rows.
+static bool make_out_map(CUtensorMap *m, void *out, uint64_t rows, uint64_t cols, uint64_t ldo, int odt) {
+    const uint64_t es = odt == LGN_F32 ? 4 : 2;
+    const cuuint64_t dim[2] = {cols, rows}, stride[1] = {ldo * es};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32}, st[2] = {1, 1};
+    return encode_tiled()(m, odt == LGN_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, out, dim, stride, box, st,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The kernels need more dynamic shared memory than the default limit; raised once per device and kernel.
@@ -767,7 +797,7 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
         ranges_overlap(out, ob, a_scales, lgn_fp8_scales_bytes(m, k)) || ranges_overlap(out, ob, b_scales, lgn_fp8_scales_bytes(n, k)))
         return LGN_ERR_INVALID_ARG;
     if (sms < 1 || encode_tiled() == nullptr) return LGN_ERR_CUDA;
-    const bool vec = aligned_to(out, 32) && (ldo * es) % 32 == 0;
+    const bool vec = aligned_to(out, 16) && (ldo * es) % 16 == 0;
     const uint64_t kblocks = (k + 127) / 128;
     const MmPlan plan = plan_matmul(m, n, kblocks, vec, out_dt, sms);
     if (plan.kernel < 0) return LGN_ERR_UNSUPPORTED;
@@ -791,7 +821,8 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     p.accumulate = accumulate != 0;
     const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c, slots = (uint64_t)(q.pair ? sms / 2 : sms);
     if (tiles > 0x3fffffffull) return LGN_ERR_UNSUPPORTED;
-    CUtensorMap mr, mc, sr, sc;
+    CUtensorMap mr, mc, sr, sc, mo = {};
+    if (q.form == kFormRows && !make_out_map(&mo, out, m, n, ldo, out_dt)) return LGN_ERR_CUDA;
     if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, q.pair ? bn / 2 : bn)) return LGN_ERR_CUDA;
     if (!allow_smem(plan.kernel)) return LGN_ERR_CUDA;
     uint64_t grid = q.form == kFormSplit ? tiles * plan.split : (tiles < slots ? tiles : slots);
@@ -800,9 +831,9 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     if (q.pair) {
         if (!make_scale_map(&sr, p.sc_rows, (uint64_t)((p.rows + 127) / 128) * p.groups) ||
             !make_scale_map(&sc, p.sc_cols, (uint64_t)((p.cols + 127) / 128) * p.groups)) return LGN_ERR_CUDA;
-        void *args[] = {&mr, &mc, &sr, &sc, &p};
+        void *args[] = {&mr, &mc, &sr, &sc, &mo, &p};
         return launch_dependent(q.fn, dim3((unsigned)(2 * grid)), dim3(kMmThreads), args, (size_t)q.smem, stream);
     }
-    void *args[] = {&mr, &mc, &p};
+    void *args[] = {&mr, &mc, &mo, &p};
     return launch_dependent(q.fn, dim3((unsigned)grid), dim3(kMmThreads), args, (size_t)q.smem, stream, q.form == kFormSplit ? plan.split : 1);
 }

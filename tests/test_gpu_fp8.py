@@ -132,6 +132,24 @@ def test_product(lgn, m, n, k, fa, fb, od):
     check_product(out, operand_values(a)[0], operand_values(b)[0], k)
 
 
+@pytest.mark.parametrize("fa,fb,od", [(0, 0, "bf16"), (0, 1, "f32")])
+@pytest.mark.parametrize("m,n,k", [(3000, 2501, 700), (2049, 4112, 1300), (5000, 1160, 2100), (1111, 5003, 1025)])
+def test_large_product(lgn, m, n, k, fa, fb, od):
+    """Sizes that take the kernels for large products, in both orientations, with ragged edges; accumulating too."""
+    a, _ = lgn.lgn_fp8_quantize(values(m, k, m + k, torch.float32), fa)
+    b, _ = lgn.lgn_fp8_quantize(values(n, k, n + 3 * k, torch.bfloat16), fb)
+    av, bv = operand_values(a)[0], operand_values(b)[0]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    buf = torch.full((m + 2, n), 7.0, dtype=DT[od], device="cuda")
+    out = lgn.lgn_fp8_matmul(a, b, out=buf[1:m + 1], status=status)
+    check_product(out, av, bv, k)
+    before = to_np(out)
+    lgn.lgn_fp8_matmul(a, b, out=out, accumulate=True, status=status)
+    check_product(out, av, bv, k, before)
+    assert int(status.item()) == 0
+    assert bool((buf[0] == 7.0).all()) and bool((buf[-1] == 7.0).all())
+
+
 @pytest.mark.parametrize("od", ["bf16", "f32"])
 @pytest.mark.parametrize("m,n,k", [(4, 300, 700), (130, 200, 300), (777, 640, 1000), (1500, 2000, 520), (40, 96, 4096)])
 def test_product_accumulates_into_views(lgn, m, n, k, od):
