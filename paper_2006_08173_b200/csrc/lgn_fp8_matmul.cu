@@ -6,18 +6,19 @@
 // byte.  Products and sums stay in fp32 in tensor memory over the whole of k and are rounded once, to the
 // output's type.
 //
-// Two kernels share one shape.  fp8_pair_kernel, for large products: two CTAs (one SM each) work on a tile of
-// 256 rows of one operand ("rows") by BN rows of the other ("cols"), each CTA bringing its own 128 rows and one half
-// of the BN, so that a step of k (128) costs an SM 32 KiB of shared-memory writes and as many operand reads for 512
-// clocks of MMA.  A single CTA's 128 x 192 tile needs 1.7 times that traffic per flop and stops at 54 % of the tensor
-// pipe (8192 x 8192 x 4096: 258 us, bound by shared memory).  fp8_matmul_kernel, for small ones: one CTA per tile of
-// 128 x BN, persistent over tiles, or (SPLIT) one tile per cluster with the CTAs of a cluster taking
-// consecutive shares of k and adding their fp32 tiles through distributed shared memory in rank order.
-//   warp 8  brings codes into a ring of shared-memory stages (TMA, 128-byte swizzle) and, every fourth step, the
-//           512-byte scale tiles of four blocks;
-//   warp 9  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step;
+// One CTA, or a pair of CTAs on two SMs (CTAS = 2), works on tiles of 128 CTAS rows of one operand ("rows") by BN rows of
+// the other ("cols").  In a pair the CTA of rank 0 issues the MMAs of both (cta_group::2) and each CTA brings
+// its own 128 rows and one half of the BN: at 256 x 256 a step of k (128) costs an SM 32 KiB of shared-memory writes
+// and as many operand reads for 512 clocks of MMA, where a lone CTA's 128 x 192 needs 1.7 times that per flop
+// (8192 x 8192 x 4096: 216 us against 258).  Small products take lone CTAs, persistent over tiles, or (SPLIT) one tile
+// per cluster with the CTAs of a cluster taking consecutive shares of k and adding their fp32 tiles through
+// distributed shared memory in rank order.
+//   warp 8  brings codes into a ring of shared-memory stages (TMA, 128-byte swizzle) and, every fourth step, the 512-byte
+//           scale tiles of four blocks;
+//   warp 9  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step.  (Scales
+//           written to tensor memory by four warps of their own, tcgen05.st, came out 8 to 16 % slower.)
 //   warps 0..7  read the finished tile from tensor memory (warp w: lanes 32 (w mod 4) on, column half w / 4), round
-//           and store.
+//               and store.
 // SWAP: `rows` runs along the contiguous dimension of the output, so that the 32 lanes of a warp, which hold
 // 32 rows, write contiguous memory whatever the alignment.
 //
@@ -47,7 +48,6 @@ constexpr int kMmGroupRows = 16;                 // row tiles walked before the 
 constexpr long long kMmWaitClocks = 4000000000ll;   // about two seconds
 
 struct MmArgs {
-    const uint8_t *sc_rows, *sc_cols;            // scale tiles
     void *out;
     uint64_t ldo;
     uint32_t *status;
@@ -63,7 +63,7 @@ constexpr uint32_t kMmChunk = 8;                 // steps of k (128 each) that s
 
 constexpr int kMmBuffer = 4096;                   // 32 rows x 128 bytes of output
 
-// CTAS: 1 (fp8_matmul_kernel) or 2 (fp8_pair_kernel); bytes and stages per CTA.
+// Bytes and stages per CTA.
 template <int BN, int CTAS, int ODT> struct MmShape {
     static constexpr int kBuffers = ODT == LGN_F32 ? 2 : 1;         // output buffers of an epilogue warp
     static constexpr int kStaging = kMmEpiWarps * kBuffers * kMmBuffer;
@@ -111,6 +111,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     if (mbar_try(bar, parity)) return true;
     return mbar_wait_slow(bar, parity, stop);
 }
+// The same for a whole warp, with a result that is uniform to the compiler too.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+    return __all_sync(0xffffffffu, mbar_wait_slow(bar, parity, stop));
+}
+// True in one lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) :: "memory");
+    return ok != 0;
+}
 // Bounded wait for what is in flight after a stop.
 __device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
@@ -118,46 +129,75 @@ __device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
         if (clock64() - t0 > kMmWaitClocks) return;
 }
 
+// A box into this CTA's shared memory; the barrier may be the other CTA's of a pair.
+template <int CTAS>
 __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                     :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                     :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
 
-// Shared-memory descriptors.  Code tiles: rows of 128 bytes, 128-byte swizzle, 8 rows = 1024 bytes apart
-// from the next 8.  Scale tiles: no swizzle, groups of 8 rows of 16 bytes 128 bytes apart.
+// Shared-memory descriptor of codes: rows of 128 bytes, 128-byte swizzle, 8 rows = 1024 bytes apart from the next 8.
 __device__ __forceinline__ uint64_t desc_codes(uint32_t addr) {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
-}
 
+template <int CTAS>
 __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add) : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add) : "memory");
 }
-__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+// A scale tile (512 bytes of shared memory, no swizzle, groups of 8 rows of 16 bytes 128 bytes apart) to four columns of
+// tensor memory, the same in each quarter of the lanes; of both CTAs of a pair.
+template <int CTAS>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t smem) {
+    const uint64_t desc = (uint64_t)((smem & 0x3ffffu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+    if constexpr (CTAS == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
 }
+// Signals a barrier (of both CTAs of a pair) when the MMAs issued so far have finished.
+template <int CTAS>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     :: "r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t in_leader(uint32_t addr) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+// Arrives at a barrier of the CTA that issues the MMAs.  Relaxed: what it announces are tensor-memory accesses that have
+// completed, ordered by the tcgen05 fence; releasing the thread's stores to the cluster as well held it up
+// for 2000 to 4000 clocks.
+template <int CTAS>
+__device__ __forceinline__ void arrive_leader(uint32_t bar) {
+    if constexpr (CTAS == 2) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(in_leader(bar)) : "memory");
+    else mbar_arrive(bar);
+}
+__device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after()  { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float *v) {
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, float *v) {
     uint32_t *r = reinterpret_cast<uint32_t *>(v);
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -273,12 +313,12 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
             __syncwarp();
             fence_after();
             #pragma unroll
-            for (int c = 0; c < kCols; c += 32) {
-                float v[32];
-                tmem_load32(tmem_at + acc * BN + c, v);
+            for (int c = 0; c < kCols; c += 16) {
+                float v[16];
+                tmem_load16(tmem_at + acc * BN + c, v);
                 tmem_load_wait();
                 #pragma unroll
-                for (int j = 0; j < 32; ++j) sum[c + j] = ch == 0 ? v[j] : sum[c + j] + v[j];
+                for (int j = 0; j < 16; ++j) sum[c + j] = ch == 0 ? v[j] : sum[c + j] + v[j];
             }
             fence_before();
             release(acc);
@@ -294,7 +334,7 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
         for (int c = 0; c < kCols; c += RUN) {
             float v[RUN];
             #pragma unroll
-            for (int j = 0; j < RUN; j += 32) tmem_load32(tmem_at + acc * BN + c + j, v + j);
+            for (int j = 0; j < RUN; j += 16) tmem_load16(tmem_at + acc * BN + c + j, v + j);
             tmem_load_wait();
             if (c + RUN >= kCols) { fence_before(); release(acc); }
             put(c, v);
@@ -304,10 +344,11 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
     return true;
 }
 
-template <int BN, int FORM, int ODT>
+template <int BN, int CTAS, int FORM, int ODT>
 __global__ void __launch_bounds__(kMmThreads, 1)
-fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const __grid_constant__ CUtensorMap map_out, const MmArgs p) {
-    using S = MmShape<BN, 1, ODT>;
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const __grid_constant__ CUtensorMap map_sc_rows,
+                  const __grid_constant__ CUtensorMap map_sc_cols, const __grid_constant__ CUtensorMap map_out, const MmArgs p) {
+    using S = MmShape<BN, CTAS, ODT>;
     constexpr bool kChunked = ODT == LGN_F32;
     constexpr int kRun = FORM == kFormRows ? OutRun<ODT>::kCols : 32;
     extern __shared__ uint8_t smem_raw[];
@@ -324,10 +365,17 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     auto acc_empty = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + S::kAccs + a); };
     const uint32_t drained = bar0 + 8 * (2 * S::kStages + 2 * S::kAccs);
 
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank = 0, nrank = 1;                           // within the cluster: a pair, or the CTAs that share k
+    if constexpr (CTAS == 2 || FORM == kFormSplit) {
+        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(nrank));
+    }
+    const bool leader = CTAS == 1 || rank == 0;             // issues the MMAs; full and acc_empty are its barriers
+    const uint32_t half = CTAS == 2 ? rank : 0;
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), kMmEpiWarps); }
+        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), CTAS * kMmEpiWarps); }
         mbar_init(drained, 1);
         stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -335,21 +383,28 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     if (warp == 8 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_rows) : "memory");
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_cols) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_sc_rows) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_sc_cols) : "memory");
+        if constexpr (FORM == kFormRows) asm volatile("prefetch.tensormap [%0];" :: "l"(&map_out) : "memory");
     }
     if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if constexpr (CTAS == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
     }
     fence_before();
     __syncthreads();
+    if constexpr (CTAS == 2) cluster_sync();                // barriers of both CTAs are set up, tensor memory of both allocated
     fence_after();
-    const uint32_t tmem = tmem_base_s;
+    const uint32_t tmem = 0;                                // where an allocation of all 512 columns begins
 
     // this CTA's tiles and steps of k
-    uint32_t rank = 0, nrank = 1, tile0 = blockIdx.x, tile_step = gridDim.x, kb0 = 0, kb1 = p.kblocks;
+    uint32_t tile0 = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS, kb0 = 0, kb1 = p.kblocks;
     if constexpr (FORM == kFormSplit) {
-        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(nrank));
         tile0 = blockIdx.x / nrank;
         tile_step = 0x7fffffffu;
         kb0 = rank * p.split_groups * 4;
@@ -357,72 +412,85 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     }
     const uint32_t tiles = p.tiles_r * p.tiles_c;
 
+    // Warps 8 and 9 run their loops whole, one elected lane issuing: in code that only one lane runs the compiler moves every
+    // operand of a TMA or MMA instruction to a uniform register at each use, which took 700 clocks per step of k.
     if (warp == 8) {
-        if (lane == 0) {
-            dep_wait();
-            uint32_t it = 0;
-            bool ok = true;
-            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
-                uint32_t tr, tc;
-                tile_at(p, t, tr, tc);
-                const uint32_t sb0 = (tc * BN) >> 7, sb_n = (p.cols + 127) >> 7;
-                for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
-                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (!(ok = mbar_wait(empty(s), ph ^ 1, &stop))) break;
-                    const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
-                    uint32_t bytes = S::kStageBytes;
-                    const bool with_scales = (kb & 3) == 0, second = S::kColBlocks > 1 && sb0 + 1 < sb_n;
-                    if (with_scales) bytes += 1024 + (second ? 512 : 0);
-                    mbar_expect(full(s), bytes);
-                    tma_tile(a, &map_rows, full(s), (int)(kb * 128), (int)(tr * 128));
-                    tma_tile(a + 128 * 128, &map_cols, full(s), (int)(kb * 128), (int)(tc * BN));
-                    if (with_scales) {
-                        const uint64_t g = kb >> 2;
-                        bulk_copy(sc, p.sc_rows + ((uint64_t)tr * p.groups + g) * 512, 512, full(s));
-                        bulk_copy(sc + 512, p.sc_cols + ((uint64_t)sb0 * p.groups + g) * 512, 512, full(s));
-                        if (second) bulk_copy(sc + 1024, p.sc_cols + ((uint64_t)(sb0 + 1) * p.groups + g) * 512, 512, full(s));
+        dep_wait();
+        uint32_t s = 0, ph = 1, it = 0;
+        bool ok = true;
+        for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
+            uint32_t tr, tc;
+            tile_at(p, t, tr, tc);
+            const int y_rows = (int)((tr * CTAS + half) * 128), y_cols = (int)(tc * BN + half * (BN / 2));
+            int y_sr = (int)((tr * CTAS + half) * p.groups + (kb0 >> 2)), y_sc = (int)(((tc * BN) >> 7) * p.groups + (kb0 >> 2));
+            for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
+                if (!(ok = mbar_wait_warp(empty(s), ph, &stop))) break;
+                const uint32_t a = smem0 + s * S::kStageBytes, bar = CTAS == 2 ? in_leader(full(s)) : full(s);
+                const bool with_scales = (kb & 3) == 0;
+                if (elect_one()) {
+                    if (leader) mbar_expect(full(s), CTAS * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));   // the bytes of both CTAs
+                    tma_tile<CTAS>(a, &map_rows, bar, (int)(kb * 128), y_rows);
+                    tma_tile<CTAS>(a + 128 * 128, &map_cols, bar, (int)(kb * 128), y_cols);
+                    if (with_scales) {                                          // tiles past the end read as zeros
+                        const uint32_t sc = scales0 + s * S::kScaleBytes;
+                        tma_tile<CTAS>(sc, &map_sc_rows, bar, 0, y_sr);
+                        #pragma unroll
+                        for (int b = 0; b < S::kColBlocks; ++b) tma_tile<CTAS>(sc + 512 * (1 + b), &map_sc_cols, bar, 0, y_sc + b * (int)p.groups);
                     }
                 }
+                if (with_scales) { ++y_sr; ++y_sc; }
+                if (++s == S::kStages) { s = 0; ph ^= 1; }
             }
-            if (!ok)                                                            // wait for the copies in flight
-                for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
-                    mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
         }
+        if (!ok && leader)                                                      // wait for the copies in flight
+            for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
+                mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
     } else if (warp == 9) {
-        if (lane == 0) {
-            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | (1u << 27);
-            uint32_t it = 0, n = 0, grp = 0;
+        if (leader) {
+            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)CTAS << 27);
+            const uint64_t desc0 = desc_codes(smem0);
+            uint32_t s = 0, ph = 0, acc = 0, acc_ph = 1, grp = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
-                uint32_t tr, tc, sa = 0, sb = 0;
+                uint32_t tr, tc, sa = 0;
                 tile_at(p, t, tr, tc);
-                const uint32_t col_off = ((tc * BN) & 127) >> 5;
-                for (uint32_t c0 = kb0; ok && c0 < kb1; ++n) {                   // one accumulator per chunk of k
-                    const uint32_t c1 = kChunked ? min(kb1, c0 + kMmChunk) : kb1, acc = n % S::kAccs, d = tmem + acc * BN;
-                    if (!(ok = mbar_wait(acc_empty(acc), ((n / S::kAccs) & 1) ^ 1, &stop))) break;
+                const uint32_t col_off = 4 + (((tc * BN) & 127) >> 5);          // columns' scales: the tile may begin inside a scale tile
+                for (uint32_t c0 = kb0; ok && c0 < kb1;) {                      // one accumulator per chunk of k
+                    const uint32_t c1 = kChunked ? min(kb1, c0 + kMmChunk) : kb1, d = tmem + acc * BN;
+                    if (!(ok = mbar_wait_warp(acc_empty(acc), acc_ph, &stop))) break;
                     fence_after();
-                    for (uint32_t kb = c0; kb < c1; ++kb, ++it) {
-                        const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                        if (!(ok = mbar_wait(full(s), ph, &stop))) break;
+                    for (uint32_t kb = c0; kb < c1; ++kb) {
+                        if (!(ok = mbar_wait_warp(full(s), ph, &stop))) break;
                         fence_after();
-                        const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
-                        if ((kb & 3) == 0) {
-                            sa = tmem + S::kScaleCol + (grp++ % S::kScaleBufs) * S::kScaleCols;
-                            sb = sa + 4;
-                            #pragma unroll
-                            for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales(sa + 4 * b, desc_scales(sc + 512 * b));
+                        const bool with_scales = (kb & 3) == 0;
+                        if (with_scales) {
+                            sa = tmem + S::kScaleCol + grp * S::kScaleCols;
+                            grp = (grp + 1) % S::kScaleBufs;
                         }
                         const uint32_t idesc = idesc0 | ((kb & 3) << 4) | ((kb & 3) << 29);
-                        const uint64_t da = desc_codes(a), db = desc_codes(a + 128 * 128);
-                        #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_scaled(d, da + 2 * k, db + 2 * k, idesc, sa, sb + col_off, kb > c0 || k > 0);
-                        mma_commit(empty(s));
+                        const uint64_t da = desc0 + s * (uint32_t)(S::kStageBytes >> 4), db = da + (128 * 128 >> 4);
+                        if (elect_one()) {
+                            if (with_scales) {
+                                #pragma unroll
+                                for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales<CTAS>(sa + 4 * b, scales0 + s * S::kScaleBytes + 512 * b);
+                            }
+                            #pragma unroll
+                            for (int k = 0; k < 4; ++k) mma_scaled<CTAS>(d, da + 2 * k, db + 2 * k, idesc, sa, sa + col_off, kb > c0 || k > 0);
+                            mma_commit<CTAS>(empty(s));
+                            if (kb + 1 == c1) mma_commit<CTAS>(acc_full(acc));
+                        }
+                        __syncwarp();
+                        if (++s == S::kStages) { s = 0; ph ^= 1; }
                     }
-                    if (ok) mma_commit(acc_full(acc));
                     c0 = c1;
+                    if (++acc == S::kAccs) { acc = 0; acc_ph ^= 1; }
                 }
             }
-            if (!ok) { mma_commit(drained); mbar_drain(drained, 0); }
+            if (!ok) {
+                if (elect_one()) mma_commit<CTAS>(drained);
+                __syncwarp();
+                mbar_drain(drained, 0);
+            }
         }
     } else {
         dep_wait();                                                             // the output may belong to work before this call
@@ -431,9 +499,9 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         for (uint32_t t = tile0; t < tiles; t += tile_step) {
             uint32_t tr, tc;
             tile_at(p, t, tr, tc);
-            const uint32_t r = tr * 128 + quad * 32 + lane, c0 = tc * BN + col0;
+            const uint32_t r = (tr * CTAS + half) * 128 + quad * 32 + lane, c0 = tc * BN + col0;
             const bool ok = drain_tile<BN, S::kAccs, kRun, kChunked>(tmem_at, chunks, n, &stop, acc_full,
-                [&](uint32_t acc) { __syncwarp(); if (lane == 0) mbar_arrive(acc_empty(acc)); },
+                [&](uint32_t acc) { __syncwarp(); if (lane == 0) arrive_leader<CTAS>(acc_empty(acc)); },
                 [&](uint32_t c, float *v) {
                     if constexpr (FORM == kFormSplit) {
                         float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
@@ -452,7 +520,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     if constexpr (FORM == kFormSplit) {
         // every CTA's partial tile is in its own shared memory: column c is added over the ranks, in rank
         // order, by the CTA c mod nrank
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        cluster_sync();
         if (threadIdx.x < kMmEpiThreads && tile0 < tiles) {
             uint32_t tr, tc;
             tile_at(p, tile0, tr, tc);
@@ -473,192 +541,16 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                 }
             }
         }
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
     fence_before();
     __syncthreads();
+    if constexpr (CTAS == 2 || FORM == kFormSplit) cluster_sync();              // nothing of the other CTAs is in flight any more
     fence_after();
     if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
-}
-
-// ------------------------------------------------------------------ pairs of CTAs
-// The CTA of rank 0 issues the MMAs of both (cta_group::2); full barriers live there and count the bytes of both CTAs'
-// copies, empty and accumulator barriers are signalled in both.
-__device__ __forceinline__ uint32_t in_leader(uint32_t addr) {
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
-    return r;
-}
-__device__ __forceinline__ void tma_tile_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void mma_scaled_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add) : "memory");
-}
-__device__ __forceinline__ void copy_scales_pair(uint32_t taddr, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
-}
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {                        // the barrier at this offset in both CTAs
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 :: "r"(bar), "h"((uint16_t)3) : "memory");
-}
-// Relaxed: what it announces are tensor-memory reads that have completed, ordered by the tcgen05 fence; releasing the
-// thread's stores to the cluster as well held it up for 2000 to 4000 clocks.
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
-}
-__device__ __forceinline__ void pair_sync() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-template <int BN, int FORM, int ODT>
-__global__ void __launch_bounds__(kMmThreads, 1) __cluster_dims__(2, 1, 1)
-fp8_pair_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols,
-                const __grid_constant__ CUtensorMap map_sc_rows, const __grid_constant__ CUtensorMap map_sc_cols,
-                const __grid_constant__ CUtensorMap map_out, const MmArgs p) {
-    using S = MmShape<BN, 2, ODT>;
-    constexpr bool kChunked = ODT == LGN_F32;
-    constexpr int kRun = FORM == kFormRows ? OutRun<ODT>::kCols : 32;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
-    __shared__ uint32_t tmem_base_s;
-    __shared__ volatile uint32_t stop;
-
-    const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t staging0 = smem0 + S::kStages * S::kStageBytes, scales0 = staging0 + S::kStaging;
-    const uint32_t bar0 = smem_u32(bars);
-    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
-    auto empty = [&](uint32_t s) { return bar0 + 8 * (S::kStages + s); };
-    auto acc_full = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + a); };
-    auto acc_empty = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + S::kAccs + a); };
-    const uint32_t drained = bar0 + 8 * (2 * S::kStages + 2 * S::kAccs);
-
-    uint32_t rank;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int a = 0; a < S::kAccs; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 2 * kMmEpiWarps); }
-        mbar_init(drained, 1);
-        stop = 0u;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == 8 && lane == 0) {
-        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_rows) : "memory");
-        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_cols) : "memory");
-        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_sc_rows) : "memory");
-        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_sc_cols) : "memory");
-    }
     if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_base_s)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        if constexpr (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
     }
-    fence_before();
-    __syncthreads();
-    pair_sync();                                            // barriers of both CTAs are set up, tensor memory of both allocated
-    fence_after();
-    const uint32_t tmem = tmem_base_s;
-    const uint32_t tile0 = blockIdx.x >> 1, tile_step = gridDim.x >> 1, tiles = p.tiles_r * p.tiles_c;
-
-    if (warp == 8) {
-        if (lane == 0) {
-            dep_wait();
-            uint32_t it = 0;
-            bool ok = true;
-            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
-                uint32_t tr, tc;
-                tile_at(p, t, tr, tc);
-                const uint32_t row0 = tr * 256 + rank * 128, sr0 = row0 >> 7, sc0 = (tc * BN) >> 7;
-                for (uint32_t kb = 0; kb < p.kblocks; ++kb, ++it) {
-                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (!(ok = mbar_wait(empty(s), ph ^ 1, &stop))) break;
-                    const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
-                    const bool with_scales = (kb & 3) == 0;
-                    if (rank == 0) mbar_expect(full(s), 2 * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));
-                    const uint32_t bar = in_leader(full(s));
-                    tma_tile_pair(a, &map_rows, bar, (int)(kb * 128), (int)row0);
-                    tma_tile_pair(a + 128 * 128, &map_cols, bar, (int)(kb * 128), (int)(tc * BN + rank * (BN / 2)));
-                    if (with_scales) {                                          // tiles past the end read as zeros
-                        const uint32_t g = kb >> 2;
-                        tma_tile_pair(sc, &map_sc_rows, bar, 0, (int)(sr0 * p.groups + g));
-                        #pragma unroll
-                        for (int b = 0; b < S::kColBlocks; ++b)
-                            tma_tile_pair(sc + 512 * (1 + b), &map_sc_cols, bar, 0, (int)((sc0 + b) * p.groups + g));
-                    }
-                }
-            }
-            if (!ok && rank == 0)                                               // wait for the copies in flight, the other CTA's too
-                for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
-                    mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
-        }
-    } else if (warp == 9) {
-        if (lane == 0 && rank == 0) {
-            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | (2u << 27);
-            uint32_t it = 0, n = 0, grp = 0;
-            bool ok = true;
-            for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
-                uint32_t tr, tc, sa = 0, sb = 0;
-                tile_at(p, t, tr, tc);
-                const uint32_t col_off = ((tc * BN) & 127) >> 5;
-                for (uint32_t c0 = 0; ok && c0 < p.kblocks; ++n) {
-                    const uint32_t c1 = kChunked ? min(p.kblocks, c0 + kMmChunk) : p.kblocks, acc = n % S::kAccs, d = tmem + acc * BN;
-                    if (!(ok = mbar_wait(acc_empty(acc), ((n / S::kAccs) & 1) ^ 1, &stop))) break;
-                    fence_after();
-                    for (uint32_t kb = c0; kb < c1; ++kb, ++it) {
-                        const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                        if (!(ok = mbar_wait(full(s), ph, &stop))) break;
-                        fence_after();
-                        const uint32_t a = smem0 + s * S::kStageBytes, sc = scales0 + s * S::kScaleBytes;
-                        if ((kb & 3) == 0) {
-                            sa = tmem + S::kScaleCol + (grp++ % S::kScaleBufs) * S::kScaleCols;
-                            sb = sa + 4;
-                            #pragma unroll
-                            for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales_pair(sa + 4 * b, desc_scales(sc + 512 * b));
-                        }
-                        const uint32_t idesc = idesc0 | ((kb & 3) << 4) | ((kb & 3) << 29);
-                        const uint64_t da = desc_codes(a), db = desc_codes(a + 128 * 128);
-                        #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_scaled_pair(d, da + 2 * k, db + 2 * k, idesc, sa, sb + col_off, kb > c0 || k > 0);
-                        mma_commit_pair(empty(s));
-                    }
-                    if (ok) mma_commit_pair(acc_full(acc));
-                    c0 = c1;
-                }
-            }
-            if (!ok) { mma_commit_pair(drained); mbar_drain(drained, 0); }
-        }
-    } else {
-        dep_wait();                                                             // the output may belong to work before this call
-        uint32_t n = 0, turn = 0;
-        const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, chunks = (p.kblocks + kMmChunk - 1) / kMmChunk;
-        for (uint32_t t = tile0; t < tiles; t += tile_step) {
-            uint32_t tr, tc;
-            tile_at(p, t, tr, tc);
-            const uint32_t r = tr * 256 + rank * 128 + quad * 32 + lane, c0 = tc * BN + col0;
-            const bool ok = drain_tile<BN, S::kAccs, kRun, kChunked>(tmem_at, chunks, n, &stop, acc_full,
-                [&](uint32_t acc) { __syncwarp(); if (lane == 0) mbar_arrive_remote(in_leader(acc_empty(acc))); },
-                [&](uint32_t c, float *v) {
-                    if constexpr (FORM == kFormSwap) {
-                        if (r < p.rows && c0 + c < p.cols)
-                            store_strided<ODT, kRun>(p.out, (uint64_t)(c0 + c) * p.ldo + r, p.ldo, p.cols - c0 - c, v, p.accumulate != 0);
-                    } else store_staged<ODT, S::kBuffers>(p, &map_out, staging0 + warp * (S::kBuffers * kMmBuffer), turn, r - lane, c0 + c, lane, v);
-                });
-            if (!ok) break;
-        }
-        if (FORM == kFormRows && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    }
-    fence_before();
-    __syncthreads();
-    pair_sync();                                            // nothing of either CTA is in flight any more
-    fence_after();
-    if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem));
 }
 
 // k = 0: nothing is added.
@@ -669,19 +561,16 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(void *out, uint64_t ldo,
         store_out<ODT>(out, (i / cols) * ldo + i % cols, 0.0f);
 }
 
-// The kernels a call may take.  `pair`: fp8_pair_kernel.
-struct MmKernel { const void *fn; int bn, pair, form, odt, smem; };
-#define LGN_MM1(BN, F, O) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, F, O>), BN, 0, F, O, MmShape<BN, 1, O>::kSmem}
-#define LGN_MM2(BN, F, O) {reinterpret_cast<const void *>(&fp8_pair_kernel<BN, F, O>), BN, 1, F, O, MmShape<BN, 2, O>::kSmem}
-#define LGN_MM3(BN, O) LGN_MM1(BN, kFormRows, O), LGN_MM1(BN, kFormSwap, O), LGN_MM1(BN, kFormSplit, O)
+// The kernels a call may take.
+struct MmKernel { const void *fn; int bn, ctas, form, odt, smem; };
+#define LGN_MM(BN, C, F, O) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, C, F, O>), BN, C, F, O, MmShape<BN, C, O>::kSmem}
 static const MmKernel kMmKernels[] = {
-    LGN_MM1(64, kFormSwap, LGN_F32), LGN_MM1(64, kFormSplit, LGN_F32), LGN_MM1(64, kFormSwap, LGN_BF16), LGN_MM1(64, kFormSplit, LGN_BF16),
-    LGN_MM3(128, LGN_F32), LGN_MM3(128, LGN_BF16),
-    LGN_MM2(192, kFormRows, LGN_F32), LGN_MM2(192, kFormSwap, LGN_F32),
-    LGN_MM2(256, kFormRows, LGN_BF16), LGN_MM2(256, kFormSwap, LGN_BF16)};
-#undef LGN_MM1
-#undef LGN_MM2
-#undef LGN_MM3
+    LGN_MM(64, 1, kFormSwap, LGN_F32), LGN_MM(64, 1, kFormSplit, LGN_F32), LGN_MM(64, 1, kFormSwap, LGN_BF16), LGN_MM(64, 1, kFormSplit, LGN_BF16),
+    LGN_MM(128, 1, kFormRows, LGN_F32), LGN_MM(128, 1, kFormSwap, LGN_F32), LGN_MM(128, 1, kFormSplit, LGN_F32),
+    LGN_MM(128, 1, kFormRows, LGN_BF16), LGN_MM(128, 1, kFormSwap, LGN_BF16), LGN_MM(128, 1, kFormSplit, LGN_BF16),
+    LGN_MM(192, 2, kFormRows, LGN_F32), LGN_MM(192, 2, kFormSwap, LGN_F32),
+    LGN_MM(256, 2, kFormRows, LGN_BF16), LGN_MM(256, 2, kFormSwap, LGN_BF16)};
+#undef LGN_MM
 constexpr int kMmCount = (int)(sizeof kMmKernels / sizeof kMmKernels[0]);
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -752,14 +641,14 @@ static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, bool vec, in
     for (int i = 0; i < kMmCount; ++i) {
         const MmKernel &q = kMmKernels[i];
         if (q.odt != odt || (q.form == kFormRows && !vec)) continue;
-        const uint64_t rows = q.pair ? 256 : 128, bn = (uint64_t)q.bn, r = q.form == kFormRows ? m : n, c = q.form == kFormRows ? n : m;
-        const uint64_t tiles = ((r + rows - 1) / rows) * ((c + bn - 1) / bn), slots = (uint64_t)(q.pair ? sms / 2 : sms);
+        const uint64_t rows = 128 * (uint64_t)q.ctas, bn = (uint64_t)q.bn, r = q.form == kFormRows ? m : n, c = q.form == kFormRows ? n : m;
+        const uint64_t tiles = ((r + rows - 1) / rows) * ((c + bn - 1) / bn), slots = (uint64_t)(sms / q.ctas);
         for (uint64_t want = q.form == kFormSplit ? 2 : 1; want <= (q.form == kFormSplit ? 8u : 1u); want *= 2) {
             const uint64_t per = (groups + want - 1) / want, s = q.form == kFormSplit ? (groups + per - 1) / per : 1;
             if (q.form == kFormSplit && (s < 2 || tiles * s > slots)) continue;
             const uint64_t steps = q.form == kFormSplit && per * 4 < kblocks ? per * 4 : kblocks;
             const double rounds = (double)((tiles * s + slots - 1) / slots);
-            const double step = q.pair ? (bn == 256 ? 600 : 500) : (bn == 128 ? 500 : 400);
+            const double step = q.ctas == 2 ? (bn == 256 ? 600 : 500) : (bn == 128 ? 500 : 400);
             const double tile = (bn == 256 ? 1500 : 400) + (q.form == kFormSwap ? 4.0 * bn : 0) + (s > 1 ? 3000 : 0);
             const double cost = rounds * (steps * step + tile);
             if (cost < best_cost) { best_cost = cost; best = {i, (uint32_t)s, (uint32_t)per}; }
@@ -803,11 +692,9 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     if (plan.kernel < 0) return LGN_ERR_UNSUPPORTED;
     const MmKernel &q = kMmKernels[plan.kernel];
     const bool swap = q.form != kFormRows;
-    const uint32_t bn = (uint32_t)q.bn, tile_rows = q.pair ? 256 : 128;
+    const uint32_t bn = (uint32_t)q.bn, tile_rows = 128 * (uint32_t)q.ctas;
     MmArgs p = {};
     const void *cr = swap ? b : a, *cc = swap ? a : b;
-    p.sc_rows = static_cast<const uint8_t *>(swap ? b_scales : a_scales);
-    p.sc_cols = static_cast<const uint8_t *>(swap ? a_scales : b_scales);
     p.rows = (uint32_t)(swap ? n : m);
     p.cols = (uint32_t)(swap ? m : n);
     p.fmt_rows = (uint32_t)(swap ? b_fmt : a_fmt);
@@ -819,21 +706,18 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     p.tiles_c = (p.cols + bn - 1) / bn;
     p.split_groups = plan.split_groups;
     p.accumulate = accumulate != 0;
-    const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c, slots = (uint64_t)(q.pair ? sms / 2 : sms);
+    const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c, slots = (uint64_t)(sms / q.ctas);
     if (tiles > 0x3fffffffull) return LGN_ERR_UNSUPPORTED;
     CUtensorMap mr, mc, sr, sc, mo = {};
     if (q.form == kFormRows && !make_out_map(&mo, out, m, n, ldo, out_dt)) return LGN_ERR_CUDA;
-    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, q.pair ? bn / 2 : bn)) return LGN_ERR_CUDA;
+    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, bn / (uint32_t)q.ctas)) return LGN_ERR_CUDA;
+    if (!make_scale_map(&sr, swap ? b_scales : a_scales, (uint64_t)((p.rows + 127) / 128) * p.groups) ||
+        !make_scale_map(&sc, swap ? a_scales : b_scales, (uint64_t)((p.cols + 127) / 128) * p.groups)) return LGN_ERR_CUDA;
     if (!allow_smem(plan.kernel)) return LGN_ERR_CUDA;
-    uint64_t grid = q.form == kFormSplit ? tiles * plan.split : (tiles < slots ? tiles : slots);
+    const uint64_t grid = q.form == kFormSplit ? tiles * plan.split : (tiles < slots ? tiles : slots);
     log_line("fp8_matmul: m %llu n %llu k %llu, %s, tile %u x %u, form %d, split %u, %llu tiles", (unsigned long long)m, (unsigned long long)n,
-             (unsigned long long)k, q.pair ? "pairs" : "single", tile_rows, bn, q.form, plan.split, (unsigned long long)tiles);
-    if (q.pair) {
-        if (!make_scale_map(&sr, p.sc_rows, (uint64_t)((p.rows + 127) / 128) * p.groups) ||
-            !make_scale_map(&sc, p.sc_cols, (uint64_t)((p.cols + 127) / 128) * p.groups)) return LGN_ERR_CUDA;
-        void *args[] = {&mr, &mc, &sr, &sc, &mo, &p};
-        return launch_dependent(q.fn, dim3((unsigned)(2 * grid)), dim3(kMmThreads), args, (size_t)q.smem, stream);
-    }
-    void *args[] = {&mr, &mc, &mo, &p};
-    return launch_dependent(q.fn, dim3((unsigned)grid), dim3(kMmThreads), args, (size_t)q.smem, stream, q.form == kFormSplit ? plan.split : 1);
+             (unsigned long long)k, q.ctas == 2 ? "pairs" : "single", tile_rows, bn, q.form, plan.split, (unsigned long long)tiles);
+    void *args[] = {&mr, &mc, &sr, &sc, &mo, &p};
+    return launch_dependent(q.fn, dim3((unsigned)grid * (unsigned)q.ctas), dim3(kMmThreads), args, (size_t)q.smem, stream,
+                            q.form == kFormSplit ? plan.split : (unsigned)q.ctas);
 }
