@@ -157,7 +157,7 @@ _lib.lgn_clip_apply.argtypes = [C.POINTER(GradT), _i32, _dbl, _vp, _vp]
 _lib.lgn_clip_apply.restype = _i32
 
 
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _uint8 = torch.uint8
 _DT_CODE = {torch.float32: F32, torch.bfloat16: BF16}
 
@@ -490,13 +490,51 @@ def lgn_prefix_decode(stream_dev: torch.Tensor, off_dev: torch.Tensor, out: torc
 
 
 # --------------------------------------------------------------------------- 8-bit matrix product
-class Fp8Operand(NamedTuple):
-    """A matrix of ``rows`` x ``k`` in 8-bit codes with one scale per block of 128 along k."""
-    codes: torch.Tensor      # uint8, lgn_fp8_codes_bytes(rows, k)
-    scales: torch.Tensor     # uint8, lgn_fp8_scales_bytes(rows, k)
-    rows: int
-    k: int
-    fmt: int
+class Fp8Operand:
+    """A matrix of ``rows`` x ``k`` in 8-bit codes with one scale per block of 128 along k.
+
+    codes   uint8, lgn_fp8_codes_bytes(rows, k), rows padded to a multiple of 16
+    scales  uint8, lgn_fp8_scales_bytes(rows, k), in the order lgn.h describes"""
+    __slots__ = ("rows", "k", "fmt", "_codes", "_scales", "_buffer", "_codes_ptr", "_scales_ptr")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int, fmt: int):
+        need_codes, need_scales = _fp8_bytes(rows, k)
+        for t, need, what in ((codes, need_codes, "codes"), (scales, need_scales, "scales")):
+            if t.dtype != _uint8:
+                raise TypeError(f"{what} are uint8")
+            if _dev(t, what) and t.numel() < need:
+                raise ValueError(f"{what} shorter than the extents need")
+        self.rows, self.k, self.fmt, self._codes, self._scales, self._buffer = rows, k, fmt, codes, scales, None
+        self._codes_ptr, self._scales_ptr = codes.data_ptr(), scales.data_ptr()
+
+    @classmethod
+    def empty(cls, rows: int, k: int, fmt: int, device) -> "Fp8Operand":
+        """Uninitialised, codes and scales in one allocation."""
+        o = cls.__new__(cls)
+        codes, scales = _fp8_bytes(rows, k)
+        o.rows, o.k, o.fmt, o._codes, o._scales = rows, k, fmt, None, None
+        o._buffer = torch.empty(codes + scales + 16, dtype=_uint8, device=device)
+        o._codes_ptr = o._buffer.data_ptr()
+        o._scales_ptr = o._codes_ptr + codes
+        return o
+
+    @property
+    def codes(self) -> torch.Tensor:
+        return self._codes if self._buffer is None else self._buffer[:max(16, _fp8_bytes(self.rows, self.k)[0])]
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._buffer is None:
+            return self._scales
+        codes, scales = _fp8_bytes(self.rows, self.k)
+        return self._buffer[codes:codes + max(16, scales)]
+
+    @property
+    def device(self) -> torch.device:
+        return (self._codes if self._buffer is None else self._buffer).device
+
+    def _replace(self, **kw) -> "Fp8Operand":
+        return Fp8Operand(*(kw.get(n, getattr(self, n)) for n in ("codes", "scales", "rows", "k", "fmt")))
 
 
 def _matrix(t: torch.Tensor, what: str) -> int:
@@ -523,17 +561,7 @@ def _fp8_bytes(rows: int, k: int) -> Tuple[int, int]:
 
 
 def new_fp8_operand(rows: int, k: int, fmt: int, device) -> Fp8Operand:
-    codes, scales = _fp8_bytes(rows, k)
-    return Fp8Operand(torch.empty(codes or 16, dtype=_uint8, device=device),
-                      torch.empty(scales or 16, dtype=_uint8, device=device), rows, k, fmt)
-
-
-def _check_operand(o: Fp8Operand, what: str) -> None:
-    codes, scales = _fp8_bytes(o.rows, o.k)
-    if not (o.codes.is_cuda and o.scales.is_cuda and o.codes.is_contiguous() and o.scales.is_contiguous()):
-        raise ValueError(f"{what} must hold contiguous CUDA tensors")
-    if o.codes.nbytes < codes or o.scales.nbytes < scales:
-        raise ValueError(f"{what} is shorter than its extents")
+    return Fp8Operand.empty(rows, k, fmt, device)
 
 
 def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, rowwise: bool = True,
@@ -553,8 +581,7 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
             q = out
             if (q.rows, q.k, q.fmt) != (rows, cols, fmt):
                 raise ValueError("out: extents or format differ from the matrix")
-            _check_operand(q, "out")
-        pq, sq = q.codes.data_ptr(), q.scales.data_ptr()
+        pq, sq = q._codes_ptr, q._scales_ptr
     if transposed:
         if out_t is None:
             t = new_fp8_operand(cols, rows, fmt, x.device)
@@ -562,8 +589,7 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
             t = out_t
             if (t.rows, t.k, t.fmt) != (cols, rows, fmt):
                 raise ValueError("out_t: extents or format differ from the transpose")
-            _check_operand(t, "out_t")
-        pt, st = t.codes.data_ptr(), t.scales.data_ptr()
+        pt, st = t._codes_ptr, t._scales_ptr
     _check(_lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), fmt, block, pq, sq, pt, st, _stream(stream)),
            "lgn_fp8_quantize")
     return q, t
@@ -576,18 +602,16 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
     m, k, n = a.rows, a.k, b.rows
     if k != b.k:
         raise ValueError("operands contract over different extents")
-    _check_operand(a, "a")
-    _check_operand(b, "b")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((m, n), dtype=out_dtype, device=a.codes.device)
+        out = torch.empty((m, n), dtype=out_dtype, device=a.device)
         ldo = n or 1
     else:
         if tuple(out.shape) != (m, n):
             raise ValueError("out must be a.rows x b.rows")
         ldo = _matrix(out, "out")
-    _check(_lib.lgn_fp8_matmul(a.codes.data_ptr(), a.scales.data_ptr(), a.fmt, b.codes.data_ptr(), b.scales.data_ptr(), b.fmt,
+    _check(_lib.lgn_fp8_matmul(a._codes_ptr, a._scales_ptr, a.fmt, b._codes_ptr, b._scales_ptr, b.fmt,
                                m, n, k, out.data_ptr() or None, ldo, dtype_code(out), 1 if accumulate else 0,
                                _dev(status, "status") if status is not None else None, _stream(stream)), "lgn_fp8_matmul")
     return out

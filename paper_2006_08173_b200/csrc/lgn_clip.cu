@@ -82,35 +82,31 @@ __device__ __forceinline__ void store_words(char *p, const Words &c) {
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-__device__ __noinline__ void add_exactly(const Words &c, uint32_t es, double &sum, unsigned long long &bad) {
+template <int ES>
+__device__ __noinline__ void add_exactly(const Words &c, double &sum, unsigned long long &bad) {
     for (int k = 0; k < 8; ++k) {
-        const float a = es == 4 ? __uint_as_float(c.w[k]) : bf_lo(c.w[k]), b = es == 4 ? 0.0f : bf_hi(c.w[k]);
+        const float a = ES == 4 ? __uint_as_float(c.w[k]) : bf_lo(c.w[k]), b = ES == 4 ? 0.0f : bf_hi(c.w[k]);
         sum += (double)a * (double)a + (double)b * (double)b;
         bad += (isfinite(a) ? 0 : 1) + (isfinite(b) ? 0 : 1);
     }
 }
 
-__device__ __forceinline__ void add_chunk(const Words &c, uint32_t es, double &sum, unsigned long long &bad) {
-    float s = 0.0f;
-    if (es == 4) {
-        float t = 0.0f;
-        #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-            s = fmaf(__uint_as_float(c.w[k]), __uint_as_float(c.w[k]), s);
-            t = fmaf(__uint_as_float(c.w[k + 1]), __uint_as_float(c.w[k + 1]), t);
-        }
-        s += t;
-    } else {
-        float t = 0.0f;
-        #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+template <int ES>
+__device__ __forceinline__ void add_chunk(const Words &c, double &sum, unsigned long long &bad) {
+    float s = 0.0f, t = 0.0f;
+    #pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if constexpr (ES == 4) {
+            if (k & 1) t = fmaf(__uint_as_float(c.w[k]), __uint_as_float(c.w[k]), t);
+            else       s = fmaf(__uint_as_float(c.w[k]), __uint_as_float(c.w[k]), s);
+        } else {
             s = fmaf(bf_lo(c.w[k]), bf_lo(c.w[k]), s);
             t = fmaf(bf_hi(c.w[k]), bf_hi(c.w[k]), t);
         }
-        s += t;
     }
+    s += t;
     if (s >= 0x1p-80f && s < __int_as_float(0x7f800000)) sum += (double)s;
-    else add_exactly(c, es, sum, bad);
+    else add_exactly<ES>(c, sum, bad);
 }
 
 __device__ __forceinline__ float load_elem(const char *p, uint32_t es) {
@@ -147,8 +143,32 @@ __device__ __forceinline__ double block_sum(double v, unsigned long long &bad, d
     return s;
 }
 
+// Tiles [t, stop) of one tensor, whose first tile is `first`.
+template <int ES>
+__device__ __forceinline__ void add_tiles(const ClipTensor &x, uint32_t first, uint32_t t, uint32_t stop, double &sum, unsigned long long &bad) {
+    const uint64_t bytes = x.lead + x.n * ES, whole = bytes / 32;                    // chunks [1 if lead, whole) lie inside
+    const char *base = x.g - x.lead;
+    for (; t < stop; ++t) {
+        const uint64_t c0 = (uint64_t)(t - first) * (kClipTileBytes / 32) + threadIdx.x;
+        Words c[4];
+        if ((t != first || x.lead == 0) && (uint64_t)(t - first + 1) * (kClipTileBytes / 32) <= whole) {
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) c[k] = load_words(base + (c0 + k * kClipThreads) * 32);
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) add_chunk<ES>(c[k], sum, bad);
+        } else {
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t at = c0 + k * kClipThreads;
+                if (at < whole && !(at == 0 && x.lead != 0)) add_chunk<ES>(load_words(base + at * 32), sum, bad);
+                else if (at * 32 < bytes) add_exactly<ES>(load_edge(x, at), sum, bad);
+            }
+        }
+    }
+}
+
+// Four CTAs per SM (64 registers): all of the grid is resident, so that no CTA's share runs alone at the end.
 template <int N>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 4)
 norm_kernel(const __grid_constant__ ClipList<N> l, ClipPartial *part) {
     __shared__ double sh[kClipThreads / 32];
     __shared__ unsigned long long shb[kClipThreads / 32];
@@ -159,29 +179,12 @@ norm_kernel(const __grid_constant__ ClipList<N> l, ClipPartial *part) {
     unsigned long long bad = 0;
     if (t0 < t1) {
         uint32_t i = clip_find(l, t0);
-        for (uint32_t t = t0; t < t1;) {
+        for (uint32_t t = t0; t < t1; ++i) {
             const ClipTensor x = clip_tensor(l, i);
-            const uint32_t next = i + 1 < l.count ? l.first[i + 1] : l.tiles, stop = min(t1, next);
-            const uint64_t bytes = x.lead + x.n * x.es, whole = bytes / 32;          // chunks [1 if lead, whole) lie inside
-            const char *base = x.g - x.lead;
-            for (; t < stop; ++t) {
-                const uint64_t c0 = (uint64_t)(t - l.first[i]) * (kClipTileBytes / 32) + threadIdx.x;
-                Words c[4];
-                bool in[4];
-                #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint64_t at = c0 + k * kClipThreads;
-                    in[k] = at < whole && !(at == 0 && x.lead != 0);
-                    if (in[k]) c[k] = load_words(base + at * 32);
-                }
-                #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint64_t at = c0 + k * kClipThreads;
-                    if (in[k]) add_chunk(c[k], x.es, sum, bad);
-                    else if (at * 32 < bytes) add_exactly(load_edge(x, at), x.es, sum, bad);
-                }
-            }
-            ++i;
+            const uint32_t stop = min(t1, i + 1 < l.count ? l.first[i + 1] : l.tiles);
+            if (x.es == 4) add_tiles<4>(x, l.first[i], t, stop, sum, bad);
+            else           add_tiles<2>(x, l.first[i], t, stop, sum, bad);
+            t = stop;
         }
     }
     sum = block_sum(sum, bad, sh, shb);
@@ -193,11 +196,12 @@ __device__ __forceinline__ float clip_coef(double sum, double max_norm, bool cli
     return clip && norm > max_norm && norm < __longlong_as_double(0x7ff0000000000000ll) ? (float)(max_norm / norm) : 1.0f;
 }
 
-__device__ __forceinline__ Words scaled_words(const Words &c, uint32_t es, float coef) {
+template <int ES>
+__device__ __forceinline__ Words scaled_words(const Words &c, float coef) {
     Words r;
     #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        if (es == 4) r.w[k] = __float_as_uint(__uint_as_float(c.w[k]) * coef);
+        if constexpr (ES == 4) r.w[k] = __float_as_uint(__uint_as_float(c.w[k]) * coef);
         else {
             const __nv_bfloat162 p = __floats2bfloat162_rn(bf_lo(c.w[k]) * coef, bf_hi(c.w[k]) * coef);
             r.w[k] = *reinterpret_cast<const uint32_t *>(&p);
@@ -206,14 +210,54 @@ __device__ __forceinline__ Words scaled_words(const Words &c, uint32_t es, float
     return r;
 }
 
+// Elements at byte offsets [lo, hi) from the first one, value by value.
+template <int ES>
+__device__ __noinline__ void scale_elements(const ClipTensor &x, int64_t lo, int64_t hi, uint32_t first, uint32_t step, float coef) {
+    const int64_t end = (int64_t)(x.n * ES), from = lo < 0 ? 0 : lo, to = hi < end ? hi : end;
+    for (int64_t p = from + (int64_t)first * ES; p < to; p += (int64_t)step * ES) {
+        const float v = load_elem(x.g + p, ES) * coef;
+        if constexpr (ES == 4) *reinterpret_cast<float *>(x.out + p) = v;
+        else *reinterpret_cast<__nv_bfloat16 *>(x.out + p) = __float2bfloat16_rn(v);
+    }
+}
+
+// Tiles [stop, t) of one tensor, whose first tile is `first`, from the last to the first.
+template <int ES>
+__device__ __forceinline__ void scale_tiles(const ClipTensor &x, uint32_t first, uint32_t t, uint32_t stop, float coef) {
+    const uint64_t bytes = x.lead + x.n * ES, whole = bytes / 32;
+    const char *base = x.g - x.lead;
+    char *obase = x.out - x.lead;
+    const bool same = ((reinterpret_cast<uintptr_t>(x.out) ^ reinterpret_cast<uintptr_t>(x.g)) & 31u) == 0;
+    for (; t > stop; --t) {
+        const uint64_t c0 = (uint64_t)(t - 1 - first) * (kClipTileBytes / 32) + threadIdx.x;
+        if (!same) {                                          // input and output aligned differently: value by value, coalesced
+            const int64_t lo = (int64_t)(t - 1 - first) * kClipTileBytes - x.lead;
+            scale_elements<ES>(x, lo, lo + kClipTileBytes, threadIdx.x, kClipThreads, coef);
+        } else if ((t - 1 != first || x.lead == 0) && (uint64_t)(t - first) * (kClipTileBytes / 32) <= whole) {
+            Words c[4];
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) c[k] = load_words(base + (c0 + k * kClipThreads) * 32);
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) store_words(obase + (c0 + k * kClipThreads) * 32, scaled_words<ES>(c[k], coef));
+        } else {
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t at = c0 + k * kClipThreads;
+                if (at < whole && !(at == 0 && x.lead != 0)) store_words(obase + at * 32, scaled_words<ES>(load_words(base + at * 32), coef));
+                else if (at * 32 < bytes) scale_elements<ES>(x, (int64_t)(at * 32) - x.lead, (int64_t)(at * 32 + 32) - x.lead, 0, 1, coef);
+            }
+        }
+    }
+}
+
 // SCALE: scale (or, for a coefficient of 1, copy) every tensor; otherwise only the record is written.
 // from_record: the sum is the record's (which a caller may have reduced over ranks), not the partial sums'.
 template <int N, bool SCALE>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 4)
 clip_kernel(const __grid_constant__ ClipList<N> l, const ClipPartial *part, uint32_t nparts, double max_norm,
             uint32_t clip, uint32_t from_record, uint32_t write_record, lgn_norm_t *record) {
     __shared__ double sh[kClipThreads / 32];
     __shared__ unsigned long long shb[kClipThreads / 32];
+    dep_launch();
     dep_wait();
     double sum = 0.0;
     unsigned long long bad = 0;
@@ -235,50 +279,14 @@ clip_kernel(const __grid_constant__ ClipList<N> l, const ClipPartial *part, uint
         const uint32_t t0 = (uint32_t)((uint64_t)l.tiles * blockIdx.x / gridDim.x), t1 = (uint32_t)((uint64_t)l.tiles * (blockIdx.x + 1) / gridDim.x);
         if (t0 >= t1) return;
         uint32_t i = clip_find(l, t1 - 1);
-        for (uint32_t t = t1; t > t0;) {
+        for (uint32_t t = t1; t > t0; --i) {
             const ClipTensor x = clip_tensor(l, i);
             const uint32_t stop = max(t0, l.first[i]);
-            const uint64_t bytes = x.lead + x.n * x.es, whole = bytes / 32;
-            const char *base = x.g - x.lead;
-            char *obase = x.out - x.lead;
-            const bool skip = coef == 1.0f && x.out == x.g, same = ((reinterpret_cast<uintptr_t>(x.out) ^ reinterpret_cast<uintptr_t>(x.g)) & 31u) == 0;
-            if (skip) { t = stop; --i; continue; }
-            for (; t > stop; --t) {
-                const uint64_t c0 = (uint64_t)(t - 1 - l.first[i]) * (kClipTileBytes / 32) + threadIdx.x;
-                Words c[4];
-                bool in[4];
-                #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint64_t at = c0 + k * kClipThreads;
-                    in[k] = same && at < whole && !(at == 0 && x.lead != 0);
-                    if (in[k]) c[k] = load_words(base + at * 32);
-                }
-                #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint64_t at = c0 + k * kClipThreads;
-                    if (in[k]) store_words(obase + at * 32, scaled_words(c[k], x.es, coef));
-                    else if (same && at * 32 < bytes) {                       // first or last chunk: value by value
-                        const int64_t b0 = (int64_t)(at * 32) - x.lead, end = (int64_t)(x.n * x.es);
-                        for (int b = 0; b < 32; b += (int)x.es) {
-                            const int64_t p = b0 + b;
-                            if (p < 0 || p >= end) continue;
-                            const float v = load_elem(x.g + p, x.es) * coef;
-                            if (x.es == 4) *reinterpret_cast<float *>(x.out + p) = v;
-                            else *reinterpret_cast<__nv_bfloat16 *>(x.out + p) = __float2bfloat16_rn(v);
-                        }
-                    }
-                }
-                if (!same) {                                                  // input and output aligned differently: value by value, coalesced
-                    const int64_t lo = (int64_t)(t - 1 - l.first[i]) * kClipTileBytes - x.lead, hi = lo + kClipTileBytes;
-                    const int64_t from = lo < 0 ? 0 : lo, to = hi < (int64_t)(x.n * x.es) ? hi : (int64_t)(x.n * x.es);
-                    for (int64_t p = from + (int64_t)threadIdx.x * x.es; p < to; p += (int64_t)kClipThreads * x.es) {
-                        const float v = load_elem(x.g + p, x.es) * coef;
-                        if (x.es == 4) *reinterpret_cast<float *>(x.out + p) = v;
-                        else *reinterpret_cast<__nv_bfloat16 *>(x.out + p) = __float2bfloat16_rn(v);
-                    }
-                }
+            if (coef != 1.0f || x.out != x.g) {
+                if (x.es == 4) scale_tiles<4>(x, l.first[i], t, stop, coef);
+                else           scale_tiles<2>(x, l.first[i], t, stop, coef);
             }
-            --i;
+            t = stop;
         }
     }
 }

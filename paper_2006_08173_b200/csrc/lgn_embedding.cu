@@ -92,6 +92,7 @@ template <int TDT, int ODT, int VE>
 __global__ void __launch_bounds__(256)
 lookup_kernel(const void *__restrict__ table, uint64_t ld_table, uint64_t vocab, uint32_t dim, const void *__restrict__ ids, uint32_t wide,
               uint64_t tokens, float scale, void *__restrict__ out, uint64_t ld_out, uint32_t span_log2, unsigned long long *outside) {
+    dep_launch();
     dep_wait();
     const uint32_t span = 1u << span_log2, rows = 256u >> span_log2, x = threadIdx.x & (span - 1);
     const uint64_t t0 = (uint64_t)blockIdx.x * (4 * rows) + (threadIdx.x >> span_log2);
@@ -127,6 +128,7 @@ lookup_kernel(const void *__restrict__ table, uint64_t ld_table, uint64_t vocab,
 
 // ------------------------------------------------------------------ sort
 constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortCtas * 32, kSortBins = 512;
+constexpr int kSortBatch = 8;                              // loads a lane has in flight
 
 __device__ __forceinline__ uint32_t ld_l2(const uint32_t *p) {       // written by other CTAs of the cluster before its barrier
     uint32_t v;
@@ -173,12 +175,12 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_ids_kernel(const SortArg
         for (uint32_t i = threadIdx.x; i < 32 * bins; i += kSortThreads) hist[i] = 0u;
         __syncthreads();
         uint32_t *mine = hist + warp * bins;
-        for (uint32_t i = lo + lane; i < hi; i += 128) {
-            uint32_t k[4];
+        for (uint32_t i = lo + lane; i < hi; i += 32 * kSortBatch) {
+            uint32_t k[kSortBatch];
             #pragma unroll
-            for (int j = 0; j < 4; ++j) k[j] = i + 32 * j < hi ? key_at(i + 32 * j) : 0u;
+            for (int j = 0; j < kSortBatch; ++j) k[j] = i + 32 * j < hi ? key_at(i + 32 * j) : 0u;
             #pragma unroll
-            for (int j = 0; j < 4; ++j) if (i + 32 * j < hi) atomicAdd(mine + ((k[j] >> shift) & mask), 1u);
+            for (int j = 0; j < kSortBatch; ++j) if (i + 32 * j < hi) atomicAdd(mine + ((k[j] >> shift) & mask), 1u);
         }
         __syncthreads();
         if (threadIdx.x < bins) {                          // places of each warp within its CTA, digit by digit
@@ -211,23 +213,32 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_ids_kernel(const SortArg
             base[threadIdx.x] = w0 + inc - all + before;
         }
         __syncthreads();
-        for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
-            const uint32_t i = i0 + lane;
-            const bool on = i < hi;
-            const uint32_t k = on ? key_at(i) : 0u, p = on ? (pass > 0 ? ld_l2(psrc + i) : i) : 0u;
-            const uint32_t digit = on ? (k >> shift) & mask : bins;                 // lanes past the end: a digit of their own
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            uint32_t at = 0;
-            if (on) at = mine[digit];
-            __syncwarp();
-            if (on) {
-                const uint32_t r = __popc(same & ((1u << lane) - 1u));
-                if (r == 0) mine[digit] = at + __popc(same);
-                at += base[digit] + r;
-                kdst[at] = k;
-                pdst[at] = p;
+        for (uint32_t i0 = lo + lane; i0 - lane < hi; i0 += 32 * kSortBatch) {
+            uint32_t kb[kSortBatch], pb[kSortBatch];
+            #pragma unroll
+            for (int j = 0; j < kSortBatch; ++j) {
+                const uint32_t i = i0 + 32 * j;
+                kb[j] = i < hi ? key_at(i) : 0u;
+                pb[j] = i < hi && pass > 0 ? ld_l2(psrc + i) : i;
             }
-            __syncwarp();
+            #pragma unroll
+            for (int j = 0; j < kSortBatch; ++j) {
+                if (i0 - lane + 32 * j >= hi) break;
+                const bool on = i0 + 32 * j < hi;
+                const uint32_t digit = on ? (kb[j] >> shift) & mask : bins;         // lanes past the end: a digit of their own
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                uint32_t at = 0;
+                if (on) at = mine[digit];
+                __syncwarp();
+                if (on) {
+                    const uint32_t r = __popc(same & ((1u << lane) - 1u));
+                    if (r == 0) mine[digit] = at + __popc(same);
+                    at += base[digit] + r;
+                    kdst[at] = kb[j];
+                    pdst[at] = pb[j];
+                }
+                __syncwarp();
+            }
         }
         cluster_sync_all();
     }
@@ -249,17 +260,17 @@ __device__ __forceinline__ void add_rows(const void *dout, uint64_t ld, const ui
     for (int j = 0; j < VE; ++j) sum[j] = 0.0f;
     for (uint32_t i0 = a; i0 < b; i0 += 32) {
         const uint32_t mine = i0 + lane < b ? ldro_u32(pos + i0 + lane) : 0u, m = min(32u, b - i0);
-        for (uint32_t k0 = 0; k0 < m; k0 += 4) {
-            float v[4][VE];
+        for (uint32_t k0 = 0; k0 < m; k0 += 8) {
+            float v[8][VE];
             #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 8; ++k) {
                 const uint32_t p = __shfl_sync(0xffffffffu, mine, k0 + k);
                 #pragma unroll
                 for (int j = 0; j < VE; ++j) v[k][j] = 0.0f;
                 if (on && k0 + k < m) load_vec<DDT, VE>(dout, (uint64_t)p * ld + c, v[k]);
             }
             #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < 8; ++k)
                 if (k0 + k < m) {
                     #pragma unroll
                     for (int j = 0; j < VE; ++j) sum[j] += v[k][j];
@@ -311,6 +322,7 @@ constexpr uint32_t kRowsPerWarp = 8;
 
 template <int DDT, int ODT, int VE>
 __global__ void __launch_bounds__(256) rows_kernel(const SumArgs a) {
+    dep_launch();
     dep_wait();
     const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const uint64_t v0 = item / a.slabs * kRowsPerWarp;
@@ -336,7 +348,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const SumArgs a) {
             // the piece of the first window is its end piece, unless the run covers that window from its start
             #pragma unroll
             for (int j = 0; j < VE; ++j) sum[j] = a.part[(uint64_t)(2 * w0 + 1) * a.pitch + c + j];
-            #pragma unroll 4
+            #pragma unroll 8
             for (uint32_t w = w0 + 1; w <= w1; ++w) {
                 #pragma unroll
                 for (int j = 0; j < VE; ++j) sum[j] += a.part[(uint64_t)(2 * w) * a.pitch + c + j];
@@ -356,11 +368,11 @@ __global__ void __launch_bounds__(256) rows_kernel(const SumArgs a) {
     }
 }
 
-// Tokens per window: half the square root of their number, so that the longest run takes about as many
-// steps within a window as over the windows.
+// Tokens per window: about a quarter of the square root of their number.  The square root itself would make the
+// worst run (all tokens one id) shortest; real runs are far shorter, and short windows spread them over more warps.
 static uint32_t window_log2_for(uint64_t tokens) {
     uint32_t l = 5;
-    while (l < 20 && (1ull << (2 * l + 2)) < tokens) ++l;
+    while (l < 20 && (1ull << (2 * l + 4)) < tokens) ++l;
     return l;
 }
 

@@ -352,6 +352,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     constexpr bool kChunked = ODT == LGN_F32;
     constexpr int kRun = FORM == kFormRows ? OutRun<ODT>::kCols : 32;
     extern __shared__ uint8_t smem_raw[];
+    dep_launch();
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t stop;
