@@ -439,7 +439,7 @@ lgn_status lgn_embedding(const void *table, uint64_t vocab, uint64_t dim, uint64
  * those rows are not touched.  Sums in fp32, rounded once to table_dt, in an order that depends on
  * the ids alone: the same inputs give the same bits.
  *   ws  device scratch of lgn_embedding_grad_workspace_bytes(tokens, vocab, dim), 16-byte aligned
- * Two launches, three for more than 32 tokens, no allocation. */
+ * Two to four launches and (without accumulate) a memset of vocab bytes, no allocation. */
 size_t lgn_embedding_grad_workspace_bytes(uint64_t tokens, uint64_t vocab, uint64_t dim);
 lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn_dtype dout_dt,
                               const void *ids, int ids_bits, uint64_t tokens,
@@ -472,11 +472,13 @@ typedef struct {
 size_t lgn_clip_workspace_bytes(int count);
 
 /* The record only.   grads: host array.  record_dev: device, one lgn_norm_t, 8-byte aligned.  ws: device,
- * 16-byte aligned.  Two launches for up to 512 tensors, one more for each further 512. */
+ * 16-byte aligned.  Two launches for up to 512 tensors, one more for each further 512, and a memset of 24 bytes ahead of
+ * them above 18 MiB of gradients or 512 tensors. */
 lgn_status lgn_grad_norm(const lgn_grad_t *grads, int count, lgn_norm_t *record_dev,
                          void *ws, size_t ws_bytes, void *stream);
 
-/* The record, and every tensor scaled, without a host round trip.  max_norm >= 0.  Two launches per 512 tensors. */
+/* The record, and every tensor scaled, without a host round trip.  max_norm >= 0.  Two launches per 512 tensors, and the
+ * memset. */
 lgn_status lgn_clip_grad_norm(const lgn_grad_t *grads, int count, double max_norm, lgn_norm_t *record_dev,
                               void *ws, size_t ws_bytes, void *stream);
 

@@ -5,12 +5,13 @@
 //
 // Both are bound by memory.  The gradient adds rows that share an id in a fixed order, without atomics on
 // values: the tokens are sorted by id (stable), so that every table row owns one run of the sorted list.
-//   sort_ids_kernel    one cluster of 8 CTAs: radix sort of (id, position), up to 9 bits per pass; then the
-//                      first and last place of every id's run
-//   window_kernel      runs longer than a window of the sorted list: the pieces a window holds of runs that
-//                      reach beyond it are added up first, each by a warp of its own
-//   rows_kernel        every row of the table: zeros, the sum of a run inside one window, or the sum of
-//                      its windows' pieces
+//   mark_kernel    (after a memset) notes which rows of the table have a token
+//   sort_kernel    cluster 0 (8 CTAs): radix sort of (id, position), up to 9 bits per pass.  The other clusters meanwhile
+//                  write zeros to the rows without a token, most of the bytes that a gradient of a large table has to write
+//   window_kernel  a warp per window of the sorted list and slab of columns walks its tokens, eight rows of dout in flight
+//                  whatever the runs' lengths, and writes each run that lies inside the window to its table row; the
+//                  pieces of runs that reach beyond it (one at its start, one at its end) go to scratch
+//   join_kernel    adds the pieces of each run of several windows
 // so that no warp adds more than one window of tokens, or one window count of pieces, in sequence.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -82,6 +83,27 @@ __device__ __forceinline__ void store_vec(void *base, uint64_t i, const float *v
     }
 }
 
+// A vector as it lies in memory, for loads that are in flight together.
+template <int DT, int VE> struct RawVec {
+    static constexpr int kWords = VE * (DT == LGN_F32 ? 4 : 2) / 4 > 0 ? VE * (DT == LGN_F32 ? 4 : 2) / 4 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void *base, uint64_t i) {
+        const char *p = static_cast<const char *>(base) + i * (DT == LGN_F32 ? 4 : 2);
+        if constexpr (kWords >= 4) {
+            #pragma unroll
+            for (int k = 0; k < kWords; k += 4)
+                asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "l"(p + 4 * k));
+        } else if constexpr (kWords == 2) asm volatile("ld.global.nc.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+        else if constexpr (DT == LGN_BF16 && VE == 1) w[0] = ldro_u16(p);
+        else w[0] = ldro_u32(p);
+    }
+    __device__ __forceinline__ float at(int k) const {
+        if constexpr (DT == LGN_F32) return __uint_as_float(w[k]);
+        else return k & 1 ? __uint_as_float(w[k >> 1] & 0xffff0000u) : __uint_as_float(w[k >> 1] << 16);
+    }
+};
+
 __device__ __forceinline__ int64_t load_id(const void *ids, uint64_t i, uint32_t wide) {
     return wide ? (int64_t)ldro_u64(static_cast<const int64_t *>(ids) + i) : (int64_t)(int32_t)ldro_u32(static_cast<const int32_t *>(ids) + i);
 }
@@ -144,34 +166,72 @@ __device__ __forceinline__ void cluster_sync_all() {
 struct SortArgs {
     const void *ids;
     uint32_t *key[2], *pos[2];
-    uint2 *run;                    // per table row: first and one past the last place in the sorted list
+    uint8_t *present;              // per table row: has a token (not used when the gradient is accumulated)
+    void *out;
+    uint64_t ld_out_bytes, dim_bytes;
     uint64_t vocab;
     int64_t padding;
-    uint32_t tokens, wide, bits, passes;
+    uint32_t tokens, wide, bits, passes, zero_unit;   // zero_unit: table rows a CTA of the other clusters looks after
 };
 
-__global__ void __launch_bounds__(kSortThreads, 1) sort_ids_kernel(const SortArgs a) {
-    extern __shared__ uint32_t hist[];                     // [32][kSortBins]
+__device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i) {       // vocab: left out, sorts last
+    const int64_t id = load_id(a.ids, i, a.wide);
+    return id < 0 || (uint64_t)id >= a.vocab || id == a.padding ? (uint32_t)a.vocab : (uint32_t)id;
+}
+
+__global__ void __launch_bounds__(256) mark_kernel(const SortArgs a) {
+    dep_launch();
+    dep_wait();
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < a.tokens; i += gridDim.x * 256) {
+        const uint32_t k = key_of(a, i);
+        if (k < a.vocab) a.present[k] = 1;
+    }
+}
+
+// Zeros to the rows [first, last) without a token, a warp per row; 32 rows' marks at a time.
+__device__ __forceinline__ void zero_rows(const SortArgs &a, uint64_t first, uint64_t last, uint32_t warp) {
+    const uint32_t lane = threadIdx.x & 31;
+    // row r of a group of 32 is warp (r mod 32)'s, so that all warps of the CTA have rows of each group
+    for (uint64_t r0 = first; r0 < last; r0 += 1024) {
+        uint8_t mark = 1;
+        const uint64_t mine = r0 + 32 * lane + warp;
+        if (mine < last) mark = *(a.present + mine);
+        uint32_t todo = __ballot_sync(0xffffffffu, mark == 0);
+        while (todo != 0) {
+            const uint32_t k = __ffs(todo) - 1;
+            todo &= todo - 1;
+            char *row = static_cast<char *>(a.out) + (r0 + 32 * k + warp) * a.ld_out_bytes, *end = row + a.dim_bytes;
+            char *body = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(row) + 15) & ~(uintptr_t)15);
+            if (body > end) body = end;
+            const uint64_t vec = (uint64_t)(end - body) / 16;
+            for (char *q = row + 2 * lane; q < body; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;      // at most 14 bytes
+            for (uint64_t v = lane; v < vec; v += 32) __stcs(reinterpret_cast<uint4 *>(body) + v, make_uint4(0, 0, 0, 0));
+            for (char *q = body + vec * 16 + 2 * lane; q < end; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a) {
+    extern __shared__ uint32_t hist[];                     // [32][bins]
     __shared__ uint32_t total[kSortBins], base[kSortBins], warp_sum[32];
     dep_launch();
     dep_wait();
     uint32_t rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1u << a.bits, mask = bins - 1;
-    for (uint64_t i = rank * kSortThreads + threadIdx.x; i < a.vocab; i += kSortCtas * kSortThreads) a.run[i] = make_uint2(0u, 0u);
+    if (blockIdx.x >= kSortCtas) {
+        const uint64_t first = (uint64_t)(blockIdx.x - kSortCtas) * a.zero_unit;
+        zero_rows(a, first, first + a.zero_unit < a.vocab ? first + a.zero_unit : a.vocab, warp);
+        return;
+    }
     const uint32_t per = (((a.tokens + kSortWarps - 1) / kSortWarps) + 31u) & ~31u;
     const uint64_t lo64 = (uint64_t)(rank * 32 + warp) * per;
     const uint32_t lo = lo64 < a.tokens ? (uint32_t)lo64 : a.tokens, hi = lo64 + per < a.tokens ? (uint32_t)(lo64 + per) : a.tokens;
-    const uint32_t absent = (uint32_t)a.vocab;             // the key of tokens that are left out: sorts last
     for (uint32_t pass = 0; pass < a.passes; ++pass) {
         const uint32_t *ksrc = a.key[(pass + 1) & 1], *psrc = a.pos[(pass + 1) & 1];
         uint32_t *kdst = a.key[pass & 1], *pdst = a.pos[pass & 1];
         const uint32_t shift = pass * a.bits;
-        auto key_at = [&](uint32_t i) -> uint32_t {
-            if (pass > 0) return ld_l2(ksrc + i);
-            const int64_t id = load_id(a.ids, i, a.wide);
-            return id < 0 || (uint64_t)id >= a.vocab || id == a.padding ? absent : (uint32_t)id;
-        };
+        auto key_at = [&](uint32_t i) -> uint32_t { return pass > 0 ? ld_l2(ksrc + i) : key_of(a, i); };
         for (uint32_t i = threadIdx.x; i < 32 * bins; i += kSortThreads) hist[i] = 0u;
         __syncthreads();
         uint32_t *mine = hist + warp * bins;
@@ -242,48 +302,13 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_ids_kernel(const SortArg
         }
         cluster_sync_all();
     }
-    const uint32_t *key = a.key[(a.passes + 1) & 1];
-    for (uint32_t i = lo + lane; i < hi; i += 32) {
-        const uint32_t k = ld_l2(key + i);
-        if (k == absent) continue;
-        if (i == 0 || ld_l2(key + i - 1) != k) a.run[k].x = i;
-        if (i + 1 == a.tokens || ld_l2(key + i + 1) != k) a.run[k].y = i + 1;
-    }
 }
 
 // ------------------------------------------------------------------ sums
-// Adds dout rows pos[a..b) , columns c .. c + VE of each lane, in order.
-template <int DDT, int VE>
-__device__ __forceinline__ void add_rows(const void *dout, uint64_t ld, const uint32_t *pos, uint32_t a, uint32_t b, uint32_t c, bool on, float *sum) {
-    const uint32_t lane = threadIdx.x & 31;
-    #pragma unroll
-    for (int j = 0; j < VE; ++j) sum[j] = 0.0f;
-    for (uint32_t i0 = a; i0 < b; i0 += 32) {
-        const uint32_t mine = i0 + lane < b ? ldro_u32(pos + i0 + lane) : 0u, m = min(32u, b - i0);
-        for (uint32_t k0 = 0; k0 < m; k0 += 8) {
-            float v[8][VE];
-            #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t p = __shfl_sync(0xffffffffu, mine, k0 + k);
-                #pragma unroll
-                for (int j = 0; j < VE; ++j) v[k][j] = 0.0f;
-                if (on && k0 + k < m) load_vec<DDT, VE>(dout, (uint64_t)p * ld + c, v[k]);
-            }
-            #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k0 + k < m) {
-                    #pragma unroll
-                    for (int j = 0; j < VE; ++j) sum[j] += v[k][j];
-                }
-        }
-    }
-}
-
 struct SumArgs {
     const void *dout;
     uint64_t ld_dout;
     const uint32_t *key, *pos;
-    const uint2 *run;
     float *part;                   // two rows of `pitch` values per window: the piece at its start, the piece at its end
     void *out;
     uint64_t ld_out, vocab;
@@ -291,81 +316,99 @@ struct SumArgs {
     float scale;
 };
 
-template <int DDT, int VE>
+template <int ODT, int VE>
+__device__ __forceinline__ void write_row(const SumArgs &a, uint32_t row, uint32_t c, float *sum) {
+    const uint64_t at = (uint64_t)row * a.ld_out + c;
+    #pragma unroll
+    for (int j = 0; j < VE; ++j) sum[j] *= a.scale;
+    if (a.accumulate) {
+        float old[VE];
+        load_vec_rw<ODT, VE>(a.out, at, old);
+        #pragma unroll
+        for (int j = 0; j < VE; ++j) sum[j] += old[j];
+    }
+    store_vec<ODT, VE>(a.out, at, sum);
+}
+
+template <int DDT, int ODT, int VE>
 __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
+    constexpr int kFlight = VE == 8 ? 8 : 16;
     dep_launch();
     dep_wait();
     const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const uint32_t w = (uint32_t)(item / a.slabs), c = ((uint32_t)(item % a.slabs) * 32 + (threadIdx.x & 31)) * VE;
+    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
     if (w >= a.windows) return;
     const uint32_t lo = w << a.window_log2, hi = min(a.tokens, (w + 1) << a.window_log2);
     const bool on = c < a.dim;
+    const uint32_t before = lo > 0 ? a.key[lo - 1] : 0xffffffffu, after = hi < a.tokens ? a.key[hi] : 0xffffffffu;
     float sum[VE];
-    auto put = [&](uint32_t row) {
-        if (on) {
-            #pragma unroll
-            for (int j = 0; j < VE; ++j) a.part[(uint64_t)row * a.pitch + c + j] = sum[j];
-        }
+    uint32_t run = 0xffffffffu, first = a.key[lo];
+    auto flush = [&](uint32_t next) {                      // the run ends, or (next == run) goes on in the next window
+        if (!on) return;
+        const bool from_before = run == first && before == run;
+        if (!from_before && next != run) { write_row<ODT, VE>(a, run, c, sum); return; }
+        float *q = a.part + (uint64_t)(2 * w + (from_before ? 0 : 1)) * a.pitch + c;
+        #pragma unroll
+        for (int j = 0; j < VE; ++j) q[j] = sum[j];
     };
-    const uint32_t k0 = a.key[lo], k1 = a.key[hi - 1];
-    if (k0 < a.vocab) {
-        const uint2 r = a.run[k0];
-        if (r.x < lo) { add_rows<DDT, VE>(a.dout, a.ld_dout, a.pos, lo, min(hi, r.y), c, on, sum); put(2 * w); }
+    for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
+        const uint32_t m = min(32u, hi - i0);
+        const uint32_t keys = lane < m ? a.key[i0 + lane] : (uint32_t)a.vocab, poss = lane < m ? a.pos[i0 + lane] : 0u;
+        for (uint32_t k0 = 0; k0 < m; k0 += kFlight) {
+            if (__shfl_sync(0xffffffffu, keys, k0) >= a.vocab) { i0 = hi; break; }      // only left-out tokens follow
+            RawVec<DDT, VE> v[kFlight];
+            #pragma unroll
+            for (int k = 0; k < kFlight; ++k) {
+                const uint32_t p = __shfl_sync(0xffffffffu, poss, k0 + k), key = __shfl_sync(0xffffffffu, keys, k0 + k);
+                if (on && key < a.vocab) v[k].load(a.dout, (uint64_t)p * a.ld_dout + c);
+            }
+            #pragma unroll
+            for (int k = 0; k < kFlight; ++k) {
+                const uint32_t key = __shfl_sync(0xffffffffu, keys, k0 + k);
+                if (key >= a.vocab) break;
+                if (key != run) {
+                    if (run != 0xffffffffu) flush(key);
+                    run = key;
+                    #pragma unroll
+                    for (int j = 0; j < VE; ++j) sum[j] = v[k].at(j);
+                } else {
+                    #pragma unroll
+                    for (int j = 0; j < VE; ++j) sum[j] += v[k].at(j);
+                }
+            }
+        }
     }
-    if (k1 < a.vocab) {
-        const uint2 r = a.run[k1];
-        if (r.x >= lo && r.y > hi) { add_rows<DDT, VE>(a.dout, a.ld_dout, a.pos, r.x, hi, c, on, sum); put(2 * w + 1); }
-    }
+    if (run != 0xffffffffu) flush(after);
 }
 
-constexpr uint32_t kRowsPerWarp = 8;
-
-template <int DDT, int ODT, int VE>
-__global__ void __launch_bounds__(256) rows_kernel(const SumArgs a) {
+// Runs that begin in window w and reach beyond it.
+template <int ODT, int VE>
+__global__ void __launch_bounds__(256) join_kernel(const SumArgs a) {
     dep_launch();
     dep_wait();
     const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const uint64_t v0 = item / a.slabs * kRowsPerWarp;
-    const uint32_t lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
-    if (v0 >= a.vocab) return;
-    const bool on = c < a.dim;
-    const uint2 runs = lane < kRowsPerWarp && v0 + lane < a.vocab ? a.run[v0 + lane] : make_uint2(0u, 0u);
-    for (uint32_t k = 0; k < kRowsPerWarp && v0 + k < a.vocab; ++k) {
-        const uint32_t lo = __shfl_sync(0xffffffffu, runs.x, k), hi = __shfl_sync(0xffffffffu, runs.y, k);
-        float sum[VE];
-        const uint64_t at = (v0 + k) * a.ld_out + c;
-        if (lo == hi) {
-            if (!a.accumulate && on) {
-                #pragma unroll
-                for (int j = 0; j < VE; ++j) sum[j] = 0.0f;
-                store_vec<ODT, VE>(a.out, at, sum);
-            }
-            continue;
-        }
-        const uint32_t w0 = lo >> a.window_log2, w1 = (hi - 1) >> a.window_log2;
-        if (w0 == w1) add_rows<DDT, VE>(a.dout, a.ld_dout, a.pos, lo, hi, c, on, sum);
-        else if (on) {
-            // the piece of the first window is its end piece, unless the run covers that window from its start
-            #pragma unroll
-            for (int j = 0; j < VE; ++j) sum[j] = a.part[(uint64_t)(2 * w0 + 1) * a.pitch + c + j];
-            #pragma unroll 8
-            for (uint32_t w = w0 + 1; w <= w1; ++w) {
-                #pragma unroll
-                for (int j = 0; j < VE; ++j) sum[j] += a.part[(uint64_t)(2 * w) * a.pitch + c + j];
-            }
-        }
-        if (on) {
-            #pragma unroll
-            for (int j = 0; j < VE; ++j) sum[j] *= a.scale;
-            if (a.accumulate) {
-                float old[VE];
-                load_vec_rw<ODT, VE>(a.out, at, old);
-                #pragma unroll
-                for (int j = 0; j < VE; ++j) sum[j] += old[j];
-            }
-            store_vec<ODT, VE>(a.out, at, sum);
-        }
+    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
+    if (w + 1 >= a.windows) return;
+    const uint32_t lo = w << a.window_log2, hi = (w + 1) << a.window_log2, run = a.key[hi - 1];
+    if (run >= a.vocab || a.key[hi] != run || (lo > 0 && a.key[lo] == run && a.key[lo - 1] == run)) return;
+    uint32_t end = w + 1;                                  // one past the last window whose first token is of this run
+    for (;;) {
+        const uint32_t q = end + lane;
+        const bool mine = q < a.windows && a.key[(uint64_t)q << a.window_log2] == run;
+        const uint32_t not_mine = __ballot_sync(0xffffffffu, !mine);
+        if (not_mine != 0) { end += __ffs(not_mine) - 1; break; }
+        end += 32;
     }
+    if (c >= a.dim) return;
+    float sum[VE];
+    #pragma unroll
+    for (int j = 0; j < VE; ++j) sum[j] = a.part[(uint64_t)(2 * w + 1) * a.pitch + c + j];
+    #pragma unroll 8
+    for (uint32_t q = w + 1; q < end; ++q) {
+        #pragma unroll
+        for (int j = 0; j < VE; ++j) sum[j] += a.part[(uint64_t)(2 * q) * a.pitch + c + j];
+    }
+    write_row<ODT, VE>(a, run, c, sum);
 }
 
 // Tokens per window: about a quarter of the square root of their number.  The square root itself would make the
@@ -376,13 +419,13 @@ static uint32_t window_log2_for(uint64_t tokens) {
     return l;
 }
 
-struct GradLayout { size_t run, key[2], pos[2], part, total; uint32_t window_log2, windows, pitch; };
+struct GradLayout { size_t present, key[2], pos[2], part, total; uint32_t window_log2, windows, pitch; };
 
 static bool grad_layout(uint64_t tokens, uint64_t vocab, uint64_t dim, GradLayout &l) {
     if (tokens > kEmbMaxTokens || vocab > kEmbMaxRows || dim > kEmbMaxDim) return false;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
-    l.run = take(vocab * 8);
+    l.present = take(vocab);
     for (int i = 0; i < 2; ++i) { l.key[i] = take(tokens * 4); l.pos[i] = take(tokens * 4); }
     l.window_log2 = window_log2_for(tokens);
     l.windows = (uint32_t)((tokens + (1ull << l.window_log2) - 1) >> l.window_log2);
@@ -403,12 +446,12 @@ static int vector_of(uint64_t dim, const void *a, uint64_t lda, uint64_t ea, con
 #define LGN_LK(T, O) {reinterpret_cast<const void *>(&lookup_kernel<T, O, 1>), reinterpret_cast<const void *>(&lookup_kernel<T, O, 2>), reinterpret_cast<const void *>(&lookup_kernel<T, O, 8>)}
 static const void *const kLookupTable[2][2][3] = {{LGN_LK(LGN_F32, LGN_F32), LGN_LK(LGN_F32, LGN_BF16)}, {LGN_LK(LGN_BF16, LGN_F32), LGN_LK(LGN_BF16, LGN_BF16)}};
 #undef LGN_LK
-#define LGN_WK(T) {reinterpret_cast<const void *>(&window_kernel<T, 1>), reinterpret_cast<const void *>(&window_kernel<T, 2>), reinterpret_cast<const void *>(&window_kernel<T, 8>)}
-static const void *const kWindowTable[2][3] = {LGN_WK(LGN_F32), LGN_WK(LGN_BF16)};
+#define LGN_WK(T, O) {reinterpret_cast<const void *>(&window_kernel<T, O, 1>), reinterpret_cast<const void *>(&window_kernel<T, O, 2>), reinterpret_cast<const void *>(&window_kernel<T, O, 8>)}
+static const void *const kWindowTable[2][2][3] = {{LGN_WK(LGN_F32, LGN_F32), LGN_WK(LGN_F32, LGN_BF16)}, {LGN_WK(LGN_BF16, LGN_F32), LGN_WK(LGN_BF16, LGN_BF16)}};
 #undef LGN_WK
-#define LGN_RK(T, O) {reinterpret_cast<const void *>(&rows_kernel<T, O, 1>), reinterpret_cast<const void *>(&rows_kernel<T, O, 2>), reinterpret_cast<const void *>(&rows_kernel<T, O, 8>)}
-static const void *const kRowTable[2][2][3] = {{LGN_RK(LGN_F32, LGN_F32), LGN_RK(LGN_F32, LGN_BF16)}, {LGN_RK(LGN_BF16, LGN_F32), LGN_RK(LGN_BF16, LGN_BF16)}};
-#undef LGN_RK
+#define LGN_JK(O) {reinterpret_cast<const void *>(&join_kernel<O, 1>), reinterpret_cast<const void *>(&join_kernel<O, 2>), reinterpret_cast<const void *>(&join_kernel<O, 8>)}
+static const void *const kJoinTable[2][3] = {LGN_JK(LGN_F32), LGN_JK(LGN_BF16)};
+#undef LGN_JK
 static const int kVe[3] = {1, 2, 8};
 
 static uint64_t esize(lgn_dtype dt) { return dt == LGN_BF16 ? 2 : 4; }
@@ -471,7 +514,8 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     SortArgs s = {};
     s.ids = ids;
     for (int i = 0; i < 2; ++i) { s.key[i] = reinterpret_cast<uint32_t *>(w + l.key[i]); s.pos[i] = reinterpret_cast<uint32_t *>(w + l.pos[i]); }
-    s.run = reinterpret_cast<uint2 *>(w + l.run);
+    s.present = reinterpret_cast<uint8_t *>(w + l.present);
+    s.out = dtable; s.ld_out_bytes = ld_table * et; s.dim_bytes = dim * et;
     s.vocab = vocab;
     s.padding = padding_idx;
     s.tokens = (uint32_t)tokens;
@@ -482,19 +526,35 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     s.bits = (bits + s.passes - 1) / s.passes;
     if (s.bits < 5) s.bits = 5;                                        // whole warps of digits
     const size_t smem = (size_t)32 * sizeof(uint32_t) << s.bits;
-    const void *sort = reinterpret_cast<const void *>(&sort_ids_kernel);
-    if (cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * kSortBins * 4) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
+    const void *sort = reinterpret_cast<const void *>(&sort_kernel);
+    const int sms = sm_count();
+    if (sms < 1 || cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * kSortBins * 4) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
     {
         void *args[] = {&s};
-        const lgn_status r = launch_dependent(sort, dim3(kSortCtas), dim3(kSortThreads), args, smem, stream, kSortCtas);
+        unsigned grid = kSortCtas;
+        if (!accumulate) {
+            if (cudaMemsetAsync(s.present, 0, (size_t)vocab, static_cast<cudaStream_t>(stream)) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
+            if (tokens > 0) {
+                const uint64_t blocks = (tokens + 255) / 256;
+                const lgn_status r = launch_dependent(reinterpret_cast<const void *>(&mark_kernel), dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), args, 0, stream);
+                if (r != LGN_OK) return r;
+            }
+            // units of 2 MiB, so that CTAs are handed out as SMs become free; at least the SMs' number of them
+            uint64_t unit = (2u << 20) / s.dim_bytes + 1, most = vocab / (uint64_t)sms + 1;
+            if (unit > most) unit = most;
+            if (unit < vocab / 1000000 + 1) unit = vocab / 1000000 + 1;
+            s.zero_unit = (uint32_t)unit;
+            grid += (unsigned)((vocab + unit * kSortCtas - 1) / (unit * kSortCtas)) * kSortCtas;
+        }
+        const lgn_status r = launch_dependent(sort, dim3(grid), dim3(kSortThreads), args, smem, stream, kSortCtas);
         if (r != LGN_OK) return r;
     }
+    if (tokens == 0) return LGN_OK;
     const int vi = vector_of(dim, dout, ld_dout, ed, dtable, ld_table, et);
     SumArgs a = {};
     a.dout = dout; a.ld_dout = ld_dout;
     a.key = s.key[(s.passes + 1) & 1];
     a.pos = s.pos[(s.passes + 1) & 1];
-    a.run = s.run;
     a.part = reinterpret_cast<float *>(w + l.part);
     a.out = dtable; a.ld_out = ld_table; a.vocab = vocab;
     a.tokens = s.tokens;
@@ -504,13 +564,11 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     a.accumulate = accumulate != 0;
     a.scale = (float)scale;
     void *args[] = {&a};
-    const uint64_t wblocks = ((uint64_t)l.windows * a.slabs + 7) / 8, groups = (vocab + kRowsPerWarp - 1) / kRowsPerWarp, rblocks = (groups * a.slabs + 7) / 8;
-    if (wblocks > 0x7fffffffull || rblocks > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
+    const uint64_t blocks = ((uint64_t)l.windows * a.slabs + 7) / 8;
+    if (blocks > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     log_line("embedding_grad: %u tokens, %llu rows, dim %u, %u passes of %u bits, %u windows, %d elements per access", s.tokens,
              (unsigned long long)vocab, a.dim, s.passes, s.bits, l.windows, kVe[vi]);
-    if (l.windows > 1) {
-        const lgn_status r = launch_dependent(kWindowTable[dout_dt][vi], dim3((unsigned)wblocks), dim3(256), args, 0, stream);
-        if (r != LGN_OK) return r;
-    }
-    return launch_dependent(kRowTable[dout_dt][table_dt][vi], dim3((unsigned)rblocks), dim3(256), args, 0, stream);
+    const lgn_status r = launch_dependent(kWindowTable[dout_dt][table_dt][vi], dim3((unsigned)blocks), dim3(256), args, 0, stream);
+    if (r != LGN_OK || l.windows <= 1) return r;
+    return launch_dependent(kJoinTable[table_dt][vi], dim3((unsigned)blocks), dim3(256), args, 0, stream);
 }
