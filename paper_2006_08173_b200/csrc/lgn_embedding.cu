@@ -5,16 +5,19 @@
 //
 // Both are bound by memory.  The gradient adds rows that share an id in a fixed order, without atomics on
 // values: the tokens are sorted by id (stable), so that every table row owns one run of the sorted list.
-//   mark_kernel    (after a memset) notes which rows of the table have a token
-//   sort_kernel    cluster 0 (8 CTAs): radix sort of (id, position), up to 9 bits per pass.  The other clusters meanwhile
-//                  write zeros to the rows without a token, most of the bytes that a gradient of a large table has to write
+//   sort_kernel    one cluster of 16 CTAs (8 where 16 do not fit): radix sort of (id, position), up to 9 bits per pass; on the way it marks the rows
+//                  of the table that have a token (the marks are cleared by a memset before)
 //   window_kernel  a warp per window of the sorted list and slab of columns walks its tokens, eight rows of dout in flight
 //                  whatever the runs' lengths, and writes each run that lies inside the window to its table row; the
-//                  pieces of runs that reach beyond it (one at its start, one at its end) go to scratch
+//                  pieces of runs that reach beyond it (one at its start, one at its end) go to scratch.  CTAs of the
+//                  same launch, mixed in between, write zeros to the rows without a token: most of the bytes that the
+//                  gradient of a large table has to write, streamed beside the gathers
 //   join_kernel    adds the pieces of each run of several windows
 // so that no warp adds more than one window of tokens, or one window count of pieces, in sequence.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+
+#include <mutex>
 
 #include "lgn.h"
 #include "lgn_launch.h"
@@ -52,11 +55,21 @@ __device__ __forceinline__ void load_vec(const void *base, uint64_t i, float *v)
 }
 
 template <int DT, int VE>
-__device__ __forceinline__ void load_vec_rw(const void *base, uint64_t i, float *v) {      // memory this kernel also writes
-    #pragma unroll
-    for (int k = 0; k < VE; ++k) {
-        if constexpr (DT == LGN_F32) v[k] = static_cast<const float *>(base)[i + k];
-        else v[k] = __bfloat162float(static_cast<const __nv_bfloat16 *>(base)[i + k]);
+__device__ __forceinline__ void load_vec_rw(const void *base, uint64_t i, float *v) {      // memory this kernel or the one before wrote
+    if constexpr (VE == 8 && DT == LGN_F32) {
+        const float4 a = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + i)[0], b = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + i)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else if constexpr (VE == 8) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(base) + i);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+        #pragma unroll
+        for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+    } else {
+        #pragma unroll
+        for (int k = 0; k < VE; ++k) {
+            if constexpr (DT == LGN_F32) v[k] = static_cast<const float *>(base)[i + k];
+            else v[k] = __bfloat162float(static_cast<const __nv_bfloat16 *>(base)[i + k]);
+        }
     }
 }
 
@@ -149,12 +162,12 @@ lookup_kernel(const void *__restrict__ table, uint64_t ld_table, uint64_t vocab,
 }
 
 // ------------------------------------------------------------------ sort
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortCtas * 32, kSortBins = 512;
+constexpr int kSortThreads = 1024, kSortBins = 512;
 constexpr int kSortBatch = 8;                              // loads a lane has in flight
 
-__device__ __forceinline__ uint32_t ld_l2(const uint32_t *p) {       // written by other CTAs of the cluster before its barrier
-    uint32_t v;
-    asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+__device__ __forceinline__ uint64_t ld_l2(const uint64_t *p) {       // written by other CTAs of the cluster before its barrier
+    uint64_t v;
+    asm volatile("ld.global.cg.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
     return v;
 }
 
@@ -165,13 +178,11 @@ __device__ __forceinline__ void cluster_sync_all() {
 
 struct SortArgs {
     const void *ids;
-    uint32_t *key[2], *pos[2];
+    uint64_t *pair[2];             // id << 32 | position
     uint8_t *present;              // per table row: has a token (not used when the gradient is accumulated)
-    void *out;
-    uint64_t ld_out_bytes, dim_bytes;
     uint64_t vocab;
     int64_t padding;
-    uint32_t tokens, wide, bits, passes, zero_unit;   // zero_unit: table rows a CTA of the other clusters looks after
+    uint32_t tokens, wide, bits, passes;
 };
 
 __device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i) {       // vocab: left out, sorts last
@@ -179,68 +190,36 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i) {     
     return id < 0 || (uint64_t)id >= a.vocab || id == a.padding ? (uint32_t)a.vocab : (uint32_t)id;
 }
 
-__global__ void __launch_bounds__(256) mark_kernel(const SortArgs a) {
-    dep_launch();
-    dep_wait();
-    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < a.tokens; i += gridDim.x * 256) {
-        const uint32_t k = key_of(a, i);
-        if (k < a.vocab) a.present[k] = 1;
-    }
-}
-
-// Zeros to the rows [first, last) without a token, a warp per row; 32 rows' marks at a time.
-__device__ __forceinline__ void zero_rows(const SortArgs &a, uint64_t first, uint64_t last, uint32_t warp) {
-    const uint32_t lane = threadIdx.x & 31;
-    // row r of a group of 32 is warp (r mod 32)'s, so that all warps of the CTA have rows of each group
-    for (uint64_t r0 = first; r0 < last; r0 += 1024) {
-        uint8_t mark = 1;
-        const uint64_t mine = r0 + 32 * lane + warp;
-        if (mine < last) mark = *(a.present + mine);
-        uint32_t todo = __ballot_sync(0xffffffffu, mark == 0);
-        while (todo != 0) {
-            const uint32_t k = __ffs(todo) - 1;
-            todo &= todo - 1;
-            char *row = static_cast<char *>(a.out) + (r0 + 32 * k + warp) * a.ld_out_bytes, *end = row + a.dim_bytes;
-            char *body = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(row) + 15) & ~(uintptr_t)15);
-            if (body > end) body = end;
-            const uint64_t vec = (uint64_t)(end - body) / 16;
-            for (char *q = row + 2 * lane; q < body; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;      // at most 14 bytes
-            for (uint64_t v = lane; v < vec; v += 32) __stcs(reinterpret_cast<uint4 *>(body) + v, make_uint4(0, 0, 0, 0));
-            for (char *q = body + vec * 16 + 2 * lane; q < end; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;
-        }
-    }
-}
-
 __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a) {
     extern __shared__ uint32_t hist[];                     // [32][bins]
     __shared__ uint32_t total[kSortBins], base[kSortBins], warp_sum[32];
     dep_launch();
     dep_wait();
-    uint32_t rank;
+    uint32_t rank, ctas;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1u << a.bits, mask = bins - 1;
-    if (blockIdx.x >= kSortCtas) {
-        const uint64_t first = (uint64_t)(blockIdx.x - kSortCtas) * a.zero_unit;
-        zero_rows(a, first, first + a.zero_unit < a.vocab ? first + a.zero_unit : a.vocab, warp);
-        return;
-    }
-    const uint32_t per = (((a.tokens + kSortWarps - 1) / kSortWarps) + 31u) & ~31u;
+    const uint32_t per = (((a.tokens + ctas * 32 - 1) / (ctas * 32)) + 31u) & ~31u;
     const uint64_t lo64 = (uint64_t)(rank * 32 + warp) * per;
     const uint32_t lo = lo64 < a.tokens ? (uint32_t)lo64 : a.tokens, hi = lo64 + per < a.tokens ? (uint32_t)(lo64 + per) : a.tokens;
     for (uint32_t pass = 0; pass < a.passes; ++pass) {
-        const uint32_t *ksrc = a.key[(pass + 1) & 1], *psrc = a.pos[(pass + 1) & 1];
-        uint32_t *kdst = a.key[pass & 1], *pdst = a.pos[pass & 1];
+        const uint64_t *src = a.pair[(pass + 1) & 1];
+        uint64_t *dst = a.pair[pass & 1];
         const uint32_t shift = pass * a.bits;
-        auto key_at = [&](uint32_t i) -> uint32_t { return pass > 0 ? ld_l2(ksrc + i) : key_of(a, i); };
+        auto pair_at = [&](uint32_t i) -> uint64_t { return pass > 0 ? ld_l2(src + i) : (uint64_t)key_of(a, i) << 32 | i; };
         for (uint32_t i = threadIdx.x; i < 32 * bins; i += kSortThreads) hist[i] = 0u;
         __syncthreads();
         uint32_t *mine = hist + warp * bins;
         for (uint32_t i = lo + lane; i < hi; i += 32 * kSortBatch) {
             uint32_t k[kSortBatch];
             #pragma unroll
-            for (int j = 0; j < kSortBatch; ++j) k[j] = i + 32 * j < hi ? key_at(i + 32 * j) : 0u;
+            for (int j = 0; j < kSortBatch; ++j) k[j] = i + 32 * j < hi ? (uint32_t)(pair_at(i + 32 * j) >> 32) : 0u;
             #pragma unroll
-            for (int j = 0; j < kSortBatch; ++j) if (i + 32 * j < hi) atomicAdd(mine + ((k[j] >> shift) & mask), 1u);
+            for (int j = 0; j < kSortBatch; ++j)
+                if (i + 32 * j < hi) {
+                    atomicAdd(mine + ((k[j] >> shift) & mask), 1u);
+                    if (pass == 0 && a.present != nullptr && k[j] < a.vocab) a.present[k[j]] = 1;
+                }
         }
         __syncthreads();
         if (threadIdx.x < bins) {                          // places of each warp within its CTA, digit by digit
@@ -253,8 +232,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a)
         uint32_t before = 0, all = 0;
         if (threadIdx.x < bins) {
             const uint32_t at = (uint32_t)__cvta_generic_to_shared(total + threadIdx.x);
-            #pragma unroll
-            for (uint32_t c = 0; c < kSortCtas; ++c) {
+            #pragma unroll 8
+            for (uint32_t c = 0; c < ctas; ++c) {
                 uint32_t remote, v;
                 asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(c));
                 asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
@@ -274,18 +253,14 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a)
         }
         __syncthreads();
         for (uint32_t i0 = lo + lane; i0 - lane < hi; i0 += 32 * kSortBatch) {
-            uint32_t kb[kSortBatch], pb[kSortBatch];
+            uint64_t kb[kSortBatch];
             #pragma unroll
-            for (int j = 0; j < kSortBatch; ++j) {
-                const uint32_t i = i0 + 32 * j;
-                kb[j] = i < hi ? key_at(i) : 0u;
-                pb[j] = i < hi && pass > 0 ? ld_l2(psrc + i) : i;
-            }
+            for (int j = 0; j < kSortBatch; ++j) kb[j] = i0 + 32 * j < hi ? pair_at(i0 + 32 * j) : 0u;
             #pragma unroll
             for (int j = 0; j < kSortBatch; ++j) {
                 if (i0 - lane + 32 * j >= hi) break;
                 const bool on = i0 + 32 * j < hi;
-                const uint32_t digit = on ? (kb[j] >> shift) & mask : bins;         // lanes past the end: a digit of their own
+                const uint32_t digit = on ? (uint32_t)(kb[j] >> (32 + shift)) & mask : bins;         // lanes past the end: a digit of their own
                 const uint32_t same = __match_any_sync(0xffffffffu, digit);
                 uint32_t at = 0;
                 if (on) at = mine[digit];
@@ -294,8 +269,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a)
                     const uint32_t r = __popc(same & ((1u << lane) - 1u));
                     if (r == 0) mine[digit] = at + __popc(same);
                     at += base[digit] + r;
-                    kdst[at] = kb[j];
-                    pdst[at] = pb[j];
+                    dst[at] = kb[j];
                 }
                 __syncwarp();
             }
@@ -305,16 +279,45 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a)
 }
 
 // ------------------------------------------------------------------ sums
+// The id of sorted place i.
+__device__ __forceinline__ uint32_t id_at(const uint64_t *pair, uint64_t i) { return reinterpret_cast<const uint32_t *>(pair + i)[1]; }
+
 struct SumArgs {
     const void *dout;
     uint64_t ld_dout;
-    const uint32_t *key, *pos;
+    const uint64_t *pair;
     float *part;                   // two rows of `pitch` values per window: the piece at its start, the piece at its end
     void *out;
     uint64_t ld_out, vocab;
     uint32_t tokens, window_log2, windows, dim, pitch, slabs, accumulate;
     float scale;
+    const uint8_t *present;        // as in SortArgs
+    uint64_t ld_out_bytes, dim_bytes;
+    uint32_t zero_unit, zero_blocks;   // table rows per CTA that writes zeros, and the number of those CTAs
 };
+
+// Zeros to the rows [first, last) without a token, a warp per row; 8 x 32 rows' marks at a time.
+__device__ __forceinline__ void zero_rows(const SumArgs &a, uint64_t first, uint64_t last) {
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // row r of a group of 256 is warp (r mod 8)'s, so that all warps of the CTA have rows of each group
+    for (uint64_t r0 = first; r0 < last; r0 += 256) {
+        uint8_t mark = 1;
+        const uint64_t mine = r0 + 8 * lane + warp;
+        if (mine < last) mark = a.present[mine];
+        uint32_t todo = __ballot_sync(0xffffffffu, mark == 0);
+        while (todo != 0) {
+            const uint32_t k = __ffs(todo) - 1;
+            todo &= todo - 1;
+            char *row = static_cast<char *>(a.out) + (r0 + 8 * k + warp) * a.ld_out_bytes, *end = row + a.dim_bytes;
+            char *body = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(row) + 15) & ~(uintptr_t)15);
+            if (body > end) body = end;
+            const uint64_t vec = (uint64_t)(end - body) / 16;
+            for (char *q = row + 2 * lane; q < body; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;      // at most 14 bytes
+            for (uint64_t v = lane; v < vec; v += 32) __stcs(reinterpret_cast<uint4 *>(body) + v, make_uint4(0, 0, 0, 0));
+            for (char *q = body + vec * 16 + 2 * lane; q < end; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;
+        }
+    }
+}
 
 template <int ODT, int VE>
 __device__ __forceinline__ void write_row(const SumArgs &a, uint32_t row, uint32_t c, float *sum) {
@@ -335,25 +338,38 @@ __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
     constexpr int kFlight = VE == 8 ? 8 : 16;
     dep_launch();
     dep_wait();
-    const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    // the CTAs that write zeros are spread evenly over the grid
+    const uint64_t zb = (uint64_t)blockIdx.x * a.zero_blocks / gridDim.x, zn = (uint64_t)(blockIdx.x + 1) * a.zero_blocks / gridDim.x;
+    if (zn != zb) {
+        const uint64_t first = zb * a.zero_unit;
+        zero_rows(a, first, first + a.zero_unit < a.vocab ? first + a.zero_unit : a.vocab);
+        return;
+    }
+    const uint64_t item = (blockIdx.x - zb) * 8 + (threadIdx.x >> 5);
     const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
     if (w >= a.windows) return;
     const uint32_t lo = w << a.window_log2, hi = min(a.tokens, (w + 1) << a.window_log2);
     const bool on = c < a.dim;
-    const uint32_t before = lo > 0 ? a.key[lo - 1] : 0xffffffffu, after = hi < a.tokens ? a.key[hi] : 0xffffffffu;
+    const uint32_t before = lo > 0 ? id_at(a.pair, lo - 1) : 0xffffffffu, after = hi < a.tokens ? id_at(a.pair, hi) : 0xffffffffu;
     float sum[VE];
-    uint32_t run = 0xffffffffu, first = a.key[lo];
+    uint32_t run = 0xffffffffu, first = id_at(a.pair, lo);
     auto flush = [&](uint32_t next) {                      // the run ends, or (next == run) goes on in the next window
         if (!on) return;
         const bool from_before = run == first && before == run;
         if (!from_before && next != run) { write_row<ODT, VE>(a, run, c, sum); return; }
         float *q = a.part + (uint64_t)(2 * w + (from_before ? 0 : 1)) * a.pitch + c;
-        #pragma unroll
-        for (int j = 0; j < VE; ++j) q[j] = sum[j];
+        if constexpr (VE == 8) {
+            reinterpret_cast<float4 *>(q)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            reinterpret_cast<float4 *>(q)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        } else {
+            #pragma unroll
+            for (int j = 0; j < VE; ++j) q[j] = sum[j];
+        }
     };
     for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
         const uint32_t m = min(32u, hi - i0);
-        const uint32_t keys = lane < m ? a.key[i0 + lane] : (uint32_t)a.vocab, poss = lane < m ? a.pos[i0 + lane] : 0u;
+        const uint64_t mine = lane < m ? a.pair[i0 + lane] : a.vocab << 32;
+        const uint32_t keys = (uint32_t)(mine >> 32), poss = (uint32_t)mine;
         for (uint32_t k0 = 0; k0 < m; k0 += kFlight) {
             if (__shfl_sync(0xffffffffu, keys, k0) >= a.vocab) { i0 = hi; break; }      // only left-out tokens follow
             RawVec<DDT, VE> v[kFlight];
@@ -389,24 +405,30 @@ __global__ void __launch_bounds__(256) join_kernel(const SumArgs a) {
     const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
     if (w + 1 >= a.windows) return;
-    const uint32_t lo = w << a.window_log2, hi = (w + 1) << a.window_log2, run = a.key[hi - 1];
-    if (run >= a.vocab || a.key[hi] != run || (lo > 0 && a.key[lo] == run && a.key[lo - 1] == run)) return;
+    const uint32_t lo = w << a.window_log2, hi = (w + 1) << a.window_log2, run = id_at(a.pair, hi - 1);
+    if (run >= a.vocab || id_at(a.pair, hi) != run || (lo > 0 && id_at(a.pair, lo) == run && id_at(a.pair, lo - 1) == run)) return;
     uint32_t end = w + 1;                                  // one past the last window whose first token is of this run
     for (;;) {
         const uint32_t q = end + lane;
-        const bool mine = q < a.windows && a.key[(uint64_t)q << a.window_log2] == run;
+        const bool mine = q < a.windows && id_at(a.pair, (uint64_t)q << a.window_log2) == run;
         const uint32_t not_mine = __ballot_sync(0xffffffffu, !mine);
         if (not_mine != 0) { end += __ffs(not_mine) - 1; break; }
         end += 32;
     }
     if (c >= a.dim) return;
     float sum[VE];
-    #pragma unroll
-    for (int j = 0; j < VE; ++j) sum[j] = a.part[(uint64_t)(2 * w + 1) * a.pitch + c + j];
-    #pragma unroll 8
-    for (uint32_t q = w + 1; q < end; ++q) {
+    load_vec_rw<LGN_F32, VE>(a.part, (uint64_t)(2 * w + 1) * a.pitch + c, sum);
+    for (uint32_t q0 = w + 1; q0 < end; q0 += 8) {
+        float v[8][VE];
         #pragma unroll
-        for (int j = 0; j < VE; ++j) sum[j] += a.part[(uint64_t)(2 * q) * a.pitch + c + j];
+        for (int k = 0; k < 8; ++k)
+            if (q0 + k < end) load_vec_rw<LGN_F32, VE>(a.part, (uint64_t)(2 * (q0 + k)) * a.pitch + c, v[k]);
+        #pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (q0 + k < end) {
+                #pragma unroll
+                for (int j = 0; j < VE; ++j) sum[j] += v[k][j];
+            }
     }
     write_row<ODT, VE>(a, run, c, sum);
 }
@@ -419,20 +441,52 @@ static uint32_t window_log2_for(uint64_t tokens) {
     return l;
 }
 
-struct GradLayout { size_t present, key[2], pos[2], part, total; uint32_t window_log2, windows, pitch; };
+struct GradLayout { size_t present, pair[2], part, total; uint32_t window_log2, windows, pitch; };
 
 static bool grad_layout(uint64_t tokens, uint64_t vocab, uint64_t dim, GradLayout &l) {
     if (tokens > kEmbMaxTokens || vocab > kEmbMaxRows || dim > kEmbMaxDim) return false;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     l.present = take(vocab);
-    for (int i = 0; i < 2; ++i) { l.key[i] = take(tokens * 4); l.pos[i] = take(tokens * 4); }
+    for (int i = 0; i < 2; ++i) l.pair[i] = take(tokens * 8);
     l.window_log2 = window_log2_for(tokens);
     l.windows = (uint32_t)((tokens + (1ull << l.window_log2) - 1) >> l.window_log2);
     l.pitch = (uint32_t)((dim + 7) & ~7ull);
     l.part = take(l.windows > 1 ? (size_t)2 * l.windows * l.pitch * 4 : 0);
     l.total = at < 256 ? 256 : at;
     return true;
+}
+
+// CTAs of the sort's cluster on the current device: 16 where the device can place such a cluster, else 8.  Found once per device;
+// 0: the runtime refused.
+static int sort_ctas() {
+    static std::mutex guard;
+    static int found[64];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+    std::lock_guard<std::mutex> lock(guard);
+    if (dev < 64 && found[dev] != 0) return found[dev];
+    const void *fn = reinterpret_cast<const void *>(&sort_kernel);
+    const int smem = 32 * kSortBins * 4;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    int n = 8;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 16;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3(16);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, fn, &cfg) == cudaSuccess && clusters >= 1) n = 16;
+    }
+    (void)cudaGetLastError();
+    if (dev < 64) found[dev] = n;
+    return n;
 }
 
 // Elements per access: 8 where every row of both matrices starts at a multiple of 16 bytes and holds
@@ -513,9 +567,9 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     char *w = static_cast<char *>(ws);
     SortArgs s = {};
     s.ids = ids;
-    for (int i = 0; i < 2; ++i) { s.key[i] = reinterpret_cast<uint32_t *>(w + l.key[i]); s.pos[i] = reinterpret_cast<uint32_t *>(w + l.pos[i]); }
+    for (int i = 0; i < 2; ++i) s.pair[i] = reinterpret_cast<uint64_t *>(w + l.pair[i]);
     s.present = reinterpret_cast<uint8_t *>(w + l.present);
-    s.out = dtable; s.ld_out_bytes = ld_table * et; s.dim_bytes = dim * et;
+   
     s.vocab = vocab;
     s.padding = padding_idx;
     s.tokens = (uint32_t)tokens;
@@ -527,34 +581,21 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     if (s.bits < 5) s.bits = 5;                                        // whole warps of digits
     const size_t smem = (size_t)32 * sizeof(uint32_t) << s.bits;
     const void *sort = reinterpret_cast<const void *>(&sort_kernel);
-    const int sms = sm_count();
-    if (sms < 1 || cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * kSortBins * 4) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
-    {
+    const int ctas = sort_ctas();
+    if (ctas == 0) return LGN_ERR_CUDA;
+    if (accumulate) {
+        s.present = nullptr;
+        if (tokens == 0) return LGN_OK;
+    } else if (cudaMemsetAsync(s.present, 0, (size_t)vocab, static_cast<cudaStream_t>(stream)) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
+    if (tokens > 0) {
         void *args[] = {&s};
-        unsigned grid = kSortCtas;
-        if (!accumulate) {
-            if (cudaMemsetAsync(s.present, 0, (size_t)vocab, static_cast<cudaStream_t>(stream)) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
-            if (tokens > 0) {
-                const uint64_t blocks = (tokens + 255) / 256;
-                const lgn_status r = launch_dependent(reinterpret_cast<const void *>(&mark_kernel), dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), args, 0, stream);
-                if (r != LGN_OK) return r;
-            }
-            // units of 2 MiB, so that CTAs are handed out as SMs become free; at least the SMs' number of them
-            uint64_t unit = (2u << 20) / s.dim_bytes + 1, most = vocab / (uint64_t)sms + 1;
-            if (unit > most) unit = most;
-            if (unit < vocab / 1000000 + 1) unit = vocab / 1000000 + 1;
-            s.zero_unit = (uint32_t)unit;
-            grid += (unsigned)((vocab + unit * kSortCtas - 1) / (unit * kSortCtas)) * kSortCtas;
-        }
-        const lgn_status r = launch_dependent(sort, dim3(grid), dim3(kSortThreads), args, smem, stream, kSortCtas);
+        const lgn_status r = launch_dependent(sort, dim3((unsigned)ctas), dim3(kSortThreads), args, smem, stream, (unsigned)ctas);
         if (r != LGN_OK) return r;
     }
-    if (tokens == 0) return LGN_OK;
     const int vi = vector_of(dim, dout, ld_dout, ed, dtable, ld_table, et);
     SumArgs a = {};
     a.dout = dout; a.ld_dout = ld_dout;
-    a.key = s.key[(s.passes + 1) & 1];
-    a.pos = s.pos[(s.passes + 1) & 1];
+    a.pair = s.pair[(s.passes + 1) & 1];
     a.part = reinterpret_cast<float *>(w + l.part);
     a.out = dtable; a.ld_out = ld_table; a.vocab = vocab;
     a.tokens = s.tokens;
@@ -565,10 +606,19 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     a.scale = (float)scale;
     void *args[] = {&a};
     const uint64_t blocks = ((uint64_t)l.windows * a.slabs + 7) / 8;
-    if (blocks > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
+    if (!accumulate) {                                                 // 256 KiB a CTA, at least 8 rows (a warp's each), at most 2^20 CTAs
+        uint64_t unit = (256u << 10) / (dim * et);
+        if (unit < 8) unit = 8;
+        if (unit < (vocab >> 20) + 1) unit = (vocab >> 20) + 1;
+        a.present = s.present;
+        a.ld_out_bytes = ld_table * et; a.dim_bytes = dim * et;
+        a.zero_unit = (uint32_t)unit;
+        a.zero_blocks = (uint32_t)((vocab + unit - 1) / unit);
+    }
+    if (blocks + a.zero_blocks > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     log_line("embedding_grad: %u tokens, %llu rows, dim %u, %u passes of %u bits, %u windows, %d elements per access", s.tokens,
              (unsigned long long)vocab, a.dim, s.passes, s.bits, l.windows, kVe[vi]);
-    const lgn_status r = launch_dependent(kWindowTable[dout_dt][table_dt][vi], dim3((unsigned)blocks), dim3(256), args, 0, stream);
+    const lgn_status r = launch_dependent(kWindowTable[dout_dt][table_dt][vi], dim3((unsigned)blocks + a.zero_blocks), dim3(256), args, 0, stream);
     if (r != LGN_OK || l.windows <= 1) return r;
     return launch_dependent(kJoinTable[table_dt][vi], dim3((unsigned)blocks), dim3(256), args, 0, stream);
 }
