@@ -562,15 +562,25 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(void *out, uint64_t ldo,
         store_out<ODT>(out, (i / cols) * ldo + i % cols, 0.0f);
 }
 
-// The kernels a call may take.
-struct MmKernel { const void *fn; int bn, ctas, form, odt, smem; };
-#define LGN_MM(BN, C, F, O) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, C, F, O>), BN, C, F, O, MmShape<BN, C, O>::kSmem}
+// The kernels a call may take, with what a call of each costs on a B200, in microseconds: `start` once, `step` for 128 of k of
+// a tile, `tile` for a tile beyond that (fitted to 60 products from 4 x 1024 x 1024 to 4096^3).  The fits leave errors of up to a
+// fifth, about as much as neighbouring kernels differ; what they must get right is which side of
+//   64 x k shares       few tokens: (4, 4096, 4096) 6.7 us in 4 shares, 9.1 whole, 7.8 with pairs of 128
+//   pairs of 128        (512, 4096, 4096) 10.1 us, 12.3 with lone 128, 14.4 with pairs of 256
+//   lone 128            where pairs would need a second round: (777, 2504, 1000) 7.1 us against 9.7
+//   pairs of 256 / 192  (4096, 4096, 4096) 48 us in bf16, 49 with pairs of 128
+// a call lies on.
+struct MmKernel { const void *fn; int bn, ctas, form, odt, smem; float start, step, tile; };
+#define LGN_MM(BN, C, F, O, A, S, T) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, C, F, O>), BN, C, F, O, MmShape<BN, C, O>::kSmem, A, S, T}
 static const MmKernel kMmKernels[] = {
-    LGN_MM(64, 1, kFormSwap, LGN_F32), LGN_MM(64, 1, kFormSplit, LGN_F32), LGN_MM(64, 1, kFormSwap, LGN_BF16), LGN_MM(64, 1, kFormSplit, LGN_BF16),
-    LGN_MM(128, 1, kFormRows, LGN_F32), LGN_MM(128, 1, kFormSwap, LGN_F32), LGN_MM(128, 1, kFormSplit, LGN_F32),
-    LGN_MM(128, 1, kFormRows, LGN_BF16), LGN_MM(128, 1, kFormSwap, LGN_BF16), LGN_MM(128, 1, kFormSplit, LGN_BF16),
-    LGN_MM(192, 2, kFormRows, LGN_F32), LGN_MM(192, 2, kFormSwap, LGN_F32),
-    LGN_MM(256, 2, kFormRows, LGN_BF16), LGN_MM(256, 2, kFormSwap, LGN_BF16)};
+    LGN_MM(64, 1, kFormSwap, LGN_F32, 2.4f, 0.2f, 0.4f), LGN_MM(64, 1, kFormSplit, LGN_F32, 2.4f, 0.2f, 0.4f),
+    LGN_MM(64, 1, kFormSwap, LGN_BF16, 2.4f, 0.2f, 0.1f), LGN_MM(64, 1, kFormSplit, LGN_BF16, 2.4f, 0.2f, 0.1f),
+    LGN_MM(128, 1, kFormRows, LGN_F32, 3.0f, 0.25f, 1.0f), LGN_MM(128, 1, kFormSwap, LGN_F32, 3.0f, 0.25f, 1.3f),
+    LGN_MM(128, 1, kFormRows, LGN_BF16, 3.0f, 0.24f, 0.4f), LGN_MM(128, 1, kFormSwap, LGN_BF16, 3.0f, 0.24f, 0.7f),
+    LGN_MM(128, 2, kFormRows, LGN_F32, 3.2f, 0.18f, 1.3f), LGN_MM(128, 2, kFormSwap, LGN_F32, 3.2f, 0.18f, 1.6f),
+    LGN_MM(128, 2, kFormRows, LGN_BF16, 3.2f, 0.17f, 0.9f), LGN_MM(128, 2, kFormSwap, LGN_BF16, 3.2f, 0.17f, 1.2f),
+    LGN_MM(192, 2, kFormRows, LGN_F32, 3.3f, 0.23f, 2.7f), LGN_MM(192, 2, kFormSwap, LGN_F32, 3.3f, 0.23f, 3.0f),
+    LGN_MM(256, 2, kFormRows, LGN_BF16, 3.3f, 0.3f, 1.1f), LGN_MM(256, 2, kFormSwap, LGN_BF16, 3.3f, 0.3f, 1.4f)};
 #undef LGN_MM
 constexpr int kMmCount = (int)(sizeof kMmKernels / sizeof kMmKernels[0]);
 
@@ -605,7 +615,7 @@ static bool make_scale_map(CUtensorMap *m, const void *scales, uint64_t tiles) {
                           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output: boxes of 32 rows x 128 bytes.  Needs 16-byte aligned rows.
+// The output: boxes of 32 rows x 128 bytes.  Needs rows aligned to, and a multiple of, 16 bytes.
 static bool make_out_map(CUtensorMap *m, void *out, uint64_t rows, uint64_t cols, uint64_t ldo, int odt) {
     const uint64_t es = odt == LGN_F32 ? 4 : 2;
     const cuuint64_t dim[2] = {cols, rows}, stride[1] = {ldo * es};
@@ -631,10 +641,35 @@ static bool allow_smem(int kernel) {
     return true;
 }
 
+// Clusters of 2, 4 or 8 CTAs of a kernel that the device can run at once (found once per device and kernel).
+static int active_clusters(int kernel, int size_log2) {
+    static std::mutex guard;
+    static int found[64][kMmCount][4];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || !allow_smem(kernel)) return 0;
+    std::lock_guard<std::mutex> lock(guard);
+    int &n = found[dev][kernel][size_log2];
+    if (n == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1u << size_log2;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3(1u << size_log2);
+        cfg.blockDim = dim3(kMmThreads);
+        cfg.dynamicSmemBytes = (size_t)kMmKernels[kernel].smem;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int c = 0;
+        if (cudaOccupancyMaxActiveClusters(&c, kMmKernels[kernel].fn, &cfg) != cudaSuccess) { (void)cudaGetLastError(); c = 0; }
+        n = c > 0 ? c : -1;
+    }
+    return n > 0 ? n : 0;
+}
+
 struct MmPlan { int kernel; uint32_t split, split_groups; };
 
-// The kernel of least estimated time, in clocks of an SM: rounds of the grid times the steps of k of a tile, plus
-// what a tile costs beyond them.
+// The kernel of least estimated time: rounds of the grid times the cost of a tile.
 static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, bool vec, int odt, int sms) {
     MmPlan best = {-1, 1, 0};
     const uint64_t groups = (kblocks + 3) / 4;
@@ -644,14 +679,16 @@ static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, bool vec, in
         if (q.odt != odt || (q.form == kFormRows && !vec)) continue;
         const uint64_t rows = 128 * (uint64_t)q.ctas, bn = (uint64_t)q.bn, r = q.form == kFormRows ? m : n, c = q.form == kFormRows ? n : m;
         const uint64_t tiles = ((r + rows - 1) / rows) * ((c + bn - 1) / bn), slots = (uint64_t)(sms / q.ctas);
-        for (uint64_t want = q.form == kFormSplit ? 2 : 1; want <= (q.form == kFormSplit ? 8u : 1u); want *= 2) {
-            const uint64_t per = (groups + want - 1) / want, s = q.form == kFormSplit ? (groups + per - 1) / per : 1;
-            if (q.form == kFormSplit && (s < 2 || tiles * s > slots)) continue;
-            const uint64_t steps = q.form == kFormSplit && per * 4 < kblocks ? per * 4 : kblocks;
-            const double rounds = (double)((tiles * s + slots - 1) / slots);
-            const double step = q.ctas == 2 ? (bn == 256 ? 600 : 500) : (bn == 128 ? 500 : 400);
-            const double tile = (bn == 256 ? 1500 : 400) + (q.form == kFormSwap ? 4.0 * bn : 0) + (s > 1 ? 3000 : 0);
-            const double cost = rounds * (steps * step + tile);
+        if (q.form != kFormSplit) {
+            const double cost = q.start + (double)((tiles + slots - 1) / slots) * ((double)kblocks * q.step + q.tile);
+            if (cost < best_cost) { best_cost = cost; best = {i, 1, 0}; }
+            continue;
+        }
+        for (int l = 1; l <= 3; ++l) {
+            // shares of whole groups of four blocks; a CTA adds up its part of min(c, bn) columns of each share
+            const uint64_t per = (groups + (1u << l) - 1) >> l, s = (groups + per - 1) / per;
+            if (s < 2 || tiles > (uint64_t)active_clusters(i, s > 4 ? 3 : s > 2 ? 2 : 1)) continue;
+            const double cost = (double)(per * 4 < kblocks ? per * 4 : kblocks) * q.step + q.start + q.tile + 0.5 + 0.05 * (double)(c < bn ? c : bn);
             if (cost < best_cost) { best_cost = cost; best = {i, (uint32_t)s, (uint32_t)per}; }
         }
     }
@@ -687,7 +724,8 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
         ranges_overlap(out, ob, a_scales, lgn_fp8_scales_bytes(m, k)) || ranges_overlap(out, ob, b_scales, lgn_fp8_scales_bytes(n, k)))
         return LGN_ERR_INVALID_ARG;
     if (sms < 1 || encode_tiled() == nullptr) return LGN_ERR_CUDA;
-    const bool vec = aligned_to(out, 16) && (ldo * es) % 16 == 0;
+    // TMA stores: aligned rows, and whole 16-byte pieces (a row's last piece is written whole, beyond the n-th element too)
+    const bool vec = aligned_to(out, 16) && (ldo * es) % 16 == 0 && (n * es) % 16 == 0;
     const uint64_t kblocks = (k + 127) / 128;
     const MmPlan plan = plan_matmul(m, n, kblocks, vec, out_dt, sms);
     if (plan.kernel < 0) return LGN_ERR_UNSUPPORTED;
