@@ -164,6 +164,7 @@ lookup_kernel(const void *__restrict__ table, uint64_t ld_table, uint64_t vocab,
 // ------------------------------------------------------------------ sort
 constexpr int kSortThreads = 1024, kSortBins = 512;
 constexpr int kSortBatch = 8;                              // loads a lane has in flight
+constexpr uint64_t kSortAlone = 1024;                      // tokens that one CTA sorts by itself (4999: 24 us, 16 with a cluster)
 
 __device__ __forceinline__ uint64_t ld_l2(const uint64_t *p) {       // written by other CTAs of the cluster before its barrier
     uint64_t v;
@@ -210,15 +211,17 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a)
         for (uint32_t i = threadIdx.x; i < 32 * bins; i += kSortThreads) hist[i] = 0u;
         __syncthreads();
         uint32_t *mine = hist + warp * bins;
-        for (uint32_t i = lo + lane; i < hi; i += 32 * kSortBatch) {
-            uint32_t k[kSortBatch];
+        const bool once = per <= 32 * kSortBatch;              // a warp's share stays in registers from the count to the scatter
+        uint64_t kb[kSortBatch];
+        for (uint32_t i = lo + lane; i - lane < hi; i += 32 * kSortBatch) {
             #pragma unroll
-            for (int j = 0; j < kSortBatch; ++j) k[j] = i + 32 * j < hi ? (uint32_t)(pair_at(i + 32 * j) >> 32) : 0u;
+            for (int j = 0; j < kSortBatch; ++j) kb[j] = i + 32 * j < hi ? pair_at(i + 32 * j) : 0u;
             #pragma unroll
             for (int j = 0; j < kSortBatch; ++j)
                 if (i + 32 * j < hi) {
-                    atomicAdd(mine + ((k[j] >> shift) & mask), 1u);
-                    if (pass == 0 && a.present != nullptr && k[j] < a.vocab) a.present[k[j]] = 1;
+                    const uint32_t k = (uint32_t)(kb[j] >> 32);
+                    atomicAdd(mine + ((k >> shift) & mask), 1u);
+                    if (pass == 0 && a.present != nullptr && k < a.vocab) a.present[k] = 1;
                 }
         }
         __syncthreads();
@@ -253,9 +256,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const SortArgs a)
         }
         __syncthreads();
         for (uint32_t i0 = lo + lane; i0 - lane < hi; i0 += 32 * kSortBatch) {
-            uint64_t kb[kSortBatch];
-            #pragma unroll
-            for (int j = 0; j < kSortBatch; ++j) kb[j] = i0 + 32 * j < hi ? pair_at(i0 + 32 * j) : 0u;
+            if (!once) {
+                #pragma unroll
+                for (int j = 0; j < kSortBatch; ++j) kb[j] = i0 + 32 * j < hi ? pair_at(i0 + 32 * j) : 0u;
+            }
             #pragma unroll
             for (int j = 0; j < kSortBatch; ++j) {
                 if (i0 - lane + 32 * j >= hi) break;
@@ -296,46 +300,82 @@ struct SumArgs {
     uint32_t zero_unit, zero_blocks;   // table rows per CTA that writes zeros, and the number of those CTAs
 };
 
-// Zeros to the rows [first, last) without a token, a warp per row; 8 x 32 rows' marks at a time.
+// Zeros to the rows [first, last) without a token.  Rows of 512 bytes and more: a warp per row.  Shorter rows that follow one
+// another without gaps are taken as one stretch of memory, 16 bytes per thread and step whatever the rows' length (91 bf16
+// columns: 100 -> 26 us a call); a piece that also holds part of a row with a token is written in two-byte steps.
+constexpr uint32_t kFlatRowBytes = 512;
 __device__ __forceinline__ void zero_rows(const SumArgs &a, uint64_t first, uint64_t last) {
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // row r of a group of 256 is warp (r mod 8)'s, so that all warps of the CTA have rows of each group
-    for (uint64_t r0 = first; r0 < last; r0 += 256) {
-        uint8_t mark = 1;
-        const uint64_t mine = r0 + 8 * lane + warp;
-        if (mine < last) mark = a.present[mine];
-        uint32_t todo = __ballot_sync(0xffffffffu, mark == 0);
-        while (todo != 0) {
-            const uint32_t k = __ffs(todo) - 1;
-            todo &= todo - 1;
-            char *row = static_cast<char *>(a.out) + (r0 + 8 * k + warp) * a.ld_out_bytes, *end = row + a.dim_bytes;
-            char *body = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(row) + 15) & ~(uintptr_t)15);
-            if (body > end) body = end;
-            const uint64_t vec = (uint64_t)(end - body) / 16;
-            for (char *q = row + 2 * lane; q < body; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;      // at most 14 bytes
-            for (uint64_t v = lane; v < vec; v += 32) __stcs(reinterpret_cast<uint4 *>(body) + v, make_uint4(0, 0, 0, 0));
-            for (char *q = body + vec * 16 + 2 * lane; q < end; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;
+    char *out = static_cast<char *>(a.out) + first * a.ld_out_bytes;
+    const uint8_t *present = a.present + first;
+    const uint32_t rows = (uint32_t)(last - first);
+    if (a.ld_out_bytes != a.dim_bytes || a.dim_bytes >= kFlatRowBytes) {
+        const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        // row r of a group of 256 is warp (r mod 8)'s, so that all warps of the CTA have rows of each group
+        for (uint32_t r0 = 0; r0 < rows; r0 += 256) {
+            uint8_t mark = 1;
+            const uint32_t mine = r0 + 8 * lane + warp;
+            if (mine < rows) mark = present[mine];
+            uint32_t todo = __ballot_sync(0xffffffffu, mark == 0);
+            while (todo != 0) {
+                const uint32_t k = __ffs(todo) - 1;
+                todo &= todo - 1;
+                char *row = out + (uint64_t)(r0 + 8 * k + warp) * a.ld_out_bytes, *end = row + a.dim_bytes;
+                char *body = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(row) + 15) & ~(uintptr_t)15);
+                if (body > end) body = end;
+                const uint64_t vec = (uint64_t)(end - body) / 16;
+                for (char *q = row + 2 * lane; q < body; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;      // at most 14 bytes
+                for (uint64_t v = lane; v < vec; v += 32) __stcs(reinterpret_cast<uint4 *>(body) + v, make_uint4(0, 0, 0, 0));
+                for (char *q = body + vec * 16 + 2 * lane; q < end; q += 64) *reinterpret_cast<uint16_t *>(q) = 0;
+            }
         }
+        return;
+    }
+    // byte o of the stretch lies in row floor(o / d) = umulhi(o, ceil(2^32 / d)): exact while o d < 2^32, and o is below 2^21 here
+    const uint32_t d = (uint32_t)a.dim_bytes, bytes = rows * d, magic = 0xffffffffu / d + 1;
+    const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15);        // pieces start at 16-byte boundaries
+    for (uint32_t v = threadIdx.x; v * 16 < bytes + lead; v += 256) {
+        const uint32_t lo = v == 0 ? 0 : v * 16 - lead, hi = min(v * 16 + 16 - lead, bytes);
+        const uint32_t r0 = __umulhi(lo, magic), r1 = __umulhi(hi - 1, magic);
+        bool all = hi - lo == 16;
+        for (uint32_t r = r0; r <= r1; ++r) all = all && !present[r];
+        if (all) { __stcs(reinterpret_cast<uint4 *>(out + lo), make_uint4(0, 0, 0, 0)); continue; }
+        for (uint32_t q = lo; q < hi; q += 2)
+            if (!present[__umulhi(q, magic)]) *reinterpret_cast<uint16_t *>(out + q) = 0;
     }
 }
 
+// The columns of a lane: 256 per warp, in 8 / VE vectors 32 VE apart, so that a row whose length or address allows
+// no wide access still has 8 columns per lane to share the work per token.
+template <int VE> struct Columns {
+    static constexpr int kReps = 8 / VE;
+    uint32_t c, dim;
+    __device__ __forceinline__ Columns(uint32_t slab, uint32_t dim_) : c(slab * 256 + (threadIdx.x & 31) * VE), dim(dim_) {}
+    __device__ __forceinline__ uint32_t at(int rep) const { return c + rep * 32 * VE; }
+    __device__ __forceinline__ bool on(int rep) const { return at(rep) < dim; }
+};
+
 template <int ODT, int VE>
-__device__ __forceinline__ void write_row(const SumArgs &a, uint32_t row, uint32_t c, float *sum) {
-    const uint64_t at = (uint64_t)row * a.ld_out + c;
+__device__ __forceinline__ void write_row(const SumArgs &a, uint32_t row, const Columns<VE> &col, float *sum) {
     #pragma unroll
-    for (int j = 0; j < VE; ++j) sum[j] *= a.scale;
-    if (a.accumulate) {
-        float old[VE];
-        load_vec_rw<ODT, VE>(a.out, at, old);
+    for (int r = 0; r < Columns<VE>::kReps; ++r) {
+        if (!col.on(r)) continue;
+        const uint64_t at = (uint64_t)row * a.ld_out + col.at(r);
+        float *x = sum + r * VE;
         #pragma unroll
-        for (int j = 0; j < VE; ++j) sum[j] += old[j];
+        for (int j = 0; j < VE; ++j) x[j] *= a.scale;
+        if (a.accumulate) {
+            float old[VE];
+            load_vec_rw<ODT, VE>(a.out, at, old);
+            #pragma unroll
+            for (int j = 0; j < VE; ++j) x[j] += old[j];
+        }
+        store_vec<ODT, VE>(a.out, at, x);
     }
-    store_vec<ODT, VE>(a.out, at, sum);
 }
 
 template <int DDT, int ODT, int VE>
 __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
-    constexpr int kFlight = VE == 8 ? 8 : 16;
+    constexpr int kFlight = 8, kReps = Columns<VE>::kReps;
     dep_launch();
     dep_wait();
     // the CTAs that write zeros are spread evenly over the grid
@@ -346,24 +386,27 @@ __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
         return;
     }
     const uint64_t item = (blockIdx.x - zb) * 8 + (threadIdx.x >> 5);
-    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
+    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31;
+    const Columns<VE> col((uint32_t)(item % a.slabs), a.dim);
     if (w >= a.windows) return;
     const uint32_t lo = w << a.window_log2, hi = min(a.tokens, (w + 1) << a.window_log2);
-    const bool on = c < a.dim;
     const uint32_t before = lo > 0 ? id_at(a.pair, lo - 1) : 0xffffffffu, after = hi < a.tokens ? id_at(a.pair, hi) : 0xffffffffu;
-    float sum[VE];
+    float sum[8];
     uint32_t run = 0xffffffffu, first = id_at(a.pair, lo);
     auto flush = [&](uint32_t next) {                      // the run ends, or (next == run) goes on in the next window
-        if (!on) return;
         const bool from_before = run == first && before == run;
-        if (!from_before && next != run) { write_row<ODT, VE>(a, run, c, sum); return; }
-        float *q = a.part + (uint64_t)(2 * w + (from_before ? 0 : 1)) * a.pitch + c;
-        if constexpr (VE == 8) {
-            reinterpret_cast<float4 *>(q)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-            reinterpret_cast<float4 *>(q)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
-        } else {
-            #pragma unroll
-            for (int j = 0; j < VE; ++j) q[j] = sum[j];
+        if (!from_before && next != run) { write_row<ODT, VE>(a, run, col, sum); return; }
+        float *q = a.part + (uint64_t)(2 * w + (from_before ? 0 : 1)) * a.pitch;
+        #pragma unroll
+        for (int r = 0; r < kReps; ++r) {
+            if (!col.on(r)) continue;
+            if constexpr (VE == 8) {
+                reinterpret_cast<float4 *>(q + col.at(r))[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                reinterpret_cast<float4 *>(q + col.at(r))[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+            } else {
+                #pragma unroll
+                for (int j = 0; j < VE; ++j) q[col.at(r) + j] = sum[r * VE + j];
+            }
         }
     };
     for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
@@ -372,24 +415,27 @@ __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
         const uint32_t keys = (uint32_t)(mine >> 32), poss = (uint32_t)mine;
         for (uint32_t k0 = 0; k0 < m; k0 += kFlight) {
             if (__shfl_sync(0xffffffffu, keys, k0) >= a.vocab) { i0 = hi; break; }      // only left-out tokens follow
-            RawVec<DDT, VE> v[kFlight];
+            RawVec<DDT, VE> v[kFlight][kReps];
             #pragma unroll
             for (int k = 0; k < kFlight; ++k) {
                 const uint32_t p = __shfl_sync(0xffffffffu, poss, k0 + k), key = __shfl_sync(0xffffffffu, keys, k0 + k);
-                if (on && key < a.vocab) v[k].load(a.dout, (uint64_t)p * a.ld_dout + c);
+                #pragma unroll
+                for (int r = 0; r < kReps; ++r)
+                    if (key < a.vocab && col.on(r)) v[k][r].load(a.dout, (uint64_t)p * a.ld_dout + col.at(r));
             }
             #pragma unroll
             for (int k = 0; k < kFlight; ++k) {
                 const uint32_t key = __shfl_sync(0xffffffffu, keys, k0 + k);
                 if (key >= a.vocab) break;
-                if (key != run) {
+                const bool fresh = key != run;
+                if (fresh) {
                     if (run != 0xffffffffu) flush(key);
                     run = key;
+                }
+                #pragma unroll
+                for (int r = 0; r < kReps; ++r) {
                     #pragma unroll
-                    for (int j = 0; j < VE; ++j) sum[j] = v[k].at(j);
-                } else {
-                    #pragma unroll
-                    for (int j = 0; j < VE; ++j) sum[j] += v[k].at(j);
+                    for (int j = 0; j < VE; ++j) sum[r * VE + j] = fresh ? v[k][r].at(j) : sum[r * VE + j] + v[k][r].at(j);
                 }
             }
         }
@@ -400,10 +446,12 @@ __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
 // Runs that begin in window w and reach beyond it.
 template <int ODT, int VE>
 __global__ void __launch_bounds__(256) join_kernel(const SumArgs a) {
+    constexpr int kReps = Columns<VE>::kReps;
     dep_launch();
     dep_wait();
     const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31, c = ((uint32_t)(item % a.slabs) * 32 + lane) * VE;
+    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31;
+    const Columns<VE> col((uint32_t)(item % a.slabs), a.dim);
     if (w + 1 >= a.windows) return;
     const uint32_t lo = w << a.window_log2, hi = (w + 1) << a.window_log2, run = id_at(a.pair, hi - 1);
     if (run >= a.vocab || id_at(a.pair, hi) != run || (lo > 0 && id_at(a.pair, lo) == run && id_at(a.pair, lo - 1) == run)) return;
@@ -415,29 +463,39 @@ __global__ void __launch_bounds__(256) join_kernel(const SumArgs a) {
         if (not_mine != 0) { end += __ffs(not_mine) - 1; break; }
         end += 32;
     }
-    if (c >= a.dim) return;
-    float sum[VE];
-    load_vec_rw<LGN_F32, VE>(a.part, (uint64_t)(2 * w + 1) * a.pitch + c, sum);
-    for (uint32_t q0 = w + 1; q0 < end; q0 += 8) {
-        float v[8][VE];
+    float sum[8];
+    auto piece = [&](uint64_t row, float *x) {
         #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (q0 + k < end) load_vec_rw<LGN_F32, VE>(a.part, (uint64_t)(2 * (q0 + k)) * a.pitch + c, v[k]);
+        for (int r = 0; r < kReps; ++r)
+            if (col.on(r)) load_vec_rw<LGN_F32, VE>(a.part, row * a.pitch + col.at(r), x + r * VE);
+    };
+    #pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    piece(2 * (uint64_t)w + 1, sum);
+    for (uint32_t q0 = w + 1; q0 < end; q0 += 8) {
+        float v[8][8];
+        #pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            #pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = 0.0f;
+            if (q0 + k < end) piece(2 * (uint64_t)(q0 + k), v[k]);
+        }
         #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (q0 + k < end) {
                 #pragma unroll
-                for (int j = 0; j < VE; ++j) sum[j] += v[k][j];
+                for (int j = 0; j < 8; ++j) sum[j] += v[k][j];
             }
     }
-    write_row<ODT, VE>(a, run, c, sum);
+    write_row<ODT, VE>(a, run, col, sum);
 }
 
 // Tokens per window: about a quarter of the square root of their number.  The square root itself would make the
 // worst run (all tokens one id) shortest; real runs are far shorter, and short windows spread them over more warps.
-static uint32_t window_log2_for(uint64_t tokens) {
+// Narrow tables take windows of 32 where longer ones would leave fewer than 16 warps per SM.
+static uint32_t window_log2_for(uint64_t tokens, uint64_t slabs) {
     uint32_t l = 5;
-    while (l < 20 && (1ull << (2 * l + 4)) < tokens) ++l;
+    while (l < 20 && (1ull << (2 * l + 4)) < tokens && (tokens * slabs >> (l + 1)) >= 2368) ++l;
     return l;
 }
 
@@ -449,7 +507,7 @@ static bool grad_layout(uint64_t tokens, uint64_t vocab, uint64_t dim, GradLayou
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     l.present = take(vocab);
     for (int i = 0; i < 2; ++i) l.pair[i] = take(tokens * 8);
-    l.window_log2 = window_log2_for(tokens);
+    l.window_log2 = window_log2_for(tokens, (dim + 255) / 256);
     l.windows = (uint32_t)((tokens + (1ull << l.window_log2) - 1) >> l.window_log2);
     l.pitch = (uint32_t)((dim + 7) & ~7ull);
     l.part = take(l.windows > 1 ? (size_t)2 * l.windows * l.pitch * 4 : 0);
@@ -581,8 +639,9 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     if (s.bits < 5) s.bits = 5;                                        // whole warps of digits
     const size_t smem = (size_t)32 * sizeof(uint32_t) << s.bits;
     const void *sort = reinterpret_cast<const void *>(&sort_kernel);
-    const int ctas = sort_ctas();
-    if (ctas == 0) return LGN_ERR_CUDA;
+    const int most = sort_ctas();
+    if (most == 0) return LGN_ERR_CUDA;
+    const int ctas = tokens <= kSortAlone ? 1 : most;
     if (accumulate) {
         s.present = nullptr;
         if (tokens == 0) return LGN_OK;
@@ -601,17 +660,19 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     a.tokens = s.tokens;
     a.window_log2 = l.window_log2; a.windows = l.windows;
     a.dim = (uint32_t)dim; a.pitch = l.pitch;
-    a.slabs = (uint32_t)((dim + 32 * kVe[vi] - 1) / (32 * kVe[vi]));
+    a.slabs = (uint32_t)((dim + 255) / 256);
     a.accumulate = accumulate != 0;
     a.scale = (float)scale;
     void *args[] = {&a};
     const uint64_t blocks = ((uint64_t)l.windows * a.slabs + 7) / 8;
-    if (!accumulate) {                                                 // 256 KiB a CTA, at least 8 rows (a warp's each), at most 2^20 CTAs
-        uint64_t unit = (256u << 10) / (dim * et);
+    if (!accumulate) {
+        // 8 to 256 KiB of the table a CTA, enough CTAs for every SM to have a few of them, at most 2^20 CTAs; at least 8 rows (a warp's each)
+        const uint64_t row = dim * et, all = vocab * row / 1024;
+        uint64_t unit = (all < (8u << 10) ? (8u << 10) : all > (256u << 10) ? (256u << 10) : all) / row;
         if (unit < 8) unit = 8;
         if (unit < (vocab >> 20) + 1) unit = (vocab >> 20) + 1;
         a.present = s.present;
-        a.ld_out_bytes = ld_table * et; a.dim_bytes = dim * et;
+        a.ld_out_bytes = ld_table * et; a.dim_bytes = row;
         a.zero_unit = (uint32_t)unit;
         a.zero_blocks = (uint32_t)((vocab + unit - 1) / unit);
     }
