@@ -1,0 +1,111 @@
+"""The library's training operators as torch modules: a linear layer whose three products run in 8-bit
+floating point (optionally with its neural gradient pruned first), an embedding whose gradient is summed
+in a fixed order, and gradient clipping that stays on the device.
+
+The modules marshal arguments for ``binding``; there is no CPU path.
+"""
+from __future__ import annotations
+
+from typing import List, Optional, Sequence
+
+import torch
+
+from . import binding as lgn
+
+
+def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
+    """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics."""
+    g = dy.contiguous()
+    out = torch.empty_like(g)
+    results, ws = lgn.new_results(1, g.device), lgn.new_workspace([g.numel()], g.device)
+    lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=sparsity, seed=seed)], results, ws)
+    return out
+
+
+class _LinearFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, sparsity, seed):
+        wq, wqt = lgn.lgn_fp8_quantize(weight, lgn.E4M3, lgn.BLOCK_SQUARE, transposed=True)
+        xq, xqt = lgn.lgn_fp8_quantize(x, lgn.E4M3, transposed=True)
+        ctx.wqt, ctx.xqt, ctx.sparsity, ctx.seed, ctx.dtypes = wqt, xqt, sparsity, seed, (x.dtype, weight.dtype)
+        return lgn.lgn_fp8_matmul(xq, wq, out_dtype=x.dtype)
+
+    @staticmethod
+    def backward(ctx, dy):
+        if ctx.sparsity > 0.0:
+            dy = _pruned(dy, ctx.sparsity, ctx.seed)
+        elif dy.stride(-1) != 1 or (dy.size(0) > 1 and dy.stride(0) < dy.size(1)):
+            dy = dy.contiguous()                                       # a broadcast gradient
+        dq, dqt = lgn.lgn_fp8_quantize(dy, lgn.E5M2, transposed=True)
+        dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0])
+        dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1])
+        return dx, dw, None, None
+
+
+class Fp8Linear(torch.nn.Module):
+    """y = x W^T with x, W and the incoming gradient in 8-bit floating point (E4M3, E4M3, E5M2; one power-of-two
+    scale per block of 128), fp32 sums.  ``sparsity`` > 0 prunes the incoming gradient to that fraction of zeros
+    before the two backward products; ``seed`` changes from step to step (advance())."""
+
+    def __init__(self, in_features: int, out_features: int, sparsity: float = 0.0, device=None):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device))
+        torch.nn.init.normal_(self.weight, std=in_features ** -0.5)
+        self.sparsity, self.seed = float(sparsity), 0
+
+    def advance(self) -> None:
+        self.seed += 1
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        y = _LinearFn.apply(x.reshape(-1, x.shape[-1]), self.weight, self.sparsity, self.seed)
+        return y.reshape(*x.shape[:-1], self.weight.shape[0])
+
+
+class _EmbeddingFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, ids, scale, padding_idx, out_dtype):
+        ctx.save_for_backward(ids)
+        ctx.args = (weight.shape[0], scale, padding_idx, weight.dtype)
+        return lgn.lgn_embedding(weight, ids, scale, out_dtype=out_dtype)
+
+    @staticmethod
+    def backward(ctx, dout):
+        (ids,) = ctx.saved_tensors
+        vocab, scale, padding_idx, dtype = ctx.args
+        if dout.stride(-1) != 1 or (dout.size(0) > 1 and dout.stride(0) < dout.size(1)):
+            dout = dout.contiguous()
+        return lgn.lgn_embedding_grad(dout, ids, vocab, scale, padding_idx, out_dtype=dtype), None, None, None, None
+
+
+class Embedding(torch.nn.Module):
+    """scale * weight[ids]; ids outside the table give zeros.  The gradient leaves padding_idx out."""
+
+    def __init__(self, vocab: int, dim: int, scale: float = 1.0, padding_idx: int = -1,
+                 out_dtype: torch.dtype = torch.bfloat16, device=None):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(vocab, dim, device=device))
+        torch.nn.init.normal_(self.weight, std=1.0 / scale)
+        self.scale, self.padding_idx, self.out_dtype = float(scale), int(padding_idx), out_dtype
+
+    def forward(self, ids: torch.Tensor) -> torch.Tensor:
+        flat = ids.reshape(-1).contiguous()
+        out = _EmbeddingFn.apply(self.weight, flat, self.scale, self.padding_idx, self.out_dtype)
+        return out.reshape(*ids.shape, self.weight.shape[1])
+
+
+class GradClipper:
+    """Clips the gradients of a fixed list of parameters by their global norm, in place, without a host round
+    trip.  The gradients have to exist and to stay where they are (zero_grad(set_to_none=False))."""
+
+    def __init__(self, parameters: Sequence[torch.nn.Parameter], max_norm: float):
+        grads: List[torch.Tensor] = [p.grad for p in parameters if p.grad is not None]
+        if not grads:
+            raise ValueError("no parameter has a gradient yet")
+        self._list, self.max_norm = lgn.make_grads(grads), float(max_norm)
+        self.record = lgn.new_norm_record(grads[0].device)
+        self._ws = lgn.new_clip_workspace(grads[0].device, len(grads))
+
+    def clip(self, stream=None) -> torch.Tensor:
+        """Scales the gradients; returns their norm before it, a scalar on the device."""
+        lgn.lgn_clip_grad_norm(self._list, self.max_norm, self.record, self._ws, stream)
+        return lgn.norm_of(self.record)
