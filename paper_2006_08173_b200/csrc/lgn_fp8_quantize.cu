@@ -177,7 +177,9 @@ fp8_rows_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32
 // them and forms the scale.  Transposed codes leave through shared memory as units of 8 bytes (8 rows of one column);
 // unit u of column c sits at place u ^ (c / 8), which spreads the 16 lanes that write units of columns 8
 // apart over all banks.
-template <int DT, int FMT, bool SQUARE, bool VEC>
+// BLOCKS: blocks of 128 along the rows of both copies, of the transpose alone, or squares.
+enum TileBlocks { kTileBoth = 0, kTileTransposed = 1, kTileSquare = 2 };
+template <int DT, int FMT, int BLOCKS, bool VEC>
 __global__ void __launch_bounds__(256, DT == LGN_F32 ? 2 : 3)
 fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t col_tiles,
                 uint8_t *codes, uint32_t ldq, uint8_t *scales, uint32_t groups,
@@ -188,6 +190,7 @@ fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32
     __shared__ uint32_t rinv[128];
     __shared__ __align__(16) uint32_t cinv[128];
     __shared__ uint32_t wmax[8];
+    constexpr bool SQUARE = BLOCKS == kTileSquare, ROWS = BLOCKS == kTileBoth, COLS = BLOCKS != kTileSquare;
     dep_launch();
     dep_wait();
     constexpr int ES = DT == LGN_F32 ? 4 : 2;
@@ -203,16 +206,19 @@ fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32
     bool special = false;
     for (int round = 0; round < 2; ++round) {             // a second round, over finite values, only where some are not
         uint32_t mine = 0;
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t a = special ? v[i].max_abs_finite() : v[i].max_abs();
-            if constexpr (SQUARE) mine = max(mine, a);
-            else rmax[(rl + i) * 17 + cg] = a;
+        if constexpr (SQUARE || ROWS) {
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t a = special ? v[i].max_abs_finite() : v[i].max_abs();
+                if constexpr (SQUARE) mine = max(mine, a);
+                else rmax[(rl + i) * 17 + cg] = a;
+            }
         }
         if constexpr (SQUARE) {
             mine = __reduce_max_sync(0xffffffffu, mine);
             if ((threadIdx.x & 31) == 0) wmax[threadIdx.x >> 5] = mine;
-        } else if (codes_t != nullptr) {
+        }
+        if constexpr (COLS) {
             uint32_t m[8];
             if (special) {
                 #pragma unroll
@@ -250,11 +256,9 @@ fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32
             #pragma unroll
             for (int k = 0; k < 8; ++k) a = max(a, wmax[k]);
         } else if (is_col) {
-            if (codes_t != nullptr) {
-                #pragma unroll
-                for (int k = 0; k < 16; ++k) a = max(a, cmax[k * 128 + t]);
-            }
-        } else {
+            #pragma unroll
+            for (int k = 0; k < 16; ++k) a = max(a, cmax[k * 128 + t]);
+        } else if constexpr (ROWS) {
             #pragma unroll
             for (int k = 0; k < 16; ++k) a = max(a, rmax[t * 17 + k]);
         }
@@ -268,12 +272,12 @@ fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32
             if (codes_t != nullptr) scales_t[4 * fp8_scale_word(ct * 128 + t, rt >> 2, groups_t) + (rt & 3)] = (uint8_t)byte;
         } else {
             rinv[t] = inverse_scale(byte);
-            if (codes != nullptr) scales[4 * fp8_scale_word(rt * 128 + t, ct >> 2, groups) + (ct & 3)] = (uint8_t)byte;
+            if (BLOCKS != kTileTransposed && codes != nullptr) scales[4 * fp8_scale_word(rt * 128 + t, ct >> 2, groups) + (ct & 3)] = (uint8_t)byte;
         }
         break;
     }
     __syncthreads();
-    if (codes != nullptr && c0 < ldq) {                                               // ldq is a multiple of 16
+    if (!(BLOCKS == kTileTransposed) && codes != nullptr && c0 < ldq) {                                               // ldq is a multiple of 16
         #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t inv = rinv[rl + i];
@@ -324,8 +328,9 @@ static const void *const kRowsTable[2][2][2] = {
     {{LGN_ROWS(LGN_BF16, LGN_E4M3, false), LGN_ROWS(LGN_BF16, LGN_E4M3, true)}, {LGN_ROWS(LGN_BF16, LGN_E5M2, false), LGN_ROWS(LGN_BF16, LGN_E5M2, true)}}};
 #undef LGN_ROWS
 #define LGN_TILE(D, F, S, V) reinterpret_cast<const void *>(&fp8_tile_kernel<D, F, S, V>)
-#define LGN_TILE4(D, F) {{LGN_TILE(D, F, false, false), LGN_TILE(D, F, false, true)}, {LGN_TILE(D, F, true, false), LGN_TILE(D, F, true, true)}}
-static const void *const kTileTable[2][2][2][2] = {{LGN_TILE4(LGN_F32, LGN_E4M3), LGN_TILE4(LGN_F32, LGN_E5M2)},
+#define LGN_TILE4(D, F) {{LGN_TILE(D, F, kTileBoth, false), LGN_TILE(D, F, kTileBoth, true)}, {LGN_TILE(D, F, kTileTransposed, false), LGN_TILE(D, F, kTileTransposed, true)}, \
+                         {LGN_TILE(D, F, kTileSquare, false), LGN_TILE(D, F, kTileSquare, true)}}
+static const void *const kTileTable[2][2][3][2] = {{LGN_TILE4(LGN_F32, LGN_E4M3), LGN_TILE4(LGN_F32, LGN_E5M2)},
                                                    {LGN_TILE4(LGN_BF16, LGN_E4M3), LGN_TILE4(LGN_BF16, LGN_E5M2)}};
 #undef LGN_TILE4
 #undef LGN_TILE
@@ -378,5 +383,6 @@ extern "C" lgn_status lgn_fp8_quantize(const void *x, uint64_t rows, uint64_t co
     if (tiles > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     log_line("fp8_quantize: rows %u cols %u, %s blocks, %llu tiles", r, c, block == LGN_BLOCK_SQUARE ? "square" : "row", (unsigned long long)tiles);
     void *args[] = {&x, &ld, &r, &c, &col_tiles, &codes, &ldq, &scales, &groups, &codes_t, &ldq_t, &scales_t, &groups_t};
-    return launch_dependent(kTileTable[dt][fmt][block == LGN_BLOCK_SQUARE][vec], dim3((unsigned)tiles), dim3(256), args, 0, stream);
+    const int blocks = block == LGN_BLOCK_SQUARE ? kTileSquare : codes == nullptr ? kTileTransposed : kTileBoth;
+    return launch_dependent(kTileTable[dt][fmt][blocks][vec], dim3((unsigned)tiles), dim3(256), args, 0, stream);
 }
