@@ -199,6 +199,17 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """Uninitialised memory that belongs to the stream the call runs on: torch hands a freed block out again as soon
+    as the stream it was allocated on allows, whatever other streams still do with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        raise ValueError("outputs and workspaces have to be given when the stream is a raw handle")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 # --------------------------------------------------------------------------- sizes
 def lgn_workspace_bytes(n_per_layer: Sequence[int]) -> int:
     arr = (_u64 * max(1, len(n_per_layer)))(*n_per_layer)
@@ -508,12 +519,12 @@ class Fp8Operand:
         self._codes_ptr, self._scales_ptr = codes.data_ptr(), scales.data_ptr()
 
     @classmethod
-    def empty(cls, rows: int, k: int, fmt: int, device) -> "Fp8Operand":
-        """Uninitialised, codes and scales in one allocation."""
+    def empty(cls, rows: int, k: int, fmt: int, device, stream=None) -> "Fp8Operand":
+        """Uninitialised, codes and scales in one allocation; for use on ``stream`` (default: the current one)."""
         o = cls.__new__(cls)
         codes, scales = _fp8_bytes(rows, k)
         o.rows, o.k, o.fmt, o._codes, o._scales = rows, k, fmt, None, None
-        o._buffer = torch.empty(codes + scales + 16, dtype=_uint8, device=device)
+        o._buffer = _empty(codes + scales + 16, _uint8, device, stream)
         o._codes_ptr = o._buffer.data_ptr()
         o._scales_ptr = o._codes_ptr + codes
         return o
@@ -576,7 +587,7 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
     q = t = pq = sq = pt = st = None
     if rowwise:
         if out is None:
-            q = new_fp8_operand(rows, cols, fmt, x.device)
+            q = Fp8Operand.empty(rows, cols, fmt, x.device, stream)
         else:
             q = out
             if (q.rows, q.k, q.fmt) != (rows, cols, fmt):
@@ -584,7 +595,7 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
         pq, sq = q._codes_ptr, q._scales_ptr
     if transposed:
         if out_t is None:
-            t = new_fp8_operand(cols, rows, fmt, x.device)
+            t = Fp8Operand.empty(cols, rows, fmt, x.device, stream)
         else:
             t = out_t
             if (t.rows, t.k, t.fmt) != (cols, rows, fmt):
@@ -605,7 +616,7 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((m, n), dtype=out_dtype, device=a.device)
+        out = _empty((m, n), out_dtype, a.device, stream)
         ldo = n or 1
     else:
         if tuple(out.shape) != (m, n):
@@ -630,17 +641,20 @@ def lgn_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ou
     """scale * table[ids], zeros for ids outside the table: ids.numel() x dim.  ``n_outside``: int64 CUDA tensor of
     one element to which the number of ids outside the table is added."""
     ld = _matrix(table, "table")
-    n, dim = ids.numel(), table.size(1)
+    vocab, dim = table.shape
+    n = ids.numel()
     if out is None:
-        out = torch.empty(n, dim, dtype=out_dtype or table.dtype, device=table.device)
-    elif tuple(out.shape) != (n, dim):
-        raise ValueError("out must be ids.numel() x dim")
+        out = _empty((n, dim), out_dtype or table.dtype, table.device, stream)
+        ldo = dim or 1
+    else:
+        if tuple(out.shape) != (n, dim):
+            raise ValueError("out must be ids.numel() x dim")
+        ldo = _matrix(out, "out")
     if n_outside is not None and n_outside.dtype != torch.int64:
         raise TypeError("n_outside is int64")
-    _check(_lib.lgn_embedding(table.data_ptr() or None, table.size(0), dim, ld, dtype_code(table),
-                              _dev(ids, "ids") or None, _ids(ids), n, float(scale), out.data_ptr() or None, _matrix(out, "out"),
-                              dtype_code(out), _dev(n_outside, "n_outside") if n_outside is not None else None, _stream(stream)),
-           "lgn_embedding")
+    _check(_lib.lgn_embedding(table.data_ptr() or None, vocab, dim, ld, dtype_code(table), _dev(ids, "ids") or None, _ids(ids), n,
+                              float(scale), out.data_ptr() or None, ldo, dtype_code(out),
+                              _dev(n_outside, "n_outside") if n_outside is not None else None, _stream(stream)), "lgn_embedding")
     return out
 
 
@@ -659,11 +673,11 @@ def lgn_embedding_grad(dout: torch.Tensor, ids: torch.Tensor, vocab: int, scale:
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty(vocab, dim, dtype=out_dtype, device=dout.device)
+        out = _empty((vocab, dim), out_dtype, dout.device, stream)
     elif tuple(out.shape) != (vocab, dim):
         raise ValueError("out must be vocab x dim")
     if ws is None:
-        ws = new_embedding_grad_workspace(n, vocab, dim, dout.device)
+        ws = _empty(max(16, int(_lib.lgn_embedding_grad_workspace_bytes(n, vocab, dim))), _uint8, dout.device, stream)
     _check(_lib.lgn_embedding_grad(dout.data_ptr() or None, ld, dtype_code(dout), _dev(ids, "ids") or None, _ids(ids), n, vocab, dim,
                                    float(scale), int(padding_idx), out.data_ptr() or None, _matrix(out, "out"), dtype_code(out),
                                    1 if accumulate else 0, _dev(ws, "ws"), ws.numel() * ws.element_size(), _stream(stream)),

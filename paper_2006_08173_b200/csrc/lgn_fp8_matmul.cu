@@ -746,7 +746,8 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     p.split_groups = plan.split_groups;
     p.accumulate = accumulate != 0;
     const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c, slots = (uint64_t)(sms / q.ctas);
-    if (tiles > 0x3fffffffull) return LGN_ERR_UNSUPPORTED;
+    if (tiles > 0x3fffffffull || (uint64_t)((p.rows + 127) / 128) * p.groups > 0x7fffffffull || (uint64_t)((p.cols + 127) / 128) * p.groups > 0x7fffffffull)
+        return LGN_ERR_UNSUPPORTED;                                             // TMA coordinates are 32-bit
     CUtensorMap mr, mc, sr, sc, mo = {};
     if (q.form == kFormRows && !make_out_map(&mo, out, m, n, ldo, out_dt)) return LGN_ERR_CUDA;
     if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, bn / (uint32_t)q.ctas)) return LGN_ERR_CUDA;

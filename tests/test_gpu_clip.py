@@ -170,6 +170,17 @@ def test_same_bits_and_other_streams(lgn):
         assert r == seen[0][0] and all(torch.equal(x, y) for x, y in zip(o, seen[0][1]))
 
 
+def test_tensor_beyond_32_bits(lgn):
+    n = 2 ** 32 + 37
+    t = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    t[0], t[2 ** 31], t[n - 1] = 3.0, 4.0, 12.0
+    rec, ws = lgn.new_norm_record("cuda"), lgn.new_clip_workspace("cuda")
+    lgn.lgn_clip_grad_norm(lgn.make_grads([t]), 6.5, rec, ws)
+    r = lgn.read_norm_record(rec)
+    assert r["sum_sq"] == 169.0 and r["norm"] == 13.0 and r["coef"] == 0.5
+    assert [float(t[i]) for i in (0, 2 ** 31, n - 1)] == [1.5, 2.0, 6.0]
+
+
 def test_refusals(lgn):
     t = torch.zeros(100, device="cuda")
     rec, ws = lgn.new_norm_record("cuda"), lgn.new_clip_workspace("cuda", 3)

@@ -181,6 +181,37 @@ def test_other_streams(lgn):
     check_grad(got, out, ids, 100, 1.0, -1)
 
 
+def test_offsets_beyond_32_bits(lgn):
+    """A table and its gradient of more than 2^32 elements."""
+    vocab, dim = 2 ** 21 + 3, 2056
+    table = torch.zeros(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, vocab - 1, 2 ** 21, 5, vocab - 1, 2 ** 20], device="cuda")
+    table[rows] = torch.randn(6, dim, device="cuda").bfloat16()
+    ids = torch.cat([rows, torch.tensor([vocab, -1], device="cuda")])
+    out = lgn.lgn_embedding(table, ids)
+    assert torch.equal(out[:6], table[rows]) and bool((out[6:] == 0).all())
+    dout = torch.randn(8, dim, device="cuda")
+    table.fill_(7.0)
+    lgn.lgn_embedding_grad(dout, ids, vocab, out=table)
+    check_grad(table[rows.unique()], dout[:6], torch.unique(rows, return_inverse=True)[1], rows.unique().numel(), 1.0, -1)
+    assert int((table != 0).any(dim=1).sum()) == rows.unique().numel()
+
+
+def test_raw_stream_handles_need_given_memory(lgn):
+    table = torch.randn(10, 16, device="cuda")
+    ids = torch.tensor([3, 4], device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with pytest.raises(ValueError):
+        lgn.lgn_embedding(table, ids, stream=s.cuda_stream)
+    out = torch.empty(2, 16, device="cuda")
+    lgn.lgn_embedding(table, ids, out=out, stream=s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(out, table[ids])
+    with pytest.raises(ValueError):
+        lgn.lgn_embedding_grad(out, ids, 10, out=torch.empty(10, 16, device="cuda"), stream=s.cuda_stream)
+
+
 def test_refusals(lgn):
     table = torch.zeros(10, 16, device="cuda")
     ids = torch.zeros(4, dtype=torch.int64, device="cuda")

@@ -218,6 +218,44 @@ def test_other_streams(lgn):
     check_product(out, av, av, 512)
 
 
+def test_raw_stream_handles_need_given_outputs(lgn):
+    x = torch.ones(4, 256, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with pytest.raises(ValueError):
+        lgn.lgn_fp8_quantize(x, stream=s.cuda_stream)
+    q = lgn.new_fp8_operand(4, 256, 0, "cuda")
+    lgn.lgn_fp8_quantize(x, out=q, stream=s.cuda_stream)
+    with pytest.raises(ValueError):
+        lgn.lgn_fp8_matmul(q, q, stream=s.cuda_stream)
+    out = torch.empty(4, 4, device="cuda")
+    lgn.lgn_fp8_matmul(q, q, out=out, stream=s.cuda_stream)
+    s.synchronize()
+    assert bool((out == 256.0).all())
+
+
+def test_offsets_beyond_32_bits(lgn):
+    """An output of more than 2^32 elements, and an input of which the last rows start beyond 2^32 elements."""
+    m, n, k = 66000, 65536, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    a, _ = lgn.lgn_fp8_quantize(torch.randn(m, k, generator=g, device="cuda").bfloat16())
+    b, _ = lgn.lgn_fp8_quantize(torch.randn(n, k, generator=g, device="cuda").bfloat16())
+    out = lgn.lgn_fp8_matmul(a, b)
+    rows = [0, 1, 65535, 65536, 65537, m - 1]
+    av, bv = operand_values(a)[0][rows], operand_values(b)[0]
+    check_product(out[rows], av, bv, k)
+    del out
+    x = torch.zeros(2 ** 22 + 8, 1040, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = torch.randn(5, 1040, generator=g, device="cuda").bfloat16()
+    q, t = lgn.lgn_fp8_quantize(x, 0, transposed=True)
+    want, e = quantise(to_np(x[-5:]), 0)
+    codes = q.codes[-5 * 1040:].cpu().reshape(5, 1040).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
+    assert np.array_equal(codes * 2.0 ** np.repeat(e, 128, axis=1)[:, :1040].astype(np.float64), want)
+    tail = t.codes.reshape(1040, 2 ** 22 + 16)[:, 2 ** 22 - 120:2 ** 22 + 8].cpu().view(torch.float8_e4m3fn).float().numpy()
+    tv, te = quantise(to_np(x[-8:]).T, 0)                       # the block of the last 8 rows
+    assert np.array_equal(tail[:, -8:] * 2.0 ** te.astype(np.float64), tv)
+
+
 def test_refusals(lgn):
     x = torch.ones(4, 256, device="cuda")
     q, _ = lgn.lgn_fp8_quantize(x)
