@@ -10,7 +10,7 @@
 // the other ("cols").  In a pair the CTA of rank 0 issues the MMAs of both (cta_group::2) and each CTA brings
 // its own 128 rows and one half of the BN: at 256 x 256 a step of k (128) costs an SM 32 KiB of shared-memory writes
 // and as many operand reads for 512 clocks of MMA, where a lone CTA's 128 x 192 needs 1.7 times that per flop
-// (8192 x 8192 x 4096: 216 us against 258).  Small products take lone CTAs, persistent over tiles, or (SPLIT) one tile
+// (8192 x 8192 x 4096: 258 -> 216 us when pairs came in).  Small products take lone CTAs, persistent over tiles, or (SPLIT) one tile
 // per cluster with the CTAs of a cluster taking consecutive shares of k and adding their fp32 tiles through
 // distributed shared memory in rank order.
 //   warp 8  brings codes into a ring of shared-memory stages (TMA, 128-byte swizzle) and, every fourth step, the 512-byte
@@ -24,8 +24,8 @@
 //
 // fp32 outputs: the tensor cores' additions truncate, which biases a sum towards zero by about 2e-10 of its
 // size per k (measured: 2.0e-7 at k = 1024, 1e-6 and more from 8192).  Every 1024 k the tile is therefore added to sums in
-// registers (round to nearest) and a fresh one begun in the other half of tensor memory; the error then stays at
-// 3e-7 whatever k.  For bf16 outputs, rounded at 2e-3, the sum stays in tensor memory.
+// registers (round to nearest) and a fresh one begun in the other half of tensor memory; the error then stays below
+// 5e-7 (k up to 16384).  For bf16 outputs, rounded at 2e-3, the sum stays in tensor memory.
 //
 // Every wait is bounded: one that runs out raises a flag on which all roles stop; the copies and MMAs in
 // flight are waited for (bounded too), tensor memory is freed and the kernel ends with *status set.
@@ -200,7 +200,17 @@ __device__ __forceinline__ void tmem_load16(uint32_t taddr, float *v) {
                    "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for the loads issued so far.  The 16 values pass through, so that no use of them can be moved ahead of the wait; further
+// values of the same wait pass through tmem_loaded16.
+__device__ __forceinline__ void tmem_load_wait16(float *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]),
+                   "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
+}
+__device__ __forceinline__ void tmem_loaded16(float *v) {
+    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]),
+                      "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
+}
 
 template <int ODT>
 __device__ __forceinline__ float load_out(const void *out, uint64_t i) {
@@ -226,8 +236,7 @@ __device__ __forceinline__ void ld128(const void *p, uint32_t *w) {
 
 // A warp's 32 rows x 128 bytes of the output from row y, column x on; lane l holds row l in v.  They go through
 // the warp's staging buffer (128-byte swizzle, so that the lanes' writes spread over all banks) and one TMA store,
-// which leaves out what lies outside the matrix: stores of 32 bytes per lane to 32 different rows took 13 us per tile of
-// 256 x 192 fp32, four times as long as the tile's MMAs at k = 1024.
+// which leaves out what lies outside the matrix and runs on while the warp reads its next columns.
 // The warp's BUFS buffers from bufs on are used in turn.
 template <int ODT, int BUFS>
 __device__ __forceinline__ void store_staged(const MmArgs &p, const CUtensorMap *map, uint32_t bufs, uint32_t &turn, uint32_t y, uint32_t x, uint32_t lane, float *v) {
@@ -244,9 +253,6 @@ __device__ __forceinline__ void store_staged(const MmArgs &p, const CUtensorMap 
                     if constexpr (ODT == LGN_F32) v[4 * q + j] += __uint_as_float(w[j]);
                     else { v[8 * q + 2 * j] += __uint_as_float(w[j] << 16); v[8 * q + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
                 }
-            } else {
-                #pragma unroll
-                for (int j = 0; j < kPer; ++j) if (x + q * kPer + j < p.cols) v[q * kPer + j] += load_out<ODT>(p.out, i + q * kPer + j);
             }
         }
     }
@@ -316,7 +322,7 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
             for (int c = 0; c < kCols; c += 16) {
                 float v[16];
                 tmem_load16(tmem_at + acc * BN + c, v);
-                tmem_load_wait();
+                tmem_load_wait16(v);
                 #pragma unroll
                 for (int j = 0; j < 16; ++j) sum[c + j] = ch == 0 ? v[j] : sum[c + j] + v[j];
             }
@@ -335,7 +341,9 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, ui
             float v[RUN];
             #pragma unroll
             for (int j = 0; j < RUN; j += 16) tmem_load16(tmem_at + acc * BN + c + j, v + j);
-            tmem_load_wait();
+            tmem_load_wait16(v);
+            #pragma unroll
+            for (int j = 16; j < RUN; j += 16) tmem_loaded16(v + j);
             if (c + RUN >= kCols) { fence_before(); release(acc); }
             put(c, v);
         }
