@@ -439,7 +439,7 @@ lgn_status lgn_embedding(const void *table, uint64_t vocab, uint64_t dim, uint64
  * those rows are not touched.  Sums in fp32, rounded once to table_dt, in an order that depends on
  * the ids alone: the same inputs give the same bits.
  *   ws  device scratch of lgn_embedding_grad_workspace_bytes(tokens, vocab, dim), 16-byte aligned
- * Two launches, three for more than 32 tokens, and (without accumulate) a memset of vocab bytes; no allocation. */
+ * A memset (of 256 bytes, without accumulate also vocab bytes), two launches, three for more than 8 tokens; no allocation. */
 size_t lgn_embedding_grad_workspace_bytes(uint64_t tokens, uint64_t vocab, uint64_t dim);
 lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn_dtype dout_dt,
                               const void *ids, int ids_bits, uint64_t tokens,

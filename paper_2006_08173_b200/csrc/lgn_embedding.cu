@@ -12,7 +12,7 @@
 //                  pieces of runs that reach beyond it (one at its start, one at its end) go to scratch.  CTAs of the
 //                  same launch, mixed in between, write zeros to the rows without a token: most of the bytes that the
 //                  gradient of a large table has to write, streamed beside the gathers
-//   join_kernel    adds the pieces of each run of several windows
+//   join_kernel    adds the pieces of each run of several windows: a CTA per run and slab, its 8 warps a share of the pieces each
 // so that no warp adds more than one window of tokens, or one window count of pieces, in sequence.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -335,6 +335,7 @@ struct SumArgs {
     uint64_t ld_dout;
     const uint64_t *pair;
     float *part;                   // two rows of `pitch` values per window: the piece at its start, the piece at its end
+    uint32_t *long_count, *long_runs;   // windows with a run that begins there and reaches beyond: how many, and which
     void *out;
     uint64_t ld_out, vocab;
     uint32_t tokens, window_log2, windows, dim, pitch, slabs, accumulate;
@@ -440,6 +441,7 @@ __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
     auto flush = [&](uint32_t next) {                      // the run ends, or (next == run) goes on in the next window
         const bool from_before = run == first && before == run;
         if (!from_before && next != run) { write_row<ODT, VE>(a, run, col, sum); return; }
+        if (!from_before && col.c == 0) a.long_runs[atomicAdd(a.long_count, 1u)] = w;    // once per window; the list's order is of no account
         float *q = a.part + (uint64_t)(2 * w + (from_before ? 0 : 1)) * a.pitch;
         #pragma unroll
         for (int r = 0; r < kReps; ++r) {
@@ -487,72 +489,91 @@ __global__ void __launch_bounds__(256) window_kernel(const SumArgs a) {
     if (run != 0xffffffffu) flush(after);
 }
 
-// Runs that begin in window w and reach beyond it.
+// Runs that begin in one window and reach beyond it.
 template <int ODT, int VE>
 __global__ void __launch_bounds__(256) join_kernel(const SumArgs a) {
     constexpr int kReps = Columns<VE>::kReps;
+    __shared__ float sh[7][256];
     dep_launch();
     dep_wait();
-    const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const uint32_t w = (uint32_t)(item / a.slabs), lane = threadIdx.x & 31;
-    const Columns<VE> col((uint32_t)(item % a.slabs), a.dim);
-    if (w + 1 >= a.windows) return;
-    const uint32_t lo = w << a.window_log2, hi = (w + 1) << a.window_log2, run = id_at(a.pair, hi - 1);
-    if (run >= a.vocab || id_at(a.pair, hi) != run || (lo > 0 && id_at(a.pair, lo) == run && id_at(a.pair, lo - 1) == run)) return;
-    uint32_t end = w + 1;                                  // one past the last window whose first token is of this run
-    for (;;) {
-        const uint32_t q = end + lane;
-        const bool mine = q < a.windows && id_at(a.pair, (uint64_t)q << a.window_log2) == run;
-        const uint32_t not_mine = __ballot_sync(0xffffffffu, !mine);
-        if (not_mine != 0) { end += __ffs(not_mine) - 1; break; }
-        end += 32;
-    }
-    float sum[8];
-    auto piece = [&](uint64_t row, float *x) {
-        #pragma unroll
-        for (int r = 0; r < kReps; ++r)
-            if (col.on(r)) load_vec_rw<LGN_F32, VE>(a.part, row * a.pitch + col.at(r), x + r * VE);
-    };
-    #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-    piece(2 * (uint64_t)w + 1, sum);
-    for (uint32_t q0 = w + 1; q0 < end; q0 += 8) {
-        float v[8][8];
-        #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = 0.0f;
-            if (q0 + k < end) piece(2 * (uint64_t)(q0 + k), v[k]);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint64_t items = (uint64_t)*a.long_count * a.slabs;
+    for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t w = a.long_runs[item / a.slabs];
+        const Columns<VE> col((uint32_t)(item % a.slabs), a.dim);
+        const uint32_t run = id_at(a.pair, ((uint64_t)(w + 1) << a.window_log2) - 1);
+        uint32_t end = w + 1;                              // one past the last window whose first token is of this run
+        for (;;) {
+            const uint32_t q = end + lane;
+            const bool mine = q < a.windows && id_at(a.pair, (uint64_t)q << a.window_log2) == run;
+            const uint32_t not_mine = __ballot_sync(0xffffffffu, !mine);
+            if (not_mine != 0) { end += __ffs(not_mine) - 1; break; }
+            end += 32;
         }
+        // pieces: the end of window w, then the starts of windows w + 1 .. end - 1; warp q adds its share of them in order
+        float sum[8];
         #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (q0 + k < end) {
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+        auto piece = [&](uint32_t i, float *x) {           // piece i: row 2 w + 1, then 2 (w + i)
+            const uint64_t row = i == 0 ? 2 * (uint64_t)w + 1 : 2 * (uint64_t)(w + i);
+            #pragma unroll
+            for (int r = 0; r < kReps; ++r)
+                if (col.on(r)) load_vec_rw<LGN_F32, VE>(a.part, row * a.pitch + col.at(r), x + r * VE);
+        };
+        const uint32_t pieces = end - w, per = (pieces + 7) / 8, i0 = min(pieces, warp * per), i1 = min(pieces, i0 + per);
+        for (uint32_t i = i0; i < i1; i += 4) {
+            float v[4][8];
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) {
                 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += v[k][j];
+                for (int j = 0; j < 8; ++j) v[k][j] = 0.0f;
+                if (i + k < i1) piece(i + k, v[k]);
             }
+            #pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < i1) {
+                    #pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += v[k][j];
+                }
+        }
+        if (warp > 0) {
+            #pragma unroll
+            for (int j = 0; j < 8; ++j) sh[warp - 1][j * 32 + lane] = sum[j];
+        }
+        __syncthreads();
+        if (warp == 0) {
+            #pragma unroll
+            for (int q = 0; q < 7; ++q) {
+                #pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += sh[q][j * 32 + lane];
+            }
+            write_row<ODT, VE>(a, run, col, sum);
+        }
+        __syncthreads();
     }
-    write_row<ODT, VE>(a, run, col, sum);
 }
 
-// Tokens per window: about a quarter of the square root of their number.  The square root itself would make the
-// worst run (all tokens one id) shortest; real runs are far shorter, and short windows spread them over more warps.
-// Narrow tables take windows of 32 where longer ones would leave fewer than 16 warps per SM.
+// Tokens per window: 8 (a batch of loads) to about a quarter of the square root of the tokens, the longer ones only where
+// that leaves 16 warps per SM: a warp walks its window alone (1022 tokens x 2402: 35 us with 32, see join_kernel for what
+// short windows leave to add).
 static uint32_t window_log2_for(uint64_t tokens, uint64_t slabs) {
-    uint32_t l = 5;
+    uint32_t l = 3;
     while (l < 20 && (1ull << (2 * l + 4)) < tokens && (tokens * slabs >> (l + 1)) >= 2368) ++l;
     return l;
 }
 
-struct GradLayout { size_t present, pair[2], part, total; uint32_t window_log2, windows, pitch; };
+struct GradLayout { size_t long_runs, present, list, pair[2], part, total; uint32_t window_log2, windows, pitch; };
 
 static bool grad_layout(uint64_t tokens, uint64_t vocab, uint64_t dim, GradLayout &l) {
     if (tokens > kEmbMaxTokens || vocab > kEmbMaxRows || dim > kEmbMaxDim) return false;
-    size_t at = 0;
-    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
-    l.present = take(vocab);
-    for (int i = 0; i < 2; ++i) l.pair[i] = take(tokens * 8);
     l.window_log2 = window_log2_for(tokens, (dim + 255) / 256);
     l.windows = (uint32_t)((tokens + (1ull << l.window_log2) - 1) >> l.window_log2);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
+    l.long_runs = take(256 + vocab);                       // the list's count and, 256 bytes on, the marks: cleared by one memset
+    l.present = l.long_runs + 256;
+    l.list = take((size_t)l.windows * 4);
+    for (int i = 0; i < 2; ++i) l.pair[i] = take(tokens * 8);
     l.pitch = (uint32_t)((dim + 7) & ~7ull);
     l.part = take(l.windows > 1 ? (size_t)2 * l.windows * l.pitch * 4 : 0);
     l.total = at < 256 ? 256 : at;
@@ -689,7 +710,11 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     if (accumulate) {
         s.present = nullptr;
         if (tokens == 0) return LGN_OK;
-    } else if (cudaMemsetAsync(s.present, 0, (size_t)vocab, static_cast<cudaStream_t>(stream)) != cudaSuccess) { (void)cudaGetLastError(); return LGN_ERR_CUDA; }
+    }
+    if (cudaMemsetAsync(w + l.long_runs, 0, accumulate ? 256 : 256 + (size_t)vocab, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return LGN_ERR_CUDA;
+    }
     if (tokens > 0) {
         void *args[] = {&s};
         const lgn_status r = launch_dependent(sort, dim3((unsigned)ctas), dim3(kSortThreads), args, smem, stream, (unsigned)ctas);
@@ -700,6 +725,8 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
     a.dout = dout; a.ld_dout = ld_dout;
     a.pair = s.pair[(s.passes + 1) & 1];
     a.part = reinterpret_cast<float *>(w + l.part);
+    a.long_count = reinterpret_cast<uint32_t *>(w + l.long_runs);
+    a.long_runs = reinterpret_cast<uint32_t *>(w + l.list);
     a.out = dtable; a.ld_out = ld_table; a.vocab = vocab;
     a.tokens = s.tokens;
     a.window_log2 = l.window_log2; a.windows = l.windows;
@@ -725,5 +752,6 @@ extern "C" lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn
              (unsigned long long)vocab, a.dim, s.passes, s.bits, l.windows, kVe[vi]);
     const lgn_status r = launch_dependent(kWindowTable[dout_dt][table_dt][vi], dim3((unsigned)blocks + a.zero_blocks), dim3(256), args, 0, stream);
     if (r != LGN_OK || l.windows <= 1) return r;
-    return launch_dependent(kJoinTable[table_dt][vi], dim3((unsigned)blocks), dim3(256), args, 0, stream);
+    const uint64_t runs = (uint64_t)(l.windows - 1) * a.slabs;            // no more runs than windows that have a successor
+    return launch_dependent(kJoinTable[table_dt][vi], dim3((unsigned)(runs < 1184 ? runs : 1184)), dim3(256), args, 0, stream);
 }

@@ -121,6 +121,18 @@ def test_gradient(lgn, n, vocab, dim, kind, ddt, odt):
     check_grad(out, dout, ids, vocab, 0.75, pad, before)
 
 
+@pytest.mark.parametrize("n", [2, 1023, 1024, 1025, 1500, 2048, 2049, 3000, 4095, 4096, 4097, 8193])
+def test_gradient_at_the_sorts_edges(lgn, n):
+    """Both sorts, at the sizes where one form ends and the next begins; ids that come many times and once."""
+    dout = torch.randn(n, 6, generator=torch.Generator().manual_seed(n)).cuda()
+    for vocab, kind in ((13, "uniform"), (70001, "skewed")):
+        for idt in (torch.int32, torch.int64):
+            ids = make_ids(n, vocab, n, kind, idt)
+            got = lgn.lgn_embedding_grad(dout, ids, vocab, padding_idx=3)
+            check_grad(got, dout, ids, vocab, 1.0, 3)
+            assert torch.equal(got, lgn.lgn_embedding_grad(dout, ids, vocab, padding_idx=3))
+
+
 def test_gradient_wide_keys(lgn):
     """More than 18 bits of ids: three passes of the sort."""
     vocab, n = 600_011, 3000
