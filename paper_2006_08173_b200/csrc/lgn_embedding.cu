@@ -345,15 +345,15 @@ struct SumArgs {
     uint32_t zero_unit, zero_blocks;   // table rows per CTA that writes zeros, and the number of those CTAs
 };
 
-// Zeros to the rows [first, last) without a token.  Rows of 512 bytes and more: a warp per row.  Shorter rows that follow one
+// Zeros to the rows [first, last) without a token.  Rows of 1 KiB and more: a warp per row.  Shorter rows that follow one
 // another without gaps are taken as one stretch of memory, 16 bytes per thread and step whatever the rows' length (91 bf16
-// columns: 100 -> 26 us a call); a piece that also holds part of a row with a token is written in two-byte steps.
-constexpr uint32_t kFlatRowBytes = 512;
+// columns: 100 -> 26 us a call; 278 columns: 39 -> 32; 502 fp32 columns: 42 -> 57, hence the limit); a piece that also holds part of a row with a token is written in two-byte steps.
+constexpr uint32_t kFlatRowBytes = 1024;
 __device__ __forceinline__ void zero_rows(const SumArgs &a, uint64_t first, uint64_t last) {
     char *out = static_cast<char *>(a.out) + first * a.ld_out_bytes;
     const uint8_t *present = a.present + first;
     const uint32_t rows = (uint32_t)(last - first);
-    if (a.ld_out_bytes != a.dim_bytes || a.dim_bytes >= kFlatRowBytes) {
+    if (a.ld_out_bytes != a.dim_bytes || a.dim_bytes >= kFlatRowBytes || rows * a.dim_bytes * a.dim_bytes >= (1ull << 32)) {
         const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         // row r of a group of 256 is warp (r mod 8)'s, so that all warps of the CTA have rows of each group
         for (uint32_t r0 = 0; r0 < rows; r0 += 256) {
@@ -375,7 +375,7 @@ __device__ __forceinline__ void zero_rows(const SumArgs &a, uint64_t first, uint
         }
         return;
     }
-    // byte o of the stretch lies in row floor(o / d) = umulhi(o, ceil(2^32 / d)): exact while o d < 2^32, and o is below 2^21 here
+    // byte o of the stretch lies in row floor(o / d) = umulhi(o, ceil(2^32 / d)): exact while o d < 2^32
     const uint32_t d = (uint32_t)a.dim_bytes, bytes = rows * d, magic = 0xffffffffu / d + 1;
     const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15);        // pieces start at 16-byte boundaries
     for (uint32_t v = threadIdx.x; v * 16 < bytes + lead; v += 256) {
