@@ -423,6 +423,14 @@ lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt,
                           uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt,
                           int accumulate, uint32_t *status_dev, void *stream);
 
+/* Self-test of the product's bounded waits, as lgn_selftest_wait_expires is of the grouped call's: an E4M3 product with
+ * contiguous output in which every CTA leaves out its first copy, so that its MMAs never get their first operands.
+ * After a few seconds the kernel ends by itself with LGN_ERR_TIMEOUT in *status_dev (zeroed by the caller, not NULL);
+ * out is not meaningful, the context and the next calls are as usual.  k must be > 0. */
+lgn_status lgn_selftest_matmul_wait_expires(const void *a, const void *a_scales, const void *b, const void *b_scales,
+                                            uint64_t m, uint64_t n, uint64_t k, void *out, lgn_dtype out_dt,
+                                            uint32_t *status_dev, void *stream);
+
 /* ---- Embedding lookup with scaling, and the gradient of the table ----
  * out[t, :] = scale * table[id_t, :], formed in fp32 and rounded once; a row of zeros for an id outside
  * [0, vocab) (the other ranks' ids, for a table split by vocabulary).

@@ -141,6 +141,8 @@ _lib.lgn_fp8_quantize.argtypes = [_vp, _u64, _u64, _u64, _i32, _i32, _i32, _vp, 
 _lib.lgn_fp8_quantize.restype = _i32
 _lib.lgn_fp8_matmul.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
 _lib.lgn_fp8_matmul.restype = _i32
+_lib.lgn_selftest_matmul_wait_expires.argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _u64, _vp, _i32, _vp, _vp]
+_lib.lgn_selftest_matmul_wait_expires.restype = _i32
 _lib.lgn_embedding.argtypes = [_vp, _u64, _u64, _u64, _i32, _vp, _i32, _u64, _dbl, _vp, _u64, _i32, _vp, _vp]
 _lib.lgn_embedding.restype = _i32
 _lib.lgn_embedding_grad_workspace_bytes.argtypes = [_u64, _u64, _u64]
@@ -626,6 +628,15 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
                                m, n, k, out.data_ptr() or None, ldo, dtype_code(out), 1 if accumulate else 0,
                                _dev(status, "status") if status is not None else None, _stream(stream)), "lgn_fp8_matmul")
     return out
+
+
+def lgn_selftest_matmul_wait_expires(a: Fp8Operand, b: Fp8Operand, out: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """A product whose first copies are withheld: ``status`` must become LGN_ERR_TIMEOUT after a few seconds."""
+    if (a.fmt, b.fmt, a.k) != (E4M3, E4M3, b.k) or tuple(out.shape) != (a.rows, b.rows):
+        raise ValueError("E4M3 operands and an out of a.rows x b.rows")
+    _check(_lib.lgn_selftest_matmul_wait_expires(a._codes_ptr, a._scales_ptr, b._codes_ptr, b._scales_ptr, a.rows, b.rows, a.k,
+                                                 _dev(out, "out"), dtype_code(out), _dev(status, "status"), _stream(stream)),
+           "lgn_selftest_matmul_wait_expires")
 
 
 # --------------------------------------------------------------------------- embedding

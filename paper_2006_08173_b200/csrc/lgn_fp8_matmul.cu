@@ -45,7 +45,7 @@ namespace lgn {
 constexpr int kMmThreads = 320;                // warps 0..7: epilogue, 8: copies, 9: MMA
 constexpr int kMmEpiThreads = 256, kMmEpiWarps = 8;
 constexpr int kMmGroupRows = 16;                 // row tiles walked before the next column tile (L2 reuse)
-constexpr long long kMmWaitClocks = 4000000000ll;   // about two seconds
+constexpr long long kMmWaitClocks = 2000000000ll;   // one to two seconds
 
 struct MmArgs {
     void *out;
@@ -57,6 +57,7 @@ struct MmArgs {
     uint32_t fmt_rows, fmt_cols;
     uint32_t split_groups;                       // groups of four blocks per CTA of a cluster
     uint32_t accumulate;
+    uint32_t withhold;                           // self-test: each CTA leaves out its first copy
 };
 
 constexpr uint32_t kMmChunk = 8;                 // steps of k (128 each) that stay in tensor memory, fp32 outputs
@@ -423,6 +424,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
 
     // Warps 8 and 9 run their loops whole, one elected lane issuing: in code that only one lane runs the compiler moves every
     // operand of a TMA or MMA instruction to a uniform register at each use, which took 700 clocks per step of k.
+    uint32_t issued = 0;                                    // stages filled so far (warp 8)
     if (warp == 8) {
         dep_wait();
         uint32_t s = 0, ph = 1, it = 0;
@@ -438,7 +440,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                 const bool with_scales = (kb & 3) == 0;
                 if (elect_one()) {
                     if (leader) mbar_expect(full(s), CTAS * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));   // the bytes of both CTAs
-                    tma_tile<CTAS>(a, &map_rows, bar, (int)(kb * 128), y_rows);
+                    if (!(p.withhold != 0 && it == 0)) tma_tile<CTAS>(a, &map_rows, bar, (int)(kb * 128), y_rows);
                     tma_tile<CTAS>(a + 128 * 128, &map_cols, bar, (int)(kb * 128), y_cols);
                     if (with_scales) {                                          // tiles past the end read as zeros
                         const uint32_t sc = scales0 + s * S::kScaleBytes;
@@ -451,9 +453,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                 if (++s == S::kStages) { s = 0; ph ^= 1; }
             }
         }
-        if (!ok && leader)                                                      // wait for the copies in flight
-            for (uint32_t b = it > (uint32_t)S::kStages ? it - S::kStages : 0; b < it; ++b)
-                mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
+        issued = it;
     } else if (warp == 9) {
         if (leader) {
             const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)CTAS << 27);
@@ -553,6 +553,9 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     }
     fence_before();
     __syncthreads();
+    if (stop && warp == 8 && leader)                                            // a wait ran out: the copies in flight, of both CTAs, end first
+        for (uint32_t b = issued > (uint32_t)S::kStages ? issued - S::kStages : 0; b < issued; ++b)
+            mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
     if constexpr (CTAS == 2 || FORM == kFormSplit) cluster_sync();              // nothing of the other CTAs is in flight any more
     fence_after();
     if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
@@ -707,9 +710,9 @@ static MmPlan plan_matmul(uint64_t m, uint64_t n, uint64_t kblocks, bool vec, in
 
 using namespace lgn;
 
-extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt, const void *b, const void *b_scales, lgn_fp8 b_fmt,
-                                     uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt, int accumulate,
-                                     uint32_t *status_dev, void *stream) {
+static lgn_status matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt, const void *b, const void *b_scales, lgn_fp8 b_fmt,
+                         uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt, int accumulate,
+                         uint32_t *status_dev, void *stream, bool withhold) {
     if ((a_fmt != LGN_E4M3 && a_fmt != LGN_E5M2) || (b_fmt != LGN_E4M3 && b_fmt != LGN_E5M2)) return LGN_ERR_INVALID_ARG;
     if (out_dt != LGN_F32 && out_dt != LGN_BF16) return LGN_ERR_INVALID_ARG;
     if (m > kFp8MaxDim || n > kFp8MaxDim || k > kFp8MaxDim) return LGN_ERR_UNSUPPORTED;
@@ -753,6 +756,7 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     p.tiles_c = (p.cols + bn - 1) / bn;
     p.split_groups = plan.split_groups;
     p.accumulate = accumulate != 0;
+    p.withhold = withhold;
     const uint64_t tiles = (uint64_t)p.tiles_r * p.tiles_c, slots = (uint64_t)(sms / q.ctas);
     if (tiles > 0x3fffffffull || (uint64_t)((p.rows + 127) / 128) * p.groups > 0x7fffffffull || (uint64_t)((p.cols + 127) / 128) * p.groups > 0x7fffffffull)
         return LGN_ERR_UNSUPPORTED;                                             // TMA coordinates are 32-bit
@@ -768,4 +772,17 @@ extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp
     void *args[] = {&mr, &mc, &sr, &sc, &mo, &p};
     return launch_dependent(q.fn, dim3((unsigned)grid * (unsigned)q.ctas), dim3(kMmThreads), args, (size_t)q.smem, stream,
                             q.form == kFormSplit ? plan.split : (unsigned)q.ctas);
+}
+
+extern "C" lgn_status lgn_fp8_matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt, const void *b, const void *b_scales, lgn_fp8 b_fmt,
+                                     uint64_t m, uint64_t n, uint64_t k, void *out, uint64_t ldo, lgn_dtype out_dt, int accumulate,
+                                     uint32_t *status_dev, void *stream) {
+    return matmul(a, a_scales, a_fmt, b, b_scales, b_fmt, m, n, k, out, ldo, out_dt, accumulate, status_dev, stream, false);
+}
+
+extern "C" lgn_status lgn_selftest_matmul_wait_expires(const void *a, const void *a_scales, const void *b, const void *b_scales,
+                                                       uint64_t m, uint64_t n, uint64_t k, void *out, lgn_dtype out_dt,
+                                                       uint32_t *status_dev, void *stream) {
+    if (status_dev == nullptr || k == 0) return LGN_ERR_INVALID_ARG;
+    return matmul(a, a_scales, LGN_E4M3, b, b_scales, LGN_E4M3, m, n, k, out, n, out_dt, 0, status_dev, stream, true);
 }
