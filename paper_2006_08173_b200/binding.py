@@ -524,11 +524,12 @@ class Fp8Operand:
     def empty(cls, rows: int, k: int, fmt: int, device, stream=None) -> "Fp8Operand":
         """Uninitialised, codes and scales in one allocation; for use on ``stream`` (default: the current one)."""
         o = cls.__new__(cls)
-        codes, scales = _fp8_bytes(rows, k)
-        o.rows, o.k, o.fmt, o._codes, o._scales = rows, k, fmt, None, None
-        o._buffer = _empty(codes + scales + 16, _uint8, device, stream)
-        o._codes_ptr = o._buffer.data_ptr()
-        o._scales_ptr = o._codes_ptr + codes
+        codes = rows * ((k + 15) & -16)                    # as in _fp8_bytes
+        total = codes + ((rows + 127) >> 7) * ((k + 511) >> 9) * 512 + 16
+        o.rows, o.k, o.fmt = rows, k, fmt
+        o._buffer = buffer = torch.empty(total, dtype=_uint8, device=device) if stream is None else _empty(total, _uint8, device, stream)
+        o._codes_ptr = at = buffer.data_ptr()
+        o._scales_ptr = at + codes
         return o
 
     @property
@@ -550,22 +551,25 @@ class Fp8Operand:
         return Fp8Operand(*(kw.get(n, getattr(self, n)) for n in ("codes", "scales", "rows", "k", "fmt")))
 
 
-def _matrix(t: torch.Tensor, what: str) -> int:
-    """Leading dimension of a CUDA matrix whose rows are contiguous."""
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
+def _matrix3(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
+    """Rows, columns and leading dimension of a CUDA matrix whose rows are contiguous."""
     shape = t.shape
-    if len(shape) != 2:
-        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    if len(shape) != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA matrix")
     rows, cols = shape
     ld, step = t.stride()
     if cols > 1 and step != 1:
         raise ValueError(f"{what} must be a matrix with contiguous rows")
     if rows <= 1:
-        return cols or 1
+        return rows, cols, cols or 1
     if ld < cols:
         raise ValueError(f"{what} must have rows that do not overlap")
-    return ld
+    return rows, cols, ld
+
+
+def _matrix(t: torch.Tensor, what: str) -> int:
+    """The leading dimension alone."""
+    return _matrix3(t, what)[2]
 
 
 def _fp8_bytes(rows: int, k: int) -> Tuple[int, int]:
@@ -582,8 +586,7 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
                      stream=None) -> Tuple[Optional[Fp8Operand], Optional[Fp8Operand]]:
     """(operand, operand of the transpose) of a matrix, each only if asked for (else None).  ``out`` and
     ``out_t`` are operands of the same extents to write to (new_fp8_operand)."""
-    ld = _matrix(x, "x")
-    rows, cols = x.shape
+    rows, cols, ld = _matrix3(x, "x")
     if not (rowwise or transposed):
         raise ValueError("neither the operand nor its transpose is asked for")
     q = t = pq = sq = pt = st = None
@@ -603,8 +606,10 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
             if (t.rows, t.k, t.fmt) != (cols, rows, fmt):
                 raise ValueError("out_t: extents or format differ from the transpose")
         pt, st = t._codes_ptr, t._scales_ptr
-    _check(_lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), fmt, block, pq, sq, pt, st, _stream(stream)),
-           "lgn_fp8_quantize")
+    code = _lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), fmt, block, pq, sq, pt, st,
+                                 _raw_stream(_current_device()) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_fp8_quantize")
     return q, t
 
 
@@ -618,15 +623,19 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = _empty((m, n), out_dtype, a.device, stream)
+        device = (a._codes if a._buffer is None else a._buffer).device
+        out = torch.empty((m, n), dtype=out_dtype, device=device) if stream is None else _empty((m, n), out_dtype, device, stream)
         ldo = n or 1
     else:
         if tuple(out.shape) != (m, n):
             raise ValueError("out must be a.rows x b.rows")
         ldo = _matrix(out, "out")
-    _check(_lib.lgn_fp8_matmul(a._codes_ptr, a._scales_ptr, a.fmt, b._codes_ptr, b._scales_ptr, b.fmt,
+    code = _lib.lgn_fp8_matmul(a._codes_ptr, a._scales_ptr, a.fmt, b._codes_ptr, b._scales_ptr, b.fmt,
                                m, n, k, out.data_ptr() or None, ldo, dtype_code(out), 1 if accumulate else 0,
-                               _dev(status, "status") if status is not None else None, _stream(stream)), "lgn_fp8_matmul")
+                               _dev(status, "status") if status is not None else None,
+                               _raw_stream(_current_device()) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_fp8_matmul")
     return out
 
 
@@ -651,8 +660,7 @@ def lgn_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ou
                   stream=None) -> torch.Tensor:
     """scale * table[ids], zeros for ids outside the table: ids.numel() x dim.  ``n_outside``: int64 CUDA tensor of
     one element to which the number of ids outside the table is added."""
-    ld = _matrix(table, "table")
-    vocab, dim = table.shape
+    vocab, dim, ld = _matrix3(table, "table")
     n = ids.numel()
     if out is None:
         out = _empty((n, dim), out_dtype or table.dtype, table.device, stream)
