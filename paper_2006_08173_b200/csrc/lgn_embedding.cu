@@ -122,7 +122,7 @@ __device__ __forceinline__ int64_t load_id(const void *ids, uint64_t i, uint32_t
 }
 
 // ------------------------------------------------------------------ lookup
-// Two mappings.  Rows of whole 16-byte pieces (lookup_kernel): items of 8 columns of one token, numbered along the output; a
+// Three mappings.  Rows of whole 16-byte pieces (lookup_kernel): items of 8 columns of one token, numbered along the output; a
 // thread takes four, 256 apart, so that all threads work whatever the row's length and four rows' loads are in flight.
 // Other rows (lookup_rows_kernel): 2^span_log2 threads walk a row, one or two elements at a time; a division per element
 // would cost more than the idle threads (65536 x 999 bf16: 181 us against 94; sixteen narrow loads in flight instead of
@@ -201,6 +201,69 @@ lookup_rows_kernel(const void *table, uint64_t ld_table, uint64_t vocab, uint32_
                 for (int j = 0; j < VE; ++j) v[k][j] *= scale;
             }
             store_vec<ODT, VE>(out, (t0 + k * rows) * ld_out + (uint64_t)c * VE, v[k]);
+        }
+    }
+}
+
+// The third mapping, for a bf16 output without gaps whose rows are not whole 16-byte pieces: items are the 16-byte pieces of
+// the output's memory, each of them part of one row or of two, filled by element loads (neighbours share their lines
+// in L1) and stored at once instead of two bytes at a time (65536 x 999: 93 -> 78 us; with an fp32 output, whose
+// elements are stored four bytes at a time, 21547 x 679 went from 21 to 24 us).  dim >= 8.
+template <int TDT>
+__global__ void __launch_bounds__(256)
+lookup_flat_kernel(const void *table, uint64_t ld_table, uint64_t vocab, uint32_t dim, const void *ids, uint32_t wide,
+                   uint64_t tokens, float scale, void *out, unsigned long long *outside) {
+    constexpr int kPer = 8;
+    dep_launch();
+    // elements between the 16-byte boundary at or below the output's first element and that element
+    const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15) / (16 / kPer);
+    const uint64_t total = tokens * dim, first = (uint64_t)blockIdx.x * (1024 * kPer);
+    const uint64_t start = first < lead ? 0 : first - lead, t0 = start / dim;
+    const uint32_t rest = (uint32_t)(start - t0 * dim);
+    dep_wait();
+    #pragma unroll
+    for (int half = 0; half < 4; half += 2) {
+        uint64_t e[2];
+        float v[2][kPer];
+        uint32_t from_table[2] = {0u, 0u};                 // a bit per element
+        #pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t n = ((half + k) * 256 + threadIdx.x) * kPer, skip = first + n < lead ? lead - (uint32_t)(first + n) : 0;   // skip: only in the first piece
+            const uint32_t i = rest + (first < lead ? (n < lead ? 0 : n - lead) : n), q = i / dim, c = i - q * dim;
+            const uint64_t t = t0 + q;
+            e[k] = first + n;                              // counted from the boundary
+            int64_t id[2] = {-1, -1};
+            if (t < tokens) id[0] = load_id(ids, t, wide);
+            if (c + kPer > dim && t + 1 < tokens) id[1] = load_id(ids, t + 1, wide);
+            const bool in0 = id[0] >= 0 && (uint64_t)id[0] < vocab, in1 = id[1] >= 0 && (uint64_t)id[1] < vocab;
+            if (outside != nullptr) {                      // a token is counted by the piece that holds its first column
+                if (c == 0 && t < tokens && !in0) atomicAdd(outside, 1ull);
+                if (c + kPer - skip > dim && t + 1 < tokens && !in1) atomicAdd(outside, 1ull);
+            }
+            #pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                v[k][j] = 0.0f;
+                const uint32_t x = c + j - skip;           // column, counted on into the next row
+                if ((uint32_t)j >= skip && (x < dim ? in0 : in1)) {
+                    load_vec<TDT, 1>(table, x < dim ? (uint64_t)id[0] * ld_table + x : (uint64_t)id[1] * ld_table + (x - dim), &v[k][j]);
+                    from_table[k] |= 1u << j;
+                }
+            }
+        }
+        #pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (scale != 1.0f) {
+                #pragma unroll
+                for (int j = 0; j < kPer; ++j) if (from_table[k] >> j & 1) v[k][j] *= scale;
+            }
+            if (e[k] >= lead && e[k] + kPer <= total + lead) {
+                reinterpret_cast<uint4 *>(static_cast<unsigned short *>(out) + (e[k] - lead))[0] =
+                    make_uint4(bf16_pair(v[k][0], v[k][1]), bf16_pair(v[k][2], v[k][3]), bf16_pair(v[k][4], v[k][5]), bf16_pair(v[k][6], v[k][7]));
+            } else {
+                #pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (e[k] + j >= lead && e[k] + j < total + lead) store_vec<LGN_BF16, 1>(out, e[k] + j - lead, &v[k][j]);
+            }
         }
     }
 }
@@ -347,7 +410,8 @@ struct SumArgs {
 
 // Zeros to the rows [first, last) without a token.  Rows of 1 KiB and more: a warp per row.  Shorter rows that follow one
 // another without gaps are taken as one stretch of memory, 16 bytes per thread and step whatever the rows' length (91 bf16
-// columns: 100 -> 26 us a call; 278 columns: 39 -> 32; 502 fp32 columns: 42 -> 57, hence the limit); a piece that also holds part of a row with a token is written in two-byte steps.
+// columns: 100 -> 26 us a call; 278 columns: 39 -> 32; 502 fp32 columns: 42 -> 57, hence the limit); a piece that also holds
+// part of a row with a token is written in two-byte steps.
 constexpr uint32_t kFlatRowBytes = 1024;
 __device__ __forceinline__ void zero_rows(const SumArgs &a, uint64_t first, uint64_t last) {
     char *out = static_cast<char *>(a.out) + first * a.ld_out_bytes;
@@ -623,6 +687,7 @@ static int vector_of(uint64_t dim, const void *a, uint64_t lda, uint64_t ea, con
 #define LGN_LK(T, O) {reinterpret_cast<const void *>(&lookup_rows_kernel<T, O, 1>), reinterpret_cast<const void *>(&lookup_rows_kernel<T, O, 2>), reinterpret_cast<const void *>(&lookup_kernel<T, O, 8>)}
 static const void *const kLookupTable[2][2][3] = {{LGN_LK(LGN_F32, LGN_F32), LGN_LK(LGN_F32, LGN_BF16)}, {LGN_LK(LGN_BF16, LGN_F32), LGN_LK(LGN_BF16, LGN_BF16)}};
 #undef LGN_LK
+static const void *const kLookupFlatTable[2] = {reinterpret_cast<const void *>(&lookup_flat_kernel<LGN_F32>), reinterpret_cast<const void *>(&lookup_flat_kernel<LGN_BF16>)};
 #define LGN_WK(T, O) {reinterpret_cast<const void *>(&window_kernel<T, O, 1>), reinterpret_cast<const void *>(&window_kernel<T, O, 2>), reinterpret_cast<const void *>(&window_kernel<T, O, 8>)}
 static const void *const kWindowTable[2][2][3] = {{LGN_WK(LGN_F32, LGN_F32), LGN_WK(LGN_F32, LGN_BF16)}, {LGN_WK(LGN_BF16, LGN_F32), LGN_WK(LGN_BF16, LGN_BF16)}};
 #undef LGN_WK
@@ -653,6 +718,16 @@ extern "C" lgn_status lgn_embedding(const void *table, uint64_t vocab, uint64_t 
     if (ranges_overlap(out, ob, table, vocab ? ((vocab - 1) * ld_table + dim) * et : 0) || ranges_overlap(out, ob, ids, tokens * ei)) return LGN_ERR_INVALID_ARG;
     const int vi = vector_of(dim, table, ld_table, et, out, ld_out, eo);
     const uint64_t chunks = (dim + kVe[vi] - 1) / kVe[vi];
+    if (kVe[vi] < 8 && dim >= 8 && ld_out == dim && out_dt == LGN_BF16) {
+        const uint64_t pieces = (tokens * dim + 7) / 8 + 1, flat_blocks = (pieces + 1023) / 1024;
+        if (flat_blocks > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
+        uint32_t d = (uint32_t)dim, wide = ids_bits == 64;
+        float s = (float)scale;
+        unsigned long long *outside = reinterpret_cast<unsigned long long *>(n_outside_dev);
+        log_line("embedding: %llu tokens, dim %u, pieces of the output, %llu CTAs", (unsigned long long)tokens, d, (unsigned long long)flat_blocks);
+        void *args[] = {&table, &ld_table, &vocab, &d, &ids, &wide, &tokens, &s, &out, &outside};
+        return launch_dependent(kLookupFlatTable[table_dt], dim3((unsigned)flat_blocks), dim3(256), args, 0, stream);
+    }
     uint32_t span = 0;
     while (span < 8 && (1ull << span) < chunks) ++span;
     const uint64_t per = 4ull * (256u >> span), blocks = kVe[vi] == 8 ? (tokens * chunks + 1023) / 1024 : (tokens + per - 1) / per;

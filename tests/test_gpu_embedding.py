@@ -59,6 +59,22 @@ def test_lookup(lgn, n, vocab, dim, tdt, odt):
         assert torch.equal(out, lgn.lgn_embedding(table, ids, 45.25, out_dtype=DT[odt]))
 
 
+@pytest.mark.parametrize("odt", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [8, 9, 10, 11, 15, 17, 33, 100, 257, 999])
+def test_lookup_without_gaps_at_any_address(lgn, dim, odt):
+    """Outputs of odd rows without gaps, at every element offset from a 16-byte boundary, and what lies around them."""
+    table = torch.randn(60, dim, device="cuda")
+    for n in (1, 2, 130, 1111):
+        ids = make_ids(n, 60, n + dim, "outside", torch.int64)
+        for off in range(9):
+            buf = torch.full((n * dim + 40,), 7.0, dtype=DT[odt], device="cuda")
+            view = buf[off:off + n * dim].view(n, dim)
+            count = torch.zeros(1, dtype=torch.int64, device="cuda")
+            lgn.lgn_embedding(table, ids, -3.0, out=view, n_outside=count)
+            assert check_lookup(view, table, ids, -3.0) == int(count.item())
+            assert bool((buf[:off] == 7.0).all()) and bool((buf[off + n * dim:] == 7.0).all())
+
+
 def test_lookup_keeps_bits_at_scale_one(lgn):
     table = torch.randn(40, 128, device="cuda")
     table[3, 7], table[3, 8], table[3, 9] = float("inf"), float("nan"), -0.0
