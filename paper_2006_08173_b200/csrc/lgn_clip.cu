@@ -129,7 +129,12 @@ __device__ __forceinline__ void add_chunk(const Words &c, double &sum, unsigned 
     }
     s += t;
     if (s >= 0x1p-80f && s < __int_as_float(0x7f800000)) sum += (double)s;
-    else add_exactly<ES>(c, sum, bad);
+    else {
+        uint32_t bits = 0;                                 // all zeros, as in pruned gradients: nothing to add (85 % zeros in bf16: 140 -> 85 us per 537 MB)
+        #pragma unroll
+        for (int k = 0; k < 8; ++k) bits |= c.w[k] & (ES == 4 ? 0x7fffffffu : 0x7fff7fffu);
+        if (bits != 0) add_exactly<ES>(c, sum, bad);
+    }
 }
 
 __device__ __forceinline__ float load_elem(const char *p, uint32_t es) {
