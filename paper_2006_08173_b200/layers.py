@@ -6,9 +6,10 @@ The modules marshal arguments for ``binding``; there is no CPU path.
 """
 from __future__ import annotations
 
-from typing import List, Optional, Sequence
+from typing import List, Sequence
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as lgn
 
@@ -31,14 +32,18 @@ class _LinearFn(torch.autograd.Function):
         return lgn.lgn_fp8_matmul(xq, wq, out_dtype=x.dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
+        need_dx, need_dw = ctx.needs_input_grad[:2]
+        if not (need_dx or need_dw):
+            return None, None, None, None
         if ctx.sparsity > 0.0:
             dy = _pruned(dy, ctx.sparsity, ctx.seed)
         elif dy.stride(-1) != 1 or (dy.size(0) > 1 and dy.stride(0) < dy.size(1)):
             dy = dy.contiguous()                                       # a broadcast gradient
-        dq, dqt = lgn.lgn_fp8_quantize(dy, lgn.E5M2, transposed=True)
-        dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0])
-        dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1])
+        dq, dqt = lgn.lgn_fp8_quantize(dy, lgn.E5M2, rowwise=need_dx, transposed=need_dw)
+        dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0]) if need_dx else None
+        dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1]) if need_dw else None
         return dx, dw, None, None
 
 
@@ -69,6 +74,7 @@ class _EmbeddingFn(torch.autograd.Function):
         return lgn.lgn_embedding(weight, ids, scale, out_dtype=out_dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         (ids,) = ctx.saved_tensors
         vocab, scale, padding_idx, dtype = ctx.args
@@ -98,14 +104,19 @@ class GradClipper:
     trip.  The gradients have to exist and to stay where they are (zero_grad(set_to_none=False))."""
 
     def __init__(self, parameters: Sequence[torch.nn.Parameter], max_norm: float):
-        grads: List[torch.Tensor] = [p.grad for p in parameters if p.grad is not None]
-        if not grads:
+        self._params = [p for p in parameters if p.grad is not None]
+        self._grads: List[torch.Tensor] = [p.grad for p in self._params]
+        if not self._grads:
             raise ValueError("no parameter has a gradient yet")
-        self._list, self.max_norm = lgn.make_grads(grads), float(max_norm)
-        self.record = lgn.new_norm_record(grads[0].device)
-        self._ws = lgn.new_clip_workspace(grads[0].device, len(grads))
+        self._list, self.max_norm = lgn.make_grads(self._grads), float(max_norm)
+        self._places = [g.data_ptr() for g in self._grads]
+        self.record = lgn.new_norm_record(self._grads[0].device)
+        self._ws = lgn.new_clip_workspace(self._grads[0].device, len(self._grads))
 
     def clip(self, stream=None) -> torch.Tensor:
         """Scales the gradients; returns their norm before it, a scalar on the device."""
+        for p, g, at in zip(self._params, self._grads, self._places):
+            if p.grad is not g or g.data_ptr() != at:
+                raise RuntimeError("a gradient has been replaced since the clipper was made")
         lgn.lgn_clip_grad_norm(self._list, self.max_norm, self.record, self._ws, stream)
         return lgn.norm_of(self.record)

@@ -82,6 +82,34 @@ def test_clipper_needs_gradients(layers):
         layers.GradClipper([torch.nn.Parameter(torch.zeros(3, device="cuda"))], 1.0)
 
 
+def test_clipper_notices_replaced_gradients(layers):
+    p = torch.nn.Parameter(torch.zeros(3, device="cuda"))
+    p.grad = torch.full((3,), 2.0, device="cuda")
+    c = layers.GradClipper([p], 1.0)
+    norm = float(c.clip())
+    assert abs(norm - 12 ** 0.5) < 1e-5 and abs(float(p.grad.norm()) - 1.0) < 1e-5
+    p.grad = torch.ones(3, device="cuda")
+    with pytest.raises(RuntimeError):
+        c.clip()
+
+
+def test_only_the_gradients_asked_for(layers):
+    lin = layers.Fp8Linear(64, 32, device="cuda")
+    x = torch.randn(7, 64, device="cuda").bfloat16()
+    lin(x).sum().backward()                                       # the input needs none
+    assert lin.weight.grad is not None
+    want = lin.weight.grad.clone()
+    lin.weight.grad = None
+    x.requires_grad_()
+    lin(x).sum().backward()
+    assert torch.equal(want, lin.weight.grad) and x.grad is not None
+    lin.weight.requires_grad_(False)
+    once = x.grad.clone()
+    x.grad = None
+    lin(x).sum().backward()
+    assert torch.equal(once, x.grad)
+
+
 def test_example_learns(lgn):
     sys.path.insert(0, os.path.join(ROOT, "examples"))
     try:
