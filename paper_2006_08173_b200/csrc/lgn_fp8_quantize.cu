@@ -179,8 +179,11 @@ fp8_rows_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32
 // apart over all banks.
 // BLOCKS: blocks of 128 along the rows of both copies, of the transpose alone, or squares.
 enum TileBlocks { kTileBoth = 0, kTileTransposed = 1, kTileSquare = 2 };
+// Four CTAs per SM (64 registers, 12 bytes of them spilled with both copies) hide the latency of the loads and of the shared
+// tile: both bf16 copies of 16384 x 8192 take 139, 126 and 115 us with two, three and four.  fp32 holds twice the values
+// per thread, so two fit without spills.
 template <int DT, int FMT, int BLOCKS, bool VEC>
-__global__ void __launch_bounds__(256, DT == LGN_F32 ? 2 : 3)
+__global__ void __launch_bounds__(256, DT == LGN_F32 ? 2 : 4)
 fp8_tile_kernel(const char *x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t col_tiles,
                 uint8_t *codes, uint32_t ldq, uint8_t *scales, uint32_t groups,
                 uint8_t *codes_t, uint32_t ldq_t, uint8_t *scales_t, uint32_t groups_t) {
