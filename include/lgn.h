@@ -413,7 +413,8 @@ lgn_status lgn_fp8_quantize(const void *x, uint64_t rows, uint64_t cols, uint64_
 
 /* out[i, j] = sum over c of A[i, c] B[j, c] (+ out[i, j] if accumulate), i < m, j < n, c < k, of the values that
  * codes and scales stand for; a is m x k, b is n x k, either format each.  Sums in fp32, rounded
- * once to out_dt.  out: leading dimension ldo >= n.  A layer Y = X W^T: its forward pass takes X and W, its
+ * once to out_dt: over 1024 c by the tensor cores, whose additions truncate (an error of about 2e-7 of sum |A B|), from there on to
+ * nearest.  out: leading dimension ldo >= n.  A layer Y = X W^T: its forward pass takes X and W, its
  * input gradient dY and the transpose of W, its weight gradient the transposes of dY and X.
  * k = 0 writes zeros (or leaves out as it is).  status_dev: device uint32, may be NULL; set to
  * LGN_ERR_TIMEOUT if a bounded device-side wait ran out (the output is then invalid), else left alone.

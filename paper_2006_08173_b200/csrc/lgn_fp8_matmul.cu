@@ -3,7 +3,7 @@
 //
 // The tensor cores apply the scales: tcgen05.mma kind::mxf8f6f4 multiplies each group of 32 k by an E8M0
 // factor per row of either operand, read from tensor memory; a block of 128 is four groups with the same
-// byte.  Products and sums stay in fp32 in tensor memory over the whole of k and are rounded once, to the
+// byte.  Sums are fp32, in tensor memory over 1024 k and in registers beyond, and are rounded once, to the
 // output's type.
 //
 // One CTA, or a pair of CTAs on two SMs (CTAS = 2), works on tiles of 128 CTAS rows of one operand ("rows") by BN rows of
@@ -22,10 +22,14 @@
 // SWAP: `rows` runs along the contiguous dimension of the output, so that the 32 lanes of a warp, which hold
 // 32 rows, write contiguous memory whatever the alignment.
 //
-// fp32 outputs: the tensor cores' additions truncate, which biases a sum towards zero by about 2e-10 of its
+// The tensor cores' additions truncate, which biases a sum towards zero by about 2e-10 of its
 // size per k (measured: 2.0e-7 at k = 1024, 1e-6 and more from 8192).  Every 1024 k the tile is therefore added to sums in
-// registers (round to nearest) and a fresh one begun in the other half of tensor memory; the error then stays below
-// 5e-7 (k up to 16384).  For bf16 outputs, rounded at 2e-3, the sum stays in tensor memory.
+// registers (round to nearest) and a fresh one begun elsewhere in tensor memory; the error then stays below
+// 5e-7 (k up to 16384).  Of bf16 outputs, 7e-5 are a neighbour of the rounded exact sum at 2048 x 2048 x 16384 (1e-5 with
+// positive operands); with the sum in tensor memory over the whole of k it was 3e-4 (1e-3).
+// Tiles of up to 192 columns have two accumulators, used in turn.  A tile of 256 would leave no columns for the scales
+// with two; its MMAs are issued for two halves of 128 columns, whose chunks of k end 512 k apart, and three accumulators
+// of 128 columns go round: while two collect, the third is read out.
 //
 // Every wait is bounded: one that runs out raises a flag on which all roles stop; the copies and MMAs in
 // flight are waited for (bounded too), tensor memory is freed and the kernel ends with *status set.
@@ -60,7 +64,7 @@ struct MmArgs {
     uint32_t withhold;                           // self-test: each CTA leaves out its first copy
 };
 
-constexpr uint32_t kMmChunk = 8;                 // steps of k (128 each) that stay in tensor memory, fp32 outputs
+constexpr uint32_t kMmChunk = 8;                 // steps of k (128 each) that stay in tensor memory
 
 constexpr int kMmBuffer = 4096;                   // 32 rows x 128 bytes of output
 
@@ -73,8 +77,11 @@ template <int BN, int CTAS, int ODT> struct MmShape {
     static constexpr int kScaleBytes = 512 * (1 + kColBlocks);
     static constexpr int kFit = (int)((225 * 1024 - kStaging) / (kStageBytes + kScaleBytes));
     static constexpr int kStages = kFit > 8 ? 8 : kFit;
-    static constexpr int kAccs = BN <= 192 ? 2 : 1;                 // accumulator tiles in tensor memory
-    static constexpr int kScaleCol = kAccs * BN;                    // first tensor-memory column of the scales
+    static constexpr int kHalves = BN == 256 ? 2 : 1;               // column parts of a tile with accumulators of their own
+    static constexpr int kMmaN = BN / kHalves;                      // columns of an MMA and of an accumulator
+    static constexpr int kAccs = kHalves + 1;                       // accumulators in tensor memory
+    static constexpr int kBoxRows = kMmaN / CTAS;                   // rows of `cols` in a copy; a half's rows come from all CTAs of a tile
+    static constexpr int kScaleCol = kAccs * kMmaN;                 // first tensor-memory column of the scales
     static constexpr int kScaleCols = 4 * (1 + kColBlocks);
     static constexpr int kScaleBufs = 4;
     static constexpr int kSmem = 1024 + kStaging + kStages * (kStageBytes + kScaleBytes);
@@ -201,18 +208,12 @@ __device__ __forceinline__ void tmem_load16(uint32_t taddr, float *v) {
                    "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
 }
-// Waits for the loads issued so far.  The 16 values pass through, so that no use of them can be moved ahead of the wait; further
-// values of the same wait pass through tmem_loaded16.
+// Waits for the loads issued so far.  The 16 values pass through, so that no use of them can be moved ahead of the wait.
 __device__ __forceinline__ void tmem_load_wait16(float *v) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]),
                    "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
 }
-__device__ __forceinline__ void tmem_loaded16(float *v) {
-    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]),
-                      "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
-}
-
 template <int ODT>
 __device__ __forceinline__ float load_out(const void *out, uint64_t i) {
     if constexpr (ODT == LGN_F32) return static_cast<const float *>(out)[i];
@@ -306,49 +307,51 @@ __device__ __forceinline__ void tile_at(const MmArgs &p, uint32_t t, uint32_t &t
     tc = in / h;
 }
 
-// An epilogue warp's part of one tile, the BN / 2 columns from tmem_at on: waits for the accumulator(s), adds chunks up
-// (fp32 outputs), hands 32 columns at a time to `put`.  `n` counts accumulators; false: a wait ran out.
-template <int BN, int ACCS, int RUN, bool CHUNKS, class Full, class Release, class Put>
-__device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t chunks, uint32_t &n, volatile uint32_t *stop, Full acc_full, Release release, Put put) {
-    constexpr int kCols = BN / 2;
+// An epilogue warp's part of one tile, kMmaN / 2 columns of each half from tmem_at on: adds the chunks of k up in registers as they are
+// finished, hands RUN columns at a time to `put` (half, column within the part).  `steps`: of k; `n` counts accumulators;
+// false: a wait ran out.
+template <class S, int RUN, class Full, class Release, class Put>
+__device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t steps, uint32_t &n, volatile uint32_t *stop, Full acc_full, Release release, Put put) {
+    constexpr int kCols = S::kMmaN / 2;
     static_assert(kCols % RUN == 0, "columns");
-    if constexpr (CHUNKS) {
-        float sum[kCols];
-        for (uint32_t ch = 0; ch < chunks; ++ch, ++n) {
-            const uint32_t acc = n % ACCS;
-            if (!mbar_wait(acc_full(acc), (n / ACCS) & 1, stop)) return false;
-            __syncwarp();
-            fence_after();
-            #pragma unroll
-            for (int c = 0; c < kCols; c += 16) {
-                float v[16];
-                tmem_load16(tmem_at + acc * BN + c, v);
-                tmem_load_wait16(v);
-                #pragma unroll
-                for (int j = 0; j < 16; ++j) sum[c + j] = ch == 0 ? v[j] : sum[c + j] + v[j];
-            }
-            fence_before();
-            release(acc);
-        }
+    float sum[S::kHalves][kCols];                           // from zero: copying the first chunk instead costs registers (spills, 4096^3 bf16 53 -> 58 us)
+    #pragma unroll
+    for (int h = 0; h < S::kHalves; ++h) {
         #pragma unroll
-        for (int c = 0; c < kCols; c += RUN) put(c, sum + c);
-    } else {
-        const uint32_t acc = n % ACCS;
-        if (!mbar_wait(acc_full(acc), (n / ACCS) & 1, stop)) return false;
+        for (int c = 0; c < kCols; ++c) sum[h][c] = 0.0f;
+    }
+    auto add = [&](float *to) {
+        const uint32_t acc = n % S::kAccs;
+        if (!mbar_wait(acc_full(acc), (n / S::kAccs) & 1, stop)) return false;
         __syncwarp();
         fence_after();
-        #pragma unroll 1
-        for (int c = 0; c < kCols; c += RUN) {
-            float v[RUN];
-            #pragma unroll
-            for (int j = 0; j < RUN; j += 16) tmem_load16(tmem_at + acc * BN + c + j, v + j);
+        #pragma unroll
+        for (int c = 0; c < kCols; c += 16) {
+            float v[16];
+            tmem_load16(tmem_at + acc * S::kMmaN + c, v);
             tmem_load_wait16(v);
             #pragma unroll
-            for (int j = 16; j < RUN; j += 16) tmem_loaded16(v + j);
-            if (c + RUN >= kCols) { fence_before(); release(acc); }
-            put(c, v);
+            for (int j = 0; j < 16; ++j) to[c + j] += v[j];
         }
+        fence_before();
+        release(acc);
         ++n;
+        return true;
+    };
+    if constexpr (S::kHalves == 1) {
+        for (uint32_t k = 0; k < steps; k += kMmChunk) if (!add(sum[0])) return false;
+    } else {
+        // in the order in which they end: after 4 steps the first of half 1, after 8 of half 0, and so on; both halves' last with the tile
+        const uint32_t items = (steps + kMmChunk / 2 - 1) / (kMmChunk / 2) + 1;
+        for (uint32_t j = 0; j < items; j += 2) {
+            if (!add(sum[1])) return false;
+            if (j + 1 < items && !add(sum[0])) return false;
+        }
+    }
+    #pragma unroll
+    for (int h = 0; h < S::kHalves; ++h) {
+        #pragma unroll
+        for (int c = 0; c < kCols; c += RUN) put(h, c, sum[h] + c);
     }
     return true;
 }
@@ -358,7 +361,6 @@ __global__ void __launch_bounds__(kMmThreads, 1)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_constant__ CUtensorMap map_cols, const __grid_constant__ CUtensorMap map_sc_rows,
                   const __grid_constant__ CUtensorMap map_sc_cols, const __grid_constant__ CUtensorMap map_out, const MmArgs p) {
     using S = MmShape<BN, CTAS, ODT>;
-    constexpr bool kChunked = ODT == LGN_F32;
     constexpr int kRun = FORM == kFormRows ? OutRun<ODT>::kCols : 32;
     extern __shared__ uint8_t smem_raw[];
     dep_launch();
@@ -432,7 +434,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
             uint32_t tr, tc;
             tile_at(p, t, tr, tc);
-            const int y_rows = (int)((tr * CTAS + half) * 128), y_cols = (int)(tc * BN + half * (BN / 2));
+            const int y_rows = (int)((tr * CTAS + half) * 128), y_cols = (int)(tc * BN + half * S::kBoxRows);
             int y_sr = (int)((tr * CTAS + half) * p.groups + (kb0 >> 2)), y_sc = (int)(((tc * BN) >> 7) * p.groups + (kb0 >> 2));
             for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
                 if (!(ok = mbar_wait_warp(empty(s), ph, &stop))) break;
@@ -441,7 +443,9 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                 if (elect_one()) {
                     if (leader) mbar_expect(full(s), CTAS * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));   // the bytes of both CTAs
                     if (!(p.withhold != 0 && it == 0)) tma_tile<CTAS>(a, &map_rows, bar, (int)(kb * 128), y_rows);
-                    tma_tile<CTAS>(a + 128 * 128, &map_cols, bar, (int)(kb * 128), y_cols);
+                    #pragma unroll
+                    for (int h = 0; h < S::kHalves; ++h)
+                        tma_tile<CTAS>(a + (128 + h * S::kBoxRows) * 128, &map_cols, bar, (int)(kb * 128), y_cols + h * S::kMmaN);
                     if (with_scales) {                                          // tiles past the end read as zeros
                         const uint32_t sc = scales0 + s * S::kScaleBytes;
                         tma_tile<CTAS>(sc, &map_sc_rows, bar, 0, y_sr);
@@ -456,17 +460,30 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         issued = it;
     } else if (warp == 9) {
         if (leader) {
-            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)CTAS << 27);
+            const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(S::kMmaN >> 3) << 17) | (1u << 23) | ((uint32_t)CTAS << 27);
             const uint64_t desc0 = desc_codes(smem0);
-            uint32_t s = 0, ph = 0, acc = 0, acc_ph = 1, grp = 0;
+            constexpr uint32_t kTurn = kMmChunk / S::kHalves;                   // steps between two changes of accumulator
+            uint32_t s = 0, ph = 0, n = 0, grp = 0;                             // n: accumulators begun
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tiles; t += tile_step) {
-                uint32_t tr, tc, sa = 0;
+                uint32_t tr, tc, sa = 0, acc[S::kHalves];
                 tile_at(p, t, tr, tc);
                 const uint32_t col_off = 4 + (((tc * BN) & 127) >> 5);          // columns' scales: the tile may begin inside a scale tile
-                for (uint32_t c0 = kb0; ok && c0 < kb1;) {                      // one accumulator per chunk of k
-                    const uint32_t c1 = kChunked ? min(kb1, c0 + kMmChunk) : kb1, d = tmem + acc * BN;
-                    if (!(ok = mbar_wait_warp(acc_empty(acc), acc_ph, &stop))) break;
+                for (uint32_t c0 = kb0, turn = 0; ok && c0 < kb1; c0 += kTurn, ++turn) {
+                    const uint32_t c1 = min(kb1, c0 + kTurn);
+                    bool fresh[S::kHalves], ends[S::kHalves];                   // an accumulator begins, ends with this turn
+                    #pragma unroll
+                    for (int h = S::kHalves - 1; h >= 0; --h) {
+                        // half 1 begins at turns 0 (for half a chunk), 1, 3, 5, half 0 at turns 0, 2, 4
+                        fresh[h] = S::kHalves == 1 || turn == 0 || (turn & 1) == (uint32_t)h;
+                        ends[h] = S::kHalves == 1 || c1 == kb1 || (turn & 1) != (uint32_t)h;
+                        if (fresh[h]) {
+                            acc[h] = n % S::kAccs;
+                            ok = ok && mbar_wait_warp(acc_empty(acc[h]), (n / S::kAccs & 1) ^ 1, &stop);
+                            ++n;
+                        }
+                    }
+                    if (!ok) break;
                     fence_after();
                     for (uint32_t kb = c0; kb < c1; ++kb) {
                         if (!(ok = mbar_wait_warp(full(s), ph, &stop))) break;
@@ -484,15 +501,21 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                                 for (int b = 0; b < 1 + S::kColBlocks; ++b) copy_scales<CTAS>(sa + 4 * b, scales0 + s * S::kScaleBytes + 512 * b);
                             }
                             #pragma unroll
-                            for (int k = 0; k < 4; ++k) mma_scaled<CTAS>(d, da + 2 * k, db + 2 * k, idesc, sa, sa + col_off, kb > c0 || k > 0);
+                            for (int k = 0; k < 4; ++k) {
+                                #pragma unroll
+                                for (int h = S::kHalves - 1; h >= 0; --h)
+                                    mma_scaled<CTAS>(tmem + acc[h] * S::kMmaN, da + 2 * k, db + h * (S::kBoxRows * 128 >> 4) + 2 * k, idesc,
+                                                     sa, sa + col_off + 4 * h, !fresh[h] || kb > c0 || k > 0);
+                            }
                             mma_commit<CTAS>(empty(s));
-                            if (kb + 1 == c1) mma_commit<CTAS>(acc_full(acc));
+                            if (kb + 1 == c1) {
+                                #pragma unroll
+                                for (int h = S::kHalves - 1; h >= 0; --h) if (ends[h]) mma_commit<CTAS>(acc_full(acc[h]));
+                            }
                         }
                         __syncwarp();
                         if (++s == S::kStages) { s = 0; ph ^= 1; }
                     }
-                    c0 = c1;
-                    if (++acc == S::kAccs) { acc = 0; acc_ph ^= 1; }
                 }
             }
             if (!ok) {
@@ -504,22 +527,23 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     } else {
         dep_wait();                                                             // the output may belong to work before this call
         uint32_t n = 0, turn = 0;
-        const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, chunks = (kb1 - kb0 + kMmChunk - 1) / kMmChunk;
+        const uint32_t quad = warp & 3, col0 = (warp >> 2) * (S::kMmaN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0;
         for (uint32_t t = tile0; t < tiles; t += tile_step) {
             uint32_t tr, tc;
             tile_at(p, t, tr, tc);
-            const uint32_t r = (tr * CTAS + half) * 128 + quad * 32 + lane, c0 = tc * BN + col0;
-            const bool ok = drain_tile<BN, S::kAccs, kRun, kChunked>(tmem_at, chunks, n, &stop, acc_full,
+            const uint32_t r = (tr * CTAS + half) * 128 + quad * 32 + lane;
+            const bool ok = drain_tile<S, kRun>(tmem_at, kb1 - kb0, n, &stop, acc_full,
                 [&](uint32_t acc) { __syncwarp(); if (lane == 0) arrive_leader<CTAS>(acc_empty(acc)); },
-                [&](uint32_t c, float *v) {
+                [&](uint32_t h, uint32_t c, float *v) {
+                    const uint32_t in_tile = h * S::kMmaN + col0 + c, x = tc * BN + in_tile;
                     if constexpr (FORM == kFormSplit) {
                         float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
                         #pragma unroll
-                        for (int j = 0; j < 32; ++j) part[(col0 + c + j) * 128 + quad * 32 + lane] = v[j];
+                        for (int j = 0; j < 32; ++j) part[(in_tile + j) * 128 + quad * 32 + lane] = v[j];
                     } else if constexpr (FORM == kFormSwap) {
-                        if (r < p.rows && c0 + c < p.cols)
-                            store_strided<ODT, kRun>(p.out, (uint64_t)(c0 + c) * p.ldo + r, p.ldo, p.cols - c0 - c, v, p.accumulate != 0);
-                    } else store_staged<ODT, S::kBuffers>(p, &map_out, staging0 + warp * (S::kBuffers * kMmBuffer), turn, r - lane, c0 + c, lane, v);
+                        if (r < p.rows && x < p.cols)
+                            store_strided<ODT, kRun>(p.out, (uint64_t)x * p.ldo + r, p.ldo, p.cols - x, v, p.accumulate != 0);
+                    } else store_staged<ODT, S::kBuffers>(p, &map_out, staging0 + warp * (S::kBuffers * kMmBuffer), turn, r - lane, x, lane, v);
                 });
             if (!ok) break;
         }
@@ -576,13 +600,13 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(void *out, uint64_t ldo,
 // The kernels a call may take, with what a call of each costs on a B200, in microseconds: `start` once, `step` for 128 of k of
 // a tile, `tile` for a tile beyond that (fitted to 60 products from 4 x 1024 x 1024 to 4096^3).  The fits leave errors of up to a
 // fifth, about as much as neighbouring kernels differ; what they must get right is which side of
-//   64 x k shares       few tokens: (4, 4096, 4096) 6.7 us in 4 shares, 9.1 whole, 7.8 with pairs of 128
-//   pairs of 128        (512, 4096, 4096) 10.1 us, 12.3 with lone 128, 14.4 with pairs of 256
-//   lone 128            where pairs would need a second round: (777, 2504, 1000) 7.1 us against 9.7
-//   pairs of 256 / 192  (4096, 4096, 4096) 48 us in bf16, 49 with pairs of 128
+//   64 x k shares       few tokens: (4, 4096, 4096) 7.5 us in 4 shares, 10.2 whole, 9.8 with pairs of 128
+//   pairs of 128        (512, 4096, 4096) 11.5 us, 13.3 with lone 128, 16.0 with pairs of 256
+//   lone 128            where pairs would need a second round: (777, 2504, 1000) 7.0 us against 9.8
+//   pairs of 256 / 192  (4096, 4096, 4096) 54 us in bf16, 57 with pairs of 128; 60 in fp32, 66 with pairs of 128
 // a call lies on.
-struct MmKernel { const void *fn; int bn, ctas, form, odt, smem; float start, step, tile; };
-#define LGN_MM(BN, C, F, O, A, S, T) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, C, F, O>), BN, C, F, O, MmShape<BN, C, O>::kSmem, A, S, T}
+struct MmKernel { const void *fn; int bn, ctas, form, odt, smem, box; float start, step, tile; };
+#define LGN_MM(BN, C, F, O, A, S, T) {reinterpret_cast<const void *>(&fp8_matmul_kernel<BN, C, F, O>), BN, C, F, O, MmShape<BN, C, O>::kSmem, MmShape<BN, C, O>::kBoxRows, A, S, T}
 static const MmKernel kMmKernels[] = {
     LGN_MM(64, 1, kFormSwap, LGN_F32, 2.4f, 0.2f, 0.4f), LGN_MM(64, 1, kFormSplit, LGN_F32, 2.4f, 0.2f, 0.4f),
     LGN_MM(64, 1, kFormSwap, LGN_BF16, 2.4f, 0.2f, 0.1f), LGN_MM(64, 1, kFormSplit, LGN_BF16, 2.4f, 0.2f, 0.1f),
@@ -590,7 +614,7 @@ static const MmKernel kMmKernels[] = {
     LGN_MM(128, 1, kFormRows, LGN_BF16, 3.0f, 0.24f, 0.4f), LGN_MM(128, 1, kFormSwap, LGN_BF16, 3.0f, 0.24f, 0.7f),
     LGN_MM(128, 2, kFormRows, LGN_F32, 3.2f, 0.18f, 1.3f), LGN_MM(128, 2, kFormSwap, LGN_F32, 3.2f, 0.18f, 1.6f),
     LGN_MM(128, 2, kFormRows, LGN_BF16, 3.2f, 0.17f, 0.9f), LGN_MM(128, 2, kFormSwap, LGN_BF16, 3.2f, 0.17f, 1.2f),
-    LGN_MM(192, 2, kFormRows, LGN_F32, 3.3f, 0.23f, 2.7f), LGN_MM(192, 2, kFormSwap, LGN_F32, 3.3f, 0.23f, 3.0f),
+    LGN_MM(192, 2, kFormRows, LGN_F32, 3.3f, 0.22f, 2.2f), LGN_MM(192, 2, kFormSwap, LGN_F32, 3.3f, 0.22f, 2.5f),
     LGN_MM(256, 2, kFormRows, LGN_BF16, 3.3f, 0.3f, 1.1f), LGN_MM(256, 2, kFormSwap, LGN_BF16, 3.3f, 0.3f, 1.4f)};
 #undef LGN_MM
 constexpr int kMmCount = (int)(sizeof kMmKernels / sizeof kMmKernels[0]);
@@ -762,7 +786,7 @@ static lgn_status matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt, con
         return LGN_ERR_UNSUPPORTED;                                             // TMA coordinates are 32-bit
     CUtensorMap mr, mc, sr, sc, mo = {};
     if (q.form == kFormRows && !make_out_map(&mo, out, m, n, ldo, out_dt)) return LGN_ERR_CUDA;
-    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, bn / (uint32_t)q.ctas)) return LGN_ERR_CUDA;
+    if (!make_map(&mr, cr, p.rows, k, 128) || !make_map(&mc, cc, p.cols, k, (uint32_t)q.box)) return LGN_ERR_CUDA;
     if (!make_scale_map(&sr, swap ? b_scales : a_scales, (uint64_t)((p.rows + 127) / 128) * p.groups) ||
         !make_scale_map(&sc, swap ? a_scales : b_scales, (uint64_t)((p.cols + 127) / 128) * p.groups)) return LGN_ERR_CUDA;
     if (!allow_smem(plan.kernel)) return LGN_ERR_CUDA;
