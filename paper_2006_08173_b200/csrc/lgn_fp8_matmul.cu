@@ -115,11 +115,7 @@ __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volat
         if (clock64() - t0 > kMmWaitClocks) { *stop = 1u; return false; }
     }
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
-    if (mbar_try(bar, parity)) return true;
-    return mbar_wait_slow(bar, parity, stop);
-}
-// The same for a whole warp, with a result that is uniform to the compiler too.
+// For a whole warp: all lanes take the same way, whatever each of them saw first, a barrier that completes or the flag.
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
     if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
     return __all_sync(0xffffffffu, mbar_wait_slow(bar, parity, stop));
@@ -322,8 +318,8 @@ __device__ __forceinline__ bool drain_tile(uint32_t tmem_at, uint32_t steps, uin
     }
     auto add = [&](float *to) {
         const uint32_t acc = n % S::kAccs;
-        if (!mbar_wait(acc_full(acc), (n / S::kAccs) & 1, stop)) return false;
-        __syncwarp();
+        if (!mbar_wait_warp(acc_full(acc), (n / S::kAccs) & 1, stop)) return false;
+        __syncwarp();                                      // after a `put` that lanes outside the output passed over, too
         fence_after();
         #pragma unroll
         for (int c = 0; c < kCols; c += 16) {
