@@ -514,11 +514,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
                     }
                 }
             }
-            if (!ok) {
-                if (elect_one()) mma_commit<CTAS>(drained);
-                __syncwarp();
-                mbar_drain(drained, 0);
-            }
         }
     } else {
         dep_wait();                                                             // the output may belong to work before this call
@@ -573,7 +568,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
     }
     fence_before();
     __syncthreads();
-    if (stop && warp == 8 && leader)                                            // a wait ran out: the copies in flight, of both CTAs, end first
+    // a wait ran out, whichever role's: the MMAs and the copies in flight, of both CTAs, end first
+    if (stop && warp == 9 && leader) {
+        if (elect_one()) mma_commit<CTAS>(drained);
+        __syncwarp();
+        mbar_drain(drained, 0);
+    }
+    if (stop && warp == 8 && leader)
         for (uint32_t b = issued > (uint32_t)S::kStages ? issued - S::kStages : 0; b < issued; ++b)
             mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
     if constexpr (CTAS == 2 || FORM == kFormSplit) cluster_sync();              // nothing of the other CTAs is in flight any more
