@@ -455,6 +455,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_rows, const __grid_con
         }
         issued = it;
     } else if (warp == 9) {
+        dep_wait();                                         // the limit of the waits below is for this kernel's work, not for what runs before it
         if (leader) {
             const uint32_t idesc0 = (p.fmt_rows << 7) | (p.fmt_cols << 10) | ((uint32_t)(S::kMmaN >> 3) << 17) | (1u << 23) | ((uint32_t)CTAS << 27);
             const uint64_t desc0 = desc_codes(smem0);
