@@ -212,6 +212,17 @@ def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _elsewhere(device: int, stream, *others) -> bool:
+    """Whether ``device``, that of a call's first tensor, is not the current one, so that the call has to be made under
+    torch.cuda.device(device).  ``others``: the device numbers of its other tensors, None for those not given."""
+    for d in others:
+        if d is not None and d != device:
+            raise ValueError(f"tensors on different devices: {device} and {d}")
+    if stream is not None and isinstance(stream, torch.cuda.Stream) and stream.device_index != device:
+        raise ValueError(f"a stream of device {stream.device_index} for tensors on device {device}")
+    return device != _current_device()
+
+
 # --------------------------------------------------------------------------- sizes
 def lgn_workspace_bytes(n_per_layer: Sequence[int]) -> int:
     arr = (_u64 * max(1, len(n_per_layer)))(*n_per_layer)
@@ -508,7 +519,7 @@ class Fp8Operand:
 
     codes   uint8, lgn_fp8_codes_bytes(rows, k), rows padded to a multiple of 16
     scales  uint8, lgn_fp8_scales_bytes(rows, k), in the order lgn.h describes"""
-    __slots__ = ("rows", "k", "fmt", "_codes", "_scales", "_buffer", "_codes_ptr", "_scales_ptr")
+    __slots__ = ("rows", "k", "fmt", "_codes", "_scales", "_buffer", "_codes_ptr", "_scales_ptr", "_device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int, fmt: int):
         need_codes, need_scales = _fp8_bytes(rows, k)
@@ -519,6 +530,9 @@ class Fp8Operand:
                 raise ValueError(f"{what} shorter than the extents need")
         self.rows, self.k, self.fmt, self._codes, self._scales, self._buffer = rows, k, fmt, codes, scales, None
         self._codes_ptr, self._scales_ptr = codes.data_ptr(), scales.data_ptr()
+        self._device = codes.get_device()
+        if scales.get_device() != self._device:
+            raise ValueError("codes and scales on different devices")
 
     @classmethod
     def empty(cls, rows: int, k: int, fmt: int, device, stream=None) -> "Fp8Operand":
@@ -530,6 +544,7 @@ class Fp8Operand:
         o._buffer = buffer = torch.empty(total, dtype=_uint8, device=device) if stream is None else _empty(total, _uint8, device, stream)
         o._codes_ptr = at = buffer.data_ptr()
         o._scales_ptr = at + codes
+        o._device = buffer.get_device()
         return o
 
     @property
@@ -589,6 +604,10 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
     rows, cols, ld = _matrix3(x, "x")
     if not (rowwise or transposed):
         raise ValueError("neither the operand nor its transpose is asked for")
+    device = x.get_device()
+    if _elsewhere(device, stream, out._device if out is not None else None, out_t._device if out_t is not None else None):
+        with torch.cuda.device(device):
+            return lgn_fp8_quantize(x, fmt, block, rowwise, transposed, out, out_t, stream)
     q = t = pq = sq = pt = st = None
     if rowwise:
         if out is None:
@@ -607,7 +626,7 @@ def lgn_fp8_quantize(x: torch.Tensor, fmt: int = E4M3, block: int = BLOCK_ROW, r
                 raise ValueError("out_t: extents or format differ from the transpose")
         pt, st = t._codes_ptr, t._scales_ptr
     code = _lib.lgn_fp8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), fmt, block, pq, sq, pt, st,
-                                 _raw_stream(_current_device()) if stream is None else _stream(stream))
+                                 _raw_stream(device) if stream is None else _stream(stream))
     if code != LGN_OK:
         _check(code, "lgn_fp8_quantize")
     return q, t
@@ -620,11 +639,14 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
     m, k, n = a.rows, a.k, b.rows
     if k != b.k:
         raise ValueError("operands contract over different extents")
+    device = a._device
+    if _elsewhere(device, stream, b._device, out.get_device() if out is not None else None, status.get_device() if status is not None else None):
+        with torch.cuda.device(device):
+            return lgn_fp8_matmul(a, b, out, out_dtype, accumulate, status, stream)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        device = (a._codes if a._buffer is None else a._buffer).device
-        out = torch.empty((m, n), dtype=out_dtype, device=device) if stream is None else _empty((m, n), out_dtype, device, stream)
+        out = torch.empty((m, n), dtype=out_dtype, device=a.device) if stream is None else _empty((m, n), out_dtype, a.device, stream)
         ldo = n or 1
     else:
         if tuple(out.shape) != (m, n):
@@ -633,7 +655,7 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
     code = _lib.lgn_fp8_matmul(a._codes_ptr, a._scales_ptr, a.fmt, b._codes_ptr, b._scales_ptr, b.fmt,
                                m, n, k, out.data_ptr() or None, ldo, dtype_code(out), 1 if accumulate else 0,
                                _dev(status, "status") if status is not None else None,
-                               _raw_stream(_current_device()) if stream is None else _stream(stream))
+                               _raw_stream(device) if stream is None else _stream(stream))
     if code != LGN_OK:
         _check(code, "lgn_fp8_matmul")
     return out
@@ -643,6 +665,9 @@ def lgn_selftest_matmul_wait_expires(a: Fp8Operand, b: Fp8Operand, out: torch.Te
     """A product whose first copies are withheld: ``status`` must become LGN_ERR_TIMEOUT after a few seconds."""
     if (a.fmt, b.fmt, a.k) != (E4M3, E4M3, b.k) or tuple(out.shape) != (a.rows, b.rows):
         raise ValueError("E4M3 operands and an out of a.rows x b.rows")
+    if _elsewhere(a._device, stream, b._device, out.get_device(), status.get_device()):
+        with torch.cuda.device(a._device):
+            return lgn_selftest_matmul_wait_expires(a, b, out, status, stream)
     _check(_lib.lgn_selftest_matmul_wait_expires(a._codes_ptr, a._scales_ptr, b._codes_ptr, b._scales_ptr, a.rows, b.rows, a.k,
                                                  _dev(out, "out"), dtype_code(out), _dev(status, "status"), _stream(stream)),
            "lgn_selftest_matmul_wait_expires")
@@ -662,6 +687,11 @@ def lgn_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ou
     one element to which the number of ids outside the table is added."""
     vocab, dim, ld = _matrix3(table, "table")
     n = ids.numel()
+    device = table.get_device()
+    if _elsewhere(device, stream, ids.get_device(), out.get_device() if out is not None else None,
+                  n_outside.get_device() if n_outside is not None else None):
+        with torch.cuda.device(device):
+            return lgn_embedding(table, ids, scale, out, out_dtype, n_outside, stream)
     if out is None:
         out = _empty((n, dim), out_dtype or table.dtype, table.device, stream)
         ldo = dim or 1
@@ -689,6 +719,10 @@ def lgn_embedding_grad(dout: torch.Tensor, ids: torch.Tensor, vocab: int, scale:
     n, dim = dout.shape
     if ids.numel() != n:
         raise ValueError("dout must have one row per id")
+    device = dout.get_device()
+    if _elsewhere(device, stream, ids.get_device(), out.get_device() if out is not None else None, ws.get_device() if ws is not None else None):
+        with torch.cuda.device(device):
+            return lgn_embedding_grad(dout, ids, vocab, scale, padding_idx, out, out_dtype, accumulate, ws, stream)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -710,6 +744,7 @@ class Grads(NamedTuple):
     array: C.Array
     count: int
     tensors: tuple           # keeps them alive
+    device: Optional[int]    # None: no tensors
 
 
 def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> Grads:
@@ -718,11 +753,14 @@ def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
     if len(outs) != len(grads):
         raise ValueError("one out per gradient")
     arr = (GradT * max(1, len(grads)))()
+    devices = {t.get_device() for t in (*grads, *outs)}
+    if len(devices) > 1:
+        raise ValueError(f"tensors on different devices: {sorted(devices)}")
     for i, (g, o) in enumerate(zip(grads, outs)):
         if o.numel() != g.numel() or o.dtype != g.dtype:
             raise ValueError("out must have its gradient's size and type")
         arr[i] = GradT(_dev(g, "gradient") or None, _dev(o, "out") or None, g.numel(), dtype_code(g), 0)
-    return Grads(arr, len(grads), (tuple(grads), tuple(outs)))
+    return Grads(arr, len(grads), (tuple(grads), tuple(outs)), devices.pop() if devices else None)
 
 
 def new_norm_record(device) -> torch.Tensor:
@@ -758,16 +796,28 @@ def _record(record: torch.Tensor) -> int:
 
 def lgn_grad_norm(grads: Grads, record: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """The record of the tensors' global norm; nothing is scaled."""
+    device = record.get_device()
+    if _elsewhere(device, stream, grads.device, ws.get_device()):
+        with torch.cuda.device(device):
+            return lgn_grad_norm(grads, record, ws, stream)
     _check(_lib.lgn_grad_norm(grads.array, grads.count, _record(record), _dev(ws, "ws"), ws.numel() * ws.element_size(),
                               _stream(stream)), "lgn_grad_norm")
 
 
 def lgn_clip_grad_norm(grads: Grads, max_norm: float, record: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """The record, and every tensor scaled by min(1, max_norm / norm); no host round trip."""
+    device = record.get_device()
+    if _elsewhere(device, stream, grads.device, ws.get_device()):
+        with torch.cuda.device(device):
+            return lgn_clip_grad_norm(grads, max_norm, record, ws, stream)
     _check(_lib.lgn_clip_grad_norm(grads.array, grads.count, float(max_norm), _record(record), _dev(ws, "ws"),
                                    ws.numel() * ws.element_size(), _stream(stream)), "lgn_clip_grad_norm")
 
 
 def lgn_clip_apply(grads: Grads, max_norm: float, record: torch.Tensor, stream=None) -> None:
     """Every tensor scaled by the norm that the record's sum of squares gives."""
+    device = record.get_device()
+    if _elsewhere(device, stream, grads.device):
+        with torch.cuda.device(device):
+            return lgn_clip_apply(grads, max_norm, record, stream)
     _check(_lib.lgn_clip_apply(grads.array, grads.count, float(max_norm), _record(record), _stream(stream)), "lgn_clip_apply")

@@ -19,7 +19,8 @@ def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
     g = dy.contiguous()
     out = torch.empty_like(g)
     results, ws = lgn.new_results(1, g.device), lgn.new_workspace([g.numel()], g.device)
-    lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=sparsity, seed=seed)], results, ws)
+    with torch.cuda.device(g.device):                                  # the grouped call takes the current device's stream
+        lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=sparsity, seed=seed)], results, ws)
     return out
 
 
