@@ -6,7 +6,7 @@ The modules marshal arguments for ``binding``; there is no CPU path.
 """
 from __future__ import annotations
 
-from typing import List, Sequence
+from typing import List, Optional, Sequence
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -102,22 +102,34 @@ class Embedding(torch.nn.Module):
 
 class GradClipper:
     """Clips the gradients of a fixed list of parameters by their global norm, in place, without a host round
-    trip.  The gradients have to exist and to stay where they are (zero_grad(set_to_none=False))."""
+    trip.  A gradient has to stay where it is from the first clip() that finds it (zero_grad(set_to_none=False)); a
+    parameter without one yet takes part from the step that brings it."""
 
     def __init__(self, parameters: Sequence[torch.nn.Parameter], max_norm: float):
-        self._params = [p for p in parameters if p.grad is not None]
-        self._grads: List[torch.Tensor] = [p.grad for p in self._params]
-        if not self._grads:
+        self._params, self.max_norm = list(parameters), float(max_norm)
+        self._grads: List[Optional[torch.Tensor]] = [None] * len(self._params)
+        self._take()
+        if self._list.count == 0:
             raise ValueError("no parameter has a gradient yet")
-        self._list, self.max_norm = lgn.make_grads(self._grads), float(max_norm)
-        self._places = [g.data_ptr() for g in self._grads]
-        self.record = lgn.new_norm_record(self._grads[0].device)
-        self._ws = lgn.new_clip_workspace(self._grads[0].device, len(self._grads))
+        device = next(g for g in self._grads if g is not None).device
+        self.record = lgn.new_norm_record(device)
+        self._ws = lgn.new_clip_workspace(device, len(self._params))
+
+    def _take(self) -> None:
+        """Descriptors of the gradients that there are."""
+        self._grads = [p.grad for p in self._params]
+        self._list = lgn.make_grads([g for g in self._grads if g is not None])
+        self._places = [None if g is None else g.data_ptr() for g in self._grads]
 
     def clip(self, stream=None) -> torch.Tensor:
         """Scales the gradients; returns their norm before it, a scalar on the device."""
+        more = False
         for p, g, at in zip(self._params, self._grads, self._places):
-            if p.grad is not g or g.data_ptr() != at:
+            if g is None:
+                more = more or p.grad is not None
+            elif p.grad is not g or g.data_ptr() != at:
                 raise RuntimeError("a gradient has been replaced since the clipper was made")
+        if more:
+            self._take()
         lgn.lgn_clip_grad_norm(self._list, self.max_norm, self.record, self._ws, stream)
         return lgn.norm_of(self.record)
