@@ -49,7 +49,7 @@ def train(steps: int = 60, sparsity: float = 0.5, vocab: int = 1000, dim: int = 
         loss.backward()
         if clipper is None:
             clipper = GradClipper(list(model.parameters()), max_norm)
-        norms.append(clipper.clip().clone())
+        norms.append(clipper.clip())
         opt.step()
         for layer in (model.up, model.down):
             layer.advance()

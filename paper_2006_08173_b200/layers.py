@@ -111,9 +111,9 @@ class GradClipper:
         self._take()
         if self._list.count == 0:
             raise ValueError("no parameter has a gradient yet")
-        device = next(g for g in self._grads if g is not None).device
-        self.record = lgn.new_norm_record(device)
-        self._ws = lgn.new_clip_workspace(device, len(self._params))
+        self._device = next(g for g in self._grads if g is not None).device
+        self.record = lgn.new_norm_record(self._device)
+        self._ws = lgn.new_clip_workspace(self._device, len(self._params))
 
     def _take(self) -> None:
         """Descriptors of the gradients that there are."""
@@ -122,7 +122,8 @@ class GradClipper:
         self._places = [None if g is None else g.data_ptr() for g in self._grads]
 
     def clip(self, stream=None) -> torch.Tensor:
-        """Scales the gradients; returns their norm before it, a scalar on the device."""
+        """Scales the gradients; returns their norm before it, a scalar on the device that later calls leave alone.  It is part
+        of the call's record, which is ``record`` until the next call."""
         more = False
         for p, g, at in zip(self._params, self._grads, self._places):
             if g is None:
@@ -131,5 +132,8 @@ class GradClipper:
                 raise RuntimeError("a gradient has been replaced since the clipper was made")
         if more:
             self._take()
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), self._device)
+        self.record = lgn._empty(self.record.shape, torch.uint8, self._device, stream)
         lgn.lgn_clip_grad_norm(self._list, self.max_norm, self.record, self._ws, stream)
         return lgn.norm_of(self.record)

@@ -35,3 +35,19 @@ def test_a_gradient_that_comes_later_takes_part(layers):
     with pytest.raises(RuntimeError):
         c.grad = torch.ones(16, device="cuda")
         clip.clip()
+
+
+def test_norms_of_several_steps_are_kept(layers):
+    """On the current stream, another one, and one given by its handle."""
+    (p,) = parameters(4)
+    p.grad = torch.zeros(4, device="cuda")
+    clip = layers.GradClipper([p], 100.0)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    norms = []
+    for step, stream in enumerate([None, None, other, other, other.cuda_stream, other.cuda_stream, None]):
+        p.grad.fill_(float(step))
+        torch.cuda.synchronize()
+        norms.append(clip.clip(stream))
+        torch.cuda.synchronize()
+    assert [float(n) for n in norms] == [0.0, 2.0, 4.0, 6.0, 8.0, 10.0, 12.0]
