@@ -17,6 +17,8 @@ from . import binding as lgn
 def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
     """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics."""
     g = dy.contiguous()
+    if g.data_ptr() % 32 != 0:                                         # a contiguous slice, as the backward pass of torch.cat hands over
+        g = g.clone()
     out = torch.empty_like(g)
     results, ws = lgn.new_results(1, g.device), lgn.new_workspace([g.numel()], g.device)
     with torch.cuda.device(g.device):                                  # the grouped call takes the current device's stream
