@@ -573,6 +573,8 @@ def _matrix3(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
         raise ValueError(f"{what} must be a CUDA matrix")
     rows, cols = shape
     ld, step = t.stride()
+    if rows == 0 or cols == 0:                             # strides without a meaning: an expanded scalar's are 0
+        return rows, cols, cols or 1
     if cols > 1 and step != 1:
         raise ValueError(f"{what} must be a matrix with contiguous rows")
     if rows <= 1:
