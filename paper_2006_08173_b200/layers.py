@@ -14,6 +14,13 @@ from torch.autograd.function import once_differentiable
 from . import binding as lgn
 
 
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """A matrix with contiguous rows that do not overlap: ``t`` as it is, or (transposed, broadcast) a copy."""
+    if t.size(1) > 1 and t.stride(1) != 1 or t.size(0) > 1 and t.stride(0) < t.size(1):
+        return t.contiguous()
+    return t
+
+
 def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
     """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics."""
     g = dy.contiguous()
@@ -29,8 +36,8 @@ def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
 class _LinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, sparsity, seed):
-        wq, wqt = lgn.lgn_fp8_quantize(weight, lgn.E4M3, lgn.BLOCK_SQUARE, transposed=True)
-        xq, xqt = lgn.lgn_fp8_quantize(x, lgn.E4M3, transposed=True)
+        wq, wqt = lgn.lgn_fp8_quantize(_rows(weight), lgn.E4M3, lgn.BLOCK_SQUARE, transposed=True)
+        xq, xqt = lgn.lgn_fp8_quantize(_rows(x), lgn.E4M3, transposed=True)
         ctx.wqt, ctx.xqt, ctx.sparsity, ctx.seed, ctx.dtypes = wqt, xqt, sparsity, seed, (x.dtype, weight.dtype)
         return lgn.lgn_fp8_matmul(xq, wq, out_dtype=x.dtype)
 
@@ -42,9 +49,7 @@ class _LinearFn(torch.autograd.Function):
             return None, None, None, None
         if ctx.sparsity > 0.0:
             dy = _pruned(dy, ctx.sparsity, ctx.seed)
-        elif dy.stride(-1) != 1 or (dy.size(0) > 1 and dy.stride(0) < dy.size(1)):
-            dy = dy.contiguous()                                       # a broadcast gradient
-        dq, dqt = lgn.lgn_fp8_quantize(dy, lgn.E5M2, rowwise=need_dx, transposed=need_dw)
+        dq, dqt = lgn.lgn_fp8_quantize(_rows(dy), lgn.E5M2, rowwise=need_dx, transposed=need_dw)
         dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0]) if need_dx else None
         dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1]) if need_dw else None
         return dx, dw, None, None
@@ -74,16 +79,14 @@ class _EmbeddingFn(torch.autograd.Function):
     def forward(ctx, weight, ids, scale, padding_idx, out_dtype):
         ctx.save_for_backward(ids)
         ctx.args = (weight.shape[0], scale, padding_idx, weight.dtype)
-        return lgn.lgn_embedding(weight, ids, scale, out_dtype=out_dtype)
+        return lgn.lgn_embedding(_rows(weight), ids, scale, out_dtype=out_dtype)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
         (ids,) = ctx.saved_tensors
         vocab, scale, padding_idx, dtype = ctx.args
-        if dout.stride(-1) != 1 or (dout.size(0) > 1 and dout.stride(0) < dout.size(1)):
-            dout = dout.contiguous()
-        return lgn.lgn_embedding_grad(dout, ids, vocab, scale, padding_idx, out_dtype=dtype), None, None, None, None
+        return lgn.lgn_embedding_grad(_rows(dout), ids, vocab, scale, padding_idx, out_dtype=dtype), None, None, None, None
 
 
 class Embedding(torch.nn.Module):
