@@ -54,6 +54,8 @@ def train(steps: int = 60, sparsity: float = 0.5, vocab: int = 1000, dim: int = 
         for layer in (model.up, model.down):
             layer.advance()
         losses.append(loss.detach())
+    for layer in (model.up, model.down, model.head):
+        layer.check()
     return torch.stack(losses).tolist(), torch.stack(norms).tolist()
 
 

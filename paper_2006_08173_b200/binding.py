@@ -416,6 +416,12 @@ def new_results(num_layers: int, device) -> torch.Tensor:
     return torch.zeros(max(1, num_layers) * C.sizeof(LayerResultT), dtype=torch.uint8, device=device)
 
 
+def status_of(results_dev: torch.Tensor, k: int = 0) -> torch.Tensor:
+    """Layer k's status as an int32 tensor of one element on the device (a view)."""
+    at = (k * C.sizeof(LayerResultT) + LayerResultT.status.offset) // 4
+    return results_dev.view(torch.int32)[at:at + 1]
+
+
 def read_results(results_dev: torch.Tensor, num_layers: int) -> List[Dict]:
     """Host copy of the per-layer results (synchronises)."""
     buf = results_dev.cpu().numpy().tobytes()

@@ -6,7 +6,7 @@ The modules marshal arguments for ``binding``; there is no CPU path.
 """
 from __future__ import annotations
 
-from typing import List, Optional, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -21,8 +21,9 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     return t
 
 
-def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
-    """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics."""
+def _pruned(dy: torch.Tensor, sparsity: float, seed: int, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics.  ``status``: int32
+    word on the device that keeps the highest status seen."""
     g = dy.contiguous()
     if g.data_ptr() % 32 != 0:                                         # a contiguous slice, as the backward pass of torch.cat hands over
         g = g.clone()
@@ -30,47 +31,63 @@ def _pruned(dy: torch.Tensor, sparsity: float, seed: int) -> torch.Tensor:
     results, ws = lgn.new_results(1, g.device), lgn.new_workspace([g.numel()], g.device)
     with torch.cuda.device(g.device):                                  # the grouped call takes the current device's stream
         lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=sparsity, seed=seed)], results, ws)
+    if status is not None:
+        torch.maximum(status, lgn.status_of(results), out=status)
     return out
 
 
 class _LinearFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, sparsity, seed):
+    def forward(ctx, x, weight, sparsity, seed, status):
         wq, wqt = lgn.lgn_fp8_quantize(_rows(weight), lgn.E4M3, lgn.BLOCK_SQUARE, transposed=True)
         xq, xqt = lgn.lgn_fp8_quantize(_rows(x), lgn.E4M3, transposed=True)
-        ctx.wqt, ctx.xqt, ctx.sparsity, ctx.seed, ctx.dtypes = wqt, xqt, sparsity, seed, (x.dtype, weight.dtype)
-        return lgn.lgn_fp8_matmul(xq, wq, out_dtype=x.dtype)
+        ctx.wqt, ctx.xqt, ctx.sparsity, ctx.seed, ctx.status, ctx.dtypes = wqt, xqt, sparsity, seed, status, (x.dtype, weight.dtype)
+        return lgn.lgn_fp8_matmul(xq, wq, out_dtype=x.dtype, status=status)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         need_dx, need_dw = ctx.needs_input_grad[:2]
         if not (need_dx or need_dw):
-            return None, None, None, None
+            return None, None, None, None, None
         if ctx.sparsity > 0.0:
-            dy = _pruned(dy, ctx.sparsity, ctx.seed)
+            dy = _pruned(dy, ctx.sparsity, ctx.seed, ctx.status)
         dq, dqt = lgn.lgn_fp8_quantize(_rows(dy), lgn.E5M2, rowwise=need_dx, transposed=need_dw)
-        dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0]) if need_dx else None
-        dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1]) if need_dw else None
-        return dx, dw, None, None
+        dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0], status=ctx.status) if need_dx else None
+        dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1], status=ctx.status) if need_dw else None
+        return dx, dw, None, None, None
 
 
 class Fp8Linear(torch.nn.Module):
     """y = x W^T with x, W and the incoming gradient in 8-bit floating point (E4M3, E4M3, E5M2; one power-of-two
     scale per block of 128), fp32 sums.  ``sparsity`` > 0 prunes the incoming gradient to that fraction of zeros
-    before the two backward products; ``seed`` changes from step to step (advance())."""
+    before the two backward products; ``seed`` changes from step to step (advance()).  The waits on the device are
+    bounded; check() tells whether one ran out."""
 
     def __init__(self, in_features: int, out_features: int, sparsity: float = 0.0, device=None):
         super().__init__()
         self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device))
         torch.nn.init.normal_(self.weight, std=in_features ** -0.5)
         self.sparsity, self.seed = float(sparsity), 0
+        self._status: Dict[torch.device, torch.Tensor] = {}            # an int32 word on each device a pass has run on
 
     def advance(self) -> None:
         self.seed += 1
 
+    def check(self) -> None:
+        """Raises LgnError (LGN_ERR_TIMEOUT) if a device-side wait of the passes since the last check ran out: what they
+        computed is then not valid.  Waits for the device."""
+        codes = []
+        for word in self._status.values():
+            codes.append(int(word.item()))
+            word.zero_()
+        if any(codes):
+            raise lgn.LgnError(max(codes), "Fp8Linear")
+
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        y = _LinearFn.apply(x.reshape(-1, x.shape[-1]), self.weight, self.sparsity, self.seed)
+        if x.device not in self._status:
+            self._status[x.device] = torch.zeros(1, dtype=torch.int32, device=x.device)
+        y = _LinearFn.apply(x.reshape(-1, x.shape[-1]), self.weight, self.sparsity, self.seed, self._status[x.device])
         return y.reshape(*x.shape[:-1], self.weight.shape[0])
 
 
