@@ -22,7 +22,8 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
 
 
 def _pruned(dy: torch.Tensor, sparsity: float, seed: int, status: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics.  ``status``: int32
+    """Stochastic pruning of a neural gradient to the requested sparsity, threshold from its own statistics.  Entries that are
+    not finite come out as NaN (the threshold is then without a meaning, and so are the others).  ``status``: int32
     word on the device that keeps the highest status seen."""
     g = dy.contiguous()
     if g.data_ptr() % 32 != 0:                                         # a contiguous slice, as the backward pass of torch.cat hands over
@@ -31,6 +32,7 @@ def _pruned(dy: torch.Tensor, sparsity: float, seed: int, status: Optional[torch
     results, ws = lgn.new_results(1, g.device), lgn.new_workspace([g.numel()], g.device)
     with torch.cuda.device(g.device):                                  # the grouped call takes the current device's stream
         lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=sparsity, seed=seed)], results, ws)
+    out.add_(g, alpha=0.0)                                             # adds 0, or NaN: pruning is for finite values and may drop others
     if status is not None:
         torch.maximum(status, lgn.status_of(results), out=status)
     return out

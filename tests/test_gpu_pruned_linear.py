@@ -30,3 +30,24 @@ def test_a_slice_of_a_larger_gradient(layers, rows, dtype):
     torch.cat([other, lin(x)]).backward(up)
     plain(x).backward(layers._pruned(up[rows:].clone(), 0.5, 0))
     assert torch.equal(lin.weight.grad, plain.weight.grad)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_non_finite_gradients_stay_visible(layers, bad, dtype):
+    """As without pruning: in the row of the input gradient and the row of the weight gradient that they meet."""
+    torch.manual_seed(1)
+    lin, plain = pair(layers, 64, 48, 0.6)
+    for layer in (lin, plain):
+        x = torch.randn(40, 64, device="cuda").to(dtype).requires_grad_()
+        up = torch.exp(torch.randn(40, 48, device="cuda") - 8).to(dtype)
+        up[7, 5] = bad
+        layer(x).backward(up)
+        assert bool((~torch.isfinite(x.grad[7])).all()) and bool((~torch.isfinite(layer.weight.grad[5])).all())
+
+
+def test_finite_gradients_are_what_the_library_prunes_them_to(lgn, layers):
+    g = torch.exp(2 * torch.randn(300, 100, device="cuda") - 12) * torch.randn(300, 100, device="cuda").sign()
+    out, res, ws = torch.empty_like(g), lgn.new_results(1, "cuda"), lgn.new_workspace([g.numel()], "cuda")
+    lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=0.7, seed=9)], res, ws)
+    assert torch.equal(layers._pruned(g, 0.7, 9), out)
