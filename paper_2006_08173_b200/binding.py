@@ -550,6 +550,8 @@ class Fp8Operand:
         o._buffer = buffer = torch.empty(total, dtype=_uint8, device=device) if stream is None else _empty(total, _uint8, device, stream)
         o._codes_ptr = at = buffer.data_ptr()
         o._scales_ptr = at + codes
+        if not buffer.is_cuda:
+            raise ValueError("operands are CUDA memory")
         o._device = buffer.get_device()
         return o
 
