@@ -195,6 +195,14 @@ def _dev(t: torch.Tensor, what: str) -> int:
     return t.data_ptr()
 
 
+def _word(t: torch.Tensor, size: int, what: str) -> int:
+    """The address of a tensor that one value of ``size`` bytes is written to."""
+    at = _dev(t, what)
+    if t.numel() * t.element_size() < size:
+        raise ValueError(f"{what} must hold {size} bytes")
+    return at
+
+
 def _stream(stream) -> int:
     if stream is None:          # the current stream of the current device, without a Stream object (3.5 us -> 0.2 us a call)
         return _raw_stream(_current_device())
@@ -664,7 +672,7 @@ def lgn_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out: Optional[torch.Tensor] = N
         ldo = _matrix(out, "out")
     code = _lib.lgn_fp8_matmul(a._codes_ptr, a._scales_ptr, a.fmt, b._codes_ptr, b._scales_ptr, b.fmt,
                                m, n, k, out.data_ptr() or None, ldo, dtype_code(out), 1 if accumulate else 0,
-                               _dev(status, "status") if status is not None else None,
+                               _word(status, 4, "status") if status is not None else None,
                                _raw_stream(device) if stream is None else _stream(stream))
     if code != LGN_OK:
         _check(code, "lgn_fp8_matmul")
@@ -679,7 +687,7 @@ def lgn_selftest_matmul_wait_expires(a: Fp8Operand, b: Fp8Operand, out: torch.Te
         with torch.cuda.device(a._device):
             return lgn_selftest_matmul_wait_expires(a, b, out, status, stream)
     _check(_lib.lgn_selftest_matmul_wait_expires(a._codes_ptr, a._scales_ptr, b._codes_ptr, b._scales_ptr, a.rows, b.rows, a.k,
-                                                 _dev(out, "out"), dtype_code(out), _dev(status, "status"), _stream(stream)),
+                                                 _dev(out, "out"), dtype_code(out), _word(status, 4, "status"), _stream(stream)),
            "lgn_selftest_matmul_wait_expires")
 
 
@@ -713,7 +721,7 @@ def lgn_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ou
         raise TypeError("n_outside is int64")
     _check(_lib.lgn_embedding(table.data_ptr() or None, vocab, dim, ld, dtype_code(table), _dev(ids, "ids") or None, _ids(ids), n,
                               float(scale), out.data_ptr() or None, ldo, dtype_code(out),
-                              _dev(n_outside, "n_outside") if n_outside is not None else None, _stream(stream)), "lgn_embedding")
+                              _word(n_outside, 8, "n_outside") if n_outside is not None else None, _stream(stream)), "lgn_embedding")
     return out
 
 
