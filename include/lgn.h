@@ -460,7 +460,8 @@ lgn_status lgn_embedding_grad(const void *dout, uint64_t ld_dout, lgn_dtype dout
  * norm = sqrt(sum of x^2 over all tensors); coef = max_norm / norm where the norm is finite and
  * above max_norm, else 1; out = x coef in fp32, rounded once to the tensor's type.  Tensors of different types may
  * be mixed, any element-aligned pointer is taken, n may be 0; out may be g itself (in place; nothing is written
- * when coef is 1) or must not overlap it.  A norm that is not finite leaves the values as they are; the record
+ * when coef is 1) or must not overlap it.  No out may overlap another tensor or its out (two CTAs would write there; not
+ * checked here, the tensors of one call being many).  A norm that is not finite leaves the values as they are; the record
  * says so.  Sums in a fixed order: the same bits on every run on the same type of device. */
 typedef struct {
     const void *g;         /* device, n elements of dt                                  */

@@ -7,6 +7,7 @@ module raises.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes as C
 import os
 from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple
@@ -763,6 +764,23 @@ class Grads(NamedTuple):
     count: int
     tensors: tuple           # keeps them alive
     device: Optional[int]    # None: no tensors
+    disjoint: bool           # no tensor's out shares memory with another tensor or its out
+
+
+def _disjoint(grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor]) -> bool:
+    span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+    writes = sorted((*span(o), i) for i, o in enumerate(outs) if o.numel())
+    if any(a[1] > b[0] for a, b in zip(writes, writes[1:])):
+        return False
+    starts = [w[0] for w in writes]
+    for i, g in enumerate(grads):
+        lo, hi = span(g)
+        for _, end, j in reversed(writes[:bisect.bisect_left(starts, hi)] if g.numel() else []):
+            if end <= lo:                                  # in order and disjoint: those before end earlier still
+                break
+            if j != i:
+                return False
+    return True
 
 
 def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> Grads:
@@ -778,7 +796,7 @@ def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
         if o.numel() != g.numel() or o.dtype != g.dtype:
             raise ValueError("out must have its gradient's size and type")
         arr[i] = GradT(_dev(g, "gradient") or None, _dev(o, "out") or None, g.numel(), dtype_code(g), 0)
-    return Grads(arr, len(grads), (tuple(grads), tuple(outs)), devices.pop() if devices else None)
+    return Grads(arr, len(grads), (tuple(grads), tuple(outs)), devices.pop() if devices else None, _disjoint(grads, outs))
 
 
 def new_norm_record(device) -> torch.Tensor:
@@ -828,6 +846,8 @@ def lgn_clip_grad_norm(grads: Grads, max_norm: float, record: torch.Tensor, ws: 
     if _elsewhere(device, stream, grads.device, ws.get_device()):
         with torch.cuda.device(device):
             return lgn_clip_grad_norm(grads, max_norm, record, ws, stream)
+    if not grads.disjoint:
+        raise ValueError("a tensor would be written over another one")
     _check(_lib.lgn_clip_grad_norm(grads.array, grads.count, float(max_norm), _record(record), _dev(ws, "ws"),
                                    ws.numel() * ws.element_size(), _stream(stream)), "lgn_clip_grad_norm")
 
@@ -838,4 +858,6 @@ def lgn_clip_apply(grads: Grads, max_norm: float, record: torch.Tensor, stream=N
     if _elsewhere(device, stream, grads.device):
         with torch.cuda.device(device):
             return lgn_clip_apply(grads, max_norm, record, stream)
+    if not grads.disjoint:
+        raise ValueError("a tensor would be written over another one")
     _check(_lib.lgn_clip_apply(grads.array, grads.count, float(max_norm), _record(record), _stream(stream)), "lgn_clip_apply")
