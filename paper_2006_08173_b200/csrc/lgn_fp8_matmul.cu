@@ -740,8 +740,8 @@ static lgn_status matmul(const void *a, const void *a_scales, lgn_fp8 a_fmt, con
     if (m > kFp8MaxDim || n > kFp8MaxDim || k > kFp8MaxDim) return LGN_ERR_UNSUPPORTED;
     if (m == 0 || n == 0) return LGN_OK;
     if (ldo < n || ldo > (1ull << 40)) return LGN_ERR_INVALID_ARG;
-    const uint64_t es = out_dt == LGN_F32 ? 4 : 2, ob = ((m - 1) * ldo + n) * es;
-    if (out == nullptr || !aligned_to(out, es) || !aligned_to(status_dev, 4)) return LGN_ERR_INVALID_ARG;
+    const uint64_t es = out_dt == LGN_F32 ? 4 : 2, ob = matrix_bytes(m, n, ldo, es);
+    if (ob == 0 || out == nullptr || !aligned_to(out, es) || !aligned_to(status_dev, 4)) return LGN_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (k == 0) {
         if (accumulate) return LGN_OK;

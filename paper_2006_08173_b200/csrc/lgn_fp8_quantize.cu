@@ -364,7 +364,8 @@ extern "C" lgn_status lgn_fp8_quantize(const void *x, uint64_t rows, uint64_t co
     if ((codes == nullptr) != (scales == nullptr) || (codes_t == nullptr) != (scales_t == nullptr)) return LGN_ERR_INVALID_ARG;
     if (codes == nullptr && codes_t == nullptr) return LGN_ERR_INVALID_ARG;
     if (!aligned_to(codes, 16) || !aligned_to(scales, 16) || !aligned_to(codes_t, 16) || !aligned_to(scales_t, 16)) return LGN_ERR_INVALID_ARG;
-    const uint64_t es = dt == LGN_F32 ? 4 : 2, xb = ((rows - 1) * ld + cols) * es;
+    const uint64_t es = dt == LGN_F32 ? 4 : 2, xb = matrix_bytes(rows, cols, ld, es);
+    if (xb == 0) return LGN_ERR_INVALID_ARG;
     struct { const void *p; uint64_t n; } b[5] = {
         {x, xb}, {codes, codes ? lgn_fp8_codes_bytes(rows, cols) : 0}, {scales, scales ? lgn_fp8_scales_bytes(rows, cols) : 0},
         {codes_t, codes_t ? lgn_fp8_codes_bytes(cols, rows) : 0}, {scales_t, scales_t ? lgn_fp8_scales_bytes(cols, rows) : 0}};

@@ -43,6 +43,13 @@ inline int sm_count() {
 
 inline bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Bytes from the first to the last element of a matrix (rows and cols > 0, ld >= cols), each extent up to 2^40; 0 if they are 2^62 or more,
+// which no memory has.
+inline uint64_t matrix_bytes(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t es) {
+    if ((rows - 1) > ((1ull << 62) / es - cols) / ld) return 0;
+    return ((rows - 1) * ld + cols) * es;
+}
+
 inline bool ranges_overlap(const void *a, uint64_t an, const void *b, uint64_t bn) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return an > 0 && bn > 0 && x < y + bn && y < x + an;
