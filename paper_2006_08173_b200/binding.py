@@ -552,15 +552,18 @@ class Fp8Operand:
     @classmethod
     def empty(cls, rows: int, k: int, fmt: int, device, stream=None) -> "Fp8Operand":
         """Uninitialised, codes and scales in one allocation; for use on ``stream`` (default: the current one)."""
-        o = cls.__new__(cls)
-        codes = rows * ((k + 15) & -16)                    # as in _fp8_bytes
-        total = codes + ((rows + 127) >> 7) * ((k + 511) >> 9) * 512 + 16
-        o.rows, o.k, o.fmt = rows, k, fmt
-        o._buffer = buffer = torch.empty(total, dtype=_uint8, device=device) if stream is None else _empty(total, _uint8, device, stream)
-        o._codes_ptr = at = buffer.data_ptr()
-        o._scales_ptr = at + codes
+        total = rows * ((k + 15) & -16) + ((rows + 127) >> 7) * ((k + 511) >> 9) * 512 + 16         # as in _fp8_bytes
+        return cls._of_buffer(torch.empty(total, dtype=_uint8, device=device) if stream is None else _empty(total, _uint8, device, stream), rows, k, fmt)
+
+    @classmethod
+    def _of_buffer(cls, buffer: torch.Tensor, rows: int, k: int, fmt: int) -> "Fp8Operand":
+        """The operand in an allocation that empty() made, or in a copy of it."""
         if not buffer.is_cuda:
             raise ValueError("operands are CUDA memory")
+        o = cls.__new__(cls)
+        o.rows, o.k, o.fmt, o._buffer = rows, k, fmt, buffer
+        o._codes_ptr = at = buffer.data_ptr()
+        o._scales_ptr = at + rows * ((k + 15) & -16)
         o._device = buffer.get_device()
         return o
 

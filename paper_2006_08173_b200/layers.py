@@ -43,7 +43,9 @@ class _LinearFn(torch.autograd.Function):
     def forward(ctx, x, weight, sparsity, seed, status):
         wq, wqt = lgn.lgn_fp8_quantize(_rows(weight), lgn.E4M3, lgn.BLOCK_SQUARE, transposed=True)
         xq, xqt = lgn.lgn_fp8_quantize(_rows(x), lgn.E4M3, transposed=True)
-        ctx.wqt, ctx.xqt, ctx.sparsity, ctx.seed, ctx.status, ctx.dtypes = wqt, xqt, sparsity, seed, status, (x.dtype, weight.dtype)
+        ctx.save_for_backward(wqt._buffer, xqt._buffer)
+        ctx.extents = [(q.rows, q.k, q.fmt) for q in (wqt, xqt)]
+        ctx.sparsity, ctx.seed, ctx.status, ctx.dtypes = sparsity, seed, status, (x.dtype, weight.dtype)
         return lgn.lgn_fp8_matmul(xq, wq, out_dtype=x.dtype, status=status)
 
     @staticmethod
@@ -52,11 +54,12 @@ class _LinearFn(torch.autograd.Function):
         need_dx, need_dw = ctx.needs_input_grad[:2]
         if not (need_dx or need_dw):
             return None, None, None, None, None
+        wqt, xqt = (lgn.Fp8Operand._of_buffer(t, *e) for t, e in zip(ctx.saved_tensors, ctx.extents))
         if ctx.sparsity > 0.0:
             dy = _pruned(dy, ctx.sparsity, ctx.seed, ctx.status)
         dq, dqt = lgn.lgn_fp8_quantize(_rows(dy), lgn.E5M2, rowwise=need_dx, transposed=need_dw)
-        dx = lgn.lgn_fp8_matmul(dq, ctx.wqt, out_dtype=ctx.dtypes[0], status=ctx.status) if need_dx else None
-        dw = lgn.lgn_fp8_matmul(dqt, ctx.xqt, out_dtype=ctx.dtypes[1], status=ctx.status) if need_dw else None
+        dx = lgn.lgn_fp8_matmul(dq, wqt, out_dtype=ctx.dtypes[0], status=ctx.status) if need_dx else None
+        dw = lgn.lgn_fp8_matmul(dqt, xqt, out_dtype=ctx.dtypes[1], status=ctx.status) if need_dw else None
         return dx, dw, None, None, None
 
 
