@@ -23,8 +23,8 @@ class Model(torch.nn.Module):
     def __init__(self, vocab: int, dim: int, hidden: int, sparsity: float):
         super().__init__()
         self.embed = Embedding(vocab, dim, scale=dim ** 0.5, device="cuda")
-        self.up = Fp8Linear(dim, hidden, sparsity, device="cuda")
-        self.down = Fp8Linear(hidden, dim, sparsity, device="cuda")
+        self.up = Fp8Linear(dim, hidden, sparsity, device="cuda", seed=1 << 32)
+        self.down = Fp8Linear(hidden, dim, sparsity, device="cuda", seed=2 << 32)
         self.head = Fp8Linear(dim, vocab, device="cuda")
 
     def forward(self, ids: torch.Tensor) -> torch.Tensor:

@@ -66,14 +66,15 @@ class _LinearFn(torch.autograd.Function):
 class Fp8Linear(torch.nn.Module):
     """y = x W^T with x, W and the incoming gradient in 8-bit floating point (E4M3, E4M3, E5M2; one power-of-two
     scale per block of 128), fp32 sums.  ``sparsity`` > 0 prunes the incoming gradient to that fraction of zeros
-    before the two backward products; ``seed`` changes from step to step (advance()).  The waits on the device are
+    before the two backward products, with random numbers that depend on ``seed`` and the place alone: it changes from step to step
+    (advance() adds 1), and layers want seeds that do not meet (the example takes multiples of 2^32).  The waits on the device are
     bounded; check() tells whether one ran out."""
 
-    def __init__(self, in_features: int, out_features: int, sparsity: float = 0.0, device=None):
+    def __init__(self, in_features: int, out_features: int, sparsity: float = 0.0, device=None, seed: int = 0):
         super().__init__()
         self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device))
         torch.nn.init.normal_(self.weight, std=in_features ** -0.5)
-        self.sparsity, self.seed = float(sparsity), 0
+        self.sparsity, self.seed = float(sparsity), int(seed)
         self._status: Dict[torch.device, torch.Tensor] = {}            # an int32 word on each device a pass has run on
 
     def advance(self) -> None:

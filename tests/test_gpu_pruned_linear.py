@@ -51,3 +51,16 @@ def test_finite_gradients_are_what_the_library_prunes_them_to(lgn, layers):
     out, res, ws = torch.empty_like(g), lgn.new_results(1, "cuda"), lgn.new_workspace([g.numel()], "cuda")
     lgn.lgn_compress_layers([lgn.make_layer(g, out, lgn.MODE_PRUNE, S=0.7, seed=9)], res, ws)
     assert torch.equal(layers._pruned(g, 0.7, 9), out)
+
+
+def test_layers_with_seeds_of_their_own(layers):
+    """The same gradient in two layers: different places with different seeds, the same with the same."""
+    up = torch.exp(2 * torch.randn(200, 64, device="cuda") - 12)
+    zeros = []
+    for seed in (1 << 32, 2 << 32, 1 << 32):
+        lin = layers.Fp8Linear(64, 64, sparsity=0.5, device="cuda", seed=seed)
+        assert lin.seed == seed
+        zeros.append(layers._pruned(up, lin.sparsity, lin.seed) == 0)
+        lin.advance()
+        assert lin.seed == seed + 1
+    assert torch.equal(zeros[0], zeros[2]) and int((zeros[0] != zeros[1]).sum()) > 1000
