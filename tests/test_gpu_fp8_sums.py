@@ -48,3 +48,19 @@ def test_sums_over_a_long_contraction(lgn, m, n, odd):
         tol = tol + (half + 2.0 ** -24) * (diff.abs() + tol)
         err = (out.double() - diff).abs()
         assert bool((err <= tol).all()), (dtype, float((err / tol).max()), float((err / want).max()))
+
+
+@pytest.mark.parametrize("positive_only", [False, True])
+def test_fp32_sums_at_16384(lgn, positive_only):
+    """The figure that the kernel's comment gives for contractions up to 16384: the error's 2-norm below 5e-7 of the output's."""
+    k = 16384
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, y = (torch.randn(2048, k, generator=g, device="cuda") for _ in range(2))
+    if positive_only:
+        x, y = x.abs_(), y.abs_()
+    a, b = lgn.lgn_fp8_quantize(x, 1)[0], lgn.lgn_fp8_quantize(y, 0)[0]
+    want = values(a, 0, k) @ values(b, 0, k).t()
+    for m in (2048, 300, 4):                                      # pairs, lone CTAs, shares of k
+        sub = lgn.lgn_fp8_quantize(x[:m], 1)[0]
+        out = lgn.lgn_fp8_matmul(sub, b, out_dtype=torch.float32)
+        assert float((out.double() - want[:m]).norm() / want[:m].norm()) <= 5e-7
