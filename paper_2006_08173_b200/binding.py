@@ -7,7 +7,6 @@ module raises.
 """
 from __future__ import annotations
 
-import bisect
 import ctypes as C
 import os
 from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple
@@ -770,19 +769,21 @@ class Grads(NamedTuple):
     disjoint: bool           # no tensor's out shares memory with another tensor or its out
 
 
-def _disjoint(grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor]) -> bool:
-    span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-    writes = sorted((*span(o), i) for i, o in enumerate(outs) if o.numel())
-    if any(a[1] > b[0] for a, b in zip(writes, writes[1:])):
-        return False
-    starts = [w[0] for w in writes]
-    for i, g in enumerate(grads):
-        lo, hi = span(g)
-        for _, end, j in reversed(writes[:bisect.bisect_left(starts, hi)] if g.numel() else []):
-            if end <= lo:                                  # in order and disjoint: those before end earlier still
-                break
-            if j != i:
-                return False
+def _disjoint(arr: C.Array, count: int) -> bool:
+    spans = []                                             # first byte, end, written?
+    for x in arr[:count]:
+        if x.n:
+            size = x.n * (2 if x.dt == BF16 else 4)
+            spans.append((x.out, x.out + size, True))
+            if x.g + size <= x.out or x.out + size <= x.g:  # not in place (or over itself, which the library refuses)
+                spans.append((x.g, x.g + size, False))
+    written = seen = 0                                     # ends so far
+    for start, end, write in sorted(spans):
+        if start < (seen if write else written):
+            return False
+        seen = max(seen, end)
+        if write:
+            written = max(written, end)
     return True
 
 
@@ -792,14 +793,16 @@ def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
     if len(outs) != len(grads):
         raise ValueError("one out per gradient")
     arr = (GradT * max(1, len(grads)))()
-    devices = {t.get_device() for t in (*grads, *outs)}
-    if len(devices) > 1:
-        raise ValueError(f"tensors on different devices: {sorted(devices)}")
+    devices = set()
     for i, (g, o) in enumerate(zip(grads, outs)):
         if o.numel() != g.numel() or o.dtype != g.dtype:
             raise ValueError("out must have its gradient's size and type")
         arr[i] = GradT(_dev(g, "gradient") or None, _dev(o, "out") or None, g.numel(), dtype_code(g), 0)
-    return Grads(arr, len(grads), (tuple(grads), tuple(outs)), devices.pop() if devices else None, _disjoint(grads, outs))
+        devices.add(g.get_device())
+        devices.add(o.get_device())
+    if len(devices) > 1:
+        raise ValueError(f"tensors on different devices: {sorted(devices)}")
+    return Grads(arr, len(grads), (tuple(grads), tuple(outs)), devices.pop() if devices else None, _disjoint(arr, len(grads)))
 
 
 def new_norm_record(device) -> torch.Tensor:
