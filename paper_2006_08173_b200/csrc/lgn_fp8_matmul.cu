@@ -9,15 +9,15 @@
 // One CTA, or a pair of CTAs on two SMs (CTAS = 2), works on tiles of 128 CTAS rows of one operand ("rows") by BN rows of
 // the other ("cols").  In a pair the CTA of rank 0 issues the MMAs of both (cta_group::2) and each CTA brings
 // its own 128 rows and one half of the BN: at 256 x 256 a step of k (128) costs an SM 32 KiB of shared-memory writes
-// and as many operand reads for 512 clocks of MMA, where a lone CTA's 128 x 192 needs 1.7 times that per flop
+// for 512 clocks of MMA, where a lone CTA's 128 x 192 needs 1.7 times that per flop
 // (8192 x 8192 x 4096: 258 -> 216 us when pairs came in).  Small products take lone CTAs, persistent over tiles, or (SPLIT) one tile
 // per cluster with the CTAs of a cluster taking consecutive shares of k and adding their fp32 tiles through
 // distributed shared memory in rank order.
 //   warp 8  brings codes into a ring of shared-memory stages (TMA, 128-byte swizzle) and, every fourth step, the 512-byte
 //           scale tiles of four blocks;
-//   warp 9  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step.  (Scales
+//   warp 9  one thread issues the scale copies into tensor memory and four MMAs (k = 32 each) per step and half (below).  (Scales
 //           written to tensor memory by four warps of their own, tcgen05.st, came out 8 to 16 % slower.)
-//   warps 0..7  read the finished tile from tensor memory (warp w: lanes 32 (w mod 4) on, column half w / 4), round
+//   warps 0..7  add up the chunks of k from tensor memory (warp w: lanes 32 (w mod 4) on, columns of part w / 4), round
 //               and store.
 // SWAP: `rows` runs along the contiguous dimension of the output, so that the 32 lanes of a warp, which hold
 // 32 rows, write contiguous memory whatever the alignment.

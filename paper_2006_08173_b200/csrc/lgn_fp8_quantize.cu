@@ -7,7 +7,8 @@
 // operations on the fp32 pattern.  x 2^-e is exact unless it falls below the smallest normal fp32
 // number, far below half of the smallest code, so each code is rounded once.
 //
-// Bound by memory: 2 or 4 bytes read and 1 (or, with the transposed copy, 2) written per value.
+// The floor is memory: 2 or 4 bytes read and 1 (or, with the transposed copy, 2) written per value.  What comes nearer to its limit is the
+// integer pipe, 62 % busy for rows, 77 % for both copies (8192 x 4096 bf16, DRAM at 41 and 29 %).
 #include <cuda_runtime.h>
 
 #include "lgn.h"
