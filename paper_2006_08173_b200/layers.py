@@ -67,8 +67,9 @@ class Fp8Linear(torch.nn.Module):
     """y = x W^T with x, W and the incoming gradient in 8-bit floating point (E4M3, E4M3, E5M2; one power-of-two
     scale per block of 128), fp32 sums.  ``sparsity`` > 0 prunes the incoming gradient to that fraction of zeros
     before the two backward products, with random numbers that depend on ``seed`` and the place alone: it changes from step to step
-    (advance() adds 1), and layers want seeds that do not meet (the example takes multiples of 2^32).  The waits on the device are
-    bounded; check() tells whether one ran out."""
+    (advance() adds 1), and layers want seeds that do not meet (the example takes multiples of 2^32).  Pruning is for
+    magnitudes below 2^104; entries that are not finite come through as NaN, as they do without pruning.  The waits on the
+    device are bounded; check() tells whether one ran out."""
 
     def __init__(self, in_features: int, out_features: int, sparsity: float = 0.0, device=None, seed: int = 0):
         super().__init__()
@@ -84,7 +85,8 @@ class Fp8Linear(torch.nn.Module):
         """Raises LgnError (LGN_ERR_TIMEOUT) if a device-side wait of the passes since the last check ran out: what they
         computed is then not valid.  Waits for the device."""
         codes = []
-        for word in self._status.values():
+        for device, word in self._status.items():
+            torch.cuda.synchronize(device)                             # passes on any of its streams
             codes.append(int(word.item()))
             word.zero_()
         if any(codes):

@@ -64,3 +64,23 @@ def test_a_pruning_that_times_out(lgn, layers, monkeypatch):
     assert e.value.code == 5
     step(lin, x)
     lin.check()
+
+
+def test_passes_on_another_stream(lgn, layers, monkeypatch):
+    """check() waits for them too."""
+    lin = layers.Fp8Linear(128, 64, device="cuda")
+    x = torch.randn(40, 128, device="cuda")
+    lin(x)
+    lin.check()
+
+    def withheld(a, b, out_dtype, status):
+        out = torch.empty(a.rows, b.rows, dtype=out_dtype, device="cuda")
+        lgn.lgn_selftest_matmul_wait_expires(a, b, out, status)
+        return out
+    side = torch.cuda.Stream()
+    with monkeypatch.context() as m, torch.cuda.stream(side):
+        m.setattr(lgn, "lgn_fp8_matmul", withheld)
+        lin(x)
+    with pytest.raises(lgn.LgnError):
+        lin.check()
+    lin.check()
