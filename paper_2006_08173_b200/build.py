@@ -19,7 +19,8 @@ SOURCES = [os.path.join(_CSRC, f) for f in (
     "lgn_prefix.cu", "lgn_dequant.cu", "lgn_quantile.cu", "lgn_host.cu", "lgn_fp8_quantize.cu", "lgn_fp8_matmul.cu",
     "lgn_embedding.cu", "lgn_clip.cu")]
 _HEADERS = [os.path.join(_CSRC, "lgn_kernels.cuh"), os.path.join(_CSRC, "lgn_device.cuh"),
-            os.path.join(_CSRC, "lgn_closed_form.cuh"), os.path.join(_CSRC, "lgn_fp8.cuh"), os.path.join(_CSRC, "lgn_launch.h"), os.path.join(_ROOT, "include", "lgn.h")]
+            os.path.join(_CSRC, "lgn_closed_form.cuh"), os.path.join(_CSRC, "lgn_fp8.cuh"), os.path.join(_CSRC, "lgn_tensor.cuh"), os.path.join(_CSRC, "lgn_values.cuh"),
+            os.path.join(_CSRC, "lgn_launch.h"), os.path.join(_ROOT, "include", "lgn.h")]
 _DEPS = SOURCES + _HEADERS
 
 
