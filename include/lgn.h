@@ -497,6 +497,73 @@ lgn_status lgn_clip_grad_norm(const lgn_grad_t *grads, int count, double max_nor
 lgn_status lgn_clip_apply(const lgn_grad_t *grads, int count, double max_norm, lgn_norm_t *record_dev,
                           void *stream);
 
+/* ---- Matrix product in 8-bit integers, one scale per row of either operand ----
+ * With a the largest magnitude of a row (2^-110 if that is larger), its scale is a / 127 and the code of x is x (127 / a) rounded to
+ * nearest even, both quotients rounded to fp32.  A row with an entry that is not finite has a scale of NaN (its codes
+ * are without a meaning): so have the results it takes part in. */
+
+/* Bytes of the codes of a rows x cols operand: row major, rows padded with zero codes to a multiple of 16 bytes.  Its scales
+ * are `rows` floats.  0 for an extent above 2^30. */
+size_t lgn_int8_codes_bytes(uint64_t rows, uint64_t cols);
+
+/* Quantises x (rows x cols of dt, leading dimension ld >= cols): codes 16-byte aligned.  One launch. */
+lgn_status lgn_int8_quantize(const void *x, uint64_t rows, uint64_t cols, uint64_t ld, lgn_dtype dt,
+                             void *codes, float *scales, void *stream);
+
+/* out[i, j] = (sum over c of A[i, c] B[j, c]) a_scale[i] b_scale[j], i < m, j < n, c < k: a sum of 32-bit integers, exact, then
+ * rounded to fp32, multiplied by a's scale, by b's, and rounded to out_dt.  k up to 2^17.
+ *   offsets  NULL with groups = 1: one product.  Else the rows of A are grouped: as for lgn_grouped_matmul, B holding
+ *            groups x n rows, group by group
+ * zero_rest, status_dev, k = 0: as there.  One launch, no workspace; the same inputs give the same bits. */
+lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, const float *b_scales,
+                           const void *offsets, int offset_bits, uint64_t groups, uint64_t m, uint64_t n, uint64_t k,
+                           void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream);
+
+/* ---- Products of rows grouped by expert ----
+ * Group e has the rows offsets[e] .. offsets[e + 1] - 1; groups may be empty, and rows ahead of the first or behind the last
+ * belong to none.  offsets: device, groups + 1 integers of offset_bits (32 or 64) bits.  The sizes are not
+ * known on the host; offsets outside [0, rows] count as the nearest end, one below an earlier one as that one, so that
+ * no offsets lead outside the buffers.
+ * Operands are bf16, 16-byte aligned, rows (ldx, ldw, lddy) and matrices (w_group) multiples of 8 elements apart.  Sums in fp32,
+ * rounded once to out_dt, the tensor cores' truncating additions limited to 1024 terms as in lgn_fp8_matmul.  status_dev: device
+ * uint32, may be NULL; set to LGN_ERR_TIMEOUT if a bounded device-side wait ran out (the output is then invalid), else left alone.
+ * One launch, no workspace; the same inputs give the same bits on the same type of device. */
+
+/* out[r, :] = W_e x[r, :]^T for the rows r of each group e: rows of x have k elements, W_e = w + e w_group is n x k with rows ldw
+ * apart.  transposed: W_e is k x n and out[r, :] = x[r, :] W_e (the input gradient of a layer with weights k x n).
+ * Rows of no group are left as they were, or set to zero with zero_rest.  k = 0 writes zeros. */
+lgn_status lgn_grouped_matmul(const void *x, uint64_t ldx, const void *w, uint64_t ldw, uint64_t w_group, int transposed,
+                              const void *offsets, int offset_bits, uint64_t groups, uint64_t rows, uint64_t n, uint64_t k,
+                              void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream);
+
+/* out_e = sum over the rows r of group e of dy[r, :]^T x[r, :] (+ out_e with accumulate): m x n at out + e out_group, rows ldo apart,
+ * dy rows x m, x rows x n.  Zeros for an empty group; rows of no group do not matter. */
+lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, const void *x, uint64_t ldx, const void *offsets, int offset_bits,
+                                   uint64_t groups, uint64_t rows, uint64_t m, uint64_t n, void *out, uint64_t ldo, uint64_t out_group,
+                                   lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream);
+
+/* ---- Loss of a student against a teacher's top logits, and its gradient ----
+ * Row t has student logits s (vocab of dt) and up to `top` (<= 1024) places ids[t, j] with the teacher's logits z_j.  An entry whose
+ * place lies outside [0, vocab) or whose logit is -infinity is absent; the same place may be named more than once.
+ *   p = softmax(z / T) over the entries present,  q = softmax(s / T),  q1 = softmax(s)
+ *   loss[t]     = alpha T^2 sum over j of p_j (ln p_j - ln q[ids_j])  +  (1 - alpha) (-ln q1[label])
+ *   dlogits[t]  = weight[t] (alpha T (q - p at the places) + (1 - alpha) (q1 - 1 at the label)),    rounded once to dt
+ * without the first part in a row with no entry present (or alpha = 0), without the second where the label lies outside
+ * [0, vocab), labels is NULL or alpha = 1.  A row with neither has loss 0 and a gradient of zeros, whatever its logits are.
+ * Logits of -infinity have q = 0; NaN, +infinity and rows of -infinity alone give NaN.
+ *   ids, teacher  device, tokens x top, rows ld_ids and ld_teacher apart; ids of ids_bits (32 or 64) bits
+ *   labels        device, `tokens` integers of label_bits bits, or NULL
+ *   weight        device, `tokens` floats, or NULL (1): the loss gradients
+ *   dlogits       device, of dt, rows ld_dlogits apart, or NULL (the loss alone); may be logits itself with the same leading
+ *                 dimension, and must not overlap it otherwise
+ * temperature 0.001 to 1000, alpha 0 to 1.  Sums in fp32 in a fixed order: the same bits on every run on the same type of device.
+ * One launch; the logits are read from memory once. */
+lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint64_t vocab, uint64_t ld, lgn_dtype dt,
+                            const void *ids, int ids_bits, uint64_t ld_ids, const void *teacher, uint64_t ld_teacher,
+                            lgn_dtype teacher_dt, uint64_t top, const void *labels, int label_bits,
+                            double temperature, double alpha, const float *weight,
+                            float *loss, void *dlogits, uint64_t ld_dlogits, void *stream);
+
 /* Self-test of the bounded device-side wait (no counterpart in the paper).
  * Same arguments and the same work as lgn_compress_layers, except that one
  * statistics tile of layer 0 is withheld from the queue, so layer 0's closed form

@@ -7,6 +7,7 @@ module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple
@@ -157,6 +158,18 @@ _lib.lgn_clip_grad_norm.argtypes = [C.POINTER(GradT), _i32, _dbl, _vp, _vp, _sz,
 _lib.lgn_clip_grad_norm.restype = _i32
 _lib.lgn_clip_apply.argtypes = [C.POINTER(GradT), _i32, _dbl, _vp, _vp]
 _lib.lgn_clip_apply.restype = _i32
+_lib.lgn_int8_codes_bytes.argtypes = [_u64, _u64]
+_lib.lgn_int8_codes_bytes.restype = _sz
+_lib.lgn_int8_quantize.argtypes = [_vp, _u64, _u64, _u64, _i32, _vp, _vp, _vp]
+_lib.lgn_int8_quantize.restype = _i32
+_lib.lgn_int8_matmul.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
+_lib.lgn_int8_matmul.restype = _i32
+_lib.lgn_grouped_matmul.argtypes = [_vp, _u64, _vp, _u64, _u64, _i32, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
+_lib.lgn_grouped_matmul.restype = _i32
+_lib.lgn_grouped_weight_grad.argtypes = [_vp, _u64, _vp, _u64, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _u64, _i32, _i32, _vp, _vp]
+_lib.lgn_grouped_weight_grad.restype = _i32
+_lib.lgn_distill_loss.argtypes = [_vp, _u64, _u64, _u64, _i32, _vp, _i32, _u64, _vp, _u64, _i32, _u64, _vp, _i32, _dbl, _dbl, _vp, _vp, _vp, _u64, _vp]
+_lib.lgn_distill_loss.restype = _i32
 
 
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
@@ -757,6 +770,226 @@ def lgn_embedding_grad(dout: torch.Tensor, ids: torch.Tensor, vocab: int, scale:
                                    1 if accumulate else 0, _dev(ws, "ws"), ws.numel() * ws.element_size(), _stream(stream)),
            "lgn_embedding_grad")
     return out
+
+
+# --------------------------------------------------------------------------- 8-bit integers
+class Int8Operand:
+    """A matrix of ``rows`` x ``k`` in 8-bit integers with one scale per row.
+
+    codes   int8, rows x (k rounded up to a multiple of 16)
+    scales  float32, rows"""
+    __slots__ = ("rows", "k", "codes", "scales")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int):
+        if codes.dtype != torch.int8 or scales.dtype != torch.float32:
+            raise TypeError("codes are int8, scales float32")
+        _dev(codes, "codes"), _dev(scales, "scales")
+        if codes.numel() < rows * ((k + 15) & -16) or scales.numel() < rows:
+            raise ValueError("codes or scales shorter than the extents need")
+        if codes.get_device() != scales.get_device():
+            raise ValueError("codes and scales on different devices")
+        self.rows, self.k, self.codes, self.scales = rows, k, codes, scales
+
+
+def new_int8_operand(rows: int, k: int, device, stream=None) -> Int8Operand:
+    """Uninitialised; for use on ``stream`` (default: the current one)."""
+    return Int8Operand(_empty((rows, (k + 15) & -16), torch.int8, device, stream), _empty(rows, torch.float32, device, stream), rows, k)
+
+
+def lgn_int8_quantize(x: torch.Tensor, out: Optional[Int8Operand] = None, stream=None) -> Int8Operand:
+    """The operand of a matrix; ``out``: one of the same extents to write to."""
+    rows, cols, ld = _matrix3(x, "x")
+    device = x.get_device()
+    if _elsewhere(device, stream, out.codes.get_device() if out is not None else None):
+        with torch.cuda.device(device):
+            return lgn_int8_quantize(x, out, stream)
+    if out is None:
+        out = new_int8_operand(rows, cols, x.device, stream)
+    elif (out.rows, out.k) != (rows, cols):
+        raise ValueError("out: extents differ from the matrix")
+    _check(_lib.lgn_int8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), out.codes.data_ptr() or None,
+                                  out.scales.data_ptr() or None, _stream(stream)), "lgn_int8_quantize")
+    return out
+
+
+def _offsets(offsets: torch.Tensor) -> Tuple[int, int, int]:
+    """Address, bits and number of groups of group offsets."""
+    if offsets.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"offsets are int32 or int64, got {offsets.dtype}")
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("offsets hold one integer more than there are groups")
+    return _dev(offsets, "offsets"), 32 if offsets.dtype == torch.int32 else 64, offsets.numel() - 1
+
+
+def _number(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.get_device()
+
+
+def _given(out: torch.Tensor, shape: Tuple[int, int]) -> int:
+    """The leading dimension of an output matrix that the caller brings."""
+    if tuple(out.shape) != shape:
+        raise ValueError(f"out must be {shape[0]} x {shape[1]}")
+    return _matrix(out, "out")
+
+
+def lgn_int8_matmul(a: Int8Operand, b: Int8Operand, out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
+                    offsets: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[i, j] = sum over c of a[i, c] b[j, c].  With ``offsets`` (groups + 1 integers) the rows of ``a`` are grouped and ``b`` holds
+    the groups' matrices one below the other; rows of no group are zero, or as they were in an ``out`` that is given."""
+    if a.k != b.k:
+        raise ValueError("operands contract over different extents")
+    at, bits, groups = (None, 32, 1) if offsets is None else _offsets(offsets)
+    if b.rows % groups:
+        raise ValueError("b holds as many rows for each group")
+    m, n = a.rows, b.rows // groups
+    device = a.codes.get_device()
+    if _elsewhere(device, stream, b.codes.get_device(), _number(out), _number(offsets), _number(status)):
+        with torch.cuda.device(device):
+            return lgn_int8_matmul(a, b, out, out_dtype, offsets, status, stream)
+    rest = out is None
+    if out is None:
+        out = _empty((m, n), out_dtype, a.codes.device, stream)
+        ldo = n or 1
+    else:
+        ldo = _given(out, (m, n))
+    _check(_lib.lgn_int8_matmul(a.codes.data_ptr() or None, a.scales.data_ptr() or None, b.codes.data_ptr() or None, b.scales.data_ptr() or None,
+                                at, bits, groups, m, n, a.k, out.data_ptr() or None, ldo, dtype_code(out), 1 if rest else 0,
+                                _word(status, 4, "status") if status is not None else None, _stream(stream)), "lgn_int8_matmul")
+    return out
+
+
+# --------------------------------------------------------------------------- products grouped by expert
+def _pieces(t: torch.Tensor, stream) -> torch.Tensor:
+    """A bf16 matrix, or a stack of matrices, as the grouped products read it: rows contiguous, rows and matrices multiples of 16 bytes apart.
+    ``t`` itself where it is so, else a copy."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"operands of grouped products are bfloat16, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError("operands are CUDA tensors")
+    shape, step = t.shape, t.stride()
+    if t.numel() == 0:
+        return t
+    fits = (step[-1] == 1 or shape[-1] == 1) and t.data_ptr() % 16 == 0
+    inner = shape[-1]                                                  # elements that the dimensions so far span
+    for d in range(t.dim() - 2, -1, -1):
+        fits = fits and (shape[d] == 1 or (step[d] >= inner and step[d] % 8 == 0))
+        inner = inner if shape[d] == 1 else (shape[d] - 1) * step[d] + inner
+    if fits:
+        return t
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(_as_stream(stream, t.device)):
+        padded = torch.empty(*shape[:-1], (shape[-1] + 7) & -8, dtype=t.dtype, device=t.device)
+        return padded[..., :shape[-1]].copy_(t)
+
+
+def _as_stream(stream, device) -> torch.cuda.Stream:
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device)
+
+
+def _strides(t: torch.Tensor) -> Tuple[int, int]:
+    """Elements between the rows and between the matrices of what _pieces returned."""
+    row = t.stride(-2) if t.size(-2) > 1 else (t.size(-1) + 7) & -8
+    group = t.stride(0) if t.dim() == 3 and t.size(0) > 1 else 0
+    return row, group
+
+
+def lgn_grouped_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
+                       out_dtype: torch.dtype = torch.bfloat16, transposed: bool = False, status: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """out[r] = x[r] w[e]^T for the rows r = offsets[e] .. offsets[e + 1] - 1 of each group e, w groups x n x k; ``transposed``:
+    x[r] w[e], w groups x k x n.  x and w are bf16; those whose rows are not multiples of 16 bytes apart are copied first.  Rows of no group
+    are zero, or as they were in an ``out`` that is given."""
+    at, bits, groups = _offsets(offsets)
+    if x.dim() != 2 or w.dim() != 3 or w.size(0) != groups:
+        raise ValueError("x is a matrix, w a stack with one matrix per group")
+    rows, k = x.shape
+    n = w.size(2 if transposed else 1)
+    if w.size(1 if transposed else 2) != k:
+        raise ValueError("x and w contract over different extents")
+    device = x.get_device()
+    if _elsewhere(device, stream, w.get_device(), offsets.get_device(), _number(out), _number(status)):
+        with torch.cuda.device(device):
+            return lgn_grouped_matmul(x, w, offsets, out, out_dtype, transposed, status, stream)
+    rest = out is None
+    if out is None:
+        out = _empty((rows, n), out_dtype, x.device, stream)
+        ldo = n or 1
+    else:
+        ldo = _given(out, (rows, n))
+    x, w = _pieces(x, stream), _pieces(w, stream)
+    (ldx, _), (ldw, w_group) = _strides(x), _strides(w)
+    _check(_lib.lgn_grouped_matmul(x.data_ptr() or None, ldx, w.data_ptr() or None, ldw, w_group, 1 if transposed else 0, at, bits, groups, rows, n, k,
+                                   out.data_ptr() or None, ldo, dtype_code(out), 1 if rest else 0,
+                                   _word(status, 4, "status") if status is not None else None, _stream(stream)), "lgn_grouped_matmul")
+    return out
+
+
+def lgn_grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
+                            out_dtype: torch.dtype = torch.float32, accumulate: bool = False, status: Optional[torch.Tensor] = None,
+                            stream=None) -> torch.Tensor:
+    """out[e] = dy^T x over the rows of each group e: groups x dy's columns x x's columns; with ``accumulate`` added to ``out``."""
+    at, bits, groups = _offsets(offsets)
+    if dy.dim() != 2 or x.dim() != 2 or dy.size(0) != x.size(0):
+        raise ValueError("dy and x are matrices with as many rows")
+    (rows, m), n = dy.shape, x.size(1)
+    device = x.get_device()
+    if _elsewhere(device, stream, dy.get_device(), offsets.get_device(), _number(out), _number(status)):
+        with torch.cuda.device(device):
+            return lgn_grouped_weight_grad(dy, x, offsets, out, out_dtype, accumulate, status, stream)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = _empty((groups, m, n), out_dtype, x.device, stream)
+    elif tuple(out.shape) != (groups, m, n):
+        raise ValueError("out must be groups x dy's columns x x's columns")
+    ldo, out_group = (n or 1), m * n
+    if not out.is_contiguous():
+        if out.numel() and (out.stride(2) != 1 and n > 1 or m > 1 and out.stride(1) < n or groups > 1 and out.stride(0) < (m - 1) * out.stride(1) + n):
+            raise ValueError("out must have contiguous rows, and rows and matrices that do not overlap")
+        ldo, out_group = (out.stride(1) if m > 1 else n or 1), out.stride(0)
+    dy, x = _pieces(dy, stream), _pieces(x, stream)
+    _check(_lib.lgn_grouped_weight_grad(dy.data_ptr() or None, _strides(dy)[0], x.data_ptr() or None, _strides(x)[0], at, bits, groups, rows, m, n,
+                                        out.data_ptr() or None, ldo, out_group, dtype_code(out), 1 if accumulate else 0,
+                                        _word(status, 4, "status") if status is not None else None, _stream(stream)), "lgn_grouped_weight_grad")
+    return out
+
+
+# --------------------------------------------------------------------------- distillation
+def lgn_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, labels: Optional[torch.Tensor] = None,
+                     temperature: float = 1.0, alpha: float = 1.0, weight: Optional[torch.Tensor] = None, grad: bool = False,
+                     loss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                     stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(loss of every row, gradient of the logits or None).  ids and teacher: tokens x top, the places and the teacher's logits there.  ``weight``:
+    what every row's gradient is multiplied by.  The gradient is formed with ``grad``, or where ``dlogits`` (may be logits) is given."""
+    tokens, vocab, ld = _matrix3(logits, "logits")
+    if ids.dim() != 2 or ids.shape != teacher.shape or ids.size(0) != tokens:
+        raise ValueError("ids and teacher must be tokens x top")
+    (_, top, ld_ids), (_, _, ld_teacher) = _matrix3(ids, "ids"), _matrix3(teacher, "teacher")
+    for t, what in ((labels, "labels"), (weight, "weight"), (loss, "loss")):
+        if t is not None and (t.dim() != 1 or t.numel() != tokens):
+            raise ValueError(f"{what} must hold one value per row")
+    for t, what in ((weight, "weight"), (loss, "loss")):
+        if t is not None and t.dtype != torch.float32:
+            raise TypeError(f"{what} must be float32")
+    device = logits.get_device()
+    if _elsewhere(device, stream, ids.get_device(), teacher.get_device(), _number(labels), _number(weight), _number(loss), _number(dlogits)):
+        with torch.cuda.device(device):
+            return lgn_distill_loss(logits, ids, teacher, labels, temperature, alpha, weight, grad, loss, dlogits, stream)
+    if loss is None:
+        loss = _empty(tokens, torch.float32, logits.device, stream)
+    ldd = vocab or 1
+    if dlogits is not None:
+        if dlogits.dtype != logits.dtype:
+            raise TypeError("dlogits has the type of the logits")
+        ldd = _given(dlogits, (tokens, vocab))
+    elif grad:
+        dlogits = _empty((tokens, vocab), logits.dtype, logits.device, stream)
+    _check(_lib.lgn_distill_loss(logits.data_ptr() or None, tokens, vocab, ld, dtype_code(logits), ids.data_ptr() or None, _ids(ids), ld_ids,
+                                 teacher.data_ptr() or None, ld_teacher, dtype_code(teacher), top,
+                                 _dev(labels, "labels") or None if labels is not None else None, _ids(labels) if labels is not None else 32,
+                                 float(temperature), float(alpha), _dev(weight, "weight") or None if weight is not None else None,
+                                 _dev(loss, "loss") or None, dlogits.data_ptr() or None if dlogits is not None else None, ldd, _stream(stream)),
+           "lgn_distill_loss")
+    return loss, dlogits
 
 
 # --------------------------------------------------------------------------- gradient norm and clipping

@@ -1,0 +1,13 @@
+// Instances of the grouped product: dY^T X over each group's rows in bf16 (weight gradients).
+#include "lgn_grouped.cuh"
+
+namespace lgn {
+
+GmKernels gm_weight_kernels() {
+    static const GmKernel table[] = {
+        gm_kernel<kGmBf16, 256, 2, kGmGrad, false, LGN_BF16>(4.0f, 0.30f, 1.5f), gm_kernel<kGmBf16, 256, 2, kGmGrad, false, LGN_F32>(4.0f, 0.30f, 2.5f),
+        gm_kernel<kGmBf16, 128, 1, kGmGrad, false, LGN_BF16>(3.5f, 0.25f, 1.0f), gm_kernel<kGmBf16, 128, 1, kGmGrad, false, LGN_F32>(3.5f, 0.25f, 1.5f)};
+    return {table, (int)(sizeof table / sizeof table[0])};
+}
+
+}  // namespace lgn

@@ -31,7 +31,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded wait; gives up as soon as another role has.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *stop) {
     const long long t0 = clock64();
     for (;;) {
         if (mbar_try(bar, parity)) return true;
@@ -51,7 +51,7 @@ __device__ __forceinline__ bool elect_one() {
     return ok != 0;
 }
 // Bounded wait for what is in flight after a stop.
-__device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
     while (!mbar_try(bar, parity))
         if (clock64() - t0 > kMmWaitClocks) return;
@@ -141,7 +141,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-static EncodeTiled encode_tiled() {
+inline EncodeTiled encode_tiled() {
     static EncodeTiled fn = [] {
         void *f = nullptr;
         cudaDriverEntryPointQueryResult q;
