@@ -14,9 +14,9 @@
 // exp is taken in base 2 of (s - M) log2(e) / T, the difference first: it is exact or small where the term
 // counts.  Sums are fp32, a few dozen terms per thread, then by lanes, warps and ranks in a fixed order.
 //
-// The gradient's places are written last, over what the pass wrote there.  A place named more than once
-// (by entries, or an entry and the label) is found by a table of the ids in shared memory, and then summed in the order of the
-// entries by every entry that names it, so that all of them write the same value.
+// The gradient's places are written last, over what the pass wrote there.  A place that several entries name is found by a table of the ids
+// in shared memory, and then summed in the order of the entries by each of them, so that all write the same value; the label
+// writes its place where no entry does.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -118,16 +118,6 @@ __device__ __noinline__ void store_edge(char *row, int64_t c, uint32_t vocab, ui
     }
 }
 
-__device__ __forceinline__ float warp_max(float v) {
-    #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
-}
-__device__ __forceinline__ float warp_sum(float v) {
-    #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
-}
 __device__ __forceinline__ float shared_of(uint32_t addr, uint32_t rank) {
     uint32_t at;
     float x;
@@ -136,15 +126,45 @@ __device__ __forceinline__ float shared_of(uint32_t addr, uint32_t rank) {
     return x;
 }
 
+// What a warp, or all of them, know of a row: the logits' maximum and sums of exponentials, the teacher's maximum, sum and
+// weighted differences dot = sum exp((z - zm) / T) ((z - zm) - (s - sm)), sm the largest of the student's logits at the places.
+template <bool DUAL> struct RowSums {
+    float m, sum, sum1, zm, sm, z_sum, dot;
+    // Over groups of WIDTH lanes, in a fixed order; the same in all of them.
+    template <int WIDTH>
+    __device__ __forceinline__ void join(float scale, float scale1) {
+        const float m0 = m, zm0 = zm, sm0 = sm;
+        #pragma unroll
+        for (int d = WIDTH / 2; d > 0; d >>= 1) {
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            zm = fmaxf(zm, __shfl_xor_sync(0xffffffffu, zm, d));
+            sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
+        }
+        sum *= exp2_approx((m0 - m) * scale);
+        if constexpr (DUAL) sum1 *= exp2_approx((m0 - m) * scale1);
+        if (z_sum != 0.0f) {                                            // where there are none the references mean nothing
+            const float f = exp2_approx((zm0 - zm) * scale);
+            dot = f != 0.0f ? f * (dot + z_sum * ((zm0 - zm) - (sm0 - sm))) : 0.0f;
+            z_sum *= f;
+        }
+        #pragma unroll
+        for (int d = WIDTH / 2; d > 0; d >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if constexpr (DUAL) sum1 += __shfl_xor_sync(0xffffffffu, sum1, d);
+            z_sum += __shfl_xor_sync(0xffffffffu, z_sum, d);
+            dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        }
+    }
+};
+
 // DUAL: the two parts take softmaxes of different temperatures.
 template <int DT, int THREADS, bool DUAL, bool GRAD>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 distill_kernel(const DistillArgs p) {
     constexpr int kVals = Piece<DT>::kVals, ES = 16 / kVals, kWarps = THREADS / 32;
     extern __shared__ uint32_t dyn[];
-    __shared__ float wmax[kWarps], wsum[kWarps], wsum1[kWarps], wtop[kWarps], wz[kWarps], wd[kWarps];
+    __shared__ float parts[7][kWarps];
     __shared__ float joint[3];
-    __shared__ uint32_t some_s;
     dep_launch();
 
     uint32_t rank, nrank;
@@ -156,9 +176,10 @@ distill_kernel(const DistillArgs p) {
     int32_t *id = reinterpret_cast<int32_t *>(dyn);     // -1: absent
     float *ze = reinterpret_cast<float *>(dyn + entries), *se = ze + entries;
     uint32_t *table = dyn + 3 * entries;                // id + 1, the top bit: named more than once
-    if (tid == 0) some_s = 0u;
-    if constexpr (GRAD) for (uint32_t i = tid; i < p.table; i += THREADS) table[i] = 0u;
-    __syncthreads();
+    if constexpr (GRAD) {
+        for (uint32_t i = tid; i < p.table; i += THREADS) table[i] = 0u;
+        __syncthreads();
+    }
     dep_wait();
 
     const char *src = p.logits + row * p.ld * ES;
@@ -167,147 +188,143 @@ distill_kernel(const DistillArgs p) {
     const bool whole = GRAD && ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0;
     const uint32_t total = (uint32_t)((shift + vocab + kVals - 1) / kVals);             // pieces of the row
     const uint32_t v0 = min(rank * p.pieces, total), v1 = min(v0 + p.pieces, total);
-    const uint32_t in0 = shift > 0 ? 1u : 0u, in1 = min(v1, (uint32_t)((shift + vocab) / kVals));   // whole pieces
+    const uint32_t in0 = shift > 0 ? 1u : 0u, in1 = max(in0, min(v1, (uint32_t)((shift + vocab) / kVals)));   // whole pieces
     const char *base = src - shift * ES;
     constexpr uint32_t kNone = DT == LGN_F32 ? 0xff800000u : 0xff80ff80u;               // -inf
 
-    // the row's first chunk is under way while the entries are looked at
+    // An entry: its place, the teacher's logit, the student's.
+    auto place_of = [&](uint32_t j, float &z) {
+        int64_t at = -1;
+        if (j < p.top) {
+            at = ds_id(p.ids, p.ids64, row * p.ld_ids + j);
+            z = p.teacher_dt == LGN_F32 ? ds_load<LGN_F32>(p.teacher, row * p.ld_teacher + j) : ds_load<LGN_BF16>(p.teacher, row * p.ld_teacher + j);
+        } else if (j == p.top && p.labels != nullptr) at = ds_id(p.labels, p.labels64, row);
+        return at;
+    };
+    auto present = [&](uint32_t j, int64_t at, float z) {
+        if (at < 0 || at >= vocab) return -1;
+        return (j < p.top ? z == -INFINITY || p.alpha == 0.0f : p.beta == 0.0f) ? -1 : (int32_t)at;
+    };
+    // Loads are issued ahead of what waits for them: the thread's first entry, the row's first chunk, the entry's logit.
+    float z0 = 0.0f, s0 = 0.0f, w = 1.0f;
+    const int64_t far0 = place_of(tid, z0);
+    if (GRAD && p.weight != nullptr) w = __uint_as_float(ldro_u32(p.weight + row));
     Piece<DT> x[kDsVecs];
     auto load = [&](uint32_t v) {
+        const char *at = base + (uint64_t)(v + tid) * 16;
         #pragma unroll
         for (int i = 0; i < kDsVecs; ++i) {
+            if (v + i * THREADS >= v1 && i > 0) break;
             const uint32_t u = v + i * THREADS + tid;
-            uint32_t (&w)[4] = x[i].w;
-            if (u >= in0 && u < in1)
-                asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(base + (uint64_t)u * 16) : "memory");
+            uint32_t (&q)[4] = x[i].w;
+            if (u - in0 < in1 - in0)
+                asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "l"(at + i * THREADS * 16) : "memory");
             else {
-                const uint4 q = u < v1 ? load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab) : make_uint4(kNone, kNone, kNone, kNone);
-                w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+                const uint4 e = u < v1 ? load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab) : make_uint4(kNone, kNone, kNone, kNone);
+                q[0] = e.x; q[1] = e.y; q[2] = e.z; q[3] = e.w;
             }
         }
     };
     load(v0);
+    const int32_t id0 = present(tid, far0, z0);
+    if (id0 >= 0) s0 = ds_load<DT>(src, (uint64_t)id0);
 
-    float top_max = kDsLowest;
-    bool some = false;
-    for (uint32_t j = tid; j < entries; j += THREADS) {
-        int64_t at = -1;
-        float z = 0.0f, s = 0.0f;
-        if (j < p.top) {
-            at = ds_id(p.ids, p.ids64, row * p.ld_ids + j);
-            z = p.teacher_dt == LGN_F32 ? ds_load<LGN_F32>(p.teacher, row * p.ld_teacher + j) : ds_load<LGN_BF16>(p.teacher, row * p.ld_teacher + j);
-            if (at < 0 || at >= vocab || z == -INFINITY || p.alpha == 0.0f) at = -1;
-            else { some = true; top_max = fmaxf(top_max, z); }
-        } else if (p.labels != nullptr && p.beta != 0.0f) {
-            at = ds_id(p.labels, p.labels64, row);
-            if (at < 0 || at >= vocab) at = -1;
-        }
-        if (at >= 0) {
-            s = ds_load<DT>(src, (uint64_t)at);
-            if constexpr (GRAD) {
-                uint32_t h = ((uint32_t)at * 2654435761u) & (p.table - 1);
-                for (;;) {                              // ends: the table has more slots than there are entries
-                    const uint32_t old = atomicCAS(&table[h], 0u, (uint32_t)at + 1u) & 0x7fffffffu;
-                    if (old == 0u) break;
-                    if (old == (uint32_t)at + 1u) { atomicOr(&table[h], 0x80000000u); break; }
-                    h = (h + 1) & (p.table - 1);
-                }
-            }
-        }
-        id[j] = (int32_t)at; ze[j] = z; se[j] = s;
-    }
-    if (some) some_s = 1u;
-
-    // M and the sums
-    float m = kDsLowest, sum = 0.0f, sum1 = 0.0f;
+    RowSums<DUAL> r = {kDsLowest, 0.0f, 0.0f, kDsLowest, kDsLowest, 0.0f, 0.0f};
     for (uint32_t v = v0;;) {
-        float c = m;
-        #pragma unroll
-        for (int i = 0; i < kDsVecs; ++i) c = x[i].max_with(c);
-        sum *= exp2_approx((m - c) * p.scale);
-        if constexpr (DUAL) sum1 *= exp2_approx((m - c) * p.scale1);
-        m = c;
+        float c = r.m;
         #pragma unroll
         for (int i = 0; i < kDsVecs; ++i) {
+            if (v + i * THREADS >= v1 && i > 0) break;
+            c = x[i].max_with(c);
+        }
+        r.sum *= exp2_approx((r.m - c) * p.scale);
+        if constexpr (DUAL) r.sum1 *= exp2_approx((r.m - c) * p.scale1);
+        r.m = c;
+        #pragma unroll
+        for (int i = 0; i < kDsVecs; ++i) {
+            if (v + i * THREADS >= v1 && i > 0) break;
             float a = 0.0f, a1 = 0.0f;
             x[i].forget();
             #pragma unroll
             for (int k = 0; k < kVals; ++k) {
-                const float t = x[i].at(k) - m;
+                const float t = x[i].at(k) - c;
                 a += exp2_approx(t * p.scale);
                 if constexpr (DUAL) a1 += exp2_approx(t * p.scale1);
             }
-            sum += a;
-            sum1 += a1;
+            r.sum += a;
+            r.sum1 += a1;
         }
         v += THREADS * kDsVecs;
         if (v >= v1) break;
         load(v);
     }
-    {
-        const float c = warp_max(m);
-        sum = warp_sum(sum * exp2_approx((m - c) * p.scale));
-        if constexpr (DUAL) sum1 = warp_sum(sum1 * exp2_approx((m - c) * p.scale1));
-        top_max = warp_max(top_max);
-        if (lane == 0) { wmax[warp] = c; wsum[warp] = sum; if constexpr (DUAL) wsum1[warp] = sum1; wtop[warp] = top_max; }
+
+    // the entries, a warp's at a time: 32 of them share their references
+    auto enter = [&](uint32_t j, int32_t at, float z, float s) {
+        if (j < entries) { id[j] = at; ze[j] = z; se[j] = s; }
+        if (GRAD && at >= 0 && j < p.top) {
+            uint32_t h = ((uint32_t)at * 2654435761u) & (p.table - 1);
+            for (;;) {                                  // ends: the table has more slots than there are entries
+                const uint32_t old = atomicCAS(&table[h], 0u, (uint32_t)at + 1u) & 0x7fffffffu;
+                if (old == 0u) break;
+                if (old == (uint32_t)at + 1u) { atomicOr(&table[h], 0x80000000u); break; }
+                h = (h + 1) & (p.table - 1);
+            }
+        }
+        if (at >= 0 && j < p.top) {
+            const float zm = fmaxf(r.zm, z), sm = fmaxf(r.sm, s), f = r.z_sum != 0.0f ? exp2_approx((r.zm - zm) * p.scale) : 0.0f, e = exp2_approx((z - zm) * p.scale);
+            r.dot = (f != 0.0f ? f * (r.dot + r.z_sum * ((r.zm - zm) - (r.sm - sm))) : 0.0f) + (e != 0.0f ? e * ((z - zm) - (s - sm)) : 0.0f);
+            r.z_sum = r.z_sum * f + e;
+            r.zm = zm;
+            r.sm = sm;
+        }
+    };
+    enter(tid, id0, z0, s0);
+    for (uint32_t j = tid + THREADS; j < entries; j += THREADS) {
+        float z = 0.0f;
+        const int32_t at = present(j, place_of(j, z), z);
+        enter(j, at, z, at >= 0 ? ds_load<DT>(src, (uint64_t)at) : 0.0f);
     }
-    __syncthreads();
-    some = some_s != 0u;
-    m = wmax[0]; top_max = wtop[0];
-    #pragma unroll
-    for (int w = 1; w < kWarps; ++w) { m = fmaxf(m, wmax[w]); top_max = fmaxf(top_max, wtop[w]); }
-    sum = 0.0f; sum1 = 0.0f;
-    #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        sum += wsum[w] * exp2_approx((wmax[w] - m) * p.scale);
-        if constexpr (DUAL) sum1 += wsum1[w] * exp2_approx((wmax[w] - m) * p.scale1);
-    }
+    r.template join<32>(p.scale, p.scale1);
+    if constexpr (kWarps > 1) {
+        if (lane == 0) {
+            parts[0][warp] = r.m; parts[1][warp] = r.sum; parts[2][warp] = r.sum1; parts[3][warp] = r.zm; parts[4][warp] = r.sm; parts[5][warp] = r.z_sum; parts[6][warp] = r.dot;
+        }
+        __syncthreads();
+        const uint32_t from = lane % kWarps;
+        r = {parts[0][from], parts[1][from], parts[2][from], parts[3][from], parts[4][from], parts[5][from], parts[6][from]};
+        r.template join<kWarps>(p.scale, p.scale1);
+    } else __syncwarp();
+    float m = r.m, sum = r.sum, sum1 = r.sum1;
     if (nrank > 1) {
         const uint32_t at = smem_u32(joint);
         if (tid == 0) { joint[0] = m; joint[1] = sum; joint[2] = sum1; }
         cluster_sync();
-        const float own = m;
-        for (uint32_t r = 0; r < nrank; ++r) m = fmaxf(m, r == rank ? own : shared_of(at, r));
-        sum = 0.0f; sum1 = 0.0f;
-        for (uint32_t r = 0; r < nrank; ++r) {
-            const float d = shared_of(at, r) - m;
-            sum += shared_of(at + 4, r) * exp2_approx(d * p.scale);
-            if constexpr (DUAL) sum1 += shared_of(at + 8, r) * exp2_approx(d * p.scale1);
-        }
-        __syncwarp();
+        const uint32_t from = lane % nrank;             // 2, 4 or 8
+        const float m0 = shared_of(at, from);
+        sum = shared_of(at + 4, from);
+        if constexpr (DUAL) sum1 = shared_of(at + 8, from);
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");           // waited for at the end
-    }
-
-    // the teacher's part
-    float z_sum = 0.0f, z_dot = 0.0f;
-    for (uint32_t j = tid; j < p.top; j += THREADS) {
-        float e = 0.0f;
-        if (id[j] >= 0) {
-            const float z = ze[j] - top_max;
-            e = exp2_approx(z * p.scale);
-            z_sum += e;
-            if (e != 0.0f) z_dot += e * (z - (se[j] - m));
+        m = m0;
+        for (uint32_t d = nrank / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        sum *= exp2_approx((m0 - m) * p.scale);
+        if constexpr (DUAL) sum1 *= exp2_approx((m0 - m) * p.scale1);
+        for (uint32_t d = nrank / 2; d > 0; d >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if constexpr (DUAL) sum1 += __shfl_xor_sync(0xffffffffu, sum1, d);
         }
-        ze[j] = e;
     }
-    z_sum = warp_sum(z_sum);
-    z_dot = warp_sum(z_dot);
-    if (lane == 0) { wz[warp] = z_sum; wd[warp] = z_dot; }
-    __syncthreads();
-    z_sum = 0.0f; z_dot = 0.0f;
-    #pragma unroll
-    for (int w = 0; w < kWarps; ++w) { z_sum += wz[w]; z_dot += wd[w]; }
     const int32_t label = id[p.top];
-    const float s1 = DUAL ? sum1 : sum;                 // the label's sum
+    const bool some = r.z_sum != 0.0f;                  // the largest entry counts 1; NaN is not 0 either
     if (rank == 0 && tid == 0) {
+        const float s1 = DUAL ? sum1 : sum;             // the label's sum
         float loss = 0.0f;
-        if (some) loss = p.alpha * p.temperature * (z_dot / z_sum + p.temperature * (logf(sum) - logf(z_sum)));
+        if (some) loss = p.alpha * p.temperature * (r.dot / r.z_sum + (m - r.sm) + p.temperature * (logf(sum) - logf(r.z_sum)));
         if (label >= 0) loss += p.beta * (logf(s1) - (se[p.top] - m));
         p.loss[row] = loss;
     }
 
     if constexpr (GRAD) {
-        const float w = p.weight != nullptr ? __uint_as_float(ldro_u32(p.weight + row)) : 1.0f;
         const float kt = some ? w * p.alpha * p.temperature : 0.0f, k1 = label >= 0 ? w * p.beta : 0.0f;
         const bool dead = !some && label < 0;           // zeros, whatever the logits are
         const float ct = DUAL ? kt / sum : (kt + k1) / sum, c1 = DUAL ? k1 / sum1 : 0.0f;
@@ -317,44 +334,52 @@ distill_kernel(const DistillArgs p) {
             if constexpr (DUAL) d += exp2_approx(t * p.scale1) * c1;
             return d;
         };
-        const bool held = v1 - v0 <= THREADS * kDsVecs;       // the one chunk is still in registers
+        const bool held = v1 - v0 <= THREADS * kDsVecs; // the one chunk is still in registers
         for (uint32_t v = v0; v < v1; v += THREADS * kDsVecs) {
             if (!held) load(v);
+            char *to = dst - shift * ES + (uint64_t)(v + tid) * 16;
             #pragma unroll
             for (int i = 0; i < kDsVecs; ++i) {
+                if (v + i * THREADS >= v1) break;
                 const uint32_t u = v + i * THREADS + tid;
                 if (u < v1) {
                     float d[kVals];
-                    uint32_t w[4];
+                    uint32_t q[4];
                     x[i].forget();
                     #pragma unroll
-                    for (int k = 0; k < kVals; ++k) d[k] = dead ? 0.0f : slope(x[i].at(k));
+                    for (int k = 0; k < kVals; ++k) d[k] = slope(x[i].at(k));
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        if constexpr (DT == LGN_F32) w[k] = __float_as_uint(d[k]);
-                        else w[k] = pack_bf16(d[2 * k], d[2 * k + 1]);
+                        if constexpr (DT == LGN_F32) q[k] = __float_as_uint(d[k]);
+                        else q[k] = pack_bf16(d[2 * k], d[2 * k + 1]);
+                        if (dead) q[k] = 0u;
                     }
-                    if (whole && u >= in0 && u < in1)
-                        asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(dst - shift * ES + (uint64_t)u * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                    else store_edge<DT>(dst, (int64_t)u * kVals - shift, p.vocab, make_uint4(w[0], w[1], w[2], w[3]));
+                    if (whole && u - in0 < in1 - in0)
+                        asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(to + i * THREADS * 16), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
+                    else store_edge<DT>(dst, (int64_t)u * kVals - shift, p.vocab, make_uint4(q[0], q[1], q[2], q[3]));
                 }
             }
         }
         __syncthreads();                                // the places are written over what other threads wrote there
-        const int64_t c0 = (int64_t)v0 * kVals - shift, c1_ = (int64_t)v1 * kVals - shift;
+        const int64_t begin = (int64_t)v0 * kVals - shift, end = (int64_t)v1 * kVals - shift;
         for (uint32_t j = tid; j < entries; j += THREADS) {
             const int32_t at = id[j];
-            if (at < 0 || at < c0 || at >= c1_) continue;
-            uint32_t h = ((uint32_t)at * 2654435761u) & (p.table - 1);
-            while ((table[h] & 0x7fffffffu) != (uint32_t)at + 1u) h = (h + 1) & (p.table - 1);   // it is there
-            float pt = j < p.top ? ze[j] : 0.0f;
-            if (table[h] >> 31) {
-                pt = 0.0f;
-                for (uint32_t i = 0; i < p.top; ++i) if (id[i] == at) pt += ze[i];
-            }
+            if (at < 0 || at < begin || at >= end) continue;
+            uint32_t h = ((uint32_t)at * 2654435761u) & (p.table - 1), slot;
+            while (((slot = table[h]) & 0x7fffffffu) != (uint32_t)at + 1u && slot != 0u) h = (h + 1) & (p.table - 1);
             float d = slope(se[j]);
-            if (some) d -= kt * (pt / z_sum);
-            if (at == label) d -= k1;
+            if (j < p.top) {
+                float pt = exp2_approx((ze[j] - r.zm) * p.scale);
+                if (slot >> 31) {
+                    pt = 0.0f;
+                    for (uint32_t i = 0; i < p.top; ++i) if (id[i] == at) pt += exp2_approx((ze[i] - r.zm) * p.scale);
+                }
+                d -= kt * (pt / r.z_sum);
+                if (at == label) d -= k1;
+            } else {
+                if (slot != 0u) continue;               // an entry has the label's place
+                d -= k1;
+            }
             ds_store<DT>(dst, (uint64_t)at, d);
         }
     }
@@ -364,7 +389,8 @@ distill_kernel(const DistillArgs p) {
 
 #define LGN_DS(D, T, U, G) reinterpret_cast<const void *>(&distill_kernel<D, T, U, G>)
 #define LGN_DS4(D, T) {{LGN_DS(D, T, false, false), LGN_DS(D, T, false, true)}, {LGN_DS(D, T, true, false), LGN_DS(D, T, true, true)}}
-static const void *const kDistillTable[2][2][2][2] = {{LGN_DS4(LGN_F32, 128), LGN_DS4(LGN_F32, 256)}, {LGN_DS4(LGN_BF16, 128), LGN_DS4(LGN_BF16, 256)}};
+static const void *const kDistillTable[2][3][2][2] = {{LGN_DS4(LGN_F32, 32), LGN_DS4(LGN_F32, 128), LGN_DS4(LGN_F32, 256)},
+                                                      {LGN_DS4(LGN_BF16, 32), LGN_DS4(LGN_BF16, 128), LGN_DS4(LGN_BF16, 256)}};
 #undef LGN_DS4
 #undef LGN_DS
 
@@ -415,18 +441,20 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     p.scale = (float)((alpha == 0.0 ? 1.0 : 1.0 / temperature) * 1.4426950408889634);
     const bool grad = dlogits != nullptr;
     if (grad) for (p.table = 16; p.table < 2 * (top + 1); p.table *= 2) {}
-    const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + vals - 1) / vals;        // however a row is aligned
-    // 128 threads where they hold the row; else 256, and as many CTAs as hold it for a gradient.  More CTAs per row where there are
+    const bool aligned = aligned_to(logits, 16) && (ld * es) % 16 == 0;
+    const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + (aligned ? 0 : vals - 1)) / vals;        // of a row that is aligned worst
+    // The fewest threads of 32, 128 and 256 that hold the row; 256 of several CTAs for a gradient where they do not.  More CTAs per row where there are
     // too few rows to fill the machine.
-    const int big = pieces > 128 * kDsVecs;
-    const uint64_t per_cta = (uint64_t)(big ? 256 : 128) * kDsVecs;
+    const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 128 * kDsVecs ? 1 : 2;
+    const unsigned threads = kind == 0 ? 32 : kind == 1 ? 128 : 256;
+    const uint64_t per_cta = (uint64_t)threads * kDsVecs;
     unsigned cluster = 1;
     while (cluster < 8 && ((grad && pieces > cluster * per_cta) || (tokens * cluster < (uint64_t)sms && pieces > cluster * per_cta / 4))) cluster *= 2;
     p.pieces = (uint32_t)((pieces + cluster - 1) / cluster);
     if (tokens * cluster > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     const size_t smem = 4 * (3 * (top + 1) + p.table);
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
-             (unsigned long long)top, dual ? "two softmaxes" : "one softmax", big ? 256 : 128, cluster, grad ? ", gradient" : "");
+             (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
     void *args[] = {&p};
-    return launch_dependent(kDistillTable[dt][big][dual][grad], dim3((unsigned)(tokens * cluster)), dim3(big ? 256 : 128), args, smem, stream, cluster);
+    return launch_dependent(kDistillTable[dt][kind][dual][grad], dim3((unsigned)(tokens * cluster)), dim3(threads), args, smem, stream, cluster);
 }
