@@ -44,6 +44,7 @@ struct DistillArgs {
     uint32_t vocab, top;
     uint32_t pieces;                                    // of 16 bytes, per CTA of a row
     uint32_t table;                                     // slots of the id table, a power of two
+    uint32_t slots;                                     // where the row's pieces begin in shared memory, in words
     int32_t ids64, labels64, teacher_dt;
     float temperature, alpha, beta;                     // beta = 1 - alpha
     float scale, scale1;                                // log2(e) / T and log2(e); the first alone where one softmax serves
@@ -86,8 +87,6 @@ template <int DT> struct Piece {
             return fmaxf(m, fmaxf(bf_lo(a), bf_hi(a)));
         }
     }
-    // What was made of the words so far is not kept for later: unpacked values would take twice the registers.
-    __device__ __forceinline__ void forget() { asm volatile("" : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])); }
 };
 // A piece that the row begins or ends in: column `c` is the first, columns outside the row read as -inf and are not written.  Of its own, so that
 // the loops over whole pieces stay short.
@@ -159,7 +158,7 @@ template <bool DUAL> struct RowSums {
 
 // DUAL: the two parts take softmaxes of different temperatures.
 template <int DT, int THREADS, bool DUAL, bool GRAD>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 1536 / THREADS)
 distill_kernel(const DistillArgs p) {
     constexpr int kVals = Piece<DT>::kVals, ES = 16 / kVals, kWarps = THREADS / 32;
     extern __shared__ uint32_t dyn[];
@@ -209,21 +208,26 @@ distill_kernel(const DistillArgs p) {
     float z0 = 0.0f, s0 = 0.0f, w = 1.0f;
     const int64_t far0 = place_of(tid, z0);
     if (GRAD && p.weight != nullptr) w = __uint_as_float(ldro_u32(p.weight + row));
-    Piece<DT> x[kDsVecs];
+    const uint32_t slots = smem_u32(dyn + p.slots) + tid * 16;      // the thread's pieces: nobody else's, no barrier
     auto load = [&](uint32_t v) {
         const char *at = base + (uint64_t)(v + tid) * 16;
         #pragma unroll
         for (int i = 0; i < kDsVecs; ++i) {
             if (v + i * THREADS >= v1 && i > 0) break;
             const uint32_t u = v + i * THREADS + tid;
-            uint32_t (&q)[4] = x[i].w;
+            const uint32_t slot = slots + i * THREADS * 16;
             if (u - in0 < in1 - in0)
-                asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "l"(at + i * THREADS * 16) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(at + i * THREADS * 16) : "memory");
             else {
                 const uint4 e = u < v1 ? load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab) : make_uint4(kNone, kNone, kNone, kNone);
-                q[0] = e.x; q[1] = e.y; q[2] = e.z; q[3] = e.w;
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(slot), "r"(e.x), "r"(e.y), "r"(e.z), "r"(e.w) : "memory");
             }
         }
+    };
+    auto piece = [&](int i) {
+        Piece<DT> x;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.w[0]), "=r"(x.w[1]), "=r"(x.w[2]), "=r"(x.w[3]) : "r"(slots + i * THREADS * 16) : "memory");
+        return x;
     };
     load(v0);
     const int32_t id0 = present(tid, far0, z0);
@@ -232,10 +236,11 @@ distill_kernel(const DistillArgs p) {
     RowSums<DUAL> r = {kDsLowest, 0.0f, 0.0f, kDsLowest, kDsLowest, 0.0f, 0.0f};
     for (uint32_t v = v0;;) {
         float c = r.m;
+        asm volatile("cp.async.wait_all;" ::: "memory");
         #pragma unroll
         for (int i = 0; i < kDsVecs; ++i) {
             if (v + i * THREADS >= v1 && i > 0) break;
-            c = x[i].max_with(c);
+            c = piece(i).max_with(c);
         }
         r.sum *= exp2_approx((r.m - c) * p.scale);
         if constexpr (DUAL) r.sum1 *= exp2_approx((r.m - c) * p.scale1);
@@ -244,10 +249,10 @@ distill_kernel(const DistillArgs p) {
         for (int i = 0; i < kDsVecs; ++i) {
             if (v + i * THREADS >= v1 && i > 0) break;
             float a = 0.0f, a1 = 0.0f;
-            x[i].forget();
+            const Piece<DT> x = piece(i);
             #pragma unroll
             for (int k = 0; k < kVals; ++k) {
-                const float t = x[i].at(k) - c;
+                const float t = x.at(k) - c;
                 a += exp2_approx(t * p.scale);
                 if constexpr (DUAL) a1 += exp2_approx(t * p.scale1);
             }
@@ -336,7 +341,10 @@ distill_kernel(const DistillArgs p) {
         };
         const bool held = v1 - v0 <= THREADS * kDsVecs; // the one chunk is still in registers
         for (uint32_t v = v0; v < v1; v += THREADS * kDsVecs) {
-            if (!held) load(v);
+            if (!held) {
+                load(v);
+                asm volatile("cp.async.wait_all;" ::: "memory");
+            }
             char *to = dst - shift * ES + (uint64_t)(v + tid) * 16;
             #pragma unroll
             for (int i = 0; i < kDsVecs; ++i) {
@@ -345,9 +353,9 @@ distill_kernel(const DistillArgs p) {
                 if (u < v1) {
                     float d[kVals];
                     uint32_t q[4];
-                    x[i].forget();
+                    const Piece<DT> x = piece(i);
                     #pragma unroll
-                    for (int k = 0; k < kVals; ++k) d[k] = slope(x[i].at(k));
+                    for (int k = 0; k < kVals; ++k) d[k] = slope(x.at(k));
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         if constexpr (DT == LGN_F32) q[k] = __float_as_uint(d[k]);
@@ -452,9 +460,15 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     while (cluster < 8 && ((grad && pieces > cluster * per_cta) || (tokens * cluster < (uint64_t)sms && pieces > cluster * per_cta / 4))) cluster *= 2;
     p.pieces = (uint32_t)((pieces + cluster - 1) / cluster);
     if (tokens * cluster > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
-    const size_t smem = 4 * (3 * (top + 1) + p.table);
+    p.slots = (uint32_t)((3 * (top + 1) + p.table + 3) & ~3ull);
+    const size_t smem = 4 * p.slots + 16 * per_cta;
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
              (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
+    const void *fn = kDistillTable[dt][kind][dual][grad];
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {     // many entries
+        (void)cudaGetLastError();
+        return LGN_ERR_CUDA;
+    }
     void *args[] = {&p};
-    return launch_dependent(kDistillTable[dt][kind][dual][grad], dim3((unsigned)(tokens * cluster)), dim3(threads), args, smem, stream, cluster);
+    return launch_dependent(fn, dim3((unsigned)(tokens * cluster)), dim3(threads), args, smem, stream, cluster);
 }
