@@ -29,7 +29,7 @@
 namespace lgn {
 
 constexpr uint64_t kDsMaxTop = 1024, kDsMaxDim = 1ull << 30;
-constexpr int kDsVecs = 8;                              // pieces of 16 bytes a thread holds
+constexpr int kDsVecs = 16;                             // pieces of 16 bytes a thread holds
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kDsLowest = -3.402823466e38f;           // starts every maximum: s - M is then never inf - inf for s = -inf
 
@@ -125,40 +125,47 @@ __device__ __forceinline__ float shared_of(uint32_t addr, uint32_t rank) {
     return x;
 }
 
-// What a warp, or all of them, know of a row: the logits' maximum and sums of exponentials, the teacher's maximum, sum and
-// weighted differences dot = sum exp((z - zm) / T) ((z - zm) - (s - sm)), sm the largest of the student's logits at the places.
-template <bool DUAL> struct RowSums {
-    float m, sum, sum1, zm, sm, z_sum, dot;
-    // Over groups of WIDTH lanes, in a fixed order; the same in all of them.
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+template <int WIDTH>
+__device__ __forceinline__ float lanes_sum(float v) {
+    #pragma unroll
+    for (int d = WIDTH / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+// What is known of a teacher's entries: their maximum, sum and weighted differences dot = sum exp((z - zm) / T) ((z - zm) - (s - sm)), sm the largest
+// of the student's logits at the places.
+struct TeacherSums {
+    float zm, sm, sum, dot;
+    __device__ __forceinline__ void rebase(float z, float s, float scale) {
+        const float f = sum != 0.0f ? exp2_approx((zm - z) * scale) : 0.0f;         // without entries the references mean nothing
+        dot = f != 0.0f ? f * (dot + sum * ((zm - z) - (sm - s))) : 0.0f;
+        sum *= f;
+        zm = z;
+        sm = s;
+    }
+    __device__ __forceinline__ void add(float z, float s, float scale) {
+        rebase(fmaxf(zm, z), fmaxf(sm, s), scale);
+        const float e = exp2_approx((z - zm) * scale);
+        sum += e;
+        if (e != 0.0f) dot += e * ((z - zm) - (s - sm));
+    }
+    // Over groups of WIDTH lanes (copies of one another beyond the first), in a fixed order.
     template <int WIDTH>
-    __device__ __forceinline__ void join(float scale, float scale1) {
-        const float m0 = m, zm0 = zm, sm0 = sm;
-        #pragma unroll
-        for (int d = WIDTH / 2; d > 0; d >>= 1) {
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            zm = fmaxf(zm, __shfl_xor_sync(0xffffffffu, zm, d));
-            sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
-        }
-        sum *= exp2_approx((m0 - m) * scale);
-        if constexpr (DUAL) sum1 *= exp2_approx((m0 - m) * scale1);
-        if (z_sum != 0.0f) {                                            // where there are none the references mean nothing
-            const float f = exp2_approx((zm0 - zm) * scale);
-            dot = f != 0.0f ? f * (dot + z_sum * ((zm0 - zm) - (sm0 - sm))) : 0.0f;
-            z_sum *= f;
-        }
-        #pragma unroll
-        for (int d = WIDTH / 2; d > 0; d >>= 1) {
-            sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if constexpr (DUAL) sum1 += __shfl_xor_sync(0xffffffffu, sum1, d);
-            z_sum += __shfl_xor_sync(0xffffffffu, z_sum, d);
-            dot += __shfl_xor_sync(0xffffffffu, dot, d);
-        }
+    __device__ __forceinline__ void join(float scale) {
+        rebase(warp_max(zm), warp_max(sm), scale);
+        sum = lanes_sum<WIDTH>(sum);
+        dot = lanes_sum<WIDTH>(dot);
     }
 };
 
 // DUAL: the two parts take softmaxes of different temperatures.
 template <int DT, int THREADS, bool DUAL, bool GRAD>
-__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 1536 / THREADS)
+__global__ void __launch_bounds__(THREADS, 768 / THREADS)
 distill_kernel(const DistillArgs p) {
     constexpr int kVals = Piece<DT>::kVals, ES = 16 / kVals, kWarps = THREADS / 32;
     extern __shared__ uint32_t dyn[];
@@ -209,11 +216,12 @@ distill_kernel(const DistillArgs p) {
     const int64_t far0 = place_of(tid, z0);
     if (GRAD && p.weight != nullptr) w = __uint_as_float(ldro_u32(p.weight + row));
     const uint32_t slots = smem_u32(dyn + p.slots) + tid * 16;      // the thread's pieces: nobody else's, no barrier
+    auto used = [&](uint32_t v) { return (int)min((uint32_t)kDsVecs, (v1 - v + THREADS - 1) / THREADS); };     // pieces per thread of the chunk from v on
     auto load = [&](uint32_t v) {
         const char *at = base + (uint64_t)(v + tid) * 16;
-        #pragma unroll
-        for (int i = 0; i < kDsVecs; ++i) {
-            if (v + i * THREADS >= v1 && i > 0) break;
+        const int n = used(v);
+        #pragma unroll 4
+        for (int i = 0; i < n; ++i) {
             const uint32_t u = v + i * THREADS + tid;
             const uint32_t slot = slots + i * THREADS * 16;
             if (u - in0 < in1 - in0)
@@ -233,21 +241,20 @@ distill_kernel(const DistillArgs p) {
     const int32_t id0 = present(tid, far0, z0);
     if (id0 >= 0) s0 = ds_load<DT>(src, (uint64_t)id0);
 
-    RowSums<DUAL> r = {kDsLowest, 0.0f, 0.0f, kDsLowest, kDsLowest, 0.0f, 0.0f};
+    float m = kDsLowest, sum = 0.0f, sum1 = 0.0f;
     for (uint32_t v = v0;;) {
-        float c = r.m;
+        float c = m;
         asm volatile("cp.async.wait_all;" ::: "memory");
-        #pragma unroll
-        for (int i = 0; i < kDsVecs; ++i) {
-            if (v + i * THREADS >= v1 && i > 0) break;
+        const int n = used(v);
+        #pragma unroll 2
+        for (int i = 0; i < n; ++i) {
             c = piece(i).max_with(c);
         }
-        r.sum *= exp2_approx((r.m - c) * p.scale);
-        if constexpr (DUAL) r.sum1 *= exp2_approx((r.m - c) * p.scale1);
-        r.m = c;
-        #pragma unroll
-        for (int i = 0; i < kDsVecs; ++i) {
-            if (v + i * THREADS >= v1 && i > 0) break;
+        sum *= exp2_approx((m - c) * p.scale);
+        if constexpr (DUAL) sum1 *= exp2_approx((m - c) * p.scale1);
+        m = c;
+        #pragma unroll 2
+        for (int i = 0; i < n; ++i) {
             float a = 0.0f, a1 = 0.0f;
             const Piece<DT> x = piece(i);
             #pragma unroll
@@ -256,18 +263,23 @@ distill_kernel(const DistillArgs p) {
                 a += exp2_approx(t * p.scale);
                 if constexpr (DUAL) a1 += exp2_approx(t * p.scale1);
             }
-            r.sum += a;
-            r.sum1 += a1;
+            sum += a;
+            if constexpr (DUAL) sum1 += a1;
         }
         v += THREADS * kDsVecs;
         if (v >= v1) break;
         load(v);
     }
 
-    // the entries, a warp's at a time: 32 of them share their references
-    auto enter = [&](uint32_t j, int32_t at, float z, float s) {
-        if (j < entries) { id[j] = at; ze[j] = z; se[j] = s; }
-        if (GRAD && at >= 0 && j < p.top) {
+    // the entries
+    TeacherSums z = {kDsLowest, kDsLowest, 0.0f, 0.0f};
+    bool some = false;
+    auto enter = [&](uint32_t j, int32_t at, float zj, float sj) {
+        if (j < entries) { id[j] = at; ze[j] = zj; se[j] = sj; }
+        if (at < 0 || j == p.top) return;
+        some = true;
+        z.add(zj, sj, p.scale);
+        if constexpr (GRAD) {
             uint32_t h = ((uint32_t)at * 2654435761u) & (p.table - 1);
             for (;;) {                                  // ends: the table has more slots than there are entries
                 const uint32_t old = atomicCAS(&table[h], 0u, (uint32_t)at + 1u) & 0x7fffffffu;
@@ -276,31 +288,40 @@ distill_kernel(const DistillArgs p) {
                 h = (h + 1) & (p.table - 1);
             }
         }
-        if (at >= 0 && j < p.top) {
-            const float zm = fmaxf(r.zm, z), sm = fmaxf(r.sm, s), f = r.z_sum != 0.0f ? exp2_approx((r.zm - zm) * p.scale) : 0.0f, e = exp2_approx((z - zm) * p.scale);
-            r.dot = (f != 0.0f ? f * (r.dot + r.z_sum * ((r.zm - zm) - (r.sm - sm))) : 0.0f) + (e != 0.0f ? e * ((z - zm) - (s - sm)) : 0.0f);
-            r.z_sum = r.z_sum * f + e;
-            r.zm = zm;
-            r.sm = sm;
-        }
     };
-    enter(tid, id0, z0, s0);
-    for (uint32_t j = tid + THREADS; j < entries; j += THREADS) {
-        float z = 0.0f;
-        const int32_t at = present(j, place_of(j, z), z);
-        enter(j, at, z, at >= 0 ? ds_load<DT>(src, (uint64_t)at) : 0.0f);
+    const bool entered = warp * 32 < entries;           // warps with entries: only they need what is known of them
+    if (entered) {
+        enter(tid, id0, z0, s0);
+        for (uint32_t j = tid + THREADS; j < entries; j += THREADS) {
+            float zj = 0.0f;
+            const int32_t at = present(j, place_of(j, zj), zj);
+            enter(j, at, zj, at >= 0 ? ds_load<DT>(src, (uint64_t)at) : 0.0f);
+        }
+        __syncwarp();
+        z.template join<32>(p.scale);
     }
-    r.template join<32>(p.scale, p.scale1);
+    {
+        const float c = warp_max(m);
+        sum = lanes_sum<32>(sum * exp2_approx((m - c) * p.scale));
+        if constexpr (DUAL) sum1 = lanes_sum<32>(sum1 * exp2_approx((m - c) * p.scale1));
+        m = c;
+    }
     if constexpr (kWarps > 1) {
         if (lane == 0) {
-            parts[0][warp] = r.m; parts[1][warp] = r.sum; parts[2][warp] = r.sum1; parts[3][warp] = r.zm; parts[4][warp] = r.sm; parts[5][warp] = r.z_sum; parts[6][warp] = r.dot;
+            parts[0][warp] = m; parts[1][warp] = sum; parts[2][warp] = sum1;
+            parts[3][warp] = z.zm; parts[4][warp] = z.sm; parts[5][warp] = z.sum; parts[6][warp] = z.dot;
         }
-        __syncthreads();
+        some = __syncthreads_or(some);
         const uint32_t from = lane % kWarps;
-        r = {parts[0][from], parts[1][from], parts[2][from], parts[3][from], parts[4][from], parts[5][from], parts[6][from]};
-        r.template join<kWarps>(p.scale, p.scale1);
-    } else __syncwarp();
-    float m = r.m, sum = r.sum, sum1 = r.sum1;
+        const float c = parts[0][from];
+        m = warp_max(c);
+        sum = lanes_sum<kWarps>(parts[1][from] * exp2_approx((c - m) * p.scale));
+        if constexpr (DUAL) sum1 = lanes_sum<kWarps>(parts[2][from] * exp2_approx((c - m) * p.scale1));
+        if (entered) {
+            z = {parts[3][from], parts[4][from], parts[5][from], parts[6][from]};
+            z.template join<kWarps>(p.scale);
+        }
+    } else some = __any_sync(0xffffffffu, some);
     if (nrank > 1) {
         const uint32_t at = smem_u32(joint);
         if (tid == 0) { joint[0] = m; joint[1] = sum; joint[2] = sum1; }
@@ -309,9 +330,9 @@ distill_kernel(const DistillArgs p) {
         const float m0 = shared_of(at, from);
         sum = shared_of(at + 4, from);
         if constexpr (DUAL) sum1 = shared_of(at + 8, from);
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");           // waited for at the end
-        m = m0;
-        for (uint32_t d = nrank / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        m = warp_max(m0);
         sum *= exp2_approx((m0 - m) * p.scale);
         if constexpr (DUAL) sum1 *= exp2_approx((m0 - m) * p.scale1);
         for (uint32_t d = nrank / 2; d > 0; d >>= 1) {
@@ -320,11 +341,10 @@ distill_kernel(const DistillArgs p) {
         }
     }
     const int32_t label = id[p.top];
-    const bool some = r.z_sum != 0.0f;                  // the largest entry counts 1; NaN is not 0 either
     if (rank == 0 && tid == 0) {
         const float s1 = DUAL ? sum1 : sum;             // the label's sum
         float loss = 0.0f;
-        if (some) loss = p.alpha * p.temperature * (r.dot / r.z_sum + (m - r.sm) + p.temperature * (logf(sum) - logf(r.z_sum)));
+        if (some) loss = p.alpha * p.temperature * (z.dot / z.sum + (m - z.sm) + p.temperature * (logf(sum) - logf(z.sum)));
         if (label >= 0) loss += p.beta * (logf(s1) - (se[p.top] - m));
         p.loss[row] = loss;
     }
@@ -339,33 +359,43 @@ distill_kernel(const DistillArgs p) {
             if constexpr (DUAL) d += exp2_approx(t * p.scale1) * c1;
             return d;
         };
-        const bool held = v1 - v0 <= THREADS * kDsVecs; // the one chunk is still in registers
+        // bf16: the factors are taken into the exponents, whose rounding (2^-24 of about forty) is far below the output's
+        constexpr bool kFold = DT == LGN_BF16;
+        const float lt = kFold ? log2f(fabsf(ct)) : 0.0f, l1 = kFold ? log2f(fabsf(c1)) : 0.0f;
+        const uint32_t sign = kFold && w < 0.0f ? 0x80008000u : 0u;
+        const bool held = v1 - v0 <= THREADS * kDsVecs; // the one chunk is still there
         for (uint32_t v = v0; v < v1; v += THREADS * kDsVecs) {
             if (!held) {
                 load(v);
                 asm volatile("cp.async.wait_all;" ::: "memory");
             }
             char *to = dst - shift * ES + (uint64_t)(v + tid) * 16;
-            #pragma unroll
-            for (int i = 0; i < kDsVecs; ++i) {
-                if (v + i * THREADS >= v1) break;
+            const int n = used(v);
+            #pragma unroll 2
+            for (int i = 0; i < n; ++i) {
                 const uint32_t u = v + i * THREADS + tid;
-                if (u < v1) {
-                    float d[kVals];
-                    uint32_t q[4];
+                uint32_t q[4];
+                if (dead) q[0] = q[1] = q[2] = q[3] = 0u;
+                else {
                     const Piece<DT> x = piece(i);
+                    float d[kVals];
                     #pragma unroll
-                    for (int k = 0; k < kVals; ++k) d[k] = slope(x.at(k));
+                    for (int k = 0; k < kVals; ++k) {
+                        if constexpr (kFold) {
+                            const float t = x.at(k) - m;
+                            d[k] = exp2_approx(fmaf(t, p.scale, lt));
+                            if constexpr (DUAL) d[k] += exp2_approx(fmaf(t, p.scale1, l1));
+                        } else d[k] = slope(x.at(k));
+                    }
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         if constexpr (DT == LGN_F32) q[k] = __float_as_uint(d[k]);
-                        else q[k] = pack_bf16(d[2 * k], d[2 * k + 1]);
-                        if (dead) q[k] = 0u;
+                        else q[k] = pack_bf16(d[2 * k], d[2 * k + 1]) ^ sign;
                     }
-                    if (whole && u - in0 < in1 - in0)
-                        asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(to + i * THREADS * 16), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
-                    else store_edge<DT>(dst, (int64_t)u * kVals - shift, p.vocab, make_uint4(q[0], q[1], q[2], q[3]));
                 }
+                if (whole && u - in0 < in1 - in0)
+                    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(to + i * THREADS * 16), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
+                else if (u < v1) store_edge<DT>(dst, (int64_t)u * kVals - shift, p.vocab, make_uint4(q[0], q[1], q[2], q[3]));
             }
         }
         __syncthreads();                                // the places are written over what other threads wrote there
@@ -377,12 +407,12 @@ distill_kernel(const DistillArgs p) {
             while (((slot = table[h]) & 0x7fffffffu) != (uint32_t)at + 1u && slot != 0u) h = (h + 1) & (p.table - 1);
             float d = slope(se[j]);
             if (j < p.top) {
-                float pt = exp2_approx((ze[j] - r.zm) * p.scale);
+                float pt = exp2_approx((ze[j] - z.zm) * p.scale);
                 if (slot >> 31) {
                     pt = 0.0f;
-                    for (uint32_t i = 0; i < p.top; ++i) if (id[i] == at) pt += exp2_approx((ze[i] - r.zm) * p.scale);
+                    for (uint32_t i = 0; i < p.top; ++i) if (id[i] == at) pt += exp2_approx((ze[i] - z.zm) * p.scale);
                 }
-                d -= kt * (pt / r.z_sum);
+                d -= kt * (pt / z.sum);
                 if (at == label) d -= k1;
             } else {
                 if (slot != 0u) continue;               // an entry has the label's place
@@ -397,8 +427,8 @@ distill_kernel(const DistillArgs p) {
 
 #define LGN_DS(D, T, U, G) reinterpret_cast<const void *>(&distill_kernel<D, T, U, G>)
 #define LGN_DS4(D, T) {{LGN_DS(D, T, false, false), LGN_DS(D, T, false, true)}, {LGN_DS(D, T, true, false), LGN_DS(D, T, true, true)}}
-static const void *const kDistillTable[2][3][2][2] = {{LGN_DS4(LGN_F32, 32), LGN_DS4(LGN_F32, 128), LGN_DS4(LGN_F32, 256)},
-                                                      {LGN_DS4(LGN_BF16, 32), LGN_DS4(LGN_BF16, 128), LGN_DS4(LGN_BF16, 256)}};
+static const void *const kDistillTable[2][3][2][2] = {{LGN_DS4(LGN_F32, 32), LGN_DS4(LGN_F32, 64), LGN_DS4(LGN_F32, 128)},
+                                                      {LGN_DS4(LGN_BF16, 32), LGN_DS4(LGN_BF16, 64), LGN_DS4(LGN_BF16, 128)}};
 #undef LGN_DS4
 #undef LGN_DS
 
@@ -453,8 +483,8 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + (aligned ? 0 : vals - 1)) / vals;        // of a row that is aligned worst
     // The fewest threads of 32, 128 and 256 that hold the row; 256 of several CTAs for a gradient where they do not.  More CTAs per row where there are
     // too few rows to fill the machine.
-    const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 128 * kDsVecs ? 1 : 2;
-    const unsigned threads = kind == 0 ? 32 : kind == 1 ? 128 : 256;
+    const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 64 * kDsVecs ? 1 : 2;
+    const unsigned threads = kind == 0 ? 32 : kind == 1 ? 64 : 128;
     const uint64_t per_cta = (uint64_t)threads * kDsVecs;
     unsigned cluster = 1;
     while (cluster < 8 && ((grad && pieces > cluster * per_cta) || (tokens * cluster < (uint64_t)sms && pieces > cluster * per_cta / 4))) cluster *= 2;
