@@ -29,7 +29,7 @@
 namespace lgn {
 
 constexpr uint64_t kDsMaxTop = 1024, kDsMaxDim = 1ull << 30;
-constexpr int kDsVecs = 16;                             // pieces of 16 bytes a thread holds
+constexpr int kDsVecs = 16;                             // pieces of 16 bytes a thread holds at most
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kDsLowest = -3.402823466e38f;           // starts every maximum: s - M is then never inf - inf for s = -inf
 
@@ -44,6 +44,7 @@ struct DistillArgs {
     uint32_t vocab, top;
     uint32_t pieces;                                    // of 16 bytes, per CTA of a row
     uint32_t table;                                     // slots of the id table, a power of two
+    uint32_t vecs;                                      // pieces of a thread in a chunk
     uint32_t slots;                                     // where the row's pieces begin in shared memory, in words
     int32_t ids64, labels64, teacher_dt;
     float temperature, alpha, beta;                     // beta = 1 - alpha
@@ -53,6 +54,11 @@ struct DistillArgs {
 __device__ __forceinline__ float exp2_approx(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float log2_approx(float x) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 template <int DT>
@@ -165,7 +171,7 @@ struct TeacherSums {
 
 // DUAL: the two parts take softmaxes of different temperatures.
 template <int DT, int THREADS, bool DUAL, bool GRAD>
-__global__ void __launch_bounds__(THREADS, 768 / THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 768 / THREADS)
 distill_kernel(const DistillArgs p) {
     constexpr int kVals = Piece<DT>::kVals, ES = 16 / kVals, kWarps = THREADS / 32;
     extern __shared__ uint32_t dyn[];
@@ -216,7 +222,7 @@ distill_kernel(const DistillArgs p) {
     const int64_t far0 = place_of(tid, z0);
     if (GRAD && p.weight != nullptr) w = __uint_as_float(ldro_u32(p.weight + row));
     const uint32_t slots = smem_u32(dyn + p.slots) + tid * 16;      // the thread's pieces: nobody else's, no barrier
-    auto used = [&](uint32_t v) { return (int)min((uint32_t)kDsVecs, (v1 - v + THREADS - 1) / THREADS); };     // pieces per thread of the chunk from v on
+    auto used = [&](uint32_t v) { return (int)min(p.vecs, (v1 - v + THREADS - 1) / THREADS); };     // pieces per thread of the chunk from v on
     auto load = [&](uint32_t v) {
         const char *at = base + (uint64_t)(v + tid) * 16;
         const int n = used(v);
@@ -266,7 +272,7 @@ distill_kernel(const DistillArgs p) {
             sum += a;
             if constexpr (DUAL) sum1 += a1;
         }
-        v += THREADS * kDsVecs;
+        v += THREADS * p.vecs;
         if (v >= v1) break;
         load(v);
     }
@@ -361,10 +367,11 @@ distill_kernel(const DistillArgs p) {
         };
         // bf16: the factors are taken into the exponents, whose rounding (2^-24 of about forty) is far below the output's
         constexpr bool kFold = DT == LGN_BF16;
-        const float lt = kFold ? log2f(fabsf(ct)) : 0.0f, l1 = kFold ? log2f(fabsf(c1)) : 0.0f;
+        const float lt = kFold ? log2_approx(fabsf(DUAL ? kt : kt + k1)) - log2_approx(sum) : 0.0f;
+        const float l1 = kFold && DUAL ? log2_approx(fabsf(k1)) - log2_approx(sum1) : 0.0f;
         const uint32_t sign = kFold && w < 0.0f ? 0x80008000u : 0u;
-        const bool held = v1 - v0 <= THREADS * kDsVecs; // the one chunk is still there
-        for (uint32_t v = v0; v < v1; v += THREADS * kDsVecs) {
+        const bool held = v1 - v0 <= THREADS * p.vecs; // the one chunk is still there
+        for (uint32_t v = v0; v < v1; v += THREADS * p.vecs) {
             if (!held) {
                 load(v);
                 asm volatile("cp.async.wait_all;" ::: "memory");
@@ -491,7 +498,10 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     p.pieces = (uint32_t)((pieces + cluster - 1) / cluster);
     if (tokens * cluster > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     p.slots = (uint32_t)((3 * (top + 1) + p.table + 3) & ~3ull);
-    const size_t smem = 4 * p.slots + 16 * per_cta;
+    // a loss alone has no use for the row after its sums: shorter chunks, more CTAs at a time
+    p.vecs = (p.pieces + threads - 1) / threads;
+    if (p.vecs > (grad ? kDsVecs : kDsVecs / 2)) p.vecs = grad ? kDsVecs : kDsVecs / 2;
+    const size_t smem = 4 * p.slots + 16 * (size_t)threads * p.vecs;
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
              (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
     const void *fn = kDistillTable[dt][kind][dual][grad];
