@@ -171,7 +171,7 @@ struct TeacherSums {
 
 // DUAL: the two parts take softmaxes of different temperatures.
 template <int DT, int THREADS, bool DUAL, bool GRAD>
-__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 768 / THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : THREADS == 256 ? 6 : 768 / THREADS)
 distill_kernel(const DistillArgs p) {
     constexpr int kVals = Piece<DT>::kVals, ES = 16 / kVals, kWarps = THREADS / 32;
     extern __shared__ uint32_t dyn[];
@@ -433,9 +433,9 @@ distill_kernel(const DistillArgs p) {
 }
 
 #define LGN_DS(D, T, U, G) reinterpret_cast<const void *>(&distill_kernel<D, T, U, G>)
-#define LGN_DS4(D, T) {{LGN_DS(D, T, false, false), LGN_DS(D, T, false, true)}, {LGN_DS(D, T, true, false), LGN_DS(D, T, true, true)}}
-static const void *const kDistillTable[2][3][2][2] = {{LGN_DS4(LGN_F32, 32), LGN_DS4(LGN_F32, 64), LGN_DS4(LGN_F32, 128)},
-                                                      {LGN_DS4(LGN_BF16, 32), LGN_DS4(LGN_BF16, 64), LGN_DS4(LGN_BF16, 128)}};
+#define LGN_DS4(D, T, L) {{LGN_DS(D, L, false, false), LGN_DS(D, T, false, true)}, {LGN_DS(D, L, true, false), LGN_DS(D, T, true, true)}}
+static const void *const kDistillTable[2][3][2][2] = {{LGN_DS4(LGN_F32, 32, 32), LGN_DS4(LGN_F32, 64, 64), LGN_DS4(LGN_F32, 128, 256)},
+                                                      {LGN_DS4(LGN_BF16, 32, 32), LGN_DS4(LGN_BF16, 64, 64), LGN_DS4(LGN_BF16, 128, 256)}};
 #undef LGN_DS4
 #undef LGN_DS
 
@@ -488,17 +488,17 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     if (grad) for (p.table = 16; p.table < 2 * (top + 1); p.table *= 2) {}
     const bool aligned = aligned_to(logits, 16) && (ld * es) % 16 == 0;
     const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + (aligned ? 0 : vals - 1)) / vals;        // of a row that is aligned worst
-    // The fewest threads of 32, 128 and 256 that hold the row; 256 of several CTAs for a gradient where they do not.  More CTAs per row where there are
-    // too few rows to fill the machine.
+    // A gradient needs the row twice: the fewest threads of 32, 64 and 128 that hold it, or up to 8 CTAs of 128 (16 pieces per thread: what a CTA does
+    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 199 us,
+    // 207 with 128).  More CTAs per row where there are too few rows to fill the machine.
     const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 64 * kDsVecs ? 1 : 2;
-    const unsigned threads = kind == 0 ? 32 : kind == 1 ? 64 : 128;
+    const unsigned threads = kind == 0 ? 32 : kind == 1 ? 64 : grad ? 128 : 256;
     const uint64_t per_cta = (uint64_t)threads * kDsVecs;
     unsigned cluster = 1;
     while (cluster < 8 && ((grad && pieces > cluster * per_cta) || (tokens * cluster < (uint64_t)sms && pieces > cluster * per_cta / 4))) cluster *= 2;
     p.pieces = (uint32_t)((pieces + cluster - 1) / cluster);
     if (tokens * cluster > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     p.slots = (uint32_t)((3 * (top + 1) + p.table + 3) & ~3ull);
-    // a loss alone has no use for the row after its sums: shorter chunks, more CTAs at a time
     p.vecs = (p.pieces + threads - 1) / threads;
     if (p.vecs > (grad ? kDsVecs : kDsVecs / 2)) p.vecs = grad ? kDsVecs : kDsVecs / 2;
     const size_t smem = 4 * p.slots + 16 * (size_t)threads * p.vecs;
