@@ -50,29 +50,36 @@ static double gm_likely_tiles(uint64_t rows, uint64_t groups, uint64_t height) {
     return met * (each < 1.0 ? 1.0 : each);
 }
 
-// The kernel of least estimated time: rounds of the grid times the cost of a tile.  What the sizes of the groups are is known on the device
-// alone; equal ones are assumed here.
+// The kernel of least estimated time: rounds of the grid times the cost of a tile, in microseconds (`start` once, `step` for 128 bytes of the contraction,
+// `tile` beyond that).  What the sizes of the groups are is known on the device alone; equal ones are assumed here.  Which side of these a
+// call lies on is what the costs must get right (one GPU, operands larger than L2 or cycled through; groups' sizes spread by a factor of 8):
+//   swapped, 4 shares    2 rows, 8 x 4096 x 4096: 12.8 us, 23.9 with pairs of 256
+//   swapped / lone 256   64 rows, the same: 45 and 47, 52 with pairs; 5003 rows, 60 x 1448 x 1000: lone 256 46 us, pairs 50, lone 128 55
+//   pairs of 256         2048 rows, 8 x 4096 x 4096: 81 us, lone 256 88, lone 128 92; 32768 rows, 8 x 1024 x 1024: 57, 63, 70
+//   pairs of 128 (8-bit) 512 rows, 4096 x 4096: 11.0 us, lone 128 11.9, pairs of 256 16.0
+//   rows shared out      gradient of 2 x 512 x 512 over 32768 rows: 35 us in 4 shares, 113 with lone 128, 134 with pairs
 static GmPlan gm_plan(const GmKernels &list, uint64_t rows, uint64_t groups, uint64_t m, uint64_t n, uint64_t steps, int odt, int sms) {
     GmPlan best = {-1, 1, 0, 0};
     double best_cost = 1e300;
     for (int i = 0; i < list.count; ++i) {
         const GmKernel &q = list.first[i];
         if (q.odt != odt) continue;
+        const bool grad = q.form == kGmGrad || q.form == kGmShare, one = q.form == kGmSwap || q.form == kGmShare;
         const uint64_t height = q.form == kGmSwap ? (uint64_t)q.bn : 128 * (uint64_t)q.ctas, width = q.form == kGmSwap ? 128 : (uint64_t)q.bn;
         const uint64_t cols = (n + width - 1) / width;
-        const double row_tiles = q.form == kGmGrad ? (double)(groups * ((m + height - 1) / height)) : gm_likely_tiles(rows, groups, height);
-        const uint64_t most = q.form == kGmGrad ? groups * ((m + height - 1) / height) : gm_most_tiles(rows, groups, height);
-        const double tiles = row_tiles * (double)cols, each_steps = q.form == kGmGrad ? (double)rows / (double)groups / 64.0 + 0.5 : (double)steps;
+        const double row_tiles = grad ? (double)(groups * ((m + height - 1) / height)) : gm_likely_tiles(rows, groups, height);
+        const uint64_t most = grad ? groups * ((m + height - 1) / height) : gm_most_tiles(rows, groups, height);
+        const double tiles = row_tiles * (double)cols, all_steps = grad ? (double)rows / (double)groups / 64.0 + 0.5 : (double)steps;
         const double slots = (double)(q.form == kGmSwap ? 2 * sms : sms / q.ctas);
-        for (uint32_t split = 1; split <= (q.form == kGmSwap ? 8u : 1u); split *= 2) {
-            if (split > 1 && split > steps) break;
-            const double share = split > 1 ? (double)((steps + split - 1) / split) : each_steps;
+        for (uint32_t split = q.form == kGmShare ? 2 : 1; split <= (one ? 8u : 1u); split *= 2) {
+            if (split > 1 && ((double)split > all_steps || tiles * split > 2.0 * slots)) break;
+            const double share = split > 1 ? (double)(uint64_t)((all_steps + split - 1) / split) : all_steps;
             double rounds = tiles * split / slots;
             rounds = rounds < 1.0 ? 1.0 : rounds < 4.0 ? (double)(uint64_t)(rounds + 0.999) : rounds + 0.5;
-            const double cost = q.start + rounds * (share * q.step + q.tile) + (split > 1 ? 1.0 : 0.0);
+            const double cost = q.start + rounds * (share * q.step + q.tile) + (split > 1 ? 1.0 + 0.3 * split : 0.0);
             if (cost < best_cost) {
                 best_cost = cost;
-                best = {i, split, (uint32_t)(split > 1 ? (steps + split - 1) / split : steps), most};
+                best = {i, split, (uint32_t)((steps + split - 1) / split), most};
             }
         }
     }
@@ -98,26 +105,25 @@ static lgn_status gm_run(GmProduct which, const GmOperand &a, const GmOperand &b
     if (most > 0x3fffffffull || most * plan.split > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     p.vec = aligned_to(p.out, 16) && (p.ldo * es) % 16 == 0 && (p.n * es) % 16 == 0 && (!grad || p.groups == 1 || (p.out_group * es) % 16 == 0);
 
-    CUtensorMap ma = {}, mb = {}, mo = {};
+    CUtensorMap ma = {}, mb = {};
     const CUtensorMapDataType type = int8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const uint64_t ies = int8 ? 1 : 2;
     const bool any = p.rows > 0 && (grad || steps > 0);                   // anything to copy in
     // the MMA's rows come from the activations, or, swapped, from the weights
     const GmOperand &r = q.form == kGmSwap ? b : a, &c = q.form == kGmSwap ? a : b;
+    const bool one = q.form == kGmSwap || q.form == kGmShare;
     const bool boxes_r = grad || (q.form == kGmSwap && !q.along), boxes_c = grad || (q.form == kGmRows && !q.along);
     if (any && (!gm_map(&ma, type, ies, r.at, r.x, r.y, r.z, r.pitch, r.group, boxes_r ? 64 : 128) ||
                 !gm_map(&mb, type, ies, c.at, c.x, c.y, c.z, c.pitch, c.group, boxes_c ? 64 : (uint32_t)(q.bn / q.ctas)))) return LGN_ERR_CUDA;
-    if (p.vec && q.form != kGmSwap && !gm_map(&mo, odt == LGN_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, es, p.out, p.n,
-                                              grad ? p.m : p.rows, grad ? p.groups : 1, p.ldo, p.out_group, 32)) return LGN_ERR_CUDA;
     if (!gm_allow_smem(which, plan.kernel, q)) return LGN_ERR_CUDA;
     const uint64_t slots = (uint64_t)(sms / q.ctas);
-    uint64_t grid = q.form == kGmSwap ? most * plan.split : (most < slots ? most : slots) * (uint64_t)q.ctas;
+    uint64_t grid = one ? most * plan.split : (most < slots ? most : slots) * (uint64_t)q.ctas;
     if (grid == 0) grid = (uint64_t)q.ctas * plan.split;
     log_line("grouped: %s, rows %u groups %u m %u n %u, %llu steps, tile %llu x %llu, form %d, split %u, up to %llu tiles",
              which == kGmForward ? "X W^T" : which == kGmInput ? "X W" : which == kGmWeight ? "dY^T X" : "8-bit X W^T", p.rows, p.groups, p.m, p.n, (unsigned long long)steps,
              (unsigned long long)height, (unsigned long long)width, q.form, plan.split, (unsigned long long)most);
-    void *args[] = {&ma, &mb, &mo, &p};
-    return launch_dependent(q.fn, dim3((unsigned)grid), dim3(kGmThreads), args, (size_t)q.smem, stream, q.form == kGmSwap ? plan.split : (unsigned)q.ctas);
+    void *args[] = {&ma, &mb, &p};
+    return launch_dependent(q.fn, dim3((unsigned)grid), dim3((unsigned)gm_threads(q.form)), args, (size_t)q.smem, stream, one ? plan.split : (unsigned)q.ctas);
 }
 
 // Checks that the entries share: group offsets and the output.

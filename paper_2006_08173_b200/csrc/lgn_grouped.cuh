@@ -5,6 +5,7 @@
 //   kGmSwap  the same with the weights' 128 rows as the MMA's rows and BN activations as its columns: few rows per group;
 //            the CTAs of a cluster take consecutive shares of k and add their tiles through distributed shared memory
 //   kGmGrad  out_e = dY^T X over the rows of group e      tiles of 128 CTAS by BN of each group's matrix
+//   kGmShare the same with each group's rows shared out over the CTAs of a cluster, as kGmSwap does: few tiles, long groups
 // bf16 operands with fp32 sums, or 8-bit integers with 32-bit integer sums (exact) times a scale per row of either.
 //
 // A step of the contraction is 128 bytes of each row: 64 bf16 or 128 integers, four MMAs.  Operands whose rows run along
@@ -14,8 +15,8 @@
 //
 // In the gradient the contraction runs over a group's rows, and its last step would reach into the next group.  The
 // rows behind the group's end are written over with zeros in shared memory, up to the next multiple of 16, and the MMAs beyond
-// are left out: the producer waits for that step's copies (on a barrier of its own, one per CTA), clears the rows
-// and hands the step on.  Nothing else sees rows of another group but the output rows that are not stored.
+// are left out: a warp of its own (10) waits for that step's copies (on a barrier of each CTA), clears the rows
+// and hands the step on, while the copies go on with the next tile's.  Nothing else sees rows of another group but the output rows that are not stored.
 //
 // Roles as in the 8-bit float product: warp 8 copies, warp 9 issues MMAs, warps 0..7 read sums out.  Sums of
 // bf16 products leave tensor memory every 1024 of the contraction for registers, because the tensor cores' additions
@@ -30,10 +31,11 @@
 
 namespace lgn {
 
-enum GmForm { kGmRows = 0, kGmSwap = 1, kGmGrad = 2 };
+enum GmForm { kGmRows = 0, kGmSwap = 1, kGmGrad = 2, kGmShare = 3 };
 enum GmKind { kGmBf16 = 0, kGmInt8 = 1 };
 
-constexpr int kGmThreads = 320, kGmEpiWarps = 8;
+constexpr int kGmEpiWarps = 8;
+constexpr int gm_threads(int form) { return form == kGmGrad || form == kGmShare ? 352 : 320; }
 constexpr int kGmGroupRows = 16;                 // row tiles walked before the next column tile (L2 reuse)
 constexpr uint32_t kGmChunk = 16;                // steps whose sum stays in tensor memory (bf16)
 constexpr int kGmBuffer = 4096;                  // 32 rows x 128 bytes of output
@@ -55,21 +57,23 @@ struct GmArgs {
 
 template <int KIND, int BN, int CTAS, int FORM> struct GmShape {
     static constexpr int kKeep = KIND == kGmInt8 ? 128 : 64;        // of the contraction in a step
-    static constexpr int kStaging = FORM == kGmSwap ? 0 : kGmEpiWarps * kGmBuffer;
+    static constexpr int kStaging = FORM == kGmSwap || FORM == kGmShare ? 0 : kGmEpiWarps * kGmBuffer;
     static constexpr int kStageBytes = 128 * 128 + BN / CTAS * 128;
     static constexpr int kFit = ((FORM == kGmSwap ? 100 : 225) * 1024 - kStaging) / kStageBytes;
     static constexpr int kStages = kFit > 8 ? 8 : kFit;
     static constexpr int kSmem = 1024 + kStaging + kStages * kStageBytes;
     static constexpr int kTmemCols = 2 * BN;                        // a power of two from 32 on
     static_assert(kSmem <= 227 * 1024 && kTmemCols <= 512 && kTmemCols >= 32, "shapes");
-    static_assert(FORM != kGmSwap || BN * 128 * 4 <= kStages * kStageBytes, "a partial tile takes the stages' place");
+    static constexpr int kPartPitch = 132;                          // floats between the rows of kGmShare's partial tile: no bank conflicts
+    static_assert((FORM != kGmSwap || BN * 128 * 4 <= kStages * kStageBytes) && (FORM != kGmShare || (BN == 128 && CTAS == 1 && kPartPitch * 128 * 4 <= kStages * kStageBytes)),
+                  "a partial tile takes the stages' place");
 };
 
 // ------------------------------------------------------------------ groups and tiles
 struct GmTile { uint32_t group, start, end, r, c; };                // the group's rows; row tile within it, column tile
 
 // A warp's walk over the tiles of all groups, in increasing order: lane l holds group base + l.
-template <int FORM, int TILE_ROWS> struct GmWalk {
+template <bool GRAD, int TILE_ROWS> struct GmWalk {
     const GmArgs &p;
     const uint32_t lane;
     uint32_t base, before, start, end, upto;                        // before: tiles ahead of the window; upto: through this lane's group
@@ -98,7 +102,7 @@ template <int FORM, int TILE_ROWS> struct GmWalk {
         }
         start = __shfl_up_sync(0xffffffffu, end, 1);
         if (lane == 0) start = carry;
-        upto = FORM == kGmGrad ? (w + lane < p.groups ? p.tiles_r * p.tiles_c : 0u) : (end - start + TILE_ROWS - 1) / TILE_ROWS * p.tiles_c;
+        upto = GRAD ? (w + lane < p.groups ? p.tiles_r * p.tiles_c : 0u) : (end - start + TILE_ROWS - 1) / TILE_ROWS * p.tiles_c;
         #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
@@ -119,7 +123,7 @@ template <int FORM, int TILE_ROWS> struct GmWalk {
         out.start = __shfl_sync(0xffffffffu, start, src);
         out.end = __shfl_sync(0xffffffffu, end, src);
         const uint32_t in = t - (src == 0 ? before : prev);
-        const uint32_t tr = FORM == kGmGrad ? p.tiles_r : (out.end - out.start + TILE_ROWS - 1) / TILE_ROWS;
+        const uint32_t tr = GRAD ? p.tiles_r : (out.end - out.start + TILE_ROWS - 1) / TILE_ROWS;
         const uint32_t span = kGmGroupRows * p.tiles_c, g = in / span, rest = in % span, h = min((uint32_t)kGmGroupRows, tr - g * kGmGroupRows);
         out.r = g * kGmGroupRows + rest % h;
         out.c = rest / h;
@@ -177,11 +181,11 @@ __device__ __forceinline__ bool mbar_wait_warp_cluster(uint32_t bar, uint32_t pa
 }
 
 // ------------------------------------------------------------------ output
-// 32 rows x 128 bytes of the output; lane l holds row l in v, column x of group z on; `valid` rows of the 32 are stored.
-// Through the warp's staging buffer (128-byte swizzle) and one TMA store, or, where rows are not whole 16-byte pieces or belong
-// to the next group, row by row with the lanes along the row.
+// 32 rows x 128 bytes of the output from row y, column x of group z on; lane l holds row l in v, `valid` rows of the 32 are stored.  They are turned in
+// the warp's staging buffer (128-byte swizzle) and leave as whole rows, 16 bytes a lane where rows are whole 16-byte pieces.  (TMA stores of the buffer
+// instead had each buffer wait for its last copy: 2048 rows, 8 x 4096 x 4096 fp32, 200 us with one buffer per warp, 136 with two.)
 template <int FORM, int ODT>
-__device__ __forceinline__ void gm_store(const GmArgs &p, const CUtensorMap *map, uint32_t buf, uint32_t y, uint32_t x, uint32_t z, uint32_t valid, uint32_t lane, float *v) {
+__device__ __forceinline__ void gm_store(const GmArgs &p, uint32_t buf, uint32_t y, uint32_t x, uint32_t z, uint32_t valid, uint32_t lane, float *v) {
     constexpr int kCols = OutRun<ODT>::kCols, kPer = kCols / 8, ES = 16 / kPer;
     char *out = p.out + ((FORM == kGmGrad ? (uint64_t)z * p.out_group : 0) + (uint64_t)y * p.ldo + x) * ES;
     if (FORM == kGmGrad && p.accumulate && lane < valid) {
@@ -204,8 +208,7 @@ __device__ __forceinline__ void gm_store(const GmArgs &p, const CUtensorMap *map
             }
         }
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the buffer's last contents have been read
-    __syncwarp();
+    __syncwarp();                                           // the buffer's last contents have been read
     #pragma unroll
     for (int q = 0; q < 8; ++q) {
         uint32_t w[4];
@@ -217,17 +220,22 @@ __device__ __forceinline__ void gm_store(const GmArgs &p, const CUtensorMap *map
         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
                      :: "r"(buf + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
     }
-    if (p.vec && (FORM == kGmGrad || valid == 32)) {                                    // the gradient's map ends with each group's matrix
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && x < p.n && valid > 0) {
-            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
-                         :: "l"(map), "r"(buf), "r"(x), "r"(y), "r"(FORM == kGmGrad ? z : 0u) : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    __syncwarp();
+    if (p.vec) {
+        const uint32_t q = lane & 7;
+        char *at = out + (uint64_t)(lane >> 3) * p.ldo * ES + q * 16;
+        #pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t r = 4 * i + (lane >> 3);
+            if (r < valid && x + (q + 1) * kPer <= p.n) {
+                uint32_t w[4];
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(buf + r * 128 + ((q ^ (r & 7)) << 4)) : "memory");
+                asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+            }
+            at += 4 * p.ldo * ES;
         }
         return;
     }
-    __syncwarp();
     for (uint32_t r = 0; r < valid; ++r) {
         uint32_t w;
         asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
@@ -243,7 +251,6 @@ __device__ __forceinline__ void gm_store(const GmArgs &p, const CUtensorMap *map
             }
         }
     }
-    __syncwarp();
 }
 
 // Zeros for the rows ahead of the first and behind the last group, by all epilogue warps of the grid.
@@ -259,16 +266,17 @@ __device__ __forceinline__ void gm_zero_rest(const GmArgs &p, Walk &walk, uint32
 
 // ------------------------------------------------------------------ the kernel
 template <int KIND, int BN, int CTAS, int FORM, bool W_ALONG, int ODT>       // W_ALONG: the weights' rows run along the contraction
-__global__ void __launch_bounds__(kGmThreads, FORM == kGmSwap ? 2 : 1)
-grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const GmArgs p) {
+__global__ void __launch_bounds__(gm_threads(FORM), FORM == kGmSwap ? 2 : 1)
+grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GmArgs p) {
     using S = GmShape<KIND, BN, CTAS, FORM>;
-    using Walk = GmWalk<FORM, FORM == kGmSwap ? BN : 128 * CTAS>;
-    constexpr bool kBoxesA = FORM == kGmGrad || (FORM == kGmSwap && !W_ALONG), kBoxesB = FORM == kGmGrad || (FORM == kGmRows && !W_ALONG);
+    constexpr bool kGrad = FORM == kGmGrad || FORM == kGmShare, kOne = FORM == kGmSwap || FORM == kGmShare;      // kOne: one tile per cluster
+    using Walk = GmWalk<kGrad, FORM == kGmSwap ? BN : 128 * CTAS>;
+    constexpr bool kBoxesA = kGrad || (FORM == kGmSwap && !W_ALONG), kBoxesB = kGrad || (FORM == kGmRows && !W_ALONG);
     constexpr int kPart = BN / CTAS;                        // columns that this CTA brings
     static_assert(!kBoxesB || kPart % 64 == 0, "boxes");
-    constexpr int kRun = FORM == kGmSwap ? BN / 2 : OutRun<ODT>::kCols;
+    constexpr int kRun = FORM == kGmSwap ? BN / 2 : FORM == kGmShare ? 32 : OutRun<ODT>::kCols;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[3 * S::kStages + 2 * 2 + 2];
+    __shared__ __align__(8) uint64_t bars[4 * S::kStages + 2 * 2 + 1];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t stop;
     dep_launch();
@@ -278,11 +286,12 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     auto empty = [&](uint32_t s) { return bar0 + 8 * (S::kStages + s); };
     auto acc_full = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + a); };
     auto acc_empty = [&](uint32_t a) { return bar0 + 8 * (2 * S::kStages + 2 + a); };
-    const uint32_t drained = bar0 + 8 * (2 * S::kStages + 4), last_in = drained + 8;
-    auto peer_clear = [&](uint32_t s) { return last_in + 8 + 8 * s; };         // one per stage: the other CTA may be stages ahead
+    const uint32_t drained = bar0 + 8 * (2 * S::kStages + 4);
+    auto last_in = [&](uint32_t s) { return drained + 8 + 8 * s; };             // a group's last step is there, in this CTA
+    auto peer_clear = [&](uint32_t s) { return drained + 8 + 8 * (S::kStages + s); };           // and cleared in the other
 
     uint32_t rank = 0, nrank = 1;                           // within the cluster: a pair, or the CTAs that share k
-    if constexpr (CTAS == 2 || FORM == kGmSwap) {
+    if constexpr (CTAS == 2 || kOne) {
         asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
         asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(nrank));
     }
@@ -290,22 +299,21 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const uint32_t half = CTAS == 2 ? rank : 0;
     const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     uint32_t tile0 = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
-    if constexpr (FORM == kGmSwap) {                        // one tile per cluster; more clusters than tiles are launched, the number being known here only
+    if constexpr (kOne) {                                   // one tile per cluster; more clusters than tiles are launched, the number being known here only
         tile0 = blockIdx.x / nrank;
         tile_step = 0x7fffffffu;
         dep_wait();
         Walk walk(p, lane);
         GmTile t;
         if (!walk.find(tile0, t)) {                         // the same for all CTAs of the cluster
-            if (warp < kGmEpiWarps) gm_zero_rest<ODT>(p, walk, warp, lane);
+            if (FORM == kGmSwap && warp < kGmEpiWarps) gm_zero_rest<ODT>(p, walk, warp, lane);
             return;
         }
     }
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); mbar_init(peer_clear(s), 1); }
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); mbar_init(last_in(s), 1); mbar_init(peer_clear(s), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), CTAS * kGmEpiWarps); }
         mbar_init(drained, 1);
-        mbar_init(last_in, 1);
         stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -323,17 +331,24 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if constexpr (CTAS == 2) cluster_sync();                // barriers of both CTAs are set up, tensor memory of both allocated
     fence_after();
     const uint32_t tmem = tmem_base_s;
-    uint32_t k0 = 0, k1 = p.steps;
+    uint32_t k0 = 0, k1 = p.steps;                          // this CTA's steps, where they do not depend on the group
     if constexpr (FORM == kGmSwap) { k0 = min(p.steps, rank * p.split_steps); k1 = min(p.steps, k0 + p.split_steps); }
-    auto steps_of = [&](const GmTile &t) { return FORM == kGmGrad ? (t.end - t.start + 63) / 64 : k1 - k0; };
+    auto steps_of = [&](const GmTile &t) {
+        if constexpr (FORM == kGmShare) {
+            const uint32_t all = (t.end - t.start + 63) / 64, each = (all + nrank - 1) / nrank;
+            k0 = min(all, rank * each);
+            return min(all, k0 + each) - k0;
+        } else return kGrad ? (t.end - t.start + 63) / 64 : k1 - k0;
+    };
     constexpr uint32_t kChunk = KIND == kGmInt8 ? 0x40000000u : kGmChunk;
 
-    uint32_t issued = 0;                                    // stages filled so far (warp 8)
+    uint32_t issued = 0, last_mask = 0, last_ph = 0;        // stages filled so far; with a last step; phases of last_in (warp 8)
+    auto ragged = [&](uint32_t left) { return kGrad && left < 64 && (left & 15) != 0; };        // rows to clear in a step with `left` rows to the group's end
     if (warp == 8) {
         dep_wait();
         Walk walk(p, lane);
         GmTile t;
-        uint32_t s = 0, ph = 1, clears = 0, peer_ph = 0;           // peer_ph: bit s, of the next phase of peer_clear(s)
+        uint32_t s = 0, ph = 1;
         bool ok = true;
         for (uint32_t i = tile0; ok && walk.find(i, t); i += tile_step) {
             const uint32_t steps = steps_of(t);
@@ -344,9 +359,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (uint32_t k = 0; k < steps; ++k) {
                 if (!(ok = mbar_wait_warp(empty(s), ph, &stop))) break;
                 const uint32_t a = smem0 + s * S::kStageBytes, b = a + 128 * 128;
-                const uint32_t left = FORM == kGmGrad ? t.end - t.start - k * 64 : 64;
-                const int kx = FORM == kGmGrad ? (int)(t.start + k * 64) : (int)((k0 + k) * S::kKeep);
-                const bool own = FORM == kGmGrad && left < 64 && (left & 15) != 0;        // rows to clear
+                const uint32_t left = kGrad ? t.end - t.start - (k0 + k) * 64 : 64;
+                const int kx = kGrad ? (int)(t.start + (k0 + k) * 64) : (int)((k0 + k) * S::kKeep);
                 // copies to barrier `bar`
                 auto copies = [&](auto group, uint32_t bar) {
                     constexpr int G = decltype(group)::value;
@@ -359,37 +373,50 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         for (int j = 0; j < kPart / 64; ++j) tma_box<G>(b + 8192 * j, &map_b, bar, at_b + 64 * j, kx, z_b);
                     } else tma_box<G>(b, &map_b, bar, kx, at_b, z_b);
                 };
-                if (!own) {
-                    if (elect_one()) {
+                const bool last = ragged(left);
+                if (elect_one()) {
+                    if (!last) {
                         if (leader) mbar_expect(full(s), CTAS * S::kStageBytes);          // the bytes of both CTAs
                         copies(std::integral_constant<int, CTAS>{}, CTAS == 2 ? in_leader(full(s)) : full(s));
+                    } else {
+                        mbar_expect(last_in(s), S::kStageBytes);
+                        copies(std::integral_constant<int, 1>{}, last_in(s));
                     }
-                } else if constexpr (FORM == kGmGrad) {
-                    if (elect_one()) {
-                        mbar_expect(last_in, S::kStageBytes);
-                        copies(std::integral_constant<int, 1>{}, last_in);
-                    }
-                    __syncwarp();
-                    if (!(ok = mbar_wait_warp(last_in, clears & 1, &stop))) { mbar_drain(last_in, clears & 1); break; }
-                    const uint32_t upper = (left + 15) & ~15u;
-                    for (uint32_t j = left * 8 + lane; j < upper * 8; j += 32) {          // 16 bytes each, in every box
-                        #pragma unroll
-                        for (int q = 0; q < S::kStageBytes / 8192; ++q)
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" :: "r"(a + q * 8192 + j * 16), "r"(0u) : "memory");
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if constexpr (CTAS == 2) {
-                        if (!leader) { if (lane == 0) arrive_leader_release(peer_clear(s)); }
-                        else if (!(ok = mbar_wait_warp_cluster(peer_clear(s), peer_ph >> s & 1, &stop))) break;
-                        peer_ph ^= 1u << s;
-                    }
-                    if (leader && lane == 0) mbar_arrive(full(s));
-                    ++clears;
                 }
+                last_mask = last ? last_mask | 1u << s : last_mask & ~(1u << s);
+                if (last) last_ph ^= 1u << s;
                 ++issued;
                 if (++s == S::kStages) { s = 0; ph ^= 1; }
             }
+        }
+    } else if (kGrad && warp == 10) {
+        dep_wait();
+        Walk walk(p, lane);
+        GmTile t;
+        uint32_t s = 0, in_ph = 0, peer_ph = 0;             // bit s: of the next phase of last_in(s), peer_clear(s)
+        bool ok = true;
+        for (uint32_t i = tile0; ok && walk.find(i, t); i += tile_step) {
+            const uint32_t steps = steps_of(t);
+            if (steps == 0) continue;
+            const uint32_t left = t.end - t.start - (k0 + steps - 1) * 64, at = (s + steps - 1) % S::kStages;
+            s = (s + steps) % S::kStages;
+            if (!ragged(left)) continue;
+            if (!(ok = mbar_wait_warp(last_in(at), in_ph >> at & 1, &stop))) break;
+            in_ph ^= 1u << at;
+            const uint32_t a = smem0 + at * S::kStageBytes, upper = (left + 15) & ~15u;
+            for (uint32_t j = left * 8 + lane; j < upper * 8; j += 32) {                  // 16 bytes each, in every box
+                #pragma unroll
+                for (int q = 0; q < S::kStageBytes / 8192; ++q)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" :: "r"(a + q * 8192 + j * 16), "r"(0u) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if constexpr (CTAS == 2) {
+                if (!leader) { if (lane == 0) arrive_leader_release(peer_clear(at)); }
+                else if (!(ok = mbar_wait_warp_cluster(peer_clear(at), peer_ph >> at & 1, &stop))) break;
+                peer_ph ^= 1u << at;
+            }
+            if (leader && lane == 0) mbar_arrive(full(at));
         }
     } else if (warp == 9) {
         dep_wait();                                         // the limit of the waits below is for this kernel's work, not for what runs before it
@@ -412,11 +439,11 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         fence_after();
                         const uint32_t a = smem0 + s * S::kStageBytes;
                         const uint64_t da = kBoxesA ? desc_boxes(a) : desc_codes(a), db = kBoxesB ? desc_boxes(a + 128 * 128) : desc_codes(a + 128 * 128);
-                        const uint32_t count = FORM == kGmGrad ? min(4u, (t.end - t.start - k * 64 + 15) / 16) : 4;
+                        const uint32_t count = kGrad ? min(4u, (t.end - t.start - (k0 + k) * 64 + 15) / 16) : 4;
                         if (elect_one()) {
                             #pragma unroll
                             for (uint32_t j = 0; j < 4; ++j)
-                                if (FORM != kGmGrad || j < count)
+                                if (!kGrad || j < count)
                                     mma_plain<KIND, CTAS>(tmem + acc * BN, da + j * kNextA, db + j * kNextB, kIdesc, k > c0 || j > 0);
                             mma_commit<CTAS>(empty(s));
                             if (k + 1 == c1) mma_commit<CTAS>(acc_full(acc));
@@ -438,7 +465,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (uint32_t i = tile0; ok && walk.find(i, t); i += tile_step) {
             const uint32_t steps = steps_of(t);
             const uint32_t y = (FORM == kGmRows ? t.start : 0) + ((FORM == kGmSwap ? t.c : t.r) * CTAS + half) * 128 + quad * 32;   // first of the warp's MMA rows
-            const uint32_t y_end = FORM == kGmRows ? t.end : FORM == kGmGrad ? p.m : p.n, valid = y < y_end ? min(32u, y_end - y) : 0;
+            const uint32_t y_end = FORM == kGmRows ? t.end : kGrad ? p.m : p.n, valid = y < y_end ? min(32u, y_end - y) : 0;
             float lane_scale = 0.0f;
             if constexpr (KIND == kGmInt8) {
                 if (lane < valid) lane_scale = __uint_as_float(ldro_u32(FORM == kGmSwap ? p.col_scales + (uint64_t)t.group * p.n + y + lane : p.row_scales + y + lane));
@@ -457,7 +484,11 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         for (int j = 0; j < kRun; ++j)
                             if (lane < valid && row + j < t.end) store_out<ODT>(p.out, (uint64_t)(row + j) * p.ldo + y + lane, v[j]);
                     }
-                } else gm_store<FORM, ODT>(p, &map_out, buf, y, t.c * BN + in_tile, t.group, valid, lane, v);
+                } else if constexpr (FORM == kGmShare) {
+                    float4 *part = reinterpret_cast<float4 *>(smem_raw + (smem0 - smem_u32(smem_raw)) + ((quad * 32 + lane) * S::kPartPitch + in_tile) * 4);
+                    #pragma unroll
+                    for (int j = 0; j < kRun / 4; ++j) part[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                } else gm_store<FORM, ODT>(p, buf, y, t.c * BN + in_tile, t.group, valid, lane, v);
             };
             if constexpr (KIND == kGmInt8) {
                 if (steps > 0) {
@@ -524,9 +555,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 for (int c = 0; c < BN / 2; c += kRun) put(c, sum + c);
             }
         }
-        if (FORM != kGmSwap && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
-        if (FORM != kGmGrad && ok) gm_zero_rest<ODT>(p, walk, warp, lane);
+        if (!kGrad && ok) gm_zero_rest<ODT>(p, walk, warp, lane);
     }
     __syncwarp();
     if constexpr (FORM == kGmSwap) {
@@ -556,6 +586,37 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
         }
     }
+    if constexpr (FORM == kGmShare) {
+        // the same, by rows: row r is added and stored by the CTA r mod nrank, four columns per lane
+        cluster_sync();
+        Walk walk(p, lane);
+        GmTile t;
+        if (walk.find(tile0, t) && warp < kGmEpiWarps) {
+            const uint32_t x = t.c * 128 + 4 * lane;
+            for (uint32_t r = rank + warp * nrank; r < 128 && t.r * 128 + r < p.m; r += kGmEpiWarps * nrank) {
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (uint32_t q = 0; q < nrank; ++q) {
+                    uint32_t at;
+                    float a[4];
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem0 + (r * S::kPartPitch + 4 * lane) * 4), "r"(q));
+                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]) : "r"(at) : "memory");
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] += a[j];
+                }
+                const uint64_t i = (uint64_t)t.group * p.out_group + (uint64_t)(t.r * 128 + r) * p.ldo + x;
+                #pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (p.accumulate && x + j < p.n) v[j] += load_out<ODT>(p.out, i + j);
+                if (p.vec && x + 4 <= p.n) {
+                    if constexpr (ODT == LGN_F32) *reinterpret_cast<float4 *>(p.out + i * 4) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *reinterpret_cast<uint2 *>(p.out + i * 2) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                } else {
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j) if (x + j < p.n) store_out<ODT>(p.out, i + j, v[j]);
+                }
+            }
+        }
+    }
     fence_before();
     __syncthreads();
     // a wait ran out, whichever role's: the MMAs and the copies in flight, of both CTAs, end first
@@ -564,10 +625,13 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
         mbar_drain(drained, 0);
     }
-    if (stop && warp == 8 && leader)
-        for (uint32_t b = issued > (uint32_t)S::kStages ? issued - S::kStages : 0; b < issued; ++b)
-            mbar_drain(full(b % S::kStages), (b / S::kStages) & 1);
-    if constexpr (CTAS == 2 || FORM == kGmSwap) cluster_sync();                 // nothing of the other CTAs is in flight any more
+    if (stop && warp == 8)
+        for (uint32_t b = issued > (uint32_t)S::kStages ? issued - S::kStages : 0; b < issued; ++b) {
+            const uint32_t s = b % S::kStages;
+            if (last_mask >> s & 1) mbar_drain(last_in(s), last_ph >> s & 1 ^ 1);
+            else if (leader) mbar_drain(full(s), (b / S::kStages) & 1);
+        }
+    if constexpr (CTAS == 2 || kOne) cluster_sync();                            // nothing of the other CTAs is in flight any more
     fence_after();
     if (threadIdx.x == 0 && stop && p.status != nullptr) *p.status = (uint32_t)LGN_ERR_TIMEOUT;
     if (warp == 9) {

@@ -213,3 +213,17 @@ def test_same_bits_every_time(lgn):
     first = lgn.lgn_grouped_matmul(x, w, offsets, out_dtype=torch.float32)
     for _ in range(5):
         assert torch.equal(lgn.lgn_grouped_matmul(x, w, offsets, out_dtype=torch.float32), first)
+
+
+@pytest.mark.parametrize("rows,groups,m,n,dtype", [(5000, 1, 100, 72, "f32"), (20000, 2, 200, 301, "f32"), (4001, 4, 256, 512, "bf16"), (9000, 8, 128, 128, "f32"), (700, 3, 129, 40, "bf16")])
+def test_weight_gradient_of_few_tiles(lgn, rows, groups, m, n, dtype):
+    """Small matrices, long groups of uneven and empty sizes: rows are shared out among CTAs."""
+    dy, x = values(rows, m, seed=rows), values(rows, n, seed=n)
+    ends = spans(rows, groups, m)
+    want, mag = gradient(dy, x, ends)
+    offsets = torch.tensor(ends, device="cuda")
+    check(lgn.lgn_grouped_weight_grad(dy, x, offsets, out_dtype=DT[dtype]), want, mag, rows)
+    before = values(groups, m, n, seed=9).to(DT[dtype])
+    out = before.clone()
+    lgn.lgn_grouped_weight_grad(dy, x, offsets, out=out, accumulate=True)
+    check(out, want + before.double(), mag + before.double().abs(), rows)
