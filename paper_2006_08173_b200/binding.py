@@ -778,37 +778,71 @@ class Int8Operand:
 
     codes   int8, rows x (k rounded up to a multiple of 16)
     scales  float32, rows"""
-    __slots__ = ("rows", "k", "codes", "scales")
+    __slots__ = ("rows", "k", "_codes", "_scales", "_buffer", "_codes_ptr", "_scales_ptr", "_device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int):
         if codes.dtype != torch.int8 or scales.dtype != torch.float32:
             raise TypeError("codes are int8, scales float32")
-        _dev(codes, "codes"), _dev(scales, "scales")
+        at, scales_at = _dev(codes, "codes"), _dev(scales, "scales")
         if codes.numel() < rows * ((k + 15) & -16) or scales.numel() < rows:
             raise ValueError("codes or scales shorter than the extents need")
         if codes.get_device() != scales.get_device():
             raise ValueError("codes and scales on different devices")
-        self.rows, self.k, self.codes, self.scales = rows, k, codes, scales
+        self.rows, self.k, self._codes, self._scales, self._buffer = rows, k, codes, scales, None
+        self._codes_ptr, self._scales_ptr, self._device = at or None, scales_at or None, codes.get_device()
+
+    @classmethod
+    def empty(cls, rows: int, k: int, device, stream=None) -> "Int8Operand":
+        """Uninitialised, codes and scales in one allocation; for use on ``stream`` (default: the current one)."""
+        codes = rows * ((k + 15) & -16)
+        o = cls.__new__(cls)
+        total = codes + 4 * rows + 16
+        o._buffer = buffer = torch.empty(total, dtype=_uint8, device=device) if stream is None else _empty(total, _uint8, device, stream)
+        if not buffer.is_cuda:
+            raise ValueError("operands are CUDA memory")
+        o.rows, o.k, o._device = rows, k, buffer.get_device()
+        o._codes_ptr = at = buffer.data_ptr()
+        o._scales_ptr = at + codes
+        return o
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._buffer is None:
+            return self._codes
+        pitch = (self.k + 15) & -16
+        return self._buffer[:self.rows * pitch].view(torch.int8).view(self.rows, pitch)
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._buffer is None:
+            return self._scales
+        at = self.rows * ((self.k + 15) & -16)
+        return self._buffer[at:at + 4 * self.rows].view(torch.float32)
+
+    @property
+    def device(self) -> torch.device:
+        return (self._codes if self._buffer is None else self._buffer).device
 
 
-def new_int8_operand(rows: int, k: int, device, stream=None) -> Int8Operand:
-    """Uninitialised; for use on ``stream`` (default: the current one)."""
-    return Int8Operand(_empty((rows, (k + 15) & -16), torch.int8, device, stream), _empty(rows, torch.float32, device, stream), rows, k)
+def new_int8_operand(rows: int, k: int, device) -> Int8Operand:
+    return Int8Operand.empty(rows, k, device)
 
 
 def lgn_int8_quantize(x: torch.Tensor, out: Optional[Int8Operand] = None, stream=None) -> Int8Operand:
     """The operand of a matrix; ``out``: one of the same extents to write to."""
     rows, cols, ld = _matrix3(x, "x")
     device = x.get_device()
-    if _elsewhere(device, stream, out.codes.get_device() if out is not None else None):
+    if _elsewhere(device, stream, out._device if out is not None else None):
         with torch.cuda.device(device):
             return lgn_int8_quantize(x, out, stream)
     if out is None:
-        out = new_int8_operand(rows, cols, x.device, stream)
+        out = Int8Operand.empty(rows, cols, x.device, stream)
     elif (out.rows, out.k) != (rows, cols):
         raise ValueError("out: extents differ from the matrix")
-    _check(_lib.lgn_int8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), out.codes.data_ptr() or None,
-                                  out.scales.data_ptr() or None, _stream(stream)), "lgn_int8_quantize")
+    code = _lib.lgn_int8_quantize(x.data_ptr() or None, rows, cols, ld, dtype_code(x), out._codes_ptr, out._scales_ptr,
+                                  _raw_stream(device) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_int8_quantize")
     return out
 
 
@@ -842,54 +876,55 @@ def lgn_int8_matmul(a: Int8Operand, b: Int8Operand, out: Optional[torch.Tensor] 
     if b.rows % groups:
         raise ValueError("b holds as many rows for each group")
     m, n = a.rows, b.rows // groups
-    device = a.codes.get_device()
-    if _elsewhere(device, stream, b.codes.get_device(), _number(out), _number(offsets), _number(status)):
+    device = a._device
+    if _elsewhere(device, stream, b._device, _number(out), _number(offsets), _number(status)):
         with torch.cuda.device(device):
             return lgn_int8_matmul(a, b, out, out_dtype, offsets, status, stream)
     rest = out is None
     if out is None:
-        out = _empty((m, n), out_dtype, a.codes.device, stream)
+        out = torch.empty((m, n), dtype=out_dtype, device=a.device) if stream is None else _empty((m, n), out_dtype, a.device, stream)
         ldo = n or 1
     else:
         ldo = _given(out, (m, n))
-    _check(_lib.lgn_int8_matmul(a.codes.data_ptr() or None, a.scales.data_ptr() or None, b.codes.data_ptr() or None, b.scales.data_ptr() or None,
-                                at, bits, groups, m, n, a.k, out.data_ptr() or None, ldo, dtype_code(out), 1 if rest else 0,
-                                _word(status, 4, "status") if status is not None else None, _stream(stream)), "lgn_int8_matmul")
+    code = _lib.lgn_int8_matmul(a._codes_ptr, a._scales_ptr, b._codes_ptr, b._scales_ptr, at, bits, groups, m, n, a.k, out.data_ptr() or None, ldo,
+                                dtype_code(out), 1 if rest else 0, _word(status, 4, "status") if status is not None else None,
+                                _raw_stream(device) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_int8_matmul")
     return out
 
 
 # --------------------------------------------------------------------------- products grouped by expert
-def _pieces(t: torch.Tensor, stream) -> torch.Tensor:
-    """A bf16 matrix, or a stack of matrices, as the grouped products read it: rows contiguous, rows and matrices multiples of 16 bytes apart.
-    ``t`` itself where it is so, else a copy."""
+def _pieces(t: torch.Tensor, stream) -> Tuple[torch.Tensor, int, int]:
+    """A bf16 matrix, or a stack of matrices, as the grouped products read it, with the elements between its rows and between its matrices:
+    rows contiguous, rows and matrices multiples of 16 bytes apart.  ``t`` itself where it is so, else a copy."""
     if t.dtype != torch.bfloat16:
         raise TypeError(f"operands of grouped products are bfloat16, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError("operands are CUDA tensors")
-    shape, step = t.shape, t.stride()
+    shape = t.shape
+    cols, rows, count = shape[-1], shape[-2], shape[0] if len(shape) == 3 else 1
     if t.numel() == 0:
-        return t
-    fits = (step[-1] == 1 or shape[-1] == 1) and t.data_ptr() % 16 == 0
-    inner = shape[-1]                                                  # elements that the dimensions so far span
-    for d in range(t.dim() - 2, -1, -1):
-        fits = fits and (shape[d] == 1 or (step[d] >= inner and step[d] % 8 == 0))
-        inner = inner if shape[d] == 1 else (shape[d] - 1) * step[d] + inner
-    if fits:
-        return t
+        return t, (cols + 7) & -8, 0
+    if t.is_contiguous():
+        row, group, fits = cols, cols * rows, cols % 8 == 0
+        if rows == 1:
+            row, fits = (cols + 7) & -8, count == 1 or fits
+    else:
+        step = t.stride()
+        row, group = step[-2] if rows > 1 else (cols + 7) & -8, step[0] if count > 1 else 0
+        fits = (step[-1] == 1 or cols == 1) and (rows == 1 or row >= cols and row % 8 == 0) and (count == 1 or group >= (rows - 1) * row + cols and group % 8 == 0)
+    if fits and t.data_ptr() % 16 == 0:
+        return t, row, group
+    row = (cols + 7) & -8
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(_as_stream(stream, t.device)):
-        padded = torch.empty(*shape[:-1], (shape[-1] + 7) & -8, dtype=t.dtype, device=t.device)
-        return padded[..., :shape[-1]].copy_(t)
+        padded = torch.empty(*shape[:-1], row, dtype=t.dtype, device=t.device)
+        padded[..., :cols].copy_(t)
+    return padded, row, row * rows
 
 
 def _as_stream(stream, device) -> torch.cuda.Stream:
     return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device)
-
-
-def _strides(t: torch.Tensor) -> Tuple[int, int]:
-    """Elements between the rows and between the matrices of what _pieces returned."""
-    row = t.stride(-2) if t.size(-2) > 1 else (t.size(-1) + 7) & -8
-    group = t.stride(0) if t.dim() == 3 and t.size(0) > 1 else 0
-    return row, group
 
 
 def lgn_grouped_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -899,11 +934,12 @@ def lgn_grouped_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, 
     x[r] w[e], w groups x k x n.  x and w are bf16; those whose rows are not multiples of 16 bytes apart are copied first.  Rows of no group
     are zero, or as they were in an ``out`` that is given."""
     at, bits, groups = _offsets(offsets)
-    if x.dim() != 2 or w.dim() != 3 or w.size(0) != groups:
+    shape = w.shape
+    if x.dim() != 2 or len(shape) != 3 or shape[0] != groups:
         raise ValueError("x is a matrix, w a stack with one matrix per group")
     rows, k = x.shape
-    n = w.size(2 if transposed else 1)
-    if w.size(1 if transposed else 2) != k:
+    n, over = (shape[2], shape[1]) if transposed else (shape[1], shape[2])
+    if over != k:
         raise ValueError("x and w contract over different extents")
     device = x.get_device()
     if _elsewhere(device, stream, w.get_device(), offsets.get_device(), _number(out), _number(status)):
@@ -915,11 +951,12 @@ def lgn_grouped_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, 
         ldo = n or 1
     else:
         ldo = _given(out, (rows, n))
-    x, w = _pieces(x, stream), _pieces(w, stream)
-    (ldx, _), (ldw, w_group) = _strides(x), _strides(w)
-    _check(_lib.lgn_grouped_matmul(x.data_ptr() or None, ldx, w.data_ptr() or None, ldw, w_group, 1 if transposed else 0, at, bits, groups, rows, n, k,
+    (x, ldx, _), (w, ldw, w_group) = _pieces(x, stream), _pieces(w, stream)
+    code = _lib.lgn_grouped_matmul(x.data_ptr() or None, ldx, w.data_ptr() or None, ldw, w_group, 1 if transposed else 0, at, bits, groups, rows, n, k,
                                    out.data_ptr() or None, ldo, dtype_code(out), 1 if rest else 0,
-                                   _word(status, 4, "status") if status is not None else None, _stream(stream)), "lgn_grouped_matmul")
+                                   _word(status, 4, "status") if status is not None else None, _raw_stream(device) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_grouped_matmul")
     return out
 
 
@@ -946,10 +983,12 @@ def lgn_grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Te
         if out.numel() and (out.stride(2) != 1 and n > 1 or m > 1 and out.stride(1) < n or groups > 1 and out.stride(0) < (m - 1) * out.stride(1) + n):
             raise ValueError("out must have contiguous rows, and rows and matrices that do not overlap")
         ldo, out_group = (out.stride(1) if m > 1 else n or 1), out.stride(0)
-    dy, x = _pieces(dy, stream), _pieces(x, stream)
-    _check(_lib.lgn_grouped_weight_grad(dy.data_ptr() or None, _strides(dy)[0], x.data_ptr() or None, _strides(x)[0], at, bits, groups, rows, m, n,
-                                        out.data_ptr() or None, ldo, out_group, dtype_code(out), 1 if accumulate else 0,
-                                        _word(status, 4, "status") if status is not None else None, _stream(stream)), "lgn_grouped_weight_grad")
+    (dy, lddy, _), (x, ldx, _) = _pieces(dy, stream), _pieces(x, stream)
+    code = _lib.lgn_grouped_weight_grad(dy.data_ptr() or None, lddy, x.data_ptr() or None, ldx, at, bits, groups, rows, m, n, out.data_ptr() or None, ldo,
+                                        out_group, dtype_code(out), 1 if accumulate else 0, _word(status, 4, "status") if status is not None else None,
+                                        _raw_stream(device) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_grouped_weight_grad")
     return out
 
 
