@@ -168,6 +168,8 @@ _lib.lgn_grouped_matmul.argtypes = [_vp, _u64, _vp, _u64, _u64, _i32, _vp, _i32,
 _lib.lgn_grouped_matmul.restype = _i32
 _lib.lgn_grouped_weight_grad.argtypes = [_vp, _u64, _vp, _u64, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _u64, _i32, _i32, _vp, _vp]
 _lib.lgn_grouped_weight_grad.restype = _i32
+_lib.lgn_selftest_grouped_wait_expires.argtypes = [_vp, _vp, _i32, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _i32, _vp, _vp]
+_lib.lgn_selftest_grouped_wait_expires.restype = _i32
 _lib.lgn_distill_loss.argtypes = [_vp, _u64, _u64, _u64, _i32, _vp, _i32, _u64, _vp, _u64, _i32, _u64, _vp, _i32, _dbl, _dbl, _vp, _vp, _vp, _u64, _vp]
 _lib.lgn_distill_loss.restype = _i32
 
@@ -898,10 +900,6 @@ def lgn_int8_matmul(a: Int8Operand, b: Int8Operand, out: Optional[torch.Tensor] 
 def _pieces(t: torch.Tensor, stream) -> Tuple[torch.Tensor, int, int]:
     """A bf16 matrix, or a stack of matrices, as the grouped products read it, with the elements between its rows and between its matrices:
     rows contiguous, rows and matrices multiples of 16 bytes apart.  ``t`` itself where it is so, else a copy."""
-    if t.dtype != torch.bfloat16:
-        raise TypeError(f"operands of grouped products are bfloat16, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError("operands are CUDA tensors")
     shape = t.shape
     cols, rows, count = shape[-1], shape[-2], shape[0] if len(shape) == 3 else 1
     if t.numel() == 0:
@@ -923,6 +921,14 @@ def _pieces(t: torch.Tensor, stream) -> Tuple[torch.Tensor, int, int]:
     return padded, row, row * rows
 
 
+def _bf16(*operands: torch.Tensor) -> None:
+    for t in operands:
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"operands of grouped products are bfloat16, got {t.dtype}")
+        if not t.is_cuda:
+            raise ValueError("operands are CUDA tensors")
+
+
 def _as_stream(stream, device) -> torch.cuda.Stream:
     return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device)
 
@@ -934,6 +940,7 @@ def lgn_grouped_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, 
     x[r] w[e], w groups x k x n.  x and w are bf16; those whose rows are not multiples of 16 bytes apart are copied first.  Rows of no group
     are zero, or as they were in an ``out`` that is given."""
     at, bits, groups = _offsets(offsets)
+    _bf16(x, w)
     shape = w.shape
     if x.dim() != 2 or len(shape) != 3 or shape[0] != groups:
         raise ValueError("x is a matrix, w a stack with one matrix per group")
@@ -965,6 +972,7 @@ def lgn_grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Te
                             stream=None) -> torch.Tensor:
     """out[e] = dy^T x over the rows of each group e: groups x dy's columns x x's columns; with ``accumulate`` added to ``out``."""
     at, bits, groups = _offsets(offsets)
+    _bf16(dy, x)
     if dy.dim() != 2 or x.dim() != 2 or dy.size(0) != x.size(0):
         raise ValueError("dy and x are matrices with as many rows")
     (rows, m), n = dy.shape, x.size(1)
@@ -992,6 +1000,24 @@ def lgn_grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Te
     return out
 
 
+def lgn_selftest_grouped_wait_expires(a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor, out: torch.Tensor, status: torch.Tensor,
+                                      gradient: bool = False, stream=None) -> None:
+    """A grouped product (``gradient``: the weights' gradient) of contiguous operands whose first copies are withheld: ``status`` must become
+    LGN_ERR_TIMEOUT after a few seconds."""
+    at, bits, groups = _offsets(offsets)
+    rows, k = a.size(0), b.size(-1)
+    n = a.size(1) if gradient else b.size(1)
+    if tuple(b.shape) != ((rows, k) if gradient else (groups, n, a.size(1))) or tuple(out.shape) != ((groups, n, k) if gradient else (rows, n)):
+        raise ValueError("extents do not belong together")
+    _bf16(a, b)
+    device = a.get_device()
+    if _elsewhere(device, stream, b.get_device(), offsets.get_device(), out.get_device(), status.get_device()):
+        with torch.cuda.device(device):
+            return lgn_selftest_grouped_wait_expires(a, b, offsets, out, status, gradient, stream)
+    _check(_lib.lgn_selftest_grouped_wait_expires(_dev(a, "a"), _dev(b, "b"), 1 if gradient else 0, at, bits, groups, rows, n, k, _dev(out, "out"),
+                                                  dtype_code(out), _word(status, 4, "status"), _stream(stream)), "lgn_selftest_grouped_wait_expires")
+
+
 # --------------------------------------------------------------------------- distillation
 def lgn_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, labels: Optional[torch.Tensor] = None,
                      temperature: float = 1.0, alpha: float = 1.0, weight: Optional[torch.Tensor] = None, grad: bool = False,
@@ -1003,6 +1029,10 @@ def lgn_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Ten
     if ids.dim() != 2 or ids.shape != teacher.shape or ids.size(0) != tokens:
         raise ValueError("ids and teacher must be tokens x top")
     (_, top, ld_ids), (_, _, ld_teacher) = _matrix3(ids, "ids"), _matrix3(teacher, "teacher")
+    dt, teacher_dt, bits = dtype_code(logits), dtype_code(teacher), _ids(ids)
+    label_bits = _ids(labels) if labels is not None else 32
+    labels_at = _dev(labels, "labels") or None if labels is not None else None
+    weight_at = _dev(weight, "weight") or None if weight is not None else None
     for t, what in ((labels, "labels"), (weight, "weight"), (loss, "loss")):
         if t is not None and (t.dim() != 1 or t.numel() != tokens):
             raise ValueError(f"{what} must hold one value per row")
@@ -1013,8 +1043,6 @@ def lgn_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Ten
     if _elsewhere(device, stream, ids.get_device(), teacher.get_device(), _number(labels), _number(weight), _number(loss), _number(dlogits)):
         with torch.cuda.device(device):
             return lgn_distill_loss(logits, ids, teacher, labels, temperature, alpha, weight, grad, loss, dlogits, stream)
-    if loss is None:
-        loss = _empty(tokens, torch.float32, logits.device, stream)
     ldd = vocab or 1
     if dlogits is not None:
         if dlogits.dtype != logits.dtype:
@@ -1022,12 +1050,13 @@ def lgn_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Ten
         ldd = _given(dlogits, (tokens, vocab))
     elif grad:
         dlogits = _empty((tokens, vocab), logits.dtype, logits.device, stream)
-    _check(_lib.lgn_distill_loss(logits.data_ptr() or None, tokens, vocab, ld, dtype_code(logits), ids.data_ptr() or None, _ids(ids), ld_ids,
-                                 teacher.data_ptr() or None, ld_teacher, dtype_code(teacher), top,
-                                 _dev(labels, "labels") or None if labels is not None else None, _ids(labels) if labels is not None else 32,
-                                 float(temperature), float(alpha), _dev(weight, "weight") or None if weight is not None else None,
-                                 _dev(loss, "loss") or None, dlogits.data_ptr() or None if dlogits is not None else None, ldd, _stream(stream)),
-           "lgn_distill_loss")
+    if loss is None:
+        loss = _empty(tokens, torch.float32, logits.device, stream)
+    code = _lib.lgn_distill_loss(logits.data_ptr() or None, tokens, vocab, ld, dt, ids.data_ptr() or None, bits, ld_ids, teacher.data_ptr() or None, ld_teacher,
+                                 teacher_dt, top, labels_at, label_bits, float(temperature), float(alpha), weight_at, _dev(loss, "loss") or None,
+                                 dlogits.data_ptr() or None if dlogits is not None else None, ldd, _raw_stream(device) if stream is None else _stream(stream))
+    if code != LGN_OK:
+        _check(code, "lgn_distill_loss")
     return loss, dlogits
 
 

@@ -152,9 +152,9 @@ static uint64_t gm_bytes(const GmOperand &o, uint64_t es) {
 
 using namespace lgn;
 
-extern "C" lgn_status lgn_grouped_matmul(const void *x, uint64_t ldx, const void *w, uint64_t ldw, uint64_t w_group, int transposed,
-                                         const void *offsets, int offset_bits, uint64_t groups, uint64_t rows, uint64_t n, uint64_t k,
-                                         void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream) {
+static lgn_status grouped_matmul(const void *x, uint64_t ldx, const void *w, uint64_t ldw, uint64_t w_group, int transposed,
+                                 const void *offsets, int offset_bits, uint64_t groups, uint64_t rows, uint64_t n, uint64_t k,
+                                 void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream, bool withhold) {
     const lgn_status bad = gm_check(offsets, offset_bits, groups, rows, n, out_dt, status_dev);
     if (bad != LGN_OK) return bad;
     if (k > kGmMaxDim) return LGN_ERR_UNSUPPORTED;
@@ -171,13 +171,13 @@ extern "C" lgn_status lgn_grouped_matmul(const void *x, uint64_t ldx, const void
     }
     GmArgs p = {};
     p.out = static_cast<char *>(out); p.ldo = ldo; p.offsets = offsets; p.offsets64 = offset_bits == 64; p.status = status_dev;
-    p.rows = (uint32_t)rows; p.groups = (uint32_t)groups; p.n = (uint32_t)n; p.zero_rest = zero_rest != 0;
+    p.rows = (uint32_t)rows; p.groups = (uint32_t)groups; p.n = (uint32_t)n; p.zero_rest = zero_rest != 0; p.withhold = withhold;
     return gm_run(transposed ? kGmInput : kGmForward, a, b, p, k, out_dt, stream);
 }
 
-extern "C" lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, const void *x, uint64_t ldx, const void *offsets, int offset_bits,
-                                              uint64_t groups, uint64_t rows, uint64_t m, uint64_t n, void *out, uint64_t ldo, uint64_t out_group,
-                                              lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream) {
+static lgn_status weight_grad(const void *dy, uint64_t lddy, const void *x, uint64_t ldx, const void *offsets, int offset_bits,
+                              uint64_t groups, uint64_t rows, uint64_t m, uint64_t n, void *out, uint64_t ldo, uint64_t out_group,
+                              lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream, bool withhold) {
     const lgn_status bad = gm_check(offsets, offset_bits, groups, rows, n, out_dt, status_dev);
     if (bad != LGN_OK) return bad;
     if (m > kGmMaxDim) return LGN_ERR_UNSUPPORTED;
@@ -194,8 +194,28 @@ extern "C" lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, con
     }
     GmArgs p = {};
     p.out = static_cast<char *>(out); p.ldo = ldo; p.out_group = out_group; p.offsets = offsets; p.offsets64 = offset_bits == 64; p.status = status_dev;
-    p.rows = (uint32_t)rows; p.groups = (uint32_t)groups; p.m = (uint32_t)m; p.n = (uint32_t)n; p.accumulate = accumulate != 0;
+    p.rows = (uint32_t)rows; p.groups = (uint32_t)groups; p.m = (uint32_t)m; p.n = (uint32_t)n; p.accumulate = accumulate != 0; p.withhold = withhold;
     return gm_run(kGmWeight, a, b, p, 0, out_dt, stream);
+}
+
+extern "C" lgn_status lgn_grouped_matmul(const void *x, uint64_t ldx, const void *w, uint64_t ldw, uint64_t w_group, int transposed,
+                                         const void *offsets, int offset_bits, uint64_t groups, uint64_t rows, uint64_t n, uint64_t k,
+                                         void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream) {
+    return grouped_matmul(x, ldx, w, ldw, w_group, transposed, offsets, offset_bits, groups, rows, n, k, out, ldo, out_dt, zero_rest, status_dev, stream, false);
+}
+
+extern "C" lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, const void *x, uint64_t ldx, const void *offsets, int offset_bits,
+                                              uint64_t groups, uint64_t rows, uint64_t m, uint64_t n, void *out, uint64_t ldo, uint64_t out_group,
+                                              lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream) {
+    return weight_grad(dy, lddy, x, ldx, offsets, offset_bits, groups, rows, m, n, out, ldo, out_group, out_dt, accumulate, status_dev, stream, false);
+}
+
+extern "C" lgn_status lgn_selftest_grouped_wait_expires(const void *a, const void *b, int gradient, const void *offsets, int offset_bits,
+                                                        uint64_t groups, uint64_t rows, uint64_t n, uint64_t k, void *out, lgn_dtype out_dt,
+                                                        uint32_t *status_dev, void *stream) {
+    if (status_dev == nullptr || rows == 0 || k == 0) return LGN_ERR_INVALID_ARG;
+    return gradient ? weight_grad(a, n, b, k, offsets, offset_bits, groups, rows, n, k, out, k, n * k, out_dt, 0, status_dev, stream, true)
+                    : grouped_matmul(a, k, b, k, n * k, 0, offsets, offset_bits, groups, rows, n, k, out, n, out_dt, 0, status_dev, stream, true);
 }
 
 extern "C" lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, const float *b_scales,
