@@ -525,7 +525,7 @@ lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, 
  * known on the host; offsets outside [0, rows] count as the nearest end, one below an earlier one as that one, so that
  * no offsets lead outside the buffers.
  * Operands are bf16, 16-byte aligned, rows (ldx, ldw, lddy) and matrices (w_group) multiples of 8 elements apart.  Sums in fp32,
- * rounded once to out_dt, the tensor cores' truncating additions limited to 1024 terms as in lgn_fp8_matmul.  status_dev: device
+ * rounded once to out_dt, the tensor cores' truncating additions limited to 512 terms (an error of up to 1e-6 of sum |x w|).  status_dev: device
  * uint32, may be NULL; set to LGN_ERR_TIMEOUT if a bounded device-side wait ran out (the output is then invalid), else left alone.
  * One launch, no workspace; the same inputs give the same bits on the same type of device. */
 

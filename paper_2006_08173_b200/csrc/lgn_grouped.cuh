@@ -19,8 +19,9 @@
 // and hands the step on, while the copies go on with the next tile's.  Nothing else sees rows of another group but the output rows that are not stored.
 //
 // Roles as in the 8-bit float product: warp 8 copies, warp 9 issues MMAs, warps 0..7 read sums out.  Sums of
-// bf16 products leave tensor memory every 1024 of the contraction for registers, because the tensor cores' additions
-// truncate; two accumulators take turns.  Every wait is bounded.
+// bf16 products leave tensor memory every 512 of the contraction for registers, because the tensor cores' additions
+// truncate, here after every 16 products: sums of positive products come out too small by 9e-7 with 512, by twice that with 1024 and by 4e-7 with
+// 256, which costs 2 to 4 % (16384 rows, 8 x 4096 x 4096: 393 us, 401).  Two accumulators take turns.  Every wait is bounded.
 #pragma once
 
 #include <type_traits>
@@ -37,7 +38,7 @@ enum GmKind { kGmBf16 = 0, kGmInt8 = 1 };
 constexpr int kGmEpiWarps = 8;
 constexpr int gm_threads(int form) { return form == kGmGrad || form == kGmShare ? 352 : 320; }
 constexpr int kGmGroupRows = 16;                 // row tiles walked before the next column tile (L2 reuse)
-constexpr uint32_t kGmChunk = 16;                // steps whose sum stays in tensor memory (bf16)
+constexpr uint32_t kGmChunk = 8;                 // steps whose sum stays in tensor memory (bf16)
 constexpr int kGmBuffer = 4096;                  // 32 rows x 128 bytes of output
 
 struct GmArgs {
@@ -224,7 +225,7 @@ __device__ __forceinline__ void gm_store(const GmArgs &p, uint32_t buf, uint32_t
     if (p.vec) {
         const uint32_t q = lane & 7;
         char *at = out + (uint64_t)(lane >> 3) * p.ldo * ES + q * 16;
-        #pragma unroll
+        #pragma unroll 2                                    // more at once spills beside 128 sums (fp32, 16384 rows, 8 x 4096 x 4096: 470 us, 411)
         for (uint32_t i = 0; i < 8; ++i) {
             const uint32_t r = 4 * i + (lane >> 3);
             if (r < valid && x + (q + 1) * kPer <= p.n) {
