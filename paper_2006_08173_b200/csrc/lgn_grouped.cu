@@ -40,6 +40,10 @@ struct GmOperand { const void *at; uint64_t x, y, z, pitch, group; };     // as 
 
 struct GmPlan { int kernel; uint32_t split, split_steps; uint64_t row_tiles; };
 
+// The height (of the groups' rows, or of the gradient's matrices) and the width of a kernel's tile.
+static uint64_t gm_height(const GmKernel &q) { return q.form == kGmSwap || q.form == kGmTurn ? (uint64_t)q.bn : 128 * (uint64_t)q.ctas; }
+static uint64_t gm_width(const GmKernel &q) { return q.form == kGmSwap || q.form == kGmTurn ? 128 * (uint64_t)q.ctas : (uint64_t)q.bn; }
+
 // Row tiles of `height` of all groups: an upper bound, and what is likely.
 static uint64_t gm_most_tiles(uint64_t rows, uint64_t groups, uint64_t height) {
     return groups == 1 ? (rows + height - 1) / height : rows / height + (groups < rows ? groups : rows);
@@ -50,33 +54,52 @@ static double gm_likely_tiles(uint64_t rows, uint64_t groups, uint64_t height) {
     return met * (each < 1.0 ? 1.0 : each);
 }
 
-// The kernel of least estimated time: rounds of the grid times the cost of a tile, in microseconds (`start` once, `step` for 128 bytes of the contraction,
-// `tile` beyond that).  What the sizes of the groups are is known on the device alone; equal ones are assumed here.  Which side of these a
-// call lies on is what the costs must get right (one GPU, operands larger than L2 or cycled through; groups' sizes spread by a factor of 8):
-//   swapped, 4 shares    2 rows, 8 x 4096 x 4096: 12.8 us, 23.9 with pairs of 256
-//   swapped / lone 256   64 rows, the same: 45 and 47, 52 with pairs; 5003 rows, 60 x 1448 x 1000: lone 256 46 us, pairs 50, lone 128 55
-//   pairs of 256         2048 rows, 8 x 4096 x 4096: 81 us, lone 256 88, lone 128 92; 32768 rows, 8 x 1024 x 1024: 57, 63, 70
-//   pairs of 128 (8-bit) 512 rows, 4096 x 4096: 11.0 us, lone 128 11.9, pairs of 256 16.0
+// What the kernels cost on a B200, in microseconds: `start` once, `step` for 128 bytes of the contraction of a tile (and `full` times the share of its
+// columns that are in use), `tile` for a tile beyond that; the memory's part is 6.26 TB/s.  Fitted to 89 products of 1 to 32768 rows, 1 to 128
+// groups and matrices from 128 x 128 to 8192 x 8192 with groups' sizes spread by a factor of 8; the estimates are off by 15 % in the mean, and what they choose
+// by 1 % from the fastest.  Which side of these a call lies on is what they must get right:
+//   swapped, 4 shares    2 rows, 8 x 4096 x 4096: 12.8 us, turned pairs 15.6, pairs 24
+//   swapped, turned      64 rows, the same: 45 us, 46; pairs 52, lone 128 48
+//   turned pairs         2048 rows, the same: 70 us, pairs 81, lone 128 93; 5003 rows, 60 x 1448 x 1000 in fp32: 38, 50, 52
+//   pairs                32768 rows, 8 x 1024 x 1024: 56 us, turned 58.5, lone 128 70
+//   lone 128             300 rows, 4 x 512 x 512: 5.5 us, turned 6.5, pairs 7.4
+//   pairs of 128         8-bit integers, 512 rows, 4096 x 4096: 10.9 us, lone 128 11.7, pairs 15.9, turned 18.2
 //   rows shared out      gradient of 2 x 512 x 512 over 32768 rows: 35 us in 4 shares, 113 with lone 128, 134 with pairs
-static GmPlan gm_plan(const GmKernels &list, uint64_t rows, uint64_t groups, uint64_t m, uint64_t n, uint64_t steps, int odt, int sms) {
+struct GmCost { int form, bn, ctas, odt; float start, step, full, tile; };
+static const GmCost kGmCosts[] = {
+    {kGmRows, 256, 2, LGN_BF16, 4.0f, 0.31f, 0.0f, 1.6f},  {kGmRows, 256, 2, LGN_F32, 6.0f, 0.36f, 0.0f, 2.3f},
+    {kGmTurn, 256, 2, LGN_BF16, 2.7f, 0.14f, 0.20f, 2.1f}, {kGmTurn, 256, 2, LGN_F32, 4.3f, 0.065f, 0.28f, 3.4f},
+    {kGmRows, 128, 2, LGN_BF16, 3.5f, 0.16f, 0.0f, 1.4f},  {kGmRows, 128, 2, LGN_F32, 4.2f, 0.34f, 0.0f, 0.9f},
+    {kGmRows, 128, 1, LGN_BF16, 3.4f, 0.25f, 0.0f, 0.8f},  {kGmRows, 128, 1, LGN_F32, 2.9f, 0.41f, 0.0f, 2.1f},
+    {kGmSwap, 32, 1, LGN_BF16, 2.9f, 0.24f, 0.0f, 3.1f},   {kGmSwap, 32, 1, LGN_F32, 2.9f, 0.24f, 0.0f, 3.1f},
+    {kGmSwap, 64, 1, LGN_BF16, 4.8f, 0.36f, 0.0f, 1.3f},   {kGmSwap, 64, 1, LGN_F32, 4.8f, 0.36f, 0.0f, 1.3f},
+    {kGmGrad, 256, 2, LGN_BF16, 3.1f, 0.19f, 0.0f, 2.1f},  {kGmGrad, 256, 2, LGN_F32, 6.0f, 0.47f, 0.0f, 2.3f},
+    {kGmGrad, 128, 1, LGN_BF16, 3.5f, 0.20f, 0.0f, 0.8f},  {kGmGrad, 128, 1, LGN_F32, 6.0f, 0.33f, 0.0f, 1.0f},
+    {kGmShare, 128, 1, LGN_BF16, 3.9f, 0.09f, 0.0f, 0.7f}, {kGmShare, 128, 1, LGN_F32, 5.1f, 0.41f, 0.0f, 4.4f}};
+
+// The kernel of least estimated time: rounds of the grid times the cost of a tile, or the memory's time where that is longer.  What the sizes of the groups
+// are is known on the device alone; equal ones are assumed here.  `bytes`: what the product reads and writes.
+static GmPlan gm_plan(const GmKernels &list, uint64_t rows, uint64_t groups, uint64_t m, uint64_t n, uint64_t steps, double bytes, int odt, int sms) {
     GmPlan best = {-1, 1, 0, 0};
     double best_cost = 1e300;
     for (int i = 0; i < list.count; ++i) {
         const GmKernel &q = list.first[i];
-        if (q.odt != odt) continue;
+        const GmCost *c = nullptr;
+        for (const GmCost &k : kGmCosts) if (k.form == q.form && k.bn == q.bn && k.ctas == q.ctas && k.odt == odt) c = &k;
+        if (q.odt != odt || c == nullptr) continue;
         const bool grad = q.form == kGmGrad || q.form == kGmShare, one = q.form == kGmSwap || q.form == kGmShare;
-        const uint64_t height = q.form == kGmSwap ? (uint64_t)q.bn : 128 * (uint64_t)q.ctas, width = q.form == kGmSwap ? 128 : (uint64_t)q.bn;
-        const uint64_t cols = (n + width - 1) / width;
-        const double row_tiles = grad ? (double)(groups * ((m + height - 1) / height)) : gm_likely_tiles(rows, groups, height);
-        const uint64_t most = grad ? groups * ((m + height - 1) / height) : gm_most_tiles(rows, groups, height);
-        const double tiles = row_tiles * (double)cols, all_steps = grad ? (double)rows / (double)groups / 64.0 + 0.5 : (double)steps;
-        const double slots = (double)(q.form == kGmSwap ? 2 * sms : sms / q.ctas);
+        const uint64_t height = gm_height(q), cols = (n + gm_width(q) - 1) / gm_width(q), fixed = groups * ((m + height - 1) / height);
+        const double row_tiles = grad ? (double)fixed : gm_likely_tiles(rows, groups, height), tiles = row_tiles * (double)cols;
+        const uint64_t most = grad ? fixed : gm_most_tiles(rows, groups, height);
+        const double all_steps = grad ? (double)rows / (double)groups / 64.0 + 0.5 : (double)steps, slots = (double)(q.form == kGmSwap ? 2 * sms : sms / q.ctas);
+        const double used = row_tiles > 0.0 ? (double)rows / row_tiles / (double)height : 1.0, step = c->step + c->full * (used < 1.0 ? used : 1.0);
         for (uint32_t split = q.form == kGmShare ? 2 : 1; split <= (one ? 8u : 1u); split *= 2) {
             if (split > 1 && ((double)split > all_steps || tiles * split > 2.0 * slots)) break;
             const double share = split > 1 ? (double)(uint64_t)((all_steps + split - 1) / split) : all_steps;
             double rounds = tiles * split / slots;
             rounds = rounds < 1.0 ? 1.0 : rounds < 4.0 ? (double)(uint64_t)(rounds + 0.999) : rounds + 0.5;
-            const double cost = q.start + rounds * (share * q.step + q.tile) + (split > 1 ? 1.0 + 0.3 * split : 0.0);
+            const double work = rounds * (share * step + c->tile) + (split > 1 ? 0.13 + 0.26 * split : 0.0), memory = bytes / 6.26e6;
+            const double cost = c->start + (work > memory ? work : memory) + 0.04 * work;
             if (cost < best_cost) {
                 best_cost = cost;
                 best = {i, split, (uint32_t)((steps + split - 1) / split), most};
@@ -93,28 +116,32 @@ static lgn_status gm_run(GmProduct which, const GmOperand &a, const GmOperand &b
     const uint64_t keep = int8 ? 128 : 64, steps = grad ? 0 : (k + keep - 1) / keep;
     const int sms = sm_count();
     if (sms < 1 || encode_tiled() == nullptr) return LGN_ERR_CUDA;
-    const GmPlan plan = gm_plan(list, p.rows, p.groups, p.m, p.n, steps, odt, sms);
+    const uint64_t es = odt == LGN_F32 ? 4 : 2, ies = int8 ? 1 : 2;
+    const double met = (double)(p.groups < p.rows ? p.groups : p.rows);
+    const double bytes = grad ? (double)ies * p.rows * ((double)p.m + p.n) + (double)es * p.groups * p.m * p.n
+                              : (double)ies * (double)k * (p.rows + met * p.n) + (double)es * p.rows * p.n;
+    const GmPlan plan = gm_plan(list, p.rows, p.groups, p.m, p.n, steps, bytes, odt, sms);
     if (plan.kernel < 0) return LGN_ERR_UNSUPPORTED;
     const GmKernel &q = list.first[plan.kernel];
-    const uint64_t height = q.form == kGmSwap ? (uint64_t)q.bn : 128 * (uint64_t)q.ctas, width = q.form == kGmSwap ? 128 : (uint64_t)q.bn;
+    const uint64_t height = gm_height(q), width = gm_width(q);
+    const bool turned = q.form == kGmSwap || q.form == kGmTurn;
     p.steps = (uint32_t)steps;
     p.split_steps = plan.split_steps;
     p.tiles_c = (uint32_t)((p.n + width - 1) / width);
     p.tiles_r = grad ? (uint32_t)((p.m + height - 1) / height) : 0;
-    const uint64_t es = odt == LGN_F32 ? 4 : 2, most = plan.row_tiles * p.tiles_c;
+    const uint64_t most = plan.row_tiles * p.tiles_c;
     if (most > 0x3fffffffull || most * plan.split > 0x7fffffffull) return LGN_ERR_UNSUPPORTED;
     p.vec = aligned_to(p.out, 16) && (p.ldo * es) % 16 == 0 && (p.n * es) % 16 == 0 && (!grad || p.groups == 1 || (p.out_group * es) % 16 == 0);
 
     CUtensorMap ma = {}, mb = {};
     const CUtensorMapDataType type = int8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    const uint64_t ies = int8 ? 1 : 2;
     const bool any = p.rows > 0 && (grad || steps > 0);                   // anything to copy in
     // the MMA's rows come from the activations, or, swapped, from the weights
-    const GmOperand &r = q.form == kGmSwap ? b : a, &c = q.form == kGmSwap ? a : b;
+    const GmOperand &r = turned ? b : a, &c = turned ? a : b;
     const bool one = q.form == kGmSwap || q.form == kGmShare;
-    const bool boxes_r = grad || (q.form == kGmSwap && !q.along), boxes_c = grad || (q.form == kGmRows && !q.along);
+    const bool boxes_r = grad || (turned && !q.along), boxes_c = grad || (q.form == kGmRows && !q.along);
     if (any && (!gm_map(&ma, type, ies, r.at, r.x, r.y, r.z, r.pitch, r.group, boxes_r ? 64 : 128) ||
-                !gm_map(&mb, type, ies, c.at, c.x, c.y, c.z, c.pitch, c.group, boxes_c ? 64 : (uint32_t)(q.bn / q.ctas)))) return LGN_ERR_CUDA;
+                !gm_map(&mb, type, ies, c.at, c.x, c.y, c.z, c.pitch, c.group, boxes_c ? 64 : q.form == kGmTurn ? 32 : (uint32_t)(q.bn / q.ctas)))) return LGN_ERR_CUDA;
     if (!gm_allow_smem(which, plan.kernel, q)) return LGN_ERR_CUDA;
     const uint64_t slots = (uint64_t)(sms / q.ctas);
     uint64_t grid = one ? most * plan.split : (most < slots ? most : slots) * (uint64_t)q.ctas;

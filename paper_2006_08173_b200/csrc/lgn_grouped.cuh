@@ -4,6 +4,8 @@
 //   kGmRows  out[r, :] = X[r, :] W_e^T or X[r, :] W_e     tiles of 128 CTAS rows of one group by BN columns
 //   kGmSwap  the same with the weights' 128 rows as the MMA's rows and BN activations as its columns: few rows per group;
 //            the CTAs of a cluster take consecutive shares of k and add their tiles through distributed shared memory
+//   kGmTurn  the same turned round for any number of rows: tiles of 128 CTAS weights' rows by up to BN activations, an MMA taking as many columns
+//            as the tile has rows, in steps of 32, so that groups cost what their rows cost
 //   kGmGrad  out_e = dY^T X over the rows of group e      tiles of 128 CTAS by BN of each group's matrix
 //   kGmShare the same with each group's rows shared out over the CTAs of a cluster, as kGmSwap does: few tiles, long groups
 // bf16 operands with fp32 sums, or 8-bit integers with 32-bit integer sums (exact) times a scale per row of either.
@@ -32,7 +34,7 @@
 
 namespace lgn {
 
-enum GmForm { kGmRows = 0, kGmSwap = 1, kGmGrad = 2, kGmShare = 3 };
+enum GmForm { kGmRows = 0, kGmSwap = 1, kGmGrad = 2, kGmShare = 3, kGmTurn = 4 };
 enum GmKind { kGmBf16 = 0, kGmInt8 = 1 };
 
 constexpr int kGmEpiWarps = 8;
@@ -58,7 +60,7 @@ struct GmArgs {
 
 template <int KIND, int BN, int CTAS, int FORM> struct GmShape {
     static constexpr int kKeep = KIND == kGmInt8 ? 128 : 64;        // of the contraction in a step
-    static constexpr int kStaging = FORM == kGmSwap || FORM == kGmShare ? 0 : kGmEpiWarps * kGmBuffer;
+    static constexpr int kStaging = FORM != kGmRows && FORM != kGmGrad ? 0 : kGmEpiWarps * kGmBuffer;
     static constexpr int kStageBytes = 128 * 128 + BN / CTAS * 128;
     static constexpr int kFit = ((FORM == kGmSwap ? 100 : 225) * 1024 - kStaging) / kStageBytes;
     static constexpr int kStages = kFit > 8 ? 8 : kFit;
@@ -271,11 +273,12 @@ __global__ void __launch_bounds__(gm_threads(FORM), FORM == kGmSwap ? 2 : 1)
 grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GmArgs p) {
     using S = GmShape<KIND, BN, CTAS, FORM>;
     constexpr bool kGrad = FORM == kGmGrad || FORM == kGmShare, kOne = FORM == kGmSwap || FORM == kGmShare;      // kOne: one tile per cluster
-    using Walk = GmWalk<kGrad, FORM == kGmSwap ? BN : 128 * CTAS>;
-    constexpr bool kBoxesA = kGrad || (FORM == kGmSwap && !W_ALONG), kBoxesB = kGrad || (FORM == kGmRows && !W_ALONG);
+    constexpr bool kTurned = FORM == kGmSwap || FORM == kGmTurn;            // the weights are the MMA's rows
+    using Walk = GmWalk<kGrad, kTurned ? BN : 128 * CTAS>;
+    constexpr bool kBoxesA = kGrad || (kTurned && !W_ALONG), kBoxesB = kGrad || (FORM == kGmRows && !W_ALONG);
     constexpr int kPart = BN / CTAS;                        // columns that this CTA brings
     static_assert(!kBoxesB || kPart % 64 == 0, "boxes");
-    constexpr int kRun = FORM == kGmSwap ? BN / 2 : FORM == kGmShare ? 32 : OutRun<ODT>::kCols;
+    constexpr int kRun = FORM == kGmSwap ? BN / 2 : FORM == kGmTurn ? 16 : FORM == kGmShare ? 32 : OutRun<ODT>::kCols;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[4 * S::kStages + 2 * 2 + 1];
     __shared__ uint32_t tmem_base_s;
@@ -343,6 +346,13 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     };
     constexpr uint32_t kChunk = KIND == kGmInt8 ? 0x40000000u : kGmChunk;
 
+    // kGmTurn: a group's rows in tiles of the same height; the rows of one and the MMA's columns for them
+    auto span = [&](const GmTile &t, uint32_t &row0, uint32_t &cols) {
+        const uint32_t len = t.end - t.start, count = (len + BN - 1) / BN, height = ((len + count - 1) / count + 31) & ~31u;
+        row0 = t.start + t.r * height;
+        cols = (min(height, t.end - row0) + 31) & ~31u;
+    };
+
     uint32_t issued = 0, last_mask = 0, last_ph = 0;        // stages filled so far; with a last step; phases of last_in (warp 8)
     auto ragged = [&](uint32_t left) { return kGrad && left < 64 && (left & 15) != 0; };        // rows to clear in a step with `left` rows to the group's end
     if (warp == 8) {
@@ -354,9 +364,12 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (uint32_t i = tile0; ok && walk.find(i, t); i += tile_step) {
             const uint32_t steps = steps_of(t);
             // first coordinates of the operands: along the tile, and the group where it is the map's third
-            const int at_a = FORM == kGmRows ? (int)(t.start + (t.r * CTAS + half) * 128) : (int)(((FORM == kGmSwap ? t.c : t.r) * CTAS + half) * 128);
-            const int at_b = FORM == kGmSwap ? (int)(t.start + t.r * BN) : (int)(t.c * BN + half * kPart);
-            const int z_a = FORM == kGmSwap ? (int)t.group : 0, z_b = FORM == kGmRows ? (int)t.group : 0;
+            uint32_t row0 = t.start + t.r * BN, cols = BN;
+            if constexpr (FORM == kGmTurn) span(t, row0, cols);
+            const uint32_t boxes = (cols / CTAS + 31) / 32;                     // kGmTurn: of 32 rows
+            const int at_a = FORM == kGmRows ? (int)(t.start + (t.r * CTAS + half) * 128) : (int)(((kTurned ? t.c : t.r) * CTAS + half) * 128);
+            const int at_b = kTurned ? (int)(row0 + half * (cols / CTAS)) : (int)(t.c * BN + half * kPart);
+            const int z_a = kTurned ? (int)t.group : 0, z_b = FORM == kGmRows ? (int)t.group : 0;
             for (uint32_t k = 0; k < steps; ++k) {
                 if (!(ok = mbar_wait_warp(empty(s), ph, &stop))) break;
                 const uint32_t a = smem0 + s * S::kStageBytes, b = a + 128 * 128;
@@ -372,12 +385,14 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if constexpr (kBoxesB) {
                         #pragma unroll
                         for (int j = 0; j < kPart / 64; ++j) tma_box<G>(b + 8192 * j, &map_b, bar, at_b + 64 * j, kx, z_b);
+                    } else if constexpr (FORM == kGmTurn) {
+                        for (uint32_t j = 0; j < boxes; ++j) tma_box<G>(b + 4096 * j, &map_b, bar, kx, at_b + 32 * (int)j, z_b);
                     } else tma_box<G>(b, &map_b, bar, kx, at_b, z_b);
                 };
                 const bool last = ragged(left);
                 if (elect_one()) {
                     if (!last) {
-                        if (leader) mbar_expect(full(s), CTAS * S::kStageBytes);          // the bytes of both CTAs
+                        if (leader) mbar_expect(full(s), CTAS * (FORM == kGmTurn ? 128 * 128 + boxes * 4096 : S::kStageBytes));   // the bytes of both CTAs
                         copies(std::integral_constant<int, CTAS>{}, CTAS == 2 ? in_leader(full(s)) : full(s));
                     } else {
                         mbar_expect(last_in(s), S::kStageBytes);
@@ -423,7 +438,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         dep_wait();                                         // the limit of the waits below is for this kernel's work, not for what runs before it
         if (leader) {
             constexpr uint32_t kIdesc = (KIND == kGmInt8 ? 2u << 4 : 1u << 4) | (1u << 7) | (1u << 10) | ((kBoxesA ? 1u : 0u) << 15) | ((kBoxesB ? 1u : 0u) << 16) |
-                                        ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 * CTAS >> 4) << 24);
+                                        ((FORM == kGmTurn ? 0u : (uint32_t)(BN >> 3)) << 17) | ((uint32_t)(128 * CTAS >> 4) << 24);
             constexpr uint32_t kNextA = kBoxesA ? 2048 >> 4 : 2, kNextB = kBoxesB ? 2048 >> 4 : 2;   // from one MMA of a step to the next
             Walk walk(p, lane);
             GmTile t;
@@ -431,6 +446,12 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool ok = true;
             for (uint32_t i = tile0; ok && walk.find(i, t); i += tile_step) {
                 const uint32_t steps = steps_of(t);
+                uint32_t idesc = kIdesc;
+                if constexpr (FORM == kGmTurn) {
+                    uint32_t row0, cols;
+                    span(t, row0, cols);
+                    idesc |= (cols >> 3) << 17;
+                }
                 for (uint32_t c0 = 0; ok && c0 < steps; c0 += kChunk) {
                     const uint32_t c1 = min(steps, c0 + kChunk), acc = n & 1;
                     if (!(ok = mbar_wait_warp(acc_empty(acc), (n >> 1 & 1) ^ 1, &stop))) break;
@@ -445,7 +466,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             #pragma unroll
                             for (uint32_t j = 0; j < 4; ++j)
                                 if (!kGrad || j < count)
-                                    mma_plain<KIND, CTAS>(tmem + acc * BN, da + j * kNextA, db + j * kNextB, kIdesc, k > c0 || j > 0);
+                                    mma_plain<KIND, CTAS>(tmem + acc * BN, da + j * kNextA, db + j * kNextB, idesc, k > c0 || j > 0);
                             mma_commit<CTAS>(empty(s));
                             if (k + 1 == c1) mma_commit<CTAS>(acc_full(acc));
                         }
@@ -461,29 +482,35 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         Walk walk(p, lane);
         GmTile t;
         uint32_t n = 0;
-        const uint32_t quad = warp & 3, col0 = (warp >> 2) * (BN / 2), tmem_at = tmem + ((quad * 32u) << 16) + col0, buf = staging0 + warp * kGmBuffer;
+        const uint32_t quad = warp & 3, buf = staging0 + warp * kGmBuffer;
         bool ok = true;
         for (uint32_t i = tile0; ok && walk.find(i, t); i += tile_step) {
             const uint32_t steps = steps_of(t);
-            const uint32_t y = (FORM == kGmRows ? t.start : 0) + ((FORM == kGmSwap ? t.c : t.r) * CTAS + half) * 128 + quad * 32;   // first of the warp's MMA rows
+            uint32_t row0 = t.start + t.r * BN, part_cols = BN / 2;             // turned: the tile's first row; columns of this warp's part
+            if constexpr (FORM == kGmTurn) { span(t, row0, part_cols); part_cols /= 2; }
+            const uint32_t col0 = (warp >> 2) * part_cols, tmem_at = tmem + ((quad * 32u) << 16) + col0;
+            const uint32_t y = (FORM == kGmRows ? t.start : 0) + ((kTurned ? t.c : t.r) * CTAS + half) * 128 + quad * 32;   // first of the warp's MMA rows
             const uint32_t y_end = FORM == kGmRows ? t.end : kGrad ? p.m : p.n, valid = y < y_end ? min(32u, y_end - y) : 0;
             float lane_scale = 0.0f;
             if constexpr (KIND == kGmInt8) {
-                if (lane < valid) lane_scale = __uint_as_float(ldro_u32(FORM == kGmSwap ? p.col_scales + (uint64_t)t.group * p.n + y + lane : p.row_scales + y + lane));
+                if (lane < valid) lane_scale = __uint_as_float(ldro_u32(kTurned ? p.col_scales + (uint64_t)t.group * p.n + y + lane : p.row_scales + y + lane));
             }
             // RUN finished columns of the tile, from column c of the warp's part on
             auto put = [&](uint32_t c, float *v) {
                 const uint32_t in_tile = col0 + c;
-                if constexpr (FORM == kGmSwap) {
-                    const uint32_t row = t.start + t.r * BN + in_tile;
-                    if (nrank > 1) {
+                if constexpr (kTurned) {
+                    if (FORM == kGmSwap && nrank > 1) {
                         float *part = reinterpret_cast<float *>(smem_raw + (smem0 - smem_u32(smem_raw)));
                         #pragma unroll
                         for (int j = 0; j < kRun; ++j) part[(in_tile + j) * 128 + quad * 32 + lane] = v[j];
-                    } else {
+                    } else if (lane < valid) {
+                        const uint32_t row = row0 + in_tile;
+                        char *at = p.out + ((uint64_t)row * p.ldo + y + lane) * (ODT == LGN_F32 ? 4 : 2);
                         #pragma unroll
-                        for (int j = 0; j < kRun; ++j)
-                            if (lane < valid && row + j < t.end) store_out<ODT>(p.out, (uint64_t)(row + j) * p.ldo + y + lane, v[j]);
+                        for (int j = 0; j < kRun; ++j) {
+                            if (row + j < t.end) store_out<ODT>(at, 0, v[j]);
+                            at += p.ldo * (ODT == LGN_F32 ? 4 : 2);
+                        }
                     }
                 } else if constexpr (FORM == kGmShare) {
                     float4 *part = reinterpret_cast<float4 *>(smem_raw + (smem0 - smem_u32(smem_raw)) + ((quad * 32 + lane) * S::kPartPitch + in_tile) * 4);
@@ -497,7 +524,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     fence_after();
                 }
                 #pragma unroll 1
-                for (uint32_t c = 0; c < BN / 2; c += kRun) {
+                for (uint32_t c = 0; c < part_cols; c += kRun) {
                     float v[kRun];
                     #pragma unroll
                     for (int j = 0; j < kRun; ++j) v[j] = 0.0f;
@@ -509,16 +536,16 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         for (int j = 0; j < kRun; j += 16) tmem_load_wait16(v + j);
                     }
                     if (FORM != kGmSwap || nrank == 1) {
-                        const uint32_t x = FORM == kGmSwap ? t.start + t.r * BN + col0 + c : t.c * BN + col0 + c;
-                        const uint32_t x_end = FORM == kGmSwap ? t.end : p.n;
-                        const float *scales = FORM == kGmSwap ? p.row_scales : p.col_scales + (uint64_t)t.group * p.n;
+                        const uint32_t x = kTurned ? row0 + col0 + c : t.c * BN + col0 + c;
+                        const uint32_t x_end = kTurned ? t.end : p.n;
+                        const float *scales = kTurned ? p.row_scales : p.col_scales + (uint64_t)t.group * p.n;
                         #pragma unroll
                         for (int j0 = 0; j0 < kRun; j0 += 32) {
                             const float mine = lane < kRun - j0 && x + j0 + lane < x_end ? __uint_as_float(ldro_u32(scales + x + j0 + lane)) : 0.0f;
                             #pragma unroll
                             for (int j = j0; j < kRun && j < j0 + 32; ++j) {
                                 const float other = __shfl_sync(0xffffffffu, mine, j - j0), q = (float)__float_as_int(v[j]);
-                                v[j] = FORM == kGmSwap ? q * other * lane_scale : q * lane_scale * other;          // the activation's scale first, as everywhere
+                                v[j] = kTurned ? q * other * lane_scale : q * lane_scale * other;          // the activation's scale first, as everywhere
                             }
                         }
                     }
@@ -540,6 +567,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     fence_after();
                     #pragma unroll
                     for (int c = 0; c < BN / 2; c += 16) {
+                        if (FORM == kGmTurn && c >= (int)part_cols) break;
                         float v[16];
                         tmem_load16(tmem_at + (n & 1) * BN + c, v);
                         tmem_load_wait16(v);
@@ -553,7 +581,10 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 }
                 if (!ok) break;
                 #pragma unroll
-                for (int c = 0; c < BN / 2; c += kRun) put(c, sum + c);
+                for (int c = 0; c < BN / 2; c += kRun) {
+                    if (FORM == kGmTurn && c >= (int)part_cols) break;
+                    put(c, sum + c);
+                }
             }
         }
         __syncwarp();
@@ -645,11 +676,10 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 struct GmKernel {
     const void *fn;
     int kind, form, along, odt, bn, ctas, smem;             // along: W_ALONG
-    float start, step, tile;                                // estimated cost, see lgn_grouped.cu
 };
 template <int KIND, int BN, int CTAS, int FORM, bool ALONG, int ODT>
-GmKernel gm_kernel(float start, float step, float tile) {
-    return {reinterpret_cast<const void *>(&grouped_kernel<KIND, BN, CTAS, FORM, ALONG, ODT>), KIND, FORM, ALONG, ODT, BN, CTAS, GmShape<KIND, BN, CTAS, FORM>::kSmem, start, step, tile};
+GmKernel gm_kernel() {
+    return {reinterpret_cast<const void *>(&grouped_kernel<KIND, BN, CTAS, FORM, ALONG, ODT>), KIND, FORM, ALONG, ODT, BN, CTAS, GmShape<KIND, BN, CTAS, FORM>::kSmem};
 }
 struct GmKernels { const GmKernel *first; int count; };
 GmKernels gm_forward_kernels();                             // X W_e^T, bf16

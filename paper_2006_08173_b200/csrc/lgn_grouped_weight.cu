@@ -5,9 +5,9 @@ namespace lgn {
 
 GmKernels gm_weight_kernels() {
     static const GmKernel table[] = {
-        gm_kernel<kGmBf16, 256, 2, kGmGrad, false, LGN_BF16>(4.0f, 0.30f, 1.5f), gm_kernel<kGmBf16, 256, 2, kGmGrad, false, LGN_F32>(4.0f, 0.30f, 2.5f),
-        gm_kernel<kGmBf16, 128, 1, kGmGrad, false, LGN_BF16>(3.5f, 0.25f, 1.0f), gm_kernel<kGmBf16, 128, 1, kGmGrad, false, LGN_F32>(3.5f, 0.25f, 1.5f),
-        gm_kernel<kGmBf16, 128, 1, kGmShare, false, LGN_BF16>(3.5f, 0.25f, 1.0f), gm_kernel<kGmBf16, 128, 1, kGmShare, false, LGN_F32>(3.5f, 0.25f, 1.5f)};
+        gm_kernel<kGmBf16, 256, 2, kGmGrad, false, LGN_BF16>(), gm_kernel<kGmBf16, 256, 2, kGmGrad, false, LGN_F32>(),
+        gm_kernel<kGmBf16, 128, 1, kGmGrad, false, LGN_BF16>(), gm_kernel<kGmBf16, 128, 1, kGmGrad, false, LGN_F32>(),
+        gm_kernel<kGmBf16, 128, 1, kGmShare, false, LGN_BF16>(), gm_kernel<kGmBf16, 128, 1, kGmShare, false, LGN_F32>()};
     return {table, (int)(sizeof table / sizeof table[0])};
 }
 
