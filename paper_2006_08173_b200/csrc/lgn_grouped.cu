@@ -55,9 +55,9 @@ static double gm_likely_tiles(uint64_t rows, uint64_t groups, uint64_t height) {
 }
 
 // What the kernels cost on a B200, in microseconds: `start` once, `step` for 128 bytes of the contraction of a tile (and `full` times the share of its
-// columns that are in use), `tile` for a tile beyond that; the memory's part is 6.26 TB/s.  Fitted to 89 products of 1 to 32768 rows, 1 to 128
-// groups and matrices from 128 x 128 to 8192 x 8192 with groups' sizes spread by a factor of 8; the estimates are off by 15 % in the mean, and what they choose
-// by 1 % from the fastest.  Which side of these a call lies on is what they must get right:
+// columns that are in use), `tile` for a tile beyond that (bf16 and fp32 outputs); the memory's part is 6.9 TB/s.  Fitted to 213 products, half of them drawn: 1 to
+// 32768 rows, 1 to 128 groups whose sizes spread by a factor of 8, widths from 96 to 8192.  The estimates are off by 17 % in the mean, what they choose
+// is 2 % slower than the fastest.  Which side of these a call lies on is what they must get right:
 //   swapped, 4 shares    2 rows, 8 x 4096 x 4096: 12.8 us, turned pairs 15.6, pairs 24
 //   swapped, turned      64 rows, the same: 45 us, 46; pairs 52, lone 128 48
 //   turned pairs         2048 rows, the same: 70 us, pairs 81, lone 128 93; 5003 rows, 60 x 1448 x 1000 in fp32: 38, 50, 52
@@ -65,17 +65,12 @@ static double gm_likely_tiles(uint64_t rows, uint64_t groups, uint64_t height) {
 //   lone 128             300 rows, 4 x 512 x 512: 5.5 us, turned 6.5, pairs 7.4
 //   pairs of 128         8-bit integers, 512 rows, 4096 x 4096: 10.9 us, lone 128 11.7, pairs 15.9, turned 18.2
 //   rows shared out      gradient of 2 x 512 x 512 over 32768 rows: 35 us in 4 shares, 113 with lone 128, 134 with pairs
-struct GmCost { int form, bn, ctas, odt; float start, step, full, tile; };
+struct GmCost { int form, bn, ctas; float start, step, full, tile[2]; };     // tile: by LGN_F32, LGN_BF16
 static const GmCost kGmCosts[] = {
-    {kGmRows, 256, 2, LGN_BF16, 4.0f, 0.31f, 0.0f, 1.6f},  {kGmRows, 256, 2, LGN_F32, 6.0f, 0.36f, 0.0f, 2.3f},
-    {kGmTurn, 256, 2, LGN_BF16, 2.7f, 0.14f, 0.20f, 2.1f}, {kGmTurn, 256, 2, LGN_F32, 4.3f, 0.065f, 0.28f, 3.4f},
-    {kGmRows, 128, 2, LGN_BF16, 3.5f, 0.16f, 0.0f, 1.4f},  {kGmRows, 128, 2, LGN_F32, 4.2f, 0.34f, 0.0f, 0.9f},
-    {kGmRows, 128, 1, LGN_BF16, 3.4f, 0.25f, 0.0f, 0.8f},  {kGmRows, 128, 1, LGN_F32, 2.9f, 0.41f, 0.0f, 2.1f},
-    {kGmSwap, 32, 1, LGN_BF16, 2.9f, 0.24f, 0.0f, 3.1f},   {kGmSwap, 32, 1, LGN_F32, 2.9f, 0.24f, 0.0f, 3.1f},
-    {kGmSwap, 64, 1, LGN_BF16, 4.8f, 0.36f, 0.0f, 1.3f},   {kGmSwap, 64, 1, LGN_F32, 4.8f, 0.36f, 0.0f, 1.3f},
-    {kGmGrad, 256, 2, LGN_BF16, 3.1f, 0.19f, 0.0f, 2.1f},  {kGmGrad, 256, 2, LGN_F32, 6.0f, 0.47f, 0.0f, 2.3f},
-    {kGmGrad, 128, 1, LGN_BF16, 3.5f, 0.20f, 0.0f, 0.8f},  {kGmGrad, 128, 1, LGN_F32, 6.0f, 0.33f, 0.0f, 1.0f},
-    {kGmShare, 128, 1, LGN_BF16, 3.9f, 0.09f, 0.0f, 0.7f}, {kGmShare, 128, 1, LGN_F32, 5.1f, 0.41f, 0.0f, 4.4f}};
+    {kGmRows, 256, 2, 2.3f, 0.30f, 0.0f, {2.7f, 1.4f}}, {kGmTurn, 256, 2, 2.5f, 0.11f, 0.20f, {2.7f, 2.0f}}, {kGmRows, 128, 2, 3.1f, 0.16f, 0.0f, {2.1f, 1.1f}},
+    {kGmRows, 128, 1, 2.6f, 0.27f, 0.0f, {2.4f, 1.1f}}, {kGmSwap, 32, 1, 1.2f, 0.23f, 0.0f, {4.6f, 3.8f}},  {kGmSwap, 64, 1, 1.2f, 0.23f, 0.0f, {5.1f, 5.4f}},
+    {kGmGrad, 256, 2, 5.1f, 0.45f, 0.0f, {2.4f, 1.4f}}, {kGmGrad, 128, 1, 4.1f, 0.42f, 0.0f, {1.0f, 0.6f}}, {kGmShare, 128, 1, 5.2f, 0.45f, 0.0f, {4.0f, 2.1f}}};
+static_assert(LGN_F32 == 0 && LGN_BF16 == 1, "GmCost::tile");
 
 // The kernel of least estimated time: rounds of the grid times the cost of a tile, or the memory's time where that is longer.  What the sizes of the groups
 // are is known on the device alone; equal ones are assumed here.  `bytes`: what the product reads and writes.
@@ -85,7 +80,7 @@ static GmPlan gm_plan(const GmKernels &list, uint64_t rows, uint64_t groups, uin
     for (int i = 0; i < list.count; ++i) {
         const GmKernel &q = list.first[i];
         const GmCost *c = nullptr;
-        for (const GmCost &k : kGmCosts) if (k.form == q.form && k.bn == q.bn && k.ctas == q.ctas && k.odt == odt) c = &k;
+        for (const GmCost &k : kGmCosts) if (k.form == q.form && k.bn == q.bn && k.ctas == q.ctas) c = &k;
         if (q.odt != odt || c == nullptr) continue;
         const bool grad = q.form == kGmGrad || q.form == kGmShare, one = q.form == kGmSwap || q.form == kGmShare;
         const uint64_t height = gm_height(q), cols = (n + gm_width(q) - 1) / gm_width(q), fixed = groups * ((m + height - 1) / height);
@@ -98,7 +93,7 @@ static GmPlan gm_plan(const GmKernels &list, uint64_t rows, uint64_t groups, uin
             const double share = split > 1 ? (double)(uint64_t)((all_steps + split - 1) / split) : all_steps;
             double rounds = tiles * split / slots;
             rounds = rounds < 1.0 ? 1.0 : rounds < 4.0 ? (double)(uint64_t)(rounds + 0.999) : rounds + 0.5;
-            const double work = rounds * (share * step + c->tile) + (split > 1 ? 0.13 + 0.26 * split : 0.0), memory = bytes / 6.26e6;
+            const double work = rounds * (share * step + c->tile[odt]) + (split > 1 ? 0.58 + 0.07 * split : 0.0), memory = bytes / 6.9e6;
             const double cost = c->start + (work > memory ? work : memory) + 0.04 * work;
             if (cost < best_cost) {
                 best_cost = cost;

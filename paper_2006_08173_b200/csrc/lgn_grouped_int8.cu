@@ -9,8 +9,7 @@ GmKernels gm_int8_kernels() {
         gm_kernel<kGmInt8, 256, 2, kGmRows, true, LGN_BF16>(), gm_kernel<kGmInt8, 256, 2, kGmRows, true, LGN_F32>(),
         gm_kernel<kGmInt8, 128, 2, kGmRows, true, LGN_BF16>(), gm_kernel<kGmInt8, 128, 2, kGmRows, true, LGN_F32>(),
         gm_kernel<kGmInt8, 128, 1, kGmRows, true, LGN_BF16>(), gm_kernel<kGmInt8, 128, 1, kGmRows, true, LGN_F32>(),
-        gm_kernel<kGmInt8, 32, 1, kGmSwap, true, LGN_BF16>(), gm_kernel<kGmInt8, 32, 1, kGmSwap, true, LGN_F32>(),
-        gm_kernel<kGmInt8, 64, 1, kGmSwap, true, LGN_BF16>(), gm_kernel<kGmInt8, 64, 1, kGmSwap, true, LGN_F32>()};
+        gm_kernel<kGmInt8, 32, 1, kGmSwap, true, LGN_BF16>(), gm_kernel<kGmInt8, 32, 1, kGmSwap, true, LGN_F32>()};
     return {table, (int)(sizeof table / sizeof table[0])};
 }
 

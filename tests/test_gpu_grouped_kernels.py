@@ -14,44 +14,42 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ROWS, SWAP, GRAD, SHARE, TURN = 0, 1, 2, 3, 4
 # product, form, tile, output -> sizes (rows, groups, n, k) (gradient: m = n, n = k)
 KERNELS = {
-    ("X W^T", ROWS, "256 x 256", "bf16"): [(24359, 19, 680, 272), (14719, 3, 1296, 824)],
-    ("X W^T", ROWS, "128 x 128", "bf16"): [(744, 35, 240, 264), (10818, 4, 840, 128)],
-    ("X W^T", SWAP, "32 x 128", "bf16"): [(380, 12, 2016, 264), (83, 6, 744, 3512)],
-    ("X W^T", SWAP, "64 x 128", "bf16"): [(687, 6, 600, 2984), (866, 36, 168, 3448)],
-    ("X W^T", TURN, "256 x 256", "bf16"): [(11638, 19, 240, 184), (2784, 3, 1216, 2208)],
-    ("X W^T", ROWS, "256 x 256", "f32"): [(6632, 8, 2000, 520), (14239, 10, 1944, 152)],
-    ("X W^T", ROWS, "128 x 128", "f32"): [(1350, 16, 208, 168), (8, 3, 2864, 312)],
-    ("X W^T", SWAP, "32 x 128", "f32"): [(103, 8, 344, 1360), (45, 3, 1616, 2240)],
-    ("X W^T", SWAP, "64 x 128", "f32"): [(18900, 5, 112, 448), (29858, 57, 344, 176)],
-    ("X W^T", TURN, "256 x 256", "f32"): [(19856, 33, 208, 496), (19840, 2, 136, 1344)],
-    ("X W", ROWS, "256 x 256", "bf16"): [(19738, 5, 872, 360), (9695, 5, 232, 2984)],
-    ("X W", ROWS, "128 x 128", "bf16"): [(52, 41, 624, 104), (5804, 14, 152, 1224)],
-    ("X W", SWAP, "32 x 128", "bf16"): [(7, 2, 1464, 2288), (483, 32, 120, 3568)],
-    ("X W", SWAP, "64 x 128", "bf16"): [(3381, 13, 104, 2704), (388, 5, 3720, 1048)],
-    ("X W", TURN, "256 x 256", "bf16"): [(1674, 10, 1504, 232), (476, 13, 832, 1560)],
-    ("X W", ROWS, "256 x 256", "f32"): [(4864, 5, 3672, 160), (11685, 2, 2592, 96)],
-    ("X W", ROWS, "128 x 128", "f32"): [(4215, 3, 136, 128), (2473, 2, 752, 248)],
-    ("X W", SWAP, "32 x 128", "f32"): [(11, 3, 616, 2128), (22, 10, 368, 3064)],
-    ("X W", SWAP, "64 x 128", "f32"): [(18033, 49, 352, 128), (322, 16, 2840, 408)],
-    ("X W", TURN, "256 x 256", "f32"): [(1190, 2, 2528, 2232), (2003, 8, 936, 2864)],
-    ("dY^T X", GRAD, "256 x 256", "bf16"): [(2433, 15, 2272, 152), (23359, 13, 184, 824)],
-    ("dY^T X", GRAD, "128 x 128", "bf16"): [(144, 40, 440, 216), (1106, 32, 2744, 120)],
-    ("dY^T X", SHARE, "128 x 128", "bf16"): [(15769, 8, 168, 232), (7355, 3, 120, 1840)],
-    ("dY^T X", GRAD, "256 x 256", "f32"): [(2695, 7, 648, 1672), (5168, 21, 1704, 472)],
-    ("dY^T X", GRAD, "128 x 128", "f32"): [(107, 2, 3544, 496), (198, 31, 2792, 160)],
-    ("dY^T X", SHARE, "128 x 128", "f32"): [(14441, 2, 192, 344), (21704, 2, 256, 584)],
-    ("8-bit X W^T", TURN, "256 x 256", "bf16"): [(14053, 1, 168, 120), (3, 1, 3672, 3160)],
-    ("8-bit X W^T", ROWS, "256 x 256", "bf16"): [(4357, 1, 3520, 1464), (10631, 4, 2240, 568)],
-    ("8-bit X W^T", ROWS, "256 x 128", "bf16"): [(669, 1, 1208, 2024), (1472, 4, 808, 2376)],
-    ("8-bit X W^T", ROWS, "128 x 128", "bf16"): [(3, 1, 3248, 304), (1423, 3, 2584, 184)],
-    ("8-bit X W^T", SWAP, "32 x 128", "bf16"): [(122, 1, 1040, 3888), (43, 16, 2032, 440)],
-    ("8-bit X W^T", SWAP, "64 x 128", "bf16"): [(484, 60, 3344, 120), (427, 35, 2736, 368)],
-    ("8-bit X W^T", TURN, "256 x 256", "f32"): [(11736, 1, 248, 1312), (2884, 2, 2328, 3072)],
-    ("8-bit X W^T", ROWS, "256 x 256", "f32"): [(10012, 3, 1032, 1288), (10766, 1, 2776, 320)],
-    ("8-bit X W^T", ROWS, "256 x 128", "f32"): [(49, 2, 2616, 160), (1563, 1, 3320, 232)],
-    ("8-bit X W^T", ROWS, "128 x 128", "f32"): [(153, 22, 736, 200), (2672, 50, 168, 536)],
-    ("8-bit X W^T", SWAP, "32 x 128", "f32"): [(56, 1, 1136, 2224), (138, 7, 408, 2544)],
-    ("8-bit X W^T", SWAP, "64 x 128", "f32"): [(372, 1, 2120, 3896), (3273, 20, 952, 792)],
+    ("X W^T", ROWS, "256 x 256", "bf16"): [(3484, 18, 1040, 512), (13409, 3, 536, 1344)],
+    ("X W^T", ROWS, "128 x 128", "bf16"): [(3504, 7, 192, 240), (7118, 10, 240, 576)],
+    ("X W^T", SWAP, "32 x 128", "bf16"): [(63, 5, 472, 2336), (620, 40, 104, 3344)],
+    ("X W^T", SWAP, "64 x 128", "bf16"): [(3644, 17, 184, 1872), (5806, 14, 96, 3288)],
+    ("X W^T", TURN, "256 x 256", "bf16"): [(103, 11, 328, 1272), (9609, 57, 168, 832)],
+    ("X W^T", ROWS, "256 x 256", "f32"): [(7081, 2, 1840, 96), (10509, 2, 144, 2344)],
+    ("X W^T", ROWS, "128 x 128", "f32"): [(2988, 2, 464, 384), (8023, 2, 256, 720)],
+    ("X W^T", SWAP, "32 x 128", "f32"): [(2304, 3, 208, 1896), (114, 59, 800, 376)],
+    ("X W^T", SWAP, "64 x 128", "f32"): [(1947, 11, 328, 1640), (1433, 38, 1744, 248)],
+    ("X W^T", TURN, "256 x 256", "f32"): [(24, 21, 208, 680), (22, 21, 544, 1248)],
+    ("X W", ROWS, "256 x 256", "bf16"): [(15523, 4, 752, 152), (10254, 5, 136, 2320)],
+    ("X W", ROWS, "128 x 128", "bf16"): [(119, 4, 2344, 160), (9440, 49, 104, 368)],
+    ("X W", SWAP, "32 x 128", "bf16"): [(976, 52, 264, 352), (51, 4, 1856, 2136)],
+    ("X W", SWAP, "64 x 128", "bf16"): [(2365, 21, 104, 3184), (9297, 3, 120, 2280)],
+    ("X W", TURN, "256 x 256", "bf16"): [(27, 8, 984, 616), (3229, 49, 680, 384)],
+    ("X W", ROWS, "256 x 256", "f32"): [(26826, 6, 328, 176), (18912, 7, 248, 1032)],
+    ("X W", ROWS, "128 x 128", "f32"): [(11278, 11, 112, 120), (4849, 6, 888, 352)],
+    ("X W", SWAP, "32 x 128", "f32"): [(197, 6, 432, 2288), (219, 35, 2008, 248)],
+    ("X W", SWAP, "64 x 128", "f32"): [(211, 2, 1784, 2336), (1488, 21, 224, 3096)],
+    ("X W", TURN, "256 x 256", "f32"): [(492, 5, 2192, 152), (777, 8, 3488, 376)],
+    ("dY^T X", GRAD, "256 x 256", "bf16"): [(1783, 19, 488, 1616), (6344, 11, 480, 2360)],
+    ("dY^T X", GRAD, "128 x 128", "bf16"): [(10, 7, 2856, 168), (180, 5, 784, 2880)],
+    ("dY^T X", SHARE, "128 x 128", "bf16"): [(7266, 4, 760, 128), (27804, 4, 384, 128)],
+    ("dY^T X", GRAD, "256 x 256", "f32"): [(7112, 2, 552, 1904), (16203, 5, 1448, 296)],
+    ("dY^T X", GRAD, "128 x 128", "f32"): [(273, 8, 592, 688), (25, 15, 440, 1928)],
+    ("dY^T X", SHARE, "128 x 128", "f32"): [(10023, 3, 496, 200), (19581, 5, 320, 448)],
+    ("8-bit X W^T", TURN, "256 x 256", "bf16"): [(8, 1, 1576, 1680), (17, 9, 1856, 656)],
+    ("8-bit X W^T", ROWS, "256 x 256", "bf16"): [(17018, 5, 648, 104), (21838, 15, 472, 504)],
+    ("8-bit X W^T", ROWS, "256 x 128", "bf16"): [(160, 2, 1408, 824), (1069, 1, 1600, 2600)],
+    ("8-bit X W^T", ROWS, "128 x 128", "bf16"): [(541, 6, 216, 264), (2208, 24, 184, 288)],
+    ("8-bit X W^T", SWAP, "32 x 128", "bf16"): [(96, 2, 344, 4064), (87, 22, 816, 504)],
+    ("8-bit X W^T", TURN, "256 x 256", "f32"): [(6, 1, 1488, 656), (12, 11, 760, 728)],
+    ("8-bit X W^T", ROWS, "256 x 256", "f32"): [(4912, 1, 712, 1704), (10738, 1, 1648, 568)],
+    ("8-bit X W^T", ROWS, "256 x 128", "f32"): [(118, 1, 1584, 1000), (10697, 1, 360, 216)],
+    ("8-bit X W^T", ROWS, "128 x 128", "f32"): [(113, 1, 1992, 112), (3543, 1, 528, 104)],
+    ("8-bit X W^T", SWAP, "32 x 128", "f32"): [(20, 6, 3936, 144), (15, 3, 1184, 2736)],
 }
 
 
