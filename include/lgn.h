@@ -529,6 +529,11 @@ lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, 
  * uint32, may be NULL; set to LGN_ERR_TIMEOUT if a bounded device-side wait ran out (the output is then invalid), else left alone.
  * One launch, no workspace; the same inputs give the same bits on the same type of device. */
 
+/* Copies `groups` bf16 matrices (rows x cols, rows ld and matrices x_group elements apart, at any 2-byte boundary) to out, 16-byte aligned, as the
+ * grouped products read them: rows (cols rounded up to a multiple of 8) elements apart, zeros behind their last column, matrices one behind
+ * the other.  One launch. */
+lgn_status lgn_align_rows(const void *x, uint64_t ld, uint64_t x_group, uint64_t groups, uint64_t rows, uint64_t cols, void *out, void *stream);
+
 /* out[r, :] = W_e x[r, :]^T for the rows r of each group e: rows of x have k elements, W_e = w + e w_group is n x k with rows ldw
  * apart.  transposed: W_e is k x n and out[r, :] = x[r, :] W_e (the input gradient of a layer with weights k x n).
  * Rows of no group are left as they were, or set to zero with zero_rest.  k = 0 writes zeros. */

@@ -164,6 +164,8 @@ _lib.lgn_int8_quantize.argtypes = [_vp, _u64, _u64, _u64, _i32, _vp, _vp, _vp]
 _lib.lgn_int8_quantize.restype = _i32
 _lib.lgn_int8_matmul.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
 _lib.lgn_int8_matmul.restype = _i32
+_lib.lgn_align_rows.argtypes = [_vp, _u64, _u64, _u64, _u64, _u64, _vp, _vp]
+_lib.lgn_align_rows.restype = _i32
 _lib.lgn_grouped_matmul.argtypes = [_vp, _u64, _vp, _u64, _u64, _i32, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _i32, _i32, _vp, _vp]
 _lib.lgn_grouped_matmul.restype = _i32
 _lib.lgn_grouped_weight_grad.argtypes = [_vp, _u64, _vp, _u64, _vp, _i32, _u64, _u64, _u64, _u64, _vp, _u64, _u64, _i32, _i32, _vp, _vp]
@@ -914,11 +916,16 @@ def _pieces(t: torch.Tensor, stream) -> Tuple[torch.Tensor, int, int]:
         fits = (step[-1] == 1 or cols == 1) and (rows == 1 or row >= cols and row % 8 == 0) and (count == 1 or group >= (rows - 1) * row + cols and group % 8 == 0)
     if fits and t.data_ptr() % 16 == 0:
         return t, row, group
-    row = (cols + 7) & -8
+    pitch = (cols + 7) & -8
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(_as_stream(stream, t.device)):
-        padded = torch.empty(*shape[:-1], row, dtype=t.dtype, device=t.device)
-        padded[..., :cols].copy_(t)
-    return padded, row, row * rows
+        padded = torch.empty(*shape[:-1], pitch, dtype=t.dtype, device=t.device)
+        step = t.stride()
+        if (step[-1] == 1 or cols == 1) and (rows == 1 or step[-2] >= cols):
+            _check(_lib.lgn_align_rows(t.data_ptr(), step[-2] if rows > 1 else cols, step[0] if count > 1 else 0, count, rows, cols, padded.data_ptr(),
+                                       _stream(stream)), "lgn_align_rows")
+        else:                                              # transposed or broadcast within a matrix
+            padded[..., :cols].copy_(t)
+    return padded, pitch, pitch * rows
 
 
 def _bf16(*operands: torch.Tensor) -> None:

@@ -227,3 +227,15 @@ def test_weight_gradient_of_few_tiles(lgn, rows, groups, m, n, dtype):
     out = before.clone()
     lgn.lgn_grouped_weight_grad(dy, x, offsets, out=out, accumulate=True)
     check(out, want + before.double(), mag + before.double().abs(), rows)
+
+
+def test_align_rows(lgn):
+    """Values and the zeros behind them, for rows at any boundary; what lies behind the copy stays."""
+    big = values(7, 40, 333, seed=4)
+    for view in (big[:, :, :3], big[1:4, 5:30, 7:300], big[:1, :1, 1:332], big[:, ::3, 1:9], big[::2, :, :332]):
+        g, r, c = view.shape
+        pitch = (c + 7) // 8 * 8
+        out = torch.full((g * r * pitch + 16,), -7.0, dtype=torch.bfloat16, device="cuda")
+        assert lgn.raw().lgn_align_rows(view.data_ptr(), view.stride(1), view.stride(0), g, r, c, out.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+        got = out[:-16].view(g, r, pitch)
+        assert torch.equal(got[..., :c], view) and not got[..., c:].any() and (out[-16:] == -7.0).all()

@@ -143,3 +143,12 @@ def test_several_devices_are_refused(lgn, monkeypatch):
             bad()
     with pytest.raises(ValueError):
         lgn.Int8Operand(Stand(4, 64, dtype=torch.int8), Stand(4, at=1), 4, 64)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(x=None), 1), (dict(x=P + 1), 1), (dict(ld=9), 1), (dict(ld=2 ** 41), 1), (dict(group=2 ** 41), 1), (dict(out=None), 1), (dict(out=64 * P + 8), 1), (dict(out=P), 1), (dict(rows=2 ** 31), 2),
+    (dict(cols=2 ** 31, ld=2 ** 31), 2), (dict(groups=2 ** 21), 2), (dict(rows=0, x=None, out=None), 0)])
+def test_align_rows_refuses(lgn, change, code):
+    a = dict(x=P, ld=10, group=50, groups=3, rows=5, cols=10, out=64 * P, stream=None)
+    a.update(change)
+    assert lgn.raw().lgn_align_rows(*a.values()) == code
