@@ -93,6 +93,8 @@ template <int DT> struct Piece {
             return fmaxf(m, fmaxf(bf_lo(a), bf_hi(a)));
         }
     }
+    // What was made of the words so far is not kept for later: unpacked values would take twice the registers.
+    __device__ __forceinline__ void forget() { asm volatile("" : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])); }
 };
 // A piece that the row begins or ends in: column `c` is the first, columns outside the row read as -inf and are not written.  Of its own, so that
 // the loops over whole pieces stay short.
@@ -171,7 +173,7 @@ struct TeacherSums {
 
 // DUAL: the two parts take softmaxes of different temperatures.
 template <int DT, int THREADS, bool DUAL, bool GRAD>
-__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : THREADS == 256 ? 6 : 768 / THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : GRAD ? 768 / THREADS : 1024 / THREADS)
 distill_kernel(const DistillArgs p) {
     constexpr int kVals = Piece<DT>::kVals, ES = 16 / kVals, kWarps = THREADS / 32;
     extern __shared__ uint32_t dyn[];
@@ -223,18 +225,36 @@ distill_kernel(const DistillArgs p) {
     if (GRAD && p.weight != nullptr) w = __uint_as_float(ldro_u32(p.weight + row));
     const uint32_t slots = smem_u32(dyn + p.slots) + tid * 16;      // the thread's pieces: nobody else's, no barrier
     auto used = [&](uint32_t v) { return (int)min(p.vecs, (v1 - v + THREADS - 1) / THREADS); };     // pieces per thread of the chunk from v on
+    // A gradient reads the row twice and keeps it in shared memory; a loss alone takes each chunk straight to registers.
+    constexpr int kHeld = GRAD ? 1 : kDsVecs / 2;
+    Piece<DT> held[kHeld];
     auto load = [&](uint32_t v) {
         const char *at = base + (uint64_t)(v + tid) * 16;
         const int n = used(v);
-        #pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const uint32_t u = v + i * THREADS + tid;
-            const uint32_t slot = slots + i * THREADS * 16;
-            if (u - in0 < in1 - in0)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(at + i * THREADS * 16) : "memory");
-            else {
-                const uint4 e = u < v1 ? load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab) : make_uint4(kNone, kNone, kNone, kNone);
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(slot), "r"(e.x), "r"(e.y), "r"(e.z), "r"(e.w) : "memory");
+        auto edge = [&](uint32_t u) { return u < v1 ? load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab) : make_uint4(kNone, kNone, kNone, kNone); };
+        if constexpr (GRAD) {
+            #pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const uint32_t u = v + i * THREADS + tid, slot = slots + i * THREADS * 16;
+                if (u - in0 < in1 - in0)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(at + i * THREADS * 16) : "memory");
+                else {
+                    const uint4 e = edge(u);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(slot), "r"(e.x), "r"(e.y), "r"(e.z), "r"(e.w) : "memory");
+                }
+            }
+        } else {
+            #pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                if (i >= n) break;
+                const uint32_t u = v + i * THREADS + tid;
+                uint32_t (&q)[4] = held[i].w;
+                if (u - in0 < in1 - in0)
+                    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "l"(at + i * THREADS * 16) : "memory");
+                else {
+                    const uint4 e = edge(u);
+                    q[0] = e.x; q[1] = e.y; q[2] = e.z; q[3] = e.w;
+                }
             }
         }
     };
@@ -243,6 +263,20 @@ distill_kernel(const DistillArgs p) {
         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.w[0]), "=r"(x.w[1]), "=r"(x.w[2]), "=r"(x.w[3]) : "r"(slots + i * THREADS * 16) : "memory");
         return x;
     };
+    // f of the thread's pieces of a chunk, one after another
+    auto each = [&](int n, auto f) {
+        if constexpr (GRAD) {
+            #pragma unroll 2
+            for (int i = 0; i < n; ++i) f(piece(i));
+        } else {
+            #pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                if (i >= n) break;
+                held[i].forget();
+                f(held[i]);
+            }
+        }
+    };
     load(v0);
     const int32_t id0 = present(tid, far0, z0);
     if (id0 >= 0) s0 = ds_load<DT>(src, (uint64_t)id0);
@@ -250,19 +284,14 @@ distill_kernel(const DistillArgs p) {
     float m = kDsLowest, sum = 0.0f, sum1 = 0.0f;
     for (uint32_t v = v0;;) {
         float c = m;
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        if constexpr (GRAD) asm volatile("cp.async.wait_all;" ::: "memory");
         const int n = used(v);
-        #pragma unroll 2
-        for (int i = 0; i < n; ++i) {
-            c = piece(i).max_with(c);
-        }
+        each(n, [&](const Piece<DT> &x) { c = x.max_with(c); });
         sum *= exp2_approx((m - c) * p.scale);
         if constexpr (DUAL) sum1 *= exp2_approx((m - c) * p.scale1);
         m = c;
-        #pragma unroll 2
-        for (int i = 0; i < n; ++i) {
+        each(n, [&](const Piece<DT> &x) {
             float a = 0.0f, a1 = 0.0f;
-            const Piece<DT> x = piece(i);
             #pragma unroll
             for (int k = 0; k < kVals; ++k) {
                 const float t = x.at(k) - c;
@@ -271,7 +300,7 @@ distill_kernel(const DistillArgs p) {
             }
             sum += a;
             if constexpr (DUAL) sum1 += a1;
-        }
+        });
         v += THREADS * p.vecs;
         if (v >= v1) break;
         load(v);
@@ -489,7 +518,7 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     const bool aligned = aligned_to(logits, 16) && (ld * es) % 16 == 0;
     const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + (aligned ? 0 : vals - 1)) / vals;        // of a row that is aligned worst
     // A gradient needs the row twice: the fewest threads of 32, 64 and 128 that hold it, or up to 8 CTAs of 128 (16 pieces per thread: what a CTA does
-    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 199 us,
+    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 186 us,
     // 207 with 128).  More CTAs per row where there are too few rows to fill the machine.
     const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 64 * kDsVecs ? 1 : 2;
     const unsigned threads = kind == 0 ? 32 : kind == 1 ? 64 : grad ? 128 : 256;
@@ -501,7 +530,7 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     p.slots = (uint32_t)((3 * (top + 1) + p.table + 3) & ~3ull);
     p.vecs = (p.pieces + threads - 1) / threads;
     if (p.vecs > (grad ? kDsVecs : kDsVecs / 2)) p.vecs = grad ? kDsVecs : kDsVecs / 2;
-    const size_t smem = 4 * p.slots + 16 * (size_t)threads * p.vecs;
+    const size_t smem = 4 * p.slots + (grad ? 16 * (size_t)threads * p.vecs : 0);
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
              (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
     const void *fn = kDistillTable[dt][kind][dual][grad];
