@@ -6,10 +6,10 @@
 //
 // With M = max s, S = sum exp((s - M) / T) and Z, zm the same of the teacher, the first part is
 //   a T (1/Z sum exp((z - zm) / T) ((z - zm) - (s[id] - M))) + a T^2 (ln S - ln Z),
-// so a row needs one pass for M and the sums and, for the gradient, one more over values that are still
-// in registers: a CTA of 128 or 256 threads holds 8 x 16 bytes of a row per thread, and a cluster of up to 8 of them a row
-// (their sums are joined through distributed shared memory).  Rows beyond that go through in chunks
-// that are read again for the gradient, from L2 mostly.
+// so a row needs one pass for M and the sums and, for the gradient, one more.  A gradient keeps its row in shared memory in between:
+// 32, 64 or 128 threads with up to 16 pieces of 16 bytes each, or a cluster of up to 8 such CTAs (their sums are joined through
+// distributed shared memory); rows beyond that go through in chunks that are read again, from L2 mostly.  The loss alone takes
+// chunks of 8 pieces per thread straight to registers.
 //
 // exp is taken in base 2 of (s - M) log2(e) / T, the difference first: it is exact or small where the term
 // counts.  Sums are fp32, a few dozen terms per thread, then by lanes, warps and ranks in a fixed order.
@@ -30,6 +30,7 @@ namespace lgn {
 
 constexpr uint64_t kDsMaxTop = 1024, kDsMaxDim = 1ull << 30;
 constexpr int kDsVecs = 16;                             // pieces of 16 bytes a thread holds at most
+constexpr int kDsMaxSmem = 64 * 1024;                   // above the most that a CTA asks for: 3 x 1025 + 4096 words of entries, 128 x 16 pieces
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kDsLowest = -3.402823466e38f;           // starts every maximum: s - M is then never inf - inf for s = -inf
 
@@ -534,7 +535,8 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
              (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
     const void *fn = kDistillTable[dt][kind][dual][grad];
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {     // many entries
+    // Many entries.  The same limit from every call: calls of two threads must not lower one another's.
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kDsMaxSmem) != cudaSuccess) {
         (void)cudaGetLastError();
         return LGN_ERR_CUDA;
     }

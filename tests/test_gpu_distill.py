@@ -203,3 +203,30 @@ def test_streams_graphs_and_the_same_bits(lgn):
         graph.replay()
         for got in (other, captured):
             assert torch.equal(got[0], first[0]) and torch.equal(got[1], first[1])
+
+
+def test_two_threads(lgn):
+    """Calls whose CTAs need different amounts of shared memory, from two threads at once."""
+    import threading
+    sets = [inputs(8, 16000, top, top, torch.bfloat16) for top in (1024, 700)]
+    want = [lgn.lgn_distill_loss(s, ids, z, labels, 2.0, 0.5, grad=True) for s, ids, z, labels, _ in sets]
+    wrong = []
+
+    def run(i):
+        s, ids, z, labels, _ = sets[i]
+        stream = torch.cuda.Stream()
+        try:
+            for _ in range(3000):
+                loss, d = lgn.lgn_distill_loss(s, ids, z, labels, 2.0, 0.5, grad=True, stream=stream)
+            stream.synchronize()
+            if not (torch.equal(loss, want[i][0]) and torch.equal(d, want[i][1])):
+                wrong.append(i)
+        except Exception as e:
+            wrong.append(e)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
