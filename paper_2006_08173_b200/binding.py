@@ -809,6 +809,10 @@ class Int8Operand:
         o._scales_ptr = at + codes
         return o
 
+    def __reduce__(self):
+        """Copies and pickles are made of the tensors: the addresses are those of this operand's memory alone."""
+        return Int8Operand, (self.codes, self.scales, self.rows, self.k)
+
     @property
     def codes(self) -> torch.Tensor:
         if self._buffer is None:

@@ -155,3 +155,18 @@ def test_empty_products(lgn):
     assert (lgn.lgn_int8_matmul(a, b) == 0).all()
     a, b = lgn.lgn_int8_quantize(torch.zeros(0, 16, device="cuda")), lgn.lgn_int8_quantize(torch.zeros(7, 16, device="cuda"))
     assert lgn.lgn_int8_matmul(a, b).shape == (0, 7) and lgn.lgn_int8_matmul(b, a).shape == (7, 0)
+
+
+@pytest.mark.parametrize("rows,k", [(33, 70), (128, 256), (0, 5), (4, 0)])
+def test_copied_operands_have_their_own_memory(lgn, rows, k):
+    import copy
+    import pickle
+    a = lgn.lgn_int8_quantize(values(rows, k, 3))
+    b = lgn.lgn_int8_quantize(values(24, k, 4))
+    want = lgn.lgn_int8_matmul(a, b)
+    copies = [copy.deepcopy(a), pickle.loads(pickle.dumps(a))]
+    shallow = copy.copy(a)
+    assert torch.equal(lgn.lgn_int8_matmul(shallow, b), want)
+    a._buffer.fill_(1)
+    for c in copies:
+        assert (c.rows, c.k) == (rows, k) and torch.equal(lgn.lgn_int8_matmul(c, b), want)
