@@ -160,7 +160,7 @@ class Int8Linear(_Bounded):
         flat, status = x.reshape(-1, x.shape[-1]), self._status_on(x.device)
         if self._frozen is None:
             y = _Int8LinearFn.apply(flat, self.weight, self.sparsity, self.seed, status)
-        elif torch.is_grad_enabled() and x.requires_grad:
+        elif torch.is_grad_enabled() and (x.requires_grad or self.weight.requires_grad):
             raise RuntimeError("the layer is frozen: no gradients")
         else:
             y = lgn.lgn_int8_matmul(lgn.lgn_int8_quantize(_rows(flat)), self._frozen, out_dtype=x.dtype, status=status)

@@ -174,3 +174,18 @@ def test_gradients_along_the_example(layers):
         check_grouped(layer.weight.grad, *grouped_gradient(y.grad.bfloat16(), x.detach().bfloat16(), ends), x.shape[0])
         check_grouped(x.grad, *grouped_forward(y.grad.bfloat16(), layer.weight.detach().bfloat16(), ends, True), y.shape[1])
     assert bool(model.embed.weight.grad.any()) and bool(model.gate.weight.grad.any())
+
+
+def test_frozen_layers_refuse_every_gradient(layers):
+    """A layer that comes first in a model: its input wants no gradient, its weights do."""
+    lin = layers.Int8Linear(64, 48, device="cuda")
+    x = torch.randn(9, 64, device="cuda")
+    lin.freeze()
+    with pytest.raises(RuntimeError):
+        lin(x)
+    lin.weight.requires_grad_(False)
+    y = lin(x)
+    with pytest.raises(RuntimeError):
+        lin(x.clone().requires_grad_())
+    with torch.inference_mode():
+        assert torch.equal(lin(x), y)
