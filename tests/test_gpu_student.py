@@ -189,3 +189,18 @@ def test_frozen_layers_refuse_every_gradient(layers):
         lin(x.clone().requires_grad_())
     with torch.inference_mode():
         assert torch.equal(lin(x), y)
+
+
+def test_first_pass_in_inference_mode(layers):
+    """check() after it, and passes that train."""
+    lin, mix, fp8_lin = layers.Int8Linear(64, 48, device="cuda"), layers.ExpertLinear(2, 64, 48, device="cuda"), layers.Fp8Linear(64, 48, device="cuda")
+    offsets = torch.tensor([0, 4, 9], device="cuda")
+    x = torch.randn(9, 64, device="cuda")
+    for layer, args in ((lin, ()), (mix, (offsets,)), (fp8_lin, ())):
+        with torch.inference_mode():
+            y = layer(x, *args)
+        layer.check()
+        z = layer(x, *args)
+        z.sum().backward()
+        layer.check()
+        assert torch.equal(y, z) and layer.weight.grad is not None
