@@ -276,6 +276,8 @@ class DistillLoss(torch.nn.Module):
     def forward(self, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, labels: Optional[torch.Tensor] = None) -> torch.Tensor:
         """logits ... x vocab, ids and teacher ... x top, labels ...; the losses have the shape of the rows."""
         shape, top = logits.shape[:-1], ids.shape[-1]
+        if ids.shape[:-1] != shape or teacher.shape != ids.shape or (labels is not None and labels.shape != shape):
+            raise ValueError("logits, ids, teacher and labels must have the same rows")
         rows = shape.numel()
         flat = None if labels is None else labels.reshape(rows).contiguous()
         loss = _DistillFn.apply(logits.reshape(rows, logits.shape[-1]), _rows(ids.reshape(rows, top)), _rows(teacher.detach().reshape(rows, top)), flat,

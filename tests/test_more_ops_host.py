@@ -152,3 +152,12 @@ def test_align_rows_refuses(lgn, change, code):
     a = dict(x=P, ld=10, group=50, groups=3, rows=5, cols=10, out=64 * P, stream=None)
     a.update(change)
     assert lgn.raw().lgn_align_rows(*a.values()) == code
+
+
+def test_distill_loss_of_other_rows_is_refused(lgn):
+    """As many values in another order would be other rows' values."""
+    from paper_2006_08173_b200.layers import DistillLoss
+    s, ids, z, labels = torch.zeros(2, 3, 50), torch.zeros(2, 3, 4, dtype=torch.int64), torch.zeros(2, 3, 4), torch.zeros(2, 3, dtype=torch.int64)
+    for bad in ((s, ids.reshape(3, 2, 4), z), (s, ids, z.reshape(3, 2, 4)), (s, ids, z.reshape(2, 6, 2)), (s, ids, z, labels.reshape(3, 2)), (s, ids, z, labels.reshape(6))):
+        with pytest.raises(ValueError, match="same rows"):
+            DistillLoss()(*bad)
