@@ -171,6 +171,8 @@ class Int8Linear(_Bounded):
 def by_expert(ids: torch.Tensor, experts: int) -> Tuple[torch.Tensor, torch.Tensor]:
     """(order, offsets) of a flat tensor of expert numbers: ids[order] is sorted, equal ones in the order they came, and expert e has the places
     offsets[e] to offsets[e + 1] of it.  Numbers outside [0, experts) come ahead of or behind all of them.  Nothing leaves the device."""
+    if ids.dtype not in (torch.int32, torch.int64):
+        ids = ids.long()                                               # narrow ones do not hold the number of experts
     ranked, order = torch.sort(ids, stable=True)
     return order, torch.searchsorted(ranked, torch.arange(experts + 1, dtype=ids.dtype, device=ids.device))
 

@@ -161,3 +161,17 @@ def test_distill_loss_of_other_rows_is_refused(lgn):
     for bad in ((s, ids.reshape(3, 2, 4), z), (s, ids, z.reshape(3, 2, 4)), (s, ids, z.reshape(2, 6, 2)), (s, ids, z, labels.reshape(3, 2)), (s, ids, z, labels.reshape(6))):
         with pytest.raises(ValueError, match="same rows"):
             DistillLoss()(*bad)
+
+
+@pytest.mark.parametrize("dtype", [torch.uint8, torch.int8, torch.int16, torch.int32, torch.int64])
+@pytest.mark.parametrize("experts", [1, 5, 127, 128, 256])
+def test_by_expert(lgn, dtype, experts):
+    from paper_2006_08173_b200.layers import by_expert
+    top = min(experts, torch.iinfo(dtype).max)
+    ids = torch.arange(500).mul(7919).remainder(top + 1).to(dtype)
+    order, offsets = by_expert(ids, experts)
+    ends = offsets.tolist()
+    assert len(ends) == experts + 1 and sorted(order.tolist()) == list(range(500))
+    for e in range(experts):
+        assert order[ends[e]:ends[e + 1]].tolist() == [i for i in range(500) if int(ids[i]) == e]
+    assert by_expert(ids[:0], experts)[1].tolist() == [0] * (experts + 1)
