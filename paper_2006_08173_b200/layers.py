@@ -193,7 +193,9 @@ class _ExpertFn(torch.autograd.Function):
         if not (need_dx or need_dw):
             return None, None, None, None, None, None
         offsets, *kept = ctx.saved_tensors
-        if ctx.sparsity > 0.0:
+        if ctx.sparsity > 0.0:                                         # whatever stands in rows of no expert must not reach the threshold
+            row = torch.arange(dy.shape[0], device=dy.device)
+            dy = dy.masked_fill(((row < offsets[0]) | (row >= offsets.max()))[:, None], 0.0)
             dy = _pruned(dy, ctx.sparsity, ctx.seed, ctx.status)
         dy = dy.to(torch.bfloat16)
         dx = lgn.lgn_grouped_matmul(dy, kept[0], offsets, out_dtype=ctx.dtypes[0], transposed=True, status=ctx.status) if need_dx else None
@@ -203,7 +205,7 @@ class _ExpertFn(torch.autograd.Function):
 
 class ExpertLinear(_Bounded):
     """y[r] = W_e x[r] for the rows r = offsets[e] .. offsets[e + 1] - 1 of each expert e (by_expert gives such offsets), in bf16 with fp32 sums; rows of no
-    expert give zeros.  ``sparsity``, ``seed``, advance() and check() are those of Fp8Linear."""
+    expert give zeros.  ``sparsity``, ``seed``, advance() and check() are those of Fp8Linear; rows of no expert count as zeros there."""
 
     def __init__(self, experts: int, in_features: int, out_features: int, sparsity: float = 0.0, device=None, seed: int = 0):
         super().__init__()

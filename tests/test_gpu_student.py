@@ -204,3 +204,21 @@ def test_first_pass_in_inference_mode(layers):
         z.sum().backward()
         layer.check()
         assert torch.equal(y, z) and layer.weight.grad is not None
+
+
+def test_rows_of_no_expert_do_not_reach_the_pruning(layers):
+    torch.manual_seed(0)
+    lin, plain = (layers.ExpertLinear(2, 128, 256, sparsity=s, device="cuda", seed=9) for s in (0.7, 0.0))
+    plain.weight.data.copy_(lin.weight.data)
+    offsets = torch.tensor([40, 200, 400], device="cuda")
+    x = torch.randn(512, 128, device="cuda").bfloat16()
+    dy = torch.exp(-12 + 2 * torch.randn(512, 256, device="cuda")).bfloat16()
+    dy[:40], dy[400:] = float("nan"), float("inf")
+    zeros = dy.clone()
+    zeros[:40], zeros[400:] = 0.0, 0.0
+    a, b = x.clone().requires_grad_(), x.clone().requires_grad_()
+    lin(a, offsets).backward(dy)
+    plain(b, offsets).backward(layers._pruned(zeros, 0.7, 9))
+    assert torch.equal(a.grad, b.grad) and torch.equal(lin.weight.grad, plain.weight.grad)
+    assert bool(a.grad.isfinite().all()) and bool(lin.weight.grad.isfinite().all())
+    lin.check()
