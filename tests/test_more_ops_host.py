@@ -1,7 +1,5 @@
 """CPU-only checks of the C entries for 8-bit integers, grouped products and distillation: sizes, and arguments refused before anything is
 enqueued."""
-import ctypes as C
-
 import pytest
 import torch
 
