@@ -3,7 +3,9 @@ floating point (optionally with its neural gradient pruned first), one whose for
 layers of experts over rows grouped by expert, an embedding whose gradient is summed in a fixed order, the loss against a
 teacher's top logits, and gradient clipping that stays on the device.
 
-The modules marshal arguments for ``binding``; there is no CPU path.
+The modules marshal arguments for ``binding``; there is no CPU path.  A step may be captured into a CUDA graph after a pass on the same
+device (which makes the status words), and while no graph of autograd from outside of the capture holds the same parameters:
+torch would have the captured gradients wait for its stream.
 """
 from __future__ import annotations
 
