@@ -62,6 +62,34 @@ __device__ __forceinline__ float log2_approx(float x) {
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// Two fp32 values in a register pair, and arithmetic on both at once: half the instructions.
+struct Two { uint64_t w; };
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.w) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void apart(Two x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.w)); }
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.w) : "l"(a.w), "l"(b.w));
+    return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.w) : "l"(a.w), "l"(b.w));
+    return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+    return r;
+}
+__device__ __forceinline__ Two exp2_approx(Two x) {
+    float a, b;
+    apart(x, a, b);
+    return two(exp2_approx(a), exp2_approx(b));
+}
 template <int DT>
 __device__ __forceinline__ float ds_load(const char *p, uint64_t i) {
     if constexpr (DT == LGN_F32) return __uint_as_float(ldro_u32(p + 4 * i));
@@ -84,6 +112,7 @@ template <int DT> struct Piece {
         if constexpr (DT == LGN_F32) return __uint_as_float(w[k]);
         else return k & 1 ? bf_hi(w[k >> 1]) : bf_lo(w[k >> 1]);
     }
+    __device__ __forceinline__ Two pair(int k) const { return two(at(2 * k), at(2 * k + 1)); }
     __device__ __forceinline__ float max_with(float m) const {           // bf16 in pairs
         if constexpr (DT == LGN_F32) return fmaxf(fmaxf(m, fmaxf(at(0), at(1))), fmaxf(at(2), at(3)));
         else {
@@ -282,29 +311,47 @@ distill_kernel(const DistillArgs p) {
     const int32_t id0 = present(tid, far0, z0);
     if (id0 >= 0) s0 = ds_load<DT>(src, (uint64_t)id0);
 
-    float m = kDsLowest, sum = 0.0f, sum1 = 0.0f;
+    const Two scales = two(p.scale, p.scale), scales1 = two(p.scale1, p.scale1);
+    float m = kDsLowest;
+    Two sums = two(0.0f, 0.0f), sums1 = sums;           // of the even and of the odd columns
     for (uint32_t v = v0;;) {
         float c = m;
         if constexpr (GRAD) asm volatile("cp.async.wait_all;" ::: "memory");
         const int n = used(v);
         each(n, [&](const Piece<DT> &x) { c = x.max_with(c); });
-        sum *= exp2_approx((m - c) * p.scale);
-        if constexpr (DUAL) sum1 *= exp2_approx((m - c) * p.scale1);
+        const float f = exp2_approx((m - c) * p.scale);
+        sums = sums * two(f, f);
+        if constexpr (DUAL) {
+            const float f1 = exp2_approx((m - c) * p.scale1);
+            sums1 = sums1 * two(f1, f1);
+        }
         m = c;
+        const Two from = two(-c, -c);
         each(n, [&](const Piece<DT> &x) {
-            float a = 0.0f, a1 = 0.0f;
+            Two a, a1;
             #pragma unroll
-            for (int k = 0; k < kVals; ++k) {
-                const float t = x.at(k) - c;
-                a += exp2_approx(t * p.scale);
-                if constexpr (DUAL) a1 += exp2_approx(t * p.scale1);
+            for (int k = 0; k < kVals / 2; ++k) {
+                const Two t = x.pair(k) + from, e = exp2_approx(t * scales);
+                a = k == 0 ? e : a + e;
+                if constexpr (DUAL) {
+                    const Two e1 = exp2_approx(t * scales1);
+                    a1 = k == 0 ? e1 : a1 + e1;
+                }
             }
-            sum += a;
-            if constexpr (DUAL) sum1 += a1;
+            sums = sums + a;
+            if constexpr (DUAL) sums1 = sums1 + a1;
         });
         v += THREADS * p.vecs;
         if (v >= v1) break;
         load(v);
+    }
+
+    float sum, sum1 = 0.0f;
+    {
+        float odd;
+        apart(sums, sum, odd);
+        sum += odd;
+        if constexpr (DUAL) { apart(sums1, sum1, odd); sum1 += odd; }
     }
 
     // the entries
@@ -397,8 +444,9 @@ distill_kernel(const DistillArgs p) {
         };
         // bf16: the factors are taken into the exponents, whose rounding (2^-24 of about forty) is far below the output's
         constexpr bool kFold = DT == LGN_BF16;
-        const float lt = kFold ? log2_approx(fabsf(DUAL ? kt : kt + k1)) - log2_approx(sum) : 0.0f;
-        const float l1 = kFold && DUAL ? log2_approx(fabsf(k1)) - log2_approx(sum1) : 0.0f;
+        const float lt = kFold ? log2_approx(fabsf(DUAL ? kt : kt + k1)) - log2_approx(sum) : ct;
+        const float l1 = kFold && DUAL ? log2_approx(fabsf(k1)) - log2_approx(sum1) : c1;
+        const Two from = two(-m, -m), lts = two(lt, lt), l1s = two(l1, l1);
         const uint32_t sign = kFold && w < 0.0f ? 0x80008000u : 0u;
         const bool held = v1 - v0 <= THREADS * p.vecs; // the one chunk is still there
         for (uint32_t v = v0; v < v1; v += THREADS * p.vecs) {
@@ -415,19 +463,15 @@ distill_kernel(const DistillArgs p) {
                 if (dead) q[0] = q[1] = q[2] = q[3] = 0u;
                 else {
                     const Piece<DT> x = piece(i);
-                    float d[kVals];
                     #pragma unroll
-                    for (int k = 0; k < kVals; ++k) {
-                        if constexpr (kFold) {
-                            const float t = x.at(k) - m;
-                            d[k] = exp2_approx(fmaf(t, p.scale, lt));
-                            if constexpr (DUAL) d[k] += exp2_approx(fmaf(t, p.scale1, l1));
-                        } else d[k] = slope(x.at(k));
-                    }
-                    #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if constexpr (DT == LGN_F32) q[k] = __float_as_uint(d[k]);
-                        else q[k] = pack_bf16(d[2 * k], d[2 * k + 1]) ^ sign;
+                    for (int k = 0; k < kVals / 2; ++k) {
+                        const Two t = x.pair(k) + from;
+                        Two d = kFold ? exp2_approx(fma(t, scales, lts)) : exp2_approx(t * scales) * lts;
+                        if constexpr (DUAL) d = kFold ? d + exp2_approx(fma(t, scales1, l1s)) : fma(exp2_approx(t * scales1), l1s, d);
+                        float lo, hi;
+                        apart(d, lo, hi);
+                        if constexpr (DT == LGN_F32) { q[2 * k] = __float_as_uint(lo); q[2 * k + 1] = __float_as_uint(hi); }
+                        else q[k] = pack_bf16(lo, hi) ^ sign;
                     }
                 }
                 if (whole && u - in0 < in1 - in0)
