@@ -57,11 +57,6 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float log2_approx(float x) {
-    float r;
-    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 // Two fp32 values in a register pair, and arithmetic on both at once: half the instructions.
 struct Two { uint64_t w; };
 __device__ __forceinline__ Two two(float a, float b) {
@@ -229,13 +224,12 @@ distill_kernel(const DistillArgs p) {
     const char *src = p.logits + row * p.ld * ES;
     char *dst = GRAD ? p.dlogits + row * p.ldd * ES : nullptr;
     const int64_t shift = (int64_t)((reinterpret_cast<uintptr_t>(src) & 15) / ES), vocab = (int64_t)p.vocab;
-    const bool whole = GRAD && ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0;
+    const bool alike = GRAD && ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0;
     const uint32_t total = (uint32_t)((shift + vocab + kVals - 1) / kVals);             // pieces of the row
     const uint32_t v0 = min(rank * p.pieces, total), v1 = min(v0 + p.pieces, total);
     const uint32_t in0 = shift > 0 ? 1u : 0u, in1 = max(in0, min(v1, (uint32_t)((shift + vocab) / kVals)));   // whole pieces
     const char *base = src - shift * ES;
-    constexpr uint32_t kNone = DT == LGN_F32 ? 0xff800000u : 0xff80ff80u;               // -inf
-
+    
     // An entry: its place, the teacher's logit, the student's.
     auto place_of = [&](uint32_t j, float &z) {
         int64_t at = -1;
@@ -254,54 +248,69 @@ distill_kernel(const DistillArgs p) {
     const int64_t far0 = place_of(tid, z0);
     if (GRAD && p.weight != nullptr) w = __uint_as_float(ldro_u32(p.weight + row));
     const uint32_t slots = smem_u32(dyn + p.slots) + tid * 16;      // the thread's pieces: nobody else's, no barrier
-    auto used = [&](uint32_t v) { return (int)min(p.vecs, (v1 - v + THREADS - 1) / THREADS); };     // pieces per thread of the chunk from v on
+    // Pieces of a thread in the chunk from v on: `all` of them, of which [skip, whole) are whole and at most one on either side is not.
+    uint32_t all, skip, whole;
+    auto count = [&](uint32_t v) {
+        const uint32_t u = v + tid, end = min(v1, v + THREADS * p.vecs), last = min(end, in1);
+        all = u < end ? (end - u + THREADS - 1) / THREADS : 0u;
+        whole = u < last ? (last - u + THREADS - 1) / THREADS : 0u;
+        skip = u < min(in0, end) ? 1u : 0u;
+    };
+    auto edge = [&](uint32_t u) { return load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab); };
     // A gradient reads the row twice and keeps it in shared memory; a loss alone takes each chunk straight to registers.
-    constexpr int kHeld = GRAD ? 1 : kDsVecs / 2;
+    constexpr uint32_t kHeld = GRAD ? 1 : kDsVecs / 2, kStride = THREADS * 16;
     Piece<DT> held[kHeld];
     auto load = [&](uint32_t v) {
+        count(v);
         const char *at = base + (uint64_t)(v + tid) * 16;
-        const int n = used(v);
-        auto edge = [&](uint32_t u) { return u < v1 ? load_edge<DT>(src, (int64_t)u * kVals - shift, p.vocab) : make_uint4(kNone, kNone, kNone, kNone); };
         if constexpr (GRAD) {
+            auto put = [&](uint32_t i) {
+                const uint4 e = edge(v + i * THREADS + tid);
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(slots + i * kStride), "r"(e.x), "r"(e.y), "r"(e.z), "r"(e.w) : "memory");
+            };
+            uint32_t slot = slots + skip * kStride;
+            at += skip * kStride;
             #pragma unroll 4
-            for (int i = 0; i < n; ++i) {
-                const uint32_t u = v + i * THREADS + tid, slot = slots + i * THREADS * 16;
-                if (u - in0 < in1 - in0)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(at + i * THREADS * 16) : "memory");
-                else {
-                    const uint4 e = edge(u);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(slot), "r"(e.x), "r"(e.y), "r"(e.z), "r"(e.w) : "memory");
-                }
-            }
+            for (uint32_t i = skip; i < whole; ++i, slot += kStride, at += kStride)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(at) : "memory");
+            if (skip != 0u) put(0);
+            if (whole < all) put(whole);
         } else {
-            #pragma unroll
-            for (int i = 0; i < kHeld; ++i) {
-                if (i >= n) break;
-                const uint32_t u = v + i * THREADS + tid;
+            auto get = [&](uint32_t i) {
                 uint32_t (&q)[4] = held[i].w;
-                if (u - in0 < in1 - in0)
-                    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "l"(at + i * THREADS * 16) : "memory");
-                else {
-                    const uint4 e = edge(u);
-                    q[0] = e.x; q[1] = e.y; q[2] = e.z; q[3] = e.w;
+                asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "l"(at + i * kStride) : "memory");
+            };
+            if (skip == 0u && whole == kHeld) {
+                #pragma unroll
+                for (uint32_t i = 0; i < kHeld; ++i) get(i);
+            } else {
+                #pragma unroll
+                for (uint32_t i = 0; i < kHeld; ++i) {
+                    if (i >= all) break;
+                    if (i >= skip && i < whole) get(i);
+                    else {
+                        const uint4 e = edge(v + i * THREADS + tid);
+                        held[i].w[0] = e.x; held[i].w[1] = e.y; held[i].w[2] = e.z; held[i].w[3] = e.w;
+                    }
                 }
             }
         }
     };
-    auto piece = [&](int i) {
+    auto piece = [&](uint32_t slot) {
         Piece<DT> x;
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.w[0]), "=r"(x.w[1]), "=r"(x.w[2]), "=r"(x.w[3]) : "r"(slots + i * THREADS * 16) : "memory");
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.w[0]), "=r"(x.w[1]), "=r"(x.w[2]), "=r"(x.w[3]) : "r"(slot) : "memory");
         return x;
     };
     // f of the thread's pieces of a chunk, one after another
-    auto each = [&](int n, auto f) {
+    auto each = [&](auto f) {
         if constexpr (GRAD) {
-            #pragma unroll 2
-            for (int i = 0; i < n; ++i) f(piece(i));
+            uint32_t slot = slots;
+            #pragma unroll 4
+            for (uint32_t i = 0; i < all; ++i, slot += kStride) f(piece(slot));
         } else {
             #pragma unroll
-            for (int i = 0; i < kHeld; ++i) {
-                if (i >= n) break;
+            for (uint32_t i = 0; i < kHeld; ++i) {
+                if (i >= all) break;
                 held[i].forget();
                 f(held[i]);
             }
@@ -317,8 +326,7 @@ distill_kernel(const DistillArgs p) {
     for (uint32_t v = v0;;) {
         float c = m;
         if constexpr (GRAD) asm volatile("cp.async.wait_all;" ::: "memory");
-        const int n = used(v);
-        each(n, [&](const Piece<DT> &x) { c = x.max_with(c); });
+        each([&](const Piece<DT> &x) { c = x.max_with(c); });
         const float f = exp2_approx((m - c) * p.scale);
         sums = sums * two(f, f);
         if constexpr (DUAL) {
@@ -327,7 +335,7 @@ distill_kernel(const DistillArgs p) {
         }
         m = c;
         const Two from = two(-c, -c);
-        each(n, [&](const Piece<DT> &x) {
+        each([&](const Piece<DT> &x) {
             Two a, a1;
             #pragma unroll
             for (int k = 0; k < kVals / 2; ++k) {
@@ -442,43 +450,46 @@ distill_kernel(const DistillArgs p) {
             if constexpr (DUAL) d += exp2_approx(t * p.scale1) * c1;
             return d;
         };
-        // bf16: the factors are taken into the exponents, whose rounding (2^-24 of about forty) is far below the output's
-        constexpr bool kFold = DT == LGN_BF16;
-        const float lt = kFold ? log2_approx(fabsf(DUAL ? kt : kt + k1)) - log2_approx(sum) : ct;
-        const float l1 = kFold && DUAL ? log2_approx(fabsf(k1)) - log2_approx(sum1) : c1;
-        const Two from = two(-m, -m), lts = two(lt, lt), l1s = two(l1, l1);
-        const uint32_t sign = kFold && w < 0.0f ? 0x80008000u : 0u;
+        const Two from = two(-m, -m), cts = two(ct, ct), c1s = two(c1, c1);
+        auto slopes = [&](uint32_t slot) {
+            const Piece<DT> x = piece(slot);
+            uint32_t q[4];
+            #pragma unroll
+            for (int k = 0; k < kVals / 2; ++k) {
+                const Two t = x.pair(k) + from;
+                Two d = exp2_approx(t * scales) * cts;
+                if constexpr (DUAL) d = fma(exp2_approx(t * scales1), c1s, d);
+                float lo, hi;
+                apart(d, lo, hi);
+                if constexpr (DT == LGN_F32) { q[2 * k] = __float_as_uint(lo); q[2 * k + 1] = __float_as_uint(hi); }
+                else q[k] = pack_bf16(lo, hi);
+            }
+            return make_uint4(q[0], q[1], q[2], q[3]);
+        };
         const bool held = v1 - v0 <= THREADS * p.vecs; // the one chunk is still there
-        for (uint32_t v = v0; v < v1; v += THREADS * p.vecs) {
-            if (!held) {
-                load(v);
-                asm volatile("cp.async.wait_all;" ::: "memory");
-            }
-            char *to = dst - shift * ES + (uint64_t)(v + tid) * 16;
-            const int n = used(v);
-            #pragma unroll 2
-            for (int i = 0; i < n; ++i) {
-                const uint32_t u = v + i * THREADS + tid;
-                uint32_t q[4];
-                if (dead) q[0] = q[1] = q[2] = q[3] = 0u;
-                else {
-                    const Piece<DT> x = piece(i);
-                    #pragma unroll
-                    for (int k = 0; k < kVals / 2; ++k) {
-                        const Two t = x.pair(k) + from;
-                        Two d = kFold ? exp2_approx(fma(t, scales, lts)) : exp2_approx(t * scales) * lts;
-                        if constexpr (DUAL) d = kFold ? d + exp2_approx(fma(t, scales1, l1s)) : fma(exp2_approx(t * scales1), l1s, d);
-                        float lo, hi;
-                        apart(d, lo, hi);
-                        if constexpr (DT == LGN_F32) { q[2 * k] = __float_as_uint(lo); q[2 * k + 1] = __float_as_uint(hi); }
-                        else q[k] = pack_bf16(lo, hi) ^ sign;
-                    }
+        auto write = [&](auto f) {
+            for (uint32_t v = v0; v < v1; v += THREADS * p.vecs) {
+                if (!held) {
+                    load(v);
+                    asm volatile("cp.async.wait_all;" ::: "memory");
                 }
-                if (whole && u - in0 < in1 - in0)
-                    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(to + i * THREADS * 16), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
-                else if (u < v1) store_edge<DT>(dst, (int64_t)u * kVals - shift, p.vocab, make_uint4(q[0], q[1], q[2], q[3]));
+                if (!alike) whole = skip = all;             // a gradient that is aligned differently from its logits
+                char *to = dst - shift * ES + (uint64_t)(v + tid) * 16 + skip * kStride;
+                uint32_t slot = slots + skip * kStride;
+                #pragma unroll 2
+                for (uint32_t i = skip; i < whole; ++i, slot += kStride, to += kStride) {
+                    const uint4 q = f(slot);
+                    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(to), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+                }
+                #pragma unroll 1
+                for (uint32_t i = 0; i < all; ++i) {
+                    if (i >= skip && i < whole) i = whole;
+                    if (i < all) store_edge<DT>(dst, (int64_t)(v + i * THREADS + tid) * kVals - shift, p.vocab, f(slots + i * kStride));
+                }
             }
-        }
+        };
+        if (dead) write([](uint32_t) { return make_uint4(0u, 0u, 0u, 0u); });
+        else write(slopes);
         __syncthreads();                                // the places are written over what other threads wrote there
         const int64_t begin = (int64_t)v0 * kVals - shift, end = (int64_t)v1 * kVals - shift;
         for (uint32_t j = tid; j < entries; j += THREADS) {
