@@ -11,6 +11,12 @@
 // distributed shared memory); rows beyond that go through in chunks that are read again, from L2 mostly.  The loss alone takes
 // chunks of 8 pieces per thread straight to registers.
 //
+// What bounds it: for one temperature the instructions (15 per value, 437 us for 4096 x 131072 bf16, 75 % of the copy rate), fp32 logits the memory
+// (8192 x 32000: 365 us, 88 %).  Two temperatures take four exponentials per value, 472 us of the special-function units alone: one of
+// the gradient's two is a polynomial for bf16 logits (614 -> 563 us; with half of the first pass's too, the instructions bind: 599).  Arithmetic is on
+// two values at a time.  Not kept: reading the row a second time from L2 instead of holding it (638 us, 506 for one temperature), and CTAs that stay for
+// several rows and ask for the next as slots of the last fall free (722 and 477: more instructions and registers, 104 clusters at once).
+//
 // exp is taken in base 2 of (s - M) log2(e) / T, the difference first: it is exact or small where the term
 // counts.  Sums are fp32, a few dozen terms per thread, then by lanes, warps and ranks in a fixed order.
 //
@@ -594,8 +600,8 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     const bool aligned = aligned_to(logits, 16) && (ld * es) % 16 == 0;
     const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + (aligned ? 0 : vals - 1)) / vals;        // of a row that is aligned worst
     // A gradient needs the row twice: the fewest threads of 32, 64 and 128 that hold it, or up to 8 CTAs of 128 (16 pieces per thread: what a CTA does
-    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 186 us,
-    // 207 with 128).  More CTAs per row where there are too few rows to fill the machine.
+    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 178 us;
+    // 128 threads took a tenth longer).  More CTAs per row where there are too few rows to fill the machine.
     const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 64 * kDsVecs ? 1 : 2;
     const unsigned threads = kind == 0 ? 32 : kind == 1 ? 64 : grad ? 128 : 256;
     const uint64_t per_cta = (uint64_t)threads * kDsVecs;
