@@ -562,7 +562,7 @@ lgn_status lgn_selftest_grouped_wait_expires(const void *a, const void *b, int g
  *   dlogits[t]  = weight[t] (alpha T (q - p at the places) + (1 - alpha) (q1 - 1 at the label)),    rounded once to dt
  * without the first part in a row with no entry present (or alpha = 0), without the second where the label lies outside
  * [0, vocab), labels is NULL or alpha = 1.  A row with neither has loss 0 and a gradient of zeros, whatever its logits are.
- * Logits of -infinity have q = 0; NaN, +infinity and rows of -infinity alone give NaN.
+ * Logits of -infinity have q = 0, probabilities below 2^-126 count as 0; NaN, +infinity and rows of -infinity alone give NaN.
  *   ids, teacher  device, tokens x top, rows ld_ids and ld_teacher apart; ids of ids_bits (32 or 64) bits
  *   labels        device, `tokens` integers of label_bits bits, or NULL
  *   weight        device, `tokens` floats, or NULL (1): the loss gradients
