@@ -13,9 +13,10 @@
 //
 // What bounds it: for one temperature the instructions (15 per value, 437 us for 4096 x 131072 bf16, 75 % of the copy rate), fp32 logits the memory
 // (8192 x 32000: 365 us, 88 %).  Two temperatures take four exponentials per value, 472 us of the special-function units alone: one of
-// the gradient's two is a polynomial for bf16 logits (614 -> 563 us; with half of the first pass's too, the instructions bind: 599).  Arithmetic is on
-// two values at a time.  Not kept: reading the row a second time from L2 instead of holding it (638 us, 506 for one temperature), and CTAs that stay for
-// several rows and ask for the next as slots of the last fall free (722 and 477: more instructions and registers, 104 clusters at once).
+// the gradient's two is a polynomial for three values in four of bf16 logits (4096 x 131072: 550 us, all of them 562, half 562; with half of the first pass's
+// too, the instructions bind: 599).  Arithmetic is on two values at a time.  Not kept: reading the row a second time from L2 instead of holding it (638 us,
+// 506 for one temperature), and CTAs that stay for several rows and ask for the next as slots of the last fall free (722 and 477: more instructions
+// and registers, 104 clusters at once).
 //
 // exp is taken in base 2 of (s - M) log2(e) / T, the difference first: it is exact or small where the term
 // counts.  Sums are fp32, a few dozen terms per thread, then by lanes, warps and ranks in a fixed order.
@@ -251,7 +252,7 @@ distill_kernel(const DistillArgs p) {
     const uint32_t v0 = min(rank * p.pieces, total), v1 = min(v0 + p.pieces, total);
     const uint32_t in0 = shift > 0 ? 1u : 0u, in1 = max(in0, min(v1, (uint32_t)((shift + vocab) / kVals)));   // whole pieces
     const char *base = src - shift * ES;
-    
+
     // An entry: its place, the teacher's logit, the student's.
     auto place_of = [&](uint32_t j, float &z) {
         int64_t at = -1;
@@ -484,7 +485,7 @@ distill_kernel(const DistillArgs p) {
             for (int k = 0; k < kVals / 2; ++k) {
                 const Two t = x.pair(k) + from;
                 Two d = exp2_approx(t * scales) * cts;
-                if constexpr (DUAL) d = fma(DT == LGN_BF16 ? exp2_poly(t * scales1) : exp2_approx(t * scales1), c1s, d);
+                if constexpr (DUAL) d = fma(DT == LGN_BF16 && k != 0 ? exp2_poly(t * scales1) : exp2_approx(t * scales1), c1s, d);
                 float lo, hi;
                 apart(d, lo, hi);
                 if constexpr (DT == LGN_F32) { q[2 * k] = __float_as_uint(lo); q[2 * k + 1] = __float_as_uint(hi); }
