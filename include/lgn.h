@@ -506,7 +506,8 @@ lgn_status lgn_clip_apply(const lgn_grad_t *grads, int count, double max_norm, l
  * are `rows` floats.  0 for an extent above 2^30. */
 size_t lgn_int8_codes_bytes(uint64_t rows, uint64_t cols);
 
-/* Quantises x (rows x cols of dt, leading dimension ld >= cols): codes 16-byte aligned.  One launch. */
+/* Quantises x (rows x cols of dt, leading dimension ld >= cols): codes 16-byte aligned.  One launch.  cols = 0: the scales of rows of zeros, x and codes
+ * are not looked at; scales may then be NULL, and nothing is done. */
 lgn_status lgn_int8_quantize(const void *x, uint64_t rows, uint64_t cols, uint64_t ld, lgn_dtype dt,
                              void *codes, float *scales, void *stream);
 
@@ -514,7 +515,8 @@ lgn_status lgn_int8_quantize(const void *x, uint64_t rows, uint64_t cols, uint64
  * rounded to fp32, multiplied by a's scale, by b's, and rounded to out_dt.  k up to 2^17.
  *   offsets  NULL with groups = 1: one product.  Else the rows of A are grouped: as for lgn_grouped_matmul, B holding
  *            groups x n rows, group by group
- * zero_rest, status_dev, k = 0: as there.  One launch, no workspace; the same inputs give the same bits. */
+ * zero_rest, status_dev, k = 0: as there (operands and scales are then not read and may be NULL).  One launch, no workspace; the same inputs give
+ * the same bits. */
 lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, const float *b_scales,
                            const void *offsets, int offset_bits, uint64_t groups, uint64_t m, uint64_t n, uint64_t k,
                            void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream);

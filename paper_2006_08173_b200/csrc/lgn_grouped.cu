@@ -263,7 +263,9 @@ extern "C" lgn_status lgn_int8_matmul(const void *a, const float *a_scales, cons
     const GmOperand x = {a, k, m, 1, pitch, 0}, w = {b, k, n, groups, pitch, n * pitch};
     GmArgs p = {};
     p.out = static_cast<char *>(out); p.ldo = ldo; p.offsets = offsets; p.offsets64 = offset_bits == 64; p.status = status_dev;
-    p.row_scales = a_scales; p.col_scales = b_scales;
     p.rows = (uint32_t)m; p.groups = (uint32_t)groups; p.n = (uint32_t)n; p.zero_rest = zero_rest != 0;
+    // Over nothing the scales may be absent or without a meaning, and the integer kernels read them: the bf16 ones write the same zeros.
+    if (k == 0) return gm_run(kGmForward, x, w, p, 0, out_dt, stream);
+    p.row_scales = a_scales; p.col_scales = b_scales;
     return gm_run(kGmIntegers, x, w, p, k, out_dt, stream);
 }

@@ -130,12 +130,16 @@ extern "C" lgn_status lgn_int8_quantize(const void *x, uint64_t rows, uint64_t c
                                         void *codes, float *scales, void *stream) {
     if (dt != LGN_F32 && dt != LGN_BF16) return LGN_ERR_INVALID_ARG;
     if (rows > kFp8MaxDim || cols > kFp8MaxDim) return LGN_ERR_UNSUPPORTED;
-    if (rows == 0 || cols == 0) return LGN_OK;
-    if (ld < cols || ld > (1ull << 40)) return LGN_ERR_INVALID_ARG;
-    const uint64_t es = dt == LGN_F32 ? 4 : 2, xb = matrix_bytes(rows, cols, ld, es), qb = lgn_int8_codes_bytes(rows, cols);
-    if (xb == 0 || x == nullptr || codes == nullptr || scales == nullptr) return LGN_ERR_INVALID_ARG;
-    if (!aligned_to(x, es) || !aligned_to(codes, 16) || !aligned_to(scales, 4)) return LGN_ERR_INVALID_ARG;
-    if (ranges_overlap(x, xb, codes, qb) || ranges_overlap(x, xb, scales, 4 * rows) || ranges_overlap(codes, qb, scales, 4 * rows)) return LGN_ERR_INVALID_ARG;
+    if (rows == 0 || (cols == 0 && scales == nullptr)) return LGN_OK;
+    const uint64_t es = dt == LGN_F32 ? 4 : 2;
+    if (!aligned_to(scales, 4)) return LGN_ERR_INVALID_ARG;
+    if (cols > 0) {                                         // rows without a column have scales, and nothing to read
+        if (ld < cols || ld > (1ull << 40)) return LGN_ERR_INVALID_ARG;
+        const uint64_t xb = matrix_bytes(rows, cols, ld, es), qb = lgn_int8_codes_bytes(rows, cols);
+        if (xb == 0 || x == nullptr || codes == nullptr || scales == nullptr) return LGN_ERR_INVALID_ARG;
+        if (!aligned_to(x, es) || !aligned_to(codes, 16)) return LGN_ERR_INVALID_ARG;
+        if (ranges_overlap(x, xb, codes, qb) || ranges_overlap(x, xb, scales, 4 * rows) || ranges_overlap(codes, qb, scales, 4 * rows)) return LGN_ERR_INVALID_ARG;
+    }
     const bool vec = aligned_to(x, 16) && (ld * es) % 16 == 0;
     uint32_t r = (uint32_t)rows, c = (uint32_t)cols, pitch = (uint32_t)fp8_pitch(cols);
     // the fewest warps that hold a row; twice as many for as long as the SMs have fewer than four each and every thread has a piece
