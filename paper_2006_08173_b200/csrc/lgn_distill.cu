@@ -38,6 +38,7 @@ namespace lgn {
 constexpr uint64_t kDsMaxTop = 1024, kDsMaxDim = 1ull << 30;
 constexpr int kDsVecs = 16;                             // pieces of 16 bytes a thread holds at most
 constexpr int kDsMaxSmem = 64 * 1024;                   // above the most that a CTA asks for: 3 x 1025 + 4096 words of entries, 128 x 16 pieces
+constexpr int kDsStatic = 1024;                         // above what the kernels declare: 7 sums of up to 8 warps and 3 of the CTA, 236 bytes
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kDsLowest = -3.402823466e38f;           // starts every maximum: s - M is then never inf - inf for s = -inf
 
@@ -620,8 +621,9 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
              (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
     const void *fn = kDistillTable[dt][kind][dual][grad];
-    // Many entries.  The same limit from every call: calls of two threads must not lower one another's.
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kDsMaxSmem) != cudaSuccess) {
+    // Many entries.  The limit that holds without asking, 48 KB, covers the kernel's own variables too.  The same limit from every call: calls of two
+    // threads must not lower one another's.
+    if (smem + kDsStatic > 48 * 1024 && cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kDsMaxSmem) != cudaSuccess) {
         (void)cudaGetLastError();
         return LGN_ERR_CUDA;
     }
