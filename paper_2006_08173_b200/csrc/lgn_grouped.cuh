@@ -23,7 +23,8 @@
 // Roles as in the 8-bit float product: warp 8 copies, warp 9 issues MMAs, warps 0..7 read sums out.  Sums of
 // bf16 products leave tensor memory every 512 of the contraction for registers, because the tensor cores' additions
 // truncate, here after every 16 products: sums of positive products come out too small by 9e-7 with 512, by twice that with 1024 and by 4e-7 with
-// 256, which costs 2 to 4 % (16384 rows, 8 x 4096 x 4096: 393 us, 401).  Two accumulators take turns.  Every wait is bounded.
+// 256, which costs 2 to 4 % (16384 rows, 8 x 4096 x 4096: 393 us, 401).  Two accumulators take turns.  Every wait is bounded: that of the clearing
+// warp, which has nothing to do until a group ends, from the last step that was copied in.
 #pragma once
 
 #include <type_traits>
@@ -183,6 +184,24 @@ __device__ __forceinline__ bool mbar_wait_warp_cluster(uint32_t bar, uint32_t pa
     return __all_sync(0xffffffffu, mbar_try_cluster(bar, parity));              // completed already: acquires for the cluster
 }
 
+// A wait that may begin long before what it is for: `steps` counts the steps that the copying warp has begun, and as long as it goes on counting the wait
+// has its whole time.
+static __device__ __noinline__ bool mbar_wait_behind_slow(uint32_t bar, uint32_t parity, volatile uint32_t *stop, volatile uint32_t *steps) {
+    long long t0 = clock64();
+    uint32_t seen = *steps;
+    for (;;) {
+        if (mbar_try(bar, parity)) return true;
+        if (*stop) return false;
+        const uint32_t now = *steps;
+        if (now != seen) { seen = now; t0 = clock64(); }
+        else if (clock64() - t0 > kMmWaitClocks) { *stop = 1u; return false; }
+    }
+}
+__device__ __forceinline__ bool mbar_wait_warp_behind(uint32_t bar, uint32_t parity, volatile uint32_t *stop, volatile uint32_t *steps) {
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+    return __all_sync(0xffffffffu, mbar_wait_behind_slow(bar, parity, stop, steps));
+}
+
 // ------------------------------------------------------------------ output
 // 32 rows x 128 bytes of the output from row y, column x of group z on; lane l holds row l in v, `valid` rows of the 32 are stored.  They are turned in
 // the warp's staging buffer (128-byte swizzle) and leave as whole rows, 16 bytes a lane where rows are whole 16-byte pieces.  (TMA stores of the buffer
@@ -282,7 +301,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[4 * S::kStages + 2 * 2 + 1];
     __shared__ uint32_t tmem_base_s;
-    __shared__ volatile uint32_t stop;
+    __shared__ volatile uint32_t stop, begun;               // begun: steps whose copies warp 8 has issued (gradient)
     dep_launch();
 
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u, staging0 = smem0 + S::kStages * S::kStageBytes, bar0 = smem_u32(bars);
@@ -319,6 +338,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), CTAS * kGmEpiWarps); }
         mbar_init(drained, 1);
         stop = 0u;
+        begun = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -402,6 +422,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 last_mask = last ? last_mask | 1u << s : last_mask & ~(1u << s);
                 if (last) last_ph ^= 1u << s;
                 ++issued;
+                if (kGrad && lane == 0) begun = issued;
                 if (++s == S::kStages) { s = 0; ph ^= 1; }
             }
         }
@@ -417,7 +438,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t left = t.end - t.start - (k0 + steps - 1) * 64, at = (s + steps - 1) % S::kStages;
             s = (s + steps) % S::kStages;
             if (!ragged(left)) continue;
-            if (!(ok = mbar_wait_warp(last_in(at), in_ph >> at & 1, &stop))) break;
+            // All steps of the tile, and of tiles with nothing to clear, come first: seconds, where a group has 10^8 rows.
+            if (!(ok = mbar_wait_warp_behind(last_in(at), in_ph >> at & 1, &stop, &begun))) break;
             in_ph ^= 1u << at;
             const uint32_t a = smem0 + at * S::kStageBytes, upper = (left + 15) & ~15u;
             for (uint32_t j = left * 8 + lane; j < upper * 8; j += 32) {                  // 16 bytes each, in every box
