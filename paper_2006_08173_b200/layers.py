@@ -12,6 +12,7 @@ from __future__ import annotations
 from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
 from . import binding as lgn
@@ -156,7 +157,8 @@ class Int8Linear(_Bounded):
         self.seed += 1
 
     def freeze(self, frozen: bool = True) -> None:
-        """From here on the layer computes with the weights as they are now, and refuses passes that want gradients; ``frozen`` false: as before."""
+        """From here on the layer computes with the weights as they are now, and refuses passes that want derivatives, in either mode; ``frozen`` false: as
+        before."""
         self._frozen = lgn.lgn_int8_quantize(_rows(self.weight.detach())) if frozen else None
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
@@ -165,6 +167,8 @@ class Int8Linear(_Bounded):
             y = _Int8LinearFn.apply(flat, self.weight, self.sparsity, self.seed, status)
         elif torch.is_grad_enabled() and (x.requires_grad or self.weight.requires_grad):
             raise RuntimeError("the layer is frozen: no gradients")
+        elif unpack_dual(x).tangent is not None or unpack_dual(self.weight).tangent is not None:
+            raise RuntimeError("the layer is frozen: no tangents")
         else:
             y = lgn.lgn_int8_matmul(lgn.lgn_int8_quantize(_rows(flat)), self._frozen, out_dtype=x.dtype, status=status)
         return y.reshape(*x.shape[:-1], self.weight.shape[0])
