@@ -76,6 +76,8 @@ class _Bounded(torch.nn.Module):
 
     def _status_on(self, device: torch.device) -> torch.Tensor:
         if device not in self._status:
+            if device.type != "cuda":                                  # check() would wait for it
+                raise ValueError("the module computes on CUDA tensors")
             with torch.inference_mode(False):                          # check() writes it outside of that mode too
                 self._status[device] = torch.zeros(1, dtype=torch.int32, device=device)
         return self._status[device]
