@@ -550,8 +550,8 @@ lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, const void *x,
                                    lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream);
 
 /* Self-test of the bounded waits of the grouped products, as lgn_selftest_matmul_wait_expires is of the 8-bit product's: contiguous operands, a is
- * rows x k and b groups x n x k (gradient: a rows x n, b rows x k, out groups x n x k), with every CTA's first copy left out.  After a
- * few seconds the kernel ends by itself with LGN_ERR_TIMEOUT in *status_dev (zeroed by the caller, not NULL); out is not meaningful. */
+ * rows x k and b groups x n x k (gradient 1: a rows x n, b rows x k, out groups x n x k; gradient 2: the product in 8-bit integers, a and b the codes
+ * of rows x k and groups n x k), with every CTA's first copy left out.  After a few seconds the kernel ends by itself with LGN_ERR_TIMEOUT in *status_dev (zeroed by the caller, not NULL); out is not meaningful. */
 lgn_status lgn_selftest_grouped_wait_expires(const void *a, const void *b, int gradient, const void *offsets, int offset_bits,
                                              uint64_t groups, uint64_t rows, uint64_t n, uint64_t k, void *out, lgn_dtype out_dt,
                                              uint32_t *status_dev, void *stream);

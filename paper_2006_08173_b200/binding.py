@@ -1012,21 +1012,26 @@ def lgn_grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Te
     return out
 
 
-def lgn_selftest_grouped_wait_expires(a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor, out: torch.Tensor, status: torch.Tensor,
-                                      gradient: bool = False, stream=None) -> None:
-    """A grouped product (``gradient``: the weights' gradient) of contiguous operands whose first copies are withheld: ``status`` must become
-    LGN_ERR_TIMEOUT after a few seconds."""
+def lgn_selftest_grouped_wait_expires(a, b, offsets: torch.Tensor, out: torch.Tensor, status: torch.Tensor, gradient: bool = False, stream=None) -> None:
+    """A grouped product (``gradient``: the weights' gradient) of contiguous operands whose first copies are withheld, in 8-bit integers where they are
+    Int8Operands: ``status`` must become LGN_ERR_TIMEOUT after a few seconds."""
     at, bits, groups = _offsets(offsets)
-    rows, k = a.size(0), b.size(-1)
-    n = a.size(1) if gradient else b.size(1)
-    if tuple(b.shape) != ((rows, k) if gradient else (groups, n, a.size(1))) or tuple(out.shape) != ((groups, n, k) if gradient else (rows, n)):
-        raise ValueError("extents do not belong together")
-    _bf16(a, b)
-    device = a.get_device()
-    if _elsewhere(device, stream, b.get_device(), offsets.get_device(), out.get_device(), status.get_device()):
+    if isinstance(a, Int8Operand):
+        rows, n, k, device, other = a.rows, b.rows // groups, a.k, a._device, b._device
+        if gradient or b.k != k or b.rows % groups or tuple(out.shape) != (rows, n):
+            raise ValueError("extents do not belong together")
+        a_at, b_at, kind = a._codes_ptr, b._codes_ptr, 2
+    else:
+        rows, k = a.size(0), b.size(-1)
+        n = a.size(1) if gradient else b.size(1)
+        if tuple(b.shape) != ((rows, k) if gradient else (groups, n, a.size(1))) or tuple(out.shape) != ((groups, n, k) if gradient else (rows, n)):
+            raise ValueError("extents do not belong together")
+        _bf16(a, b)
+        device, other, a_at, b_at, kind = a.get_device(), b.get_device(), _dev(a, "a"), _dev(b, "b"), 1 if gradient else 0
+    if _elsewhere(device, stream, other, offsets.get_device(), out.get_device(), status.get_device()):
         with torch.cuda.device(device):
             return lgn_selftest_grouped_wait_expires(a, b, offsets, out, status, gradient, stream)
-    _check(_lib.lgn_selftest_grouped_wait_expires(_dev(a, "a"), _dev(b, "b"), 1 if gradient else 0, at, bits, groups, rows, n, k, _dev(out, "out"),
+    _check(_lib.lgn_selftest_grouped_wait_expires(a_at, b_at, kind, at, bits, groups, rows, n, k, _dev(out, "out"),
                                                   dtype_code(out), _word(status, 4, "status"), _stream(stream)), "lgn_selftest_grouped_wait_expires")
 
 

@@ -223,29 +223,9 @@ static lgn_status weight_grad(const void *dy, uint64_t lddy, const void *x, uint
     return gm_run(kGmWeight, a, b, p, 0, out_dt, stream);
 }
 
-extern "C" lgn_status lgn_grouped_matmul(const void *x, uint64_t ldx, const void *w, uint64_t ldw, uint64_t w_group, int transposed,
-                                         const void *offsets, int offset_bits, uint64_t groups, uint64_t rows, uint64_t n, uint64_t k,
-                                         void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream) {
-    return grouped_matmul(x, ldx, w, ldw, w_group, transposed, offsets, offset_bits, groups, rows, n, k, out, ldo, out_dt, zero_rest, status_dev, stream, false);
-}
-
-extern "C" lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, const void *x, uint64_t ldx, const void *offsets, int offset_bits,
-                                              uint64_t groups, uint64_t rows, uint64_t m, uint64_t n, void *out, uint64_t ldo, uint64_t out_group,
-                                              lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream) {
-    return weight_grad(dy, lddy, x, ldx, offsets, offset_bits, groups, rows, m, n, out, ldo, out_group, out_dt, accumulate, status_dev, stream, false);
-}
-
-extern "C" lgn_status lgn_selftest_grouped_wait_expires(const void *a, const void *b, int gradient, const void *offsets, int offset_bits,
-                                                        uint64_t groups, uint64_t rows, uint64_t n, uint64_t k, void *out, lgn_dtype out_dt,
-                                                        uint32_t *status_dev, void *stream) {
-    if (status_dev == nullptr || rows == 0 || k == 0) return LGN_ERR_INVALID_ARG;
-    return gradient ? weight_grad(a, n, b, k, offsets, offset_bits, groups, rows, n, k, out, k, n * k, out_dt, 0, status_dev, stream, true)
-                    : grouped_matmul(a, k, b, k, n * k, 0, offsets, offset_bits, groups, rows, n, k, out, n, out_dt, 0, status_dev, stream, true);
-}
-
-extern "C" lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, const float *b_scales,
-                                      const void *offsets, int offset_bits, uint64_t groups, uint64_t m, uint64_t n, uint64_t k,
-                                      void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream) {
+static lgn_status int8_matmul(const void *a, const float *a_scales, const void *b, const float *b_scales,
+                              const void *offsets, int offset_bits, uint64_t groups, uint64_t m, uint64_t n, uint64_t k,
+                              void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream, bool withhold) {
     const lgn_status bad = gm_check(offsets, offset_bits, groups, m, n, out_dt, status_dev);
     if (bad != LGN_OK) return bad;
     if (k > kGmMaxInt8K || groups * n > kGmMaxDim) return LGN_ERR_UNSUPPORTED;
@@ -263,9 +243,38 @@ extern "C" lgn_status lgn_int8_matmul(const void *a, const float *a_scales, cons
     const GmOperand x = {a, k, m, 1, pitch, 0}, w = {b, k, n, groups, pitch, n * pitch};
     GmArgs p = {};
     p.out = static_cast<char *>(out); p.ldo = ldo; p.offsets = offsets; p.offsets64 = offset_bits == 64; p.status = status_dev;
-    p.rows = (uint32_t)m; p.groups = (uint32_t)groups; p.n = (uint32_t)n; p.zero_rest = zero_rest != 0;
+    p.rows = (uint32_t)m; p.groups = (uint32_t)groups; p.n = (uint32_t)n; p.zero_rest = zero_rest != 0; p.withhold = withhold;
     // Over nothing the scales may be absent or without a meaning, and the integer kernels read them: the bf16 ones write the same zeros.
     if (k == 0) return gm_run(kGmForward, x, w, p, 0, out_dt, stream);
     p.row_scales = a_scales; p.col_scales = b_scales;
     return gm_run(kGmIntegers, x, w, p, k, out_dt, stream);
+}
+
+extern "C" lgn_status lgn_grouped_matmul(const void *x, uint64_t ldx, const void *w, uint64_t ldw, uint64_t w_group, int transposed,
+                                         const void *offsets, int offset_bits, uint64_t groups, uint64_t rows, uint64_t n, uint64_t k,
+                                         void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream) {
+    return grouped_matmul(x, ldx, w, ldw, w_group, transposed, offsets, offset_bits, groups, rows, n, k, out, ldo, out_dt, zero_rest, status_dev, stream, false);
+}
+
+extern "C" lgn_status lgn_grouped_weight_grad(const void *dy, uint64_t lddy, const void *x, uint64_t ldx, const void *offsets, int offset_bits,
+                                              uint64_t groups, uint64_t rows, uint64_t m, uint64_t n, void *out, uint64_t ldo, uint64_t out_group,
+                                              lgn_dtype out_dt, int accumulate, uint32_t *status_dev, void *stream) {
+    return weight_grad(dy, lddy, x, ldx, offsets, offset_bits, groups, rows, m, n, out, ldo, out_group, out_dt, accumulate, status_dev, stream, false);
+}
+
+extern "C" lgn_status lgn_selftest_grouped_wait_expires(const void *a, const void *b, int gradient, const void *offsets, int offset_bits,
+                                                        uint64_t groups, uint64_t rows, uint64_t n, uint64_t k, void *out, lgn_dtype out_dt,
+                                                        uint32_t *status_dev, void *stream) {
+    if (status_dev == nullptr || rows == 0 || k == 0) return LGN_ERR_INVALID_ARG;
+    // The codes are at least as long as the scales: any floats do, nothing comes of them.
+    if (gradient == 2) return int8_matmul(a, static_cast<const float *>(a), b, static_cast<const float *>(b), offsets, offset_bits, groups, rows, n, k, out, n, out_dt, 0,
+                                          status_dev, stream, true);
+    return gradient ? weight_grad(a, n, b, k, offsets, offset_bits, groups, rows, n, k, out, k, n * k, out_dt, 0, status_dev, stream, true)
+                    : grouped_matmul(a, k, b, k, n * k, 0, offsets, offset_bits, groups, rows, n, k, out, n, out_dt, 0, status_dev, stream, true);
+}
+
+extern "C" lgn_status lgn_int8_matmul(const void *a, const float *a_scales, const void *b, const float *b_scales,
+                                      const void *offsets, int offset_bits, uint64_t groups, uint64_t m, uint64_t n, uint64_t k,
+                                      void *out, uint64_t ldo, lgn_dtype out_dt, int zero_rest, uint32_t *status_dev, void *stream) {
+    return int8_matmul(a, a_scales, b, b_scales, offsets, offset_bits, groups, m, n, k, out, ldo, out_dt, zero_rest, status_dev, stream, false);
 }
