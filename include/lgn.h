@@ -571,7 +571,10 @@ lgn_status lgn_selftest_grouped_wait_expires(const void *a, const void *b, int g
  *   dlogits       device, of dt, rows ld_dlogits apart, or NULL (the loss alone); may be logits itself with the same leading
  *                 dimension, and must not overlap it otherwise
  * temperature 0.001 to 1000, alpha 0 to 1.  Sums in fp32 in a fixed order: the same bits on every run on the same type of device.
- * One launch; the logits are read from memory once. */
+ * Exponentials are off by up to 2^-22, relative, and 3 2^-24 per unit of their argument; where both parts count and T is not 1, those of q1 in a gradient of bf16 logits by up to 2.9e-6 (for three values in
+ * four, by their place within 16 aligned bytes: a row at another alignment may differ in bits), a thousandth of the rounding to bf16.
+ * One launch.  The logits are read from memory once, but for gradients of rows that are longer than the 256 KB that a cluster holds (131072 bf16 or 65536
+ * fp32 values, 16-byte aligned): those are read a second time, from L2 where they are still there. */
 lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint64_t vocab, uint64_t ld, lgn_dtype dt,
                             const void *ids, int ids_bits, uint64_t ld_ids, const void *teacher, uint64_t ld_teacher,
                             lgn_dtype teacher_dt, uint64_t top, const void *labels, int label_bits,

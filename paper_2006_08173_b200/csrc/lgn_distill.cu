@@ -11,10 +11,14 @@
 // distributed shared memory); rows beyond that go through in chunks that are read again, from L2 mostly.  The loss alone takes
 // chunks of 8 pieces per thread straight to registers.
 //
-// What bounds it: for one temperature the instructions (15 per value, 437 us for 4096 x 131072 bf16, 75 % of the copy rate), fp32 logits the memory
-// (8192 x 32000: 365 us, 88 %).  Two temperatures take four exponentials per value, 472 us of the special-function units alone: one of
-// the gradient's two is a polynomial for three values in four of bf16 logits (4096 x 131072: 550 us, all of them 562, half 562; with half of the first pass's
-// too, the instructions bind: 599).  Arithmetic is on two values at a time.  Not kept: reading the row a second time from L2 instead of holding it (638 us,
+// What bounds it (calls back to back; one after other work takes 2 to 5 % longer, and two GPUs differ by as much): for one temperature the instructions
+// (15 per value, 437 to 446 us for 4096 x 131072 bf16, 0.73 of the copy rate), fp32 logits the memory (8192 x 32000: 365 to 386 us, 0.83 to 0.88).  Two
+// temperatures take four exponentials per value, 472 us of the special-function units alone: one of
+// the gradient's two is a polynomial for three values in four of bf16 logits (4096 x 131072: 550 to 558 us, 573 to 600 after other work; on one GPU 550, all of them 562, half 562;
+// with half of the first pass's too, the instructions bind: 599).  Which values those are goes by the place within 16 aligned bytes, so a value's last bits
+// before the rounding to bf16 go by its column and by the row's alignment; 2.9e-6 is below a thousandth of that rounding.
+// Rows beyond a cluster are read twice: 4096 x 140000 fp32 1060 us, 0.66.
+// Arithmetic is on two values at a time.  Not kept: reading the row a second time from L2 instead of holding it (638 us,
 // 506 for one temperature), and CTAs that stay for several rows and ask for the next as slots of the last fall free (722 and 477: more instructions
 // and registers, 104 clusters at once).
 //
@@ -602,7 +606,7 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     const bool aligned = aligned_to(logits, 16) && (ld * es) % 16 == 0;
     const uint64_t vals = 16 / es, pieces = (vocab + vals - 1 + (aligned ? 0 : vals - 1)) / vals;        // of a row that is aligned worst
     // A gradient needs the row twice: the fewest threads of 32, 64 and 128 that hold it, or up to 8 CTAs of 128 (16 pieces per thread: what a CTA does
-    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 178 us;
+    // once costs as much as 40 values of each thread).  A loss alone passes through it once: 256 threads from 1024 pieces on, in chunks (4096 x 131072 bf16: 178 us after other work, 166 back to back;
     // 128 threads took a tenth longer).  More CTAs per row where there are too few rows to fill the machine.
     const int kind = pieces <= 32 * kDsVecs && top <= 128 && tokens >= 8 * (uint64_t)sms ? 0 : pieces <= 64 * kDsVecs ? 1 : 2;
     const unsigned threads = kind == 0 ? 32 : kind == 1 ? 64 : grad ? 128 : 256;
@@ -616,7 +620,7 @@ extern "C" lgn_status lgn_distill_loss(const void *logits, uint64_t tokens, uint
     if (grad) {                                             // chunks of one size
         const uint32_t chunks = (p.vecs + kDsVecs - 1) / kDsVecs;
         if (chunks > 1) p.vecs = (p.vecs + chunks - 1) / chunks;
-    } else if (p.vecs > kDsVecs / 2) p.vecs = kDsVecs / 2;  // full ones, whose loads need no checks (4096 x 50021 bf16: 88 us, 102 with chunks of one size)
+    } else if (p.vecs > kDsVecs / 2) p.vecs = kDsVecs / 2;  // full ones, whose loads need no checks (4096 x 50021 bf16 after other work: 88 us, 102 with chunks of one size)
     const size_t smem = 4 * p.slots + (grad ? 16 * (size_t)threads * p.vecs : 0);
     log_line("distill_loss: tokens %llu vocab %llu top %llu, %s, %d threads, %u CTAs per row%s", (unsigned long long)tokens, (unsigned long long)vocab,
              (unsigned long long)top, dual ? "two softmaxes" : "one softmax", (int)threads, cluster, grad ? ", gradient" : "");
